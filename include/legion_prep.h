@@ -389,6 +389,110 @@ int lgp_check(lgp_ctx* ctx, void* stream);
 int lgp_set_profiling(lgp_ctx* ctx, int mode);
 int lgp_get_profile(lgp_ctx* ctx, lgp_profile* out);
 
+/* ---- Operators of a model layer over sampled neighbourhoods ----
+ * They need no context and run on `device`; all arrays are [device].  Only `stream` orders them: they allocate nothing, never
+ * synchronise and may be captured into a HIP graph.  Results do not change from run to run: no sum depends on the order in which
+ * workgroups finish. */
+#define LGP_F32 0
+#define LGP_F16 1
+#define LGP_BF16 2
+
+/* Rows of tokens cut into documents: a query attends to the keys of its own document.  Document d owns rows offsets[d] ..
+ * offsets[d + 1] (n_docs + 1 ascending entries, the first 0, the last the number of rows), and the first lens[d] of them hold tokens (NULL:
+ * all).  The sampler's lists are such documents as they stand: row i of nbr[h] begins at i * fanouts[h] and has cnt[h][i] tokens.  Rows
+ * without a token are never read, whatever they hold.  Positions are whole numbers of at most 2^24 in magnitude -- the
+ * hop, or the place in a document -- and needed only where scores fall with the distance.  Queries and keys may be the same rows. */
+typedef struct {
+  int64_t n_docs;
+  int64_t q_rows, k_rows;               /* rows of q and out; rows of k and v                                */
+  const int32_t *q_offsets, *k_offsets; /* n_docs + 1 each                                                   */
+  const int32_t *q_lens, *k_lens;       /* n_docs each, or NULL                                              */
+  const int32_t *q_pos, *k_pos;         /* q_rows and k_rows, or NULL where slopes is NULL                   */
+} lgp_documents;
+
+/* Queries, keys and values.  Strides are in elements, between rows and between heads; elements of a head are consecutive.  Strides are
+ * multiples of 8 and pointers of 16 bytes.  heads is a multiple of kv_heads: consecutive heads / kv_heads query heads share a key head. */
+typedef struct {
+  const void *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  int32_t heads, kv_heads;
+  int32_t dim;                          /* of a head: a multiple of 8, at most 128                           */
+  int32_t dtype;                        /* LGP_F16 or LGP_BF16, of q, k, v, out and their gradients          */
+  float scale;                          /* usually dim^-1/2                                                  */
+  float cap;                            /* 0: scores are not capped                                          */
+  const float* slopes;                  /* float[heads], or NULL: no bias                                    */
+} lgp_attention;
+
+/* Attention inside documents.  The score of a query i and a key j of its document is
+ *     z = scale * q_i.k_j,  capped:  z = cap * tanh(z / cap),  with slopes:  z - slopes[head] * |q_pos[i] - k_pos[j]|
+ * and out[i] = sum_j softmax_j(z) v_j, lse[i] = log sum_j exp(z) (natural logarithm, fp32, [q_rows, heads]).  out is [q_rows, heads, dim],
+ * rows end to end.  A query without keys, and a row without a token, gets zeros and an lse of -inf.  rest (NULL, or like out) receives
+ * what the rounding of out took off, for a backward pass that is as exact as the rounding of its own results.
+ * Few queries over long documents are split over the keys and joined, in `workspace` (lgp_attend_workspace). */
+int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, void* out, void* rest, float* lse, void* workspace,
+               size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that lgp_attend (backward = 0) or lgp_attend_backward (1) want for these arguments; may be 0. */
+int lgp_attend_workspace(int device, const lgp_documents* docs, const lgp_attention* att, int backward, size_t* bytes);
+
+/* Gradients of lgp_attend by q, k and v (dq [q_rows, heads, dim], dk and dv [k_rows, kv_heads, dim]: rows end to end, zeros where no token
+ * is) and by the slopes (float[heads], NULL if not wanted), from d_out, which lies like out, and from what lgp_attend wrote.  rest may be NULL. */
+int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attention* att, const void* d_out, const void* out, const void* rest,
+                        const float* lse, void* dq, void* dk, void* dv, float* d_slopes, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The queries and keys of tokens, before attention.  Strides are in elements, multiples of 8; pointers are aligned to 16 bytes. */
+typedef struct {
+  const void *q, *k;                    /* either may be absent: heads or kv_heads = 0                       */
+  int64_t q_row, q_head, k_row, k_head; /* strides between tokens and between heads                          */
+  int64_t tokens;
+  int32_t heads, kv_heads;
+  int32_t dim;                          /* of a head: a multiple of 8, at most 256                           */
+  int32_t dtype;                        /* LGP_F32, LGP_F16 or LGP_BF16                                      */
+  const float *q_weight, *k_weight;     /* float[dim] each                                                   */
+  const int32_t* pos;                   /* tokens positions; a negative one: there is no token in this row.
+                                           NULL: all rows have tokens (only if rot = 0)                      */
+  int32_t rot;                          /* leading elements of a head that are rotated: a multiple of 16     */
+  int32_t n_pos;                        /* rows of table                                                     */
+  const float* table;                   /* float[n_pos][rot]: rot / 2 cosines, then rot / 2 sines            */
+  float eps;
+} lgp_heads;
+
+/* y = x * w / sqrt(mean(x^2) + eps) for every head, then elements i and i + rot / 2 (i < rot / 2) turned by the angle of the token's position:
+ * y[i] cos - y[i + rot / 2] sin and y[i + rot / 2] cos + y[i] sin.  q_out is [tokens, heads, dim] and k_out [tokens, kv_heads, dim], rows end to
+ * end.  Rows without a token are not read and become zeros; rows with a position beyond the table become NaN. */
+int lgp_norm_rotate(int device, const lgp_heads* in, void* q_out, void* k_out, void* stream);
+
+/* Gradients of lgp_norm_rotate by q, k (dq and dk lie like q_out and k_out; zeros where no token is) and the weights (float[dim] each, summed
+ * over tokens and heads), from those of its results.  `in` is what lgp_norm_rotate was given. */
+int lgp_norm_rotate_workspace(int device, const lgp_heads* in, size_t* bytes);
+int lgp_norm_rotate_backward(int device, const lgp_heads* in, const void* dq_out, const void* dk_out, void* dq, void* dk, float* dq_weight,
+                             float* dk_weight, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Activations kept for the backward pass in 8 bits.  32 consecutive values of a row share a power of two: value = values * 2^(exps - 127), with
+ * the largest of them at 64 to 127 steps, ties to even.  The step is never smaller than 2^-24 for activations that came in fp16 and 2^-126 for
+ * others, so that what is held is a number of the type that came.  A group with an infinity or a NaN has exps = 255 and stands for NaN. */
+typedef struct {
+  int64_t tokens;
+  int32_t width;                        /* values of a row                                                   */
+  int32_t dtype;                        /* LGP_F32, LGP_F16 or LGP_BF16: of the activations                  */
+  int8_t* values;                       /* [tokens][width rounded up to 16], aligned to 16 bytes             */
+  uint8_t* exps;                        /* [tokens][(width + 31) / 32]                                       */
+  const int32_t* pos;                   /* tokens entries, or NULL; a negative one: there is no token in this
+                                           row, it is packed as zeros and its row of dy counts for nothing   */
+} lgp_packed;
+
+/* x: x_row elements from row to row, consecutive within one; no alignment beyond that of an element is needed. */
+int lgp_pack_activations(int device, const void* x, int64_t x_row, const lgp_packed* out, void* stream);
+/* x: [tokens, width], rows end to end, in the type that came. */
+int lgp_unpack_activations(int device, const lgp_packed* in, void* x, void* stream);
+
+/* Gradients of a linear layer y = x W^T + b from its packed input: dw [out, width] = sum over tokens of dy^T x and db [out] = sum of dy (NULL:
+ * not wanted), both fp32, added up in fp32 from exact products.  dy: fp16 or bf16, dy_row elements from row to row; fp16 only if x came in
+ * fp16. */
+int lgp_packed_weight_grad_workspace(int device, const lgp_packed* x, int32_t out, size_t* bytes);
+int lgp_packed_weight_grad(int device, const lgp_packed* x, const void* dy, int64_t dy_row, int32_t dy_dtype, int32_t out, float* dw, float* db,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 const char* lgp_strerror(int status);
 const char* lgp_last_error(const lgp_ctx* ctx); /* text of the last failure on this context */
 

@@ -53,6 +53,29 @@ class _BlocksOut(C.Structure):
                 ("feat_row", C.c_void_p * (MAX_HOPS + 1))]
 
 
+class _Documents(C.Structure):
+    _fields_ = [("n_docs", C.c_int64), ("q_rows", C.c_int64), ("k_rows", C.c_int64), ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p),
+                ("q_lens", C.c_void_p), ("k_lens", C.c_void_p), ("q_pos", C.c_void_p), ("k_pos", C.c_void_p)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64),
+                ("k_head", C.c_int64), ("v_row", C.c_int64), ("v_head", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("dim", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("q_row", C.c_int64), ("q_head", C.c_int64), ("k_row", C.c_int64), ("k_head", C.c_int64),
+                ("tokens", C.c_int64), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("dtype", C.c_int32),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("pos", C.c_void_p), ("rot", C.c_int32), ("n_pos", C.c_int32),
+                ("table", C.c_void_p), ("eps", C.c_float)]
+
+
+class _Packed(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32), ("values", C.c_void_p), ("exps", C.c_void_p),
+                ("pos", C.c_void_p)]
+
+
 class Profile(C.Structure):
     _fields_ = [("n_sample", C.c_int64), ("n_partition", C.c_int64), ("n_hit", C.c_int64), ("n_miss", C.c_int64),
                 ("ms_sample", C.c_double), ("ms_partition", C.c_double), ("ms_hit", C.c_double),
@@ -63,6 +86,8 @@ EXPORTS = ["lgp_host_alloc", "lgp_host_free", "lgp_shuffle_tablet", "lgp_create"
            "lgp_set_hotness", "lgp_plan_cache", "lgp_search_cache_plan", "lgp_cslp", "lgp_build_cache", "lgp_build_clique_cache", "lgp_get_clique_plan",
            "lgp_gather_features_clique", "lgp_get_cache_plan", "lgp_get_cache", "lgp_get_cache_part", "lgp_reserve",
            "lgp_sample_khop", "lgp_sample_extract", "lgp_build_blocks", "lgp_gather_features", "lgp_gather_features_static", "lgp_set_overlap", "lgp_workspace_bytes", "lgp_check", "lgp_set_wait_polls", "lgp_get_sample_marks", "lgp_set_profiling", "lgp_get_profile",
+           "lgp_attend", "lgp_attend_workspace", "lgp_attend_backward", "lgp_norm_rotate", "lgp_norm_rotate_workspace", "lgp_norm_rotate_backward",
+           "lgp_pack_activations", "lgp_unpack_activations", "lgp_packed_weight_grad_workspace", "lgp_packed_weight_grad",
            "lgp_strerror", "lgp_last_error"]
 
 _lib = None
@@ -112,6 +137,16 @@ def load_library():
     L.lgp_get_sample_marks.argtypes = [vp, vp]
     L.lgp_set_profiling.argtypes = [vp, C.c_int]
     L.lgp_get_profile.argtypes = [vp, C.POINTER(Profile)]
+    L.lgp_attend.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_attend_workspace.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), C.c_int, vp]
+    L.lgp_attend_backward.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_norm_rotate.argtypes = [C.c_int, C.POINTER(_Heads), vp, vp, vp]
+    L.lgp_norm_rotate_workspace.argtypes = [C.c_int, C.POINTER(_Heads), vp]
+    L.lgp_norm_rotate_backward.argtypes = [C.c_int, C.POINTER(_Heads), vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_pack_activations.argtypes = [C.c_int, vp, i64, C.POINTER(_Packed), vp]
+    L.lgp_unpack_activations.argtypes = [C.c_int, C.POINTER(_Packed), vp, vp]
+    L.lgp_packed_weight_grad_workspace.argtypes = [C.c_int, C.POINTER(_Packed), i32, vp]
+    L.lgp_packed_weight_grad.argtypes = [C.c_int, C.POINTER(_Packed), vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
     L.lgp_strerror.argtypes = [C.c_int]
     L.lgp_strerror.restype = C.c_char_p
     L.lgp_last_error.argtypes = [vp]

@@ -1,0 +1,62 @@
+// Attention inside documents: what the forward and the backward kernels share.
+#pragma once
+
+#include "layer_dev.hpp"
+
+namespace lgp {
+namespace layer {
+
+// Queries are handled as folded rows: the G query heads of a key head are G rows of each token, row t * G + g of key head hk being head
+// hk * G + g of token t.  Keys and values are then read once for all of them, single tokens fill tiles, and the sum over the heads that
+// share a key head is a sum over rows.
+struct AttendParams {
+  const void *q, *k, *v;
+  int64_t q_row, q_head, k_row, k_head, v_row, v_head;
+  Side qs, ks;
+  int32_t n_docs, heads, kv_heads, group, dim;
+  // Scores in powers of two: z * log2(e) = capped ? tanh(qk * scale / cap) * cap * log2(e) : qk * scale * log2(e).
+  float scale, z_mul;        // z_mul: scale * log2(e), or cap * log2(e)
+  float t_mul;               // 2 * log2(e) * scale / cap, so that tanh = 1 - 2 / (exp2(qk * t_mul) + 1)
+  const float* slopes;
+  int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys
+  // forward
+  void *out, *rest;
+  float* lse;
+  float *part_o, *part_ml;   // [split][q_rows][heads][dim] and [split][q_rows][heads][2], if splits > 1
+  // backward
+  const void* d_out;
+  const float* lse_in;
+  void *dq, *dk, *dv;
+  float* delta;              // [q_rows][heads]: d_out . out
+  float* sums;               // [split][q_rows][heads][3], if the gradient of the slopes is wanted: see attend_dq_kernel
+};
+
+template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p) { return *reinterpret_cast<const vec8<T>*>(p); }
+template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
+
+// 2^(z * log2(e)) needs z in powers of two; the tanh of the cap is kept for the backward pass.
+template <bool CAP> __device__ __forceinline__ float score(const AttendParams& p, float qk, float& tanh_out) {
+  if constexpr (CAP) {
+    tanh_out = 1.f - 2.f * rcp_fast(exp2_fast(qk * p.t_mul) + 1.f);
+    return tanh_out * p.z_mul;
+  }
+  return qk * p.z_mul;
+}
+
+// The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys.
+__device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, int32_t splits, int32_t& begin, int32_t& end) {
+  const int32_t tiles = (keys + size - 1) / size, each = (tiles + splits - 1) / splits;
+  begin = s * each * size < keys ? s * each * size : keys;
+  end = (s + 1) * each * size < keys ? (s + 1) * each * size : keys;
+}
+
+int check_attend(const lgp_documents* d, const lgp_attention* a);
+AttendParams attend_params(const lgp_documents* d, const lgp_attention* a);
+
+// Launch shapes, chosen on the host by what it knows: rows and documents.
+constexpr int kForwardRows = 32;        // folded rows of a wave
+struct ForwardShape { int waves; int64_t tiles; int splits; };
+ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a);
+
+}  // namespace layer
+}  // namespace lgp

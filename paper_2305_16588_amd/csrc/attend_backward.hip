@@ -1,0 +1,470 @@
+// Attention inside documents, backward.  Scores are computed again, in two kernels: one has a wave per 32 queries and walks over the keys
+// (gradients of q and of the slopes), the other a wave per 32 keys and walks over the queries (gradients of k and v).  Seven products
+// instead of the five of a single kernel, and no sum in memory: nothing depends on the order in which workgroups finish.
+#include "attend.hpp"
+
+#include <algorithm>
+
+namespace lgp {
+namespace layer {
+namespace {
+
+// With fp16 a probability below 2^-14 would lose digits, and over 16 000 keys most are: the second product takes them times 2^12, which
+// cannot overflow, and its result times 2^-12.
+template <typename T> constexpr float kLift = 1.f;
+template <> constexpr float kLift<f16> = 4096.f;
+template <typename T> constexpr float kLiftLog2 = 0.f;
+template <> constexpr float kLiftLog2<f16> = 12.f;
+
+// Gradient of q: with u = scale * q.k, z the score, P = exp(z - lse), dP = d_out . v and delta = d_out . out,
+//     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
+// Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
+// delta is taken from out and what its rounding took off.  The slope of a head has the gradient
+//     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|)),
+// whose three sums per row go to `sums`: so it does not depend on how out was rounded.
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
+__global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p) {
+  constexpr int kThreads = 64 * NW, kRows = 32 * NW;
+  __shared__ __align__(16) T lds_k[BN * D];
+  __shared__ __align__(16) T lds_v[BN * D];
+  __shared__ __align__(16) float lds_pos[BIAS ? BN : 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t split = 0, hk, tile;
+  if constexpr (NW == 1) {
+    hk = piece % p.kv_heads;
+    piece /= p.kv_heads;
+    split = piece % p.splits;
+    tile = piece / p.splits;
+  } else {
+    tile = piece % p.tiles;
+    piece /= p.tiles;
+    split = piece % p.splits;
+    hk = piece / p.splits;
+  }
+  const int32_t doc = document_of(p.qs, p.n_docs, p.group, kRows, tile, lane);
+  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
+  const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
+  if (row0 < 0 || row0 >= qd.owned * p.group) return;
+
+  const int32_t row = row0 + 32 * wave + col;
+  const bool live = row < qd.tokens * p.group;
+  const int32_t token = qd.begin + row / p.group, head = hk * p.group + row % p.group;
+  const int64_t at_out = int64_t(token) * p.heads + head;
+  vec8<T> qf[D / 16], df[D / 16];
+  float delta = 0.f;
+  {
+    const T* q = static_cast<const T*>(p.q) + int64_t(token) * p.q_row + int64_t(head) * p.q_head;
+    const T* g = static_cast<const T*>(p.d_out) + at_out * p.dim;
+    const T* o = static_cast<const T*>(p.out) + at_out * p.dim;
+    const T* o2 = p.rest ? static_cast<const T*>(p.rest) + at_out * p.dim : nullptr;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const int d = 16 * kk + 8 * half;
+      const bool there = live && d < p.dim;
+      qf[kk] = there ? load8(q + d) : zero8<T>();
+      df[kk] = there ? load8(g + d) : zero8<T>();
+      const vec8<T> of = there ? load8(o + d) : zero8<T>(), o2f = there && o2 ? load8(o2 + d) : zero8<T>();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) delta += float(df[kk][i]) * (float(of[i]) + float(o2f[i]));
+    }
+  }
+  delta += other_half(delta);
+  float lse = INFINITY;           // no probability where there is no token or no key
+  float slope = 0.f, at = 0.f;
+  if (live) {
+    lse = p.lse_in[at_out] * kLog2e;
+    if (lse == -INFINITY) lse = INFINITY;
+    if constexpr (BIAS) {
+      slope = p.slopes[head] * kLog2e;
+      at = float(p.qs.pos[token]);
+    }
+    if (split == 0 && half == 0) p.delta[at_out] = delta;
+  }
+
+  floatx16 dq[D / 32] = {};
+  float sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
+  int32_t k_begin, k_end;
+  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
+  const T* kp = static_cast<const T*>(p.k) + int64_t(hk) * p.k_head;
+  const T* vp = static_cast<const T*>(p.v) + int64_t(hk) * p.v_head;
+
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN) {
+    constexpr int kChunks = BN * D / 8;
+#pragma unroll
+    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
+      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
+      if (kChunks % kThreads == 0 || i < kChunks) {
+        const bool there = k0 + r < k_end && d < p.dim;
+        const int64_t key = int64_t(kd.begin) + k0 + r;
+        const vec8<T> kv = there ? load8(kp + key * p.k_row + d) : zero8<T>();
+        const vec8<T> vv = there ? load8(vp + key * p.v_row + d) : zero8<T>();
+        *reinterpret_cast<vec8<T>*>(lds_k + chunk_at<D>(r, d / 8)) = kv;
+        *reinterpret_cast<vec8<T>*>(lds_v + chunk_at<D>(r, d / 8)) = vv;
+      }
+    }
+    if constexpr (BIAS) {
+      for (int i = tid; i < BN; i += kThreads) lds_pos[i] = k0 + i < k_end ? float(p.ks.pos[kd.begin + k0 + i]) : 0.f;
+    }
+    __syncthreads();
+    const bool whole = k0 + BN <= k_end;
+#pragma unroll
+    for (int b = 0; b < BN / 32; ++b) {
+      floatx16 s = {}, g = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], s);
+        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_v + chunk_at<D>(32 * b + col, 2 * kk + half)), df[kk], g);
+      }
+      vec8<T> uf[2];
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        floatx4 kpos = {};
+        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(lds_pos + 32 * b + 8 * r4 + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * r4 + i;
+          float t = 0.f, z = score<CAP>(p, s[r], t), far = 0.f;
+          if constexpr (BIAS) {
+            far = fabsf(at - kpos[i]);
+            z -= slope * far;
+          }
+          float e = exp2_fast(z - lse);
+          if (!whole && k0 + 32 * b + 8 * r4 + 4 * half + i >= k_end) e = 0.f;
+          if constexpr (BIAS) {
+            const float pd = e * g[r];
+            sum_pd += pd;
+            sum_pf += e * far;
+            sum_pdf += pd * far;
+          }
+          float u = e * (g[r] - delta);
+          if constexpr (CAP) u *= 1.f - t * t;
+          uf[r / 8][r % 8] = T(u);
+        }
+      }
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(transposed8<T, D>(lds_k, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dq[db]);
+    }
+    __syncthreads();
+  }
+
+  if (row >= qd.owned * p.group) return;
+  if constexpr (BIAS) {
+    sum_pd += other_half(sum_pd);
+    sum_pf += other_half(sum_pf);
+    sum_pdf += other_half(sum_pdf);
+    if (p.sums && half == 0) {
+      float* x = p.sums + (int64_t(split) * p.qs.rows * p.heads + at_out) * 3;
+      x[0] = live ? sum_pd : 0.f;
+      x[1] = live ? sum_pf : 0.f;
+      x[2] = live ? sum_pdf : 0.f;
+    }
+  }
+  float* part = p.splits > 1 ? p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim : nullptr;
+  T* out = static_cast<T*>(p.dq) + at_out * p.dim;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d = 32 * db + 8 * r4 + 4 * half;
+      if (d < p.dim) {
+        floatx4 x = {};
+        if (live) x = floatx4{dq[db][4 * r4], dq[db][4 * r4 + 1], dq[db][4 * r4 + 2], dq[db][4 * r4 + 3]} * p.scale;
+        if (part) *reinterpret_cast<floatx4*>(part + d) = x;
+        else *reinterpret_cast<vec4<T>*>(out + d) = vec4<T>{T(x[0]), T(x[1]), T(x[2]), T(x[3])};
+      }
+    }
+}
+
+// Adds the parts of dq.  A thread has four elements of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
+  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4, all = int64_t(p.qs.rows) * p.heads * p.dim;
+  if (i >= all) return;
+  floatx4 x = {};
+  for (int32_t s = 0; s < p.splits; ++s) x += *reinterpret_cast<const floatx4*>(p.part_o + s * all + i);
+  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.dq) + i) = vec4<T>{T(x[0]), T(x[1]), T(x[2]), T(x[3])};
+}
+
+// Gradient of the slopes from the sums of all rows, in two steps of a fixed order: kSlopeGroups workgroups take every kSlopeGroups-th token
+// of a head, then one adds theirs.
+constexpr int kSlopeGroups = 64;
+__device__ __forceinline__ float workgroup_sum(float x, float* lds) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return lds[0] + lds[1] + lds[2] + lds[3];
+}
+__global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, float* partial) {
+  __shared__ float lds[4];
+  const int32_t head = blockIdx.x;
+  const int64_t rows = int64_t(p.qs.rows) * p.heads;
+  float x = 0.f;
+  for (int64_t t = int64_t(blockIdx.y) * 256 + threadIdx.x; t < p.qs.rows; t += kSlopeGroups * 256) {
+    float pd = 0.f, pf = 0.f, pdf = 0.f;
+    for (int32_t s = 0; s < p.splits; ++s) {
+      const float* m = p.sums + (s * rows + t * p.heads + head) * 3;
+      pd += m[0];
+      pf += m[1];
+      pdf += m[2];
+    }
+    x -= pdf - pd * pf;
+  }
+  x = workgroup_sum(x, lds);
+  if (threadIdx.x == 0) partial[head * kSlopeGroups + blockIdx.y] = x;
+}
+__global__ __launch_bounds__(64) void slopes_end_kernel(const float* partial, float* out) {
+  float x = partial[blockIdx.x * kSlopeGroups + threadIdx.x];
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
+  if (threadIdx.x == 0) out[blockIdx.x] = x;
+}
+
+// Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
+//     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
+__global__ __launch_bounds__(64 * NW) void attend_dkv_kernel(const AttendParams p) {
+  constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
+  __shared__ __align__(16) T lds_q[BQ * D];
+  __shared__ __align__(16) T lds_g[BQ * D];
+  __shared__ __align__(16) float lds_row[4][BQ];       // lse, delta, slope, position
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t hk, tile;
+  if constexpr (NW == 1) {
+    hk = piece % p.kv_heads;
+    tile = piece / p.kv_heads;
+  } else {
+    tile = piece % p.tiles;
+    hk = piece / p.tiles;
+  }
+  const int32_t doc = document_of(p.ks, p.n_docs, 1, kKeys, tile, lane);
+  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
+  const int32_t key0 = (tile - first_tile(p.ks, doc, p.n_docs, 1, kKeys)) * kKeys;
+  if (key0 < 0 || key0 >= kd.owned) return;
+
+  const int32_t key = key0 + 32 * wave + col;
+  const bool live = key < kd.tokens;
+  const int64_t key_row = int64_t(kd.begin) + key;
+  vec8<T> kf[D / 16], vf[D / 16];
+  {
+    const T* k = static_cast<const T*>(p.k) + key_row * p.k_row + int64_t(hk) * p.k_head;
+    const T* v = static_cast<const T*>(p.v) + key_row * p.v_row + int64_t(hk) * p.v_head;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const int d = 16 * kk + 8 * half;
+      kf[kk] = live && d < p.dim ? load8(k + d) : zero8<T>();
+      vf[kk] = live && d < p.dim ? load8(v + d) : zero8<T>();
+    }
+  }
+  float at = 0.f;
+  if constexpr (BIAS) at = live ? float(p.ks.pos[key_row]) : 0.f;
+
+  floatx16 dk[D / 32] = {}, dv[D / 32] = {};
+  const int32_t rows = key0 < kd.tokens ? qd.tokens * p.group : 0;
+  for (int32_t r0 = 0; r0 < rows; r0 += BQ) {
+    constexpr int kChunks = BQ * D / 8;
+#pragma unroll
+    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
+      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
+      if (kChunks % kThreads == 0 || i < kChunks) {
+        const bool there = r0 + r < rows && d < p.dim;
+        const int64_t token = qd.begin + (r0 + r) / p.group, head = hk * p.group + (r0 + r) % p.group;
+        const vec8<T> qv = there ? load8(static_cast<const T*>(p.q) + token * p.q_row + head * p.q_head + d) : zero8<T>();
+        const vec8<T> gv = there ? load8(static_cast<const T*>(p.d_out) + (token * p.heads + head) * p.dim + d) : zero8<T>();
+        *reinterpret_cast<vec8<T>*>(lds_q + chunk_at<D>(r, d / 8)) = qv;
+        *reinterpret_cast<vec8<T>*>(lds_g + chunk_at<D>(r, d / 8)) = gv;
+      }
+    }
+    for (int i = tid; i < BQ; i += kThreads) {
+      float lse = INFINITY, delta = 0.f, slope = 0.f, pos = 0.f;
+      if (r0 + i < rows) {
+        const int64_t token = qd.begin + (r0 + i) / p.group, head = hk * p.group + (r0 + i) % p.group;
+        lse = p.lse_in[token * p.heads + head] * kLog2e;
+        if (lse == -INFINITY) lse = INFINITY;
+        delta = p.delta[token * p.heads + head];
+        if constexpr (BIAS) {
+          slope = p.slopes[head] * kLog2e;
+          pos = float(p.qs.pos[token]);
+        }
+      }
+      lds_row[0][i] = lse - kLiftLog2<T>;
+      lds_row[1][i] = delta;
+      lds_row[2][i] = slope;
+      lds_row[3][i] = pos;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int b = 0; b < BQ / 32; ++b) {
+      floatx16 s = {}, g = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_q + chunk_at<D>(32 * b + col, 2 * kk + half)), kf[kk], s);
+        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_g + chunk_at<D>(32 * b + col, 2 * kk + half)), vf[kk], g);
+      }
+      vec8<T> pf[2], uf[2];
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int r_at = 32 * b + 8 * r4 + 4 * half;
+        const floatx4 lse = *reinterpret_cast<const floatx4*>(&lds_row[0][r_at]), delta = *reinterpret_cast<const floatx4*>(&lds_row[1][r_at]);
+        floatx4 slope = {}, pos = {};
+        if constexpr (BIAS) {
+          slope = *reinterpret_cast<const floatx4*>(&lds_row[2][r_at]);
+          pos = *reinterpret_cast<const floatx4*>(&lds_row[3][r_at]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * r4 + i;
+          float t = 0.f, z = score<CAP>(p, s[r], t);
+          if constexpr (BIAS) z -= slope[i] * fabsf(at - pos[i]);
+          const float e = exp2_fast(z - lse[i]);             // times kLift
+          float u = e * ((g[r] - delta[i]) * (1.f / kLift<T>));
+          if constexpr (CAP) u *= 1.f - t * t;
+          pf[r / 8][r % 8] = T(e);
+          uf[r / 8][r % 8] = T(u);
+        }
+      }
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) {
+          dv[db] = Elem<T>::mfma(transposed8<T, D>(lds_g, 32 * b + 16 * h2, 32 * db, lane), pf[h2], dv[db]);
+          dk[db] = Elem<T>::mfma(transposed8<T, D>(lds_q, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dk[db]);
+        }
+    }
+    __syncthreads();
+  }
+
+  if (key >= kd.owned) return;
+  T* dk_out = static_cast<T*>(p.dk) + (key_row * p.kv_heads + hk) * p.dim;
+  T* dv_out = static_cast<T*>(p.dv) + (key_row * p.kv_heads + hk) * p.dim;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d = 32 * db + 8 * r4 + 4 * half;
+      if (d < p.dim) {
+        vec4<T> x, y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[i] = T(live ? dk[db][4 * r4 + i] * p.scale : 0.f);
+          y[i] = T(live ? dv[db][4 * r4 + i] * (1.f / kLift<T>) : 0.f);
+        }
+        *reinterpret_cast<vec4<T>*>(dk_out + d) = x;
+        *reinterpret_cast<vec4<T>*>(dv_out + d) = y;
+      }
+    }
+}
+
+struct BackwardShape {
+  ForwardShape q;             // of the kernel by queries
+  int key_waves;              // of the kernel by keys
+  int64_t key_tiles;
+  size_t delta, sums, parts, partial, bytes;      // offsets into the workspace, in floats; all of it, in bytes
+};
+BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
+  BackwardShape b;
+  b.q = forward_shape(device, d, a);
+  b.key_waves = d->k_rows <= 32 * std::max<int64_t>(d->n_docs, 1) ? 1 : 4;
+  b.key_tiles = tiles_of(d->k_rows, 1, d->n_docs, 32 * b.key_waves);
+  const size_t rows = size_t(d->q_rows) * a->heads;
+  auto up = [](size_t x) { return (x + 3) / 4 * 4; };
+  b.delta = 0;
+  b.sums = up(rows);
+  b.partial = b.sums + (a->slopes ? up(rows * 3 * b.q.splits) : 0);
+  b.parts = b.partial + (a->slopes ? size_t(a->heads) * kSlopeGroups : 0);
+  b.bytes = (b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0)) * sizeof(float);
+  return b;
+}
+
+template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const BackwardShape& b, hipStream_t s) {
+  AttendParams x = p;
+  x.tiles = int32_t(b.q.tiles);
+  const uint32_t blocks = uint32_t(b.q.tiles) * p.kv_heads * p.splits, key_blocks = uint32_t(b.key_tiles) * p.kv_heads;
+  if (p.qs.rows) {
+    if (b.q.waves == 1) attend_dq_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
+    else attend_dq_kernel<T, D, CAP, BIAS, 4, 64><<<blocks, 256, 0, s>>>(x);
+  }
+  x.tiles = int32_t(b.key_tiles);
+  if (p.ks.rows) {
+    if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<key_blocks, 64, 0, s>>>(x);
+    else attend_dkv_kernel<T, D, CAP, BIAS, 4, 64><<<key_blocks, 256, 0, s>>>(x);
+  }
+}
+template <typename T, int D> void launch(const AttendParams& p, const BackwardShape& b, bool cap, hipStream_t s) {
+  if (cap) p.slopes ? launch<T, D, true, true>(p, b, s) : launch<T, D, true, false>(p, b, s);
+  else p.slopes ? launch<T, D, false, true>(p, b, s) : launch<T, D, false, false>(p, b, s);
+}
+template <typename T> void launch(const AttendParams& p, const BackwardShape& b, bool cap, hipStream_t s) {
+  if (p.dim <= 32) launch<T, 32>(p, b, cap, s);
+  else if (p.dim <= 64) launch<T, 64>(p, b, cap, s);
+  else launch<T, 128>(p, b, cap, s);
+  if (p.splits > 1) {
+    const int64_t threads = int64_t(p.qs.rows) * p.heads * (p.dim / 4);
+    add_kernel<T><<<uint32_t((threads + 255) / 256), 256, 0, s>>>(p);
+  }
+}
+
+}  // namespace
+}  // namespace layer
+}  // namespace lgp
+
+using namespace lgp::layer;
+
+extern "C" {
+
+int lgp_attend_workspace(int device, const lgp_documents* docs, const lgp_attention* att, int backward, size_t* bytes) {
+  if (!bytes) return LGP_EINVAL;
+  *bytes = 0;
+  if (int st = check_attend(docs, att)) return st;
+  if (backward) {
+    *bytes = backward_shape(device, docs, att).bytes;
+  } else {
+    const ForwardShape f = forward_shape(device, docs, att);
+    if (f.splits > 1) *bytes = size_t(f.splits) * docs->q_rows * att->heads * (att->dim + 2) * sizeof(float);
+  }
+  return LGP_OK;
+}
+
+int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attention* att, const void* d_out, const void* out, const void* rest,
+                        const float* lse, void* dq, void* dk, void* dv, float* d_slopes, void* workspace, size_t workspace_bytes, void* stream) {
+  if (int st = check_attend(docs, att)) return st;
+  if (docs->q_rows && (!d_out || !out || !lse || !dq)) return LGP_EINVAL;
+  if (docs->k_rows && (!dk || !dv)) return LGP_EINVAL;
+  if (d_slopes && !att->slopes) return LGP_EINVAL;
+  if (!aligned16(d_out) || !aligned16(out) || !aligned16(rest) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv)) return LGP_EINVAL;
+  if (int st = use_device(device)) return st;
+  const BackwardShape b = backward_shape(device, docs, att);
+  const int64_t most = int64_t(1) << 31;
+  if (b.q.tiles * att->kv_heads * b.q.splits >= most || b.key_tiles * att->kv_heads >= most) return LGP_EUNSUPPORTED;
+  if (workspace_bytes < b.bytes) return LGP_ECAPACITY;
+  if (b.bytes && (!workspace || !aligned16(workspace))) return LGP_EINVAL;
+  AttendParams p = attend_params(docs, att);
+  float* w = static_cast<float*>(workspace);
+  p.splits = b.q.splits;
+  p.out = const_cast<void*>(out);
+  p.rest = const_cast<void*>(rest);
+  p.d_out = d_out;
+  p.lse_in = lse;
+  p.dq = dq;
+  p.dk = dk;
+  p.dv = dv;
+  p.delta = w + b.delta;
+  p.sums = d_slopes ? w + b.sums : nullptr;
+  p.part_o = w + b.parts;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
+  else launch<bf16>(p, b, att->cap > 0.f, s);
+  if (d_slopes) {
+    slopes_kernel<<<dim3(att->heads, kSlopeGroups), 256, 0, s>>>(p, w + b.partial);
+    slopes_end_kernel<<<att->heads, 64, 0, s>>>(w + b.partial, d_slopes);
+  }
+  return launched();
+}
+
+}  // extern "C"

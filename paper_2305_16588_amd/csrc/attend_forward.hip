@@ -1,0 +1,319 @@
+// Attention inside documents, forward: out = softmax(scores) v in one pass over the keys with a running maximum and sum.
+#include "attend.hpp"
+
+#include <algorithm>
+#include <cmath>
+
+namespace lgp {
+namespace layer {
+namespace {
+
+// A wave has 32 folded rows, as columns of the transposed scores S^T = K Q^T: every lane then holds scores of one row, so maximum and sum
+// need one exchange between the halves of the wave, and the rounded probabilities are the operand of O^T = V^T P^T as they stand
+// (layer_dev.hpp).  NW waves share the tiles of keys and values in LDS.  D is the head's dimension rounded up to 32, 64 or 128, with zeros.
+// Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
+__global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
+  constexpr int kThreads = 64 * NW, kRows = 32 * NW;
+  __shared__ __align__(16) T lds_k[BN * D];
+  __shared__ __align__(16) T lds_v[BN * D];
+  __shared__ __align__(16) float lds_pos[BIAS ? BN : 4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t split = 0, hk, tile;
+  if constexpr (NW == 1) {          // short documents: the heads of a token lie side by side in memory
+    hk = piece % p.kv_heads;
+    piece /= p.kv_heads;
+    split = piece % p.splits;
+    tile = piece / p.splits;
+  } else {                          // long ones: the tiles that share keys one after the other
+    tile = piece % p.tiles;
+    piece /= p.tiles;
+    split = piece % p.splits;
+    hk = piece / p.splits;
+  }
+  const int32_t doc = document_of(p.qs, p.n_docs, p.group, kRows, tile, lane);
+  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
+  const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
+  if (row0 < 0 || row0 >= qd.owned * p.group) return;
+
+  const int32_t row = row0 + 32 * wave + col;
+  const bool live = row < qd.tokens * p.group;
+  const int32_t token = qd.begin + row / p.group, head = hk * p.group + row % p.group;
+  vec8<T> qf[D / 16];
+  {
+    const T* q = static_cast<const T*>(p.q) + int64_t(token) * p.q_row + int64_t(head) * p.q_head;
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      const int d = 16 * kk + 8 * half;
+      qf[kk] = live && d < p.dim ? load8(q + d) : zero8<T>();
+    }
+  }
+  float slope = 0.f, at = 0.f;
+  if constexpr (BIAS) {
+    if (live) {
+      slope = p.slopes[head] * kLog2e;
+      at = float(p.qs.pos[token]);
+    }
+  }
+
+  floatx16 o[D / 32] = {};
+  float top = -INFINITY, sum = 0.f;
+  int32_t k_begin, k_end;
+  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
+  const T* kp = static_cast<const T*>(p.k) + int64_t(hk) * p.k_head;
+  const T* vp = static_cast<const T*>(p.v) + int64_t(hk) * p.v_head;
+
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN) {
+    constexpr int kChunks = BN * D / 8;
+#pragma unroll
+    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
+      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
+      if (kChunks % kThreads == 0 || i < kChunks) {
+        const bool there = k0 + r < k_end && d < p.dim;
+        const int64_t key = int64_t(kd.begin) + k0 + r;
+        const vec8<T> kv = there ? load8(kp + key * p.k_row + d) : zero8<T>();
+        const vec8<T> vv = there ? load8(vp + key * p.v_row + d) : zero8<T>();
+        *reinterpret_cast<vec8<T>*>(lds_k + chunk_at<D>(r, d / 8)) = kv;
+        *reinterpret_cast<vec8<T>*>(lds_v + chunk_at<D>(r, d / 8)) = vv;
+      }
+    }
+    if constexpr (BIAS) {
+      for (int i = tid; i < BN; i += kThreads) lds_pos[i] = k0 + i < k_end ? float(p.ks.pos[kd.begin + k0 + i]) : 0.f;
+    }
+    __syncthreads();
+
+    floatx16 s[BN / 32];
+#pragma unroll
+    for (int b = 0; b < BN / 32; ++b) {
+      floatx16 acc = {};
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const vec8<T> kf = *reinterpret_cast<const vec8<T>*>(lds_k + chunk_at<D>(32 * b + col, 2 * kk + half));
+        acc = Elem<T>::mfma(kf, qf[kk], acc);
+      }
+      s[b] = acc;
+    }
+    float most = -INFINITY;
+    const bool whole = k0 + BN <= k_end;
+#pragma unroll
+    for (int b = 0; b < BN / 32; ++b) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        floatx4 kpos = {};
+        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(lds_pos + 32 * b + 8 * r4 + 4 * half);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float t, z = score<CAP>(p, s[b][4 * r4 + i], t);
+          if constexpr (BIAS) z -= slope * fabsf(at - kpos[i]);
+          if (!whole && k0 + 32 * b + 8 * r4 + 4 * half + i >= k_end) z = -INFINITY;
+          s[b][4 * r4 + i] = z;
+          most = fmaxf(most, z);
+        }
+      }
+    }
+    most = fmaxf(most, other_half(most));
+    const float new_top = fmaxf(top, most);
+    const float base = new_top == -INFINITY ? 0.f : new_top;      // a row whose scores are all -inf keeps a sum of zero
+    const float shrink = exp2_fast(top - base);
+    top = new_top;
+    sum *= shrink;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
+#pragma unroll
+    for (int b = 0; b < BN / 32; ++b) {
+#pragma unroll
+      for (int h2 = 0; h2 < 2; ++h2) {
+        vec8<T> pf;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float e = exp2_fast(s[b][8 * h2 + j] - base);
+          sum += e;
+          pf[j] = T(e);
+        }
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(transposed8<T, D>(lds_v, 32 * b + 16 * h2, 32 * db, lane), pf, o[db]);
+      }
+    }
+    __syncthreads();
+  }
+
+  sum += other_half(sum);
+  if (row >= qd.owned * p.group) return;
+  const int64_t at_out = int64_t(token) * p.heads + head;
+  if (p.splits > 1) {
+    float* po = p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int d = 32 * db + 8 * r4 + 4 * half;
+        if (d < p.dim) {
+          floatx4 x = {};
+          if (live) x = floatx4{o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]};
+          *reinterpret_cast<floatx4*>(po + d) = x;
+        }
+      }
+    if (half == 0) {
+      float* ml = p.part_ml + (int64_t(split) * p.qs.rows * p.heads + at_out) * 2;
+      ml[0] = live ? top : -INFINITY;
+      ml[1] = live ? sum : 0.f;
+    }
+    return;
+  }
+  const float inv = sum > 0.f ? 1.f / sum : sum;        // zero keys: zeros; NaN stays
+  T* out = static_cast<T*>(p.out) + at_out * p.dim;
+  T* rest = p.rest ? static_cast<T*>(p.rest) + at_out * p.dim : nullptr;
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int d = 32 * db + 8 * r4 + 4 * half;
+      if (d < p.dim) {
+        vec4<T> x, y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float f = live ? o[db][4 * r4 + i] * inv : 0.f;
+          x[i] = T(f);
+          y[i] = T(f - float(x[i]));
+        }
+        *reinterpret_cast<vec4<T>*>(out + d) = x;
+        if (rest) *reinterpret_cast<vec4<T>*>(rest + d) = y;
+      }
+    }
+  if (half == 0) p.lse[at_out] = live && sum != 0.f ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
+}
+
+// Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A thread has four elements of a row.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
+  const int32_t per_row = p.dim / 4;
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, row = i / per_row, rows = int64_t(p.qs.rows) * p.heads;
+  if (row >= rows) return;
+  const int d = int(i % per_row) * 4;
+  float top = -INFINITY;
+  for (int32_t s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[(s * rows + row) * 2]);
+  const float base = top == -INFINITY ? 0.f : top;
+  floatx4 o = {};
+  float sum = 0.f;
+  for (int32_t s = 0; s < p.splits; ++s) {
+    const float w = exp2_fast(p.part_ml[(s * rows + row) * 2] - base);
+    sum += w * p.part_ml[(s * rows + row) * 2 + 1];
+    o += w * *reinterpret_cast<const floatx4*>(p.part_o + (s * rows + row) * p.dim + d);
+  }
+  const float inv = sum > 0.f ? 1.f / sum : sum;
+  vec4<T> x, y;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[j] = T(o[j] * inv);
+    y[j] = T(o[j] * inv - float(x[j]));
+  }
+  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.out) + row * p.dim + d) = x;
+  if (p.rest) *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.rest) + row * p.dim + d) = y;
+  if (d == 0) p.lse[row] = sum != 0.f ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
+}
+
+template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, int waves, hipStream_t s) {
+  const uint32_t blocks = uint32_t(p.tiles) * p.kv_heads * p.splits;
+  if (waves == 1) attend_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(p);
+  else attend_kernel<T, D, CAP, BIAS, 4, 64><<<blocks, 256, 0, s>>>(p);
+}
+template <typename T, int D> void launch(const AttendParams& p, int waves, bool cap, hipStream_t s) {
+  if (cap) p.slopes ? launch<T, D, true, true>(p, waves, s) : launch<T, D, true, false>(p, waves, s);
+  else p.slopes ? launch<T, D, false, true>(p, waves, s) : launch<T, D, false, false>(p, waves, s);
+}
+template <typename T> void launch(const AttendParams& p, int waves, bool cap, hipStream_t s) {
+  if (p.dim <= 32) launch<T, 32>(p, waves, cap, s);
+  else if (p.dim <= 64) launch<T, 64>(p, waves, cap, s);
+  else launch<T, 128>(p, waves, cap, s);
+  if (p.splits > 1) {
+    const int64_t threads = int64_t(p.qs.rows) * p.heads * (p.dim / 4);
+    join_kernel<T><<<uint32_t((threads + 255) / 256), 256, 0, s>>>(p);
+  }
+}
+
+}  // namespace
+
+int check_attend(const lgp_documents* d, const lgp_attention* a) {
+  if (!d || !a) return LGP_EINVAL;
+  if (d->n_docs < 0 || d->q_rows < 0 || d->k_rows < 0 || a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads || a->dim < 1) return LGP_EINVAL;
+  if (d->n_docs == 0 && (d->q_rows || d->k_rows)) return LGP_EINVAL;
+  if (a->dtype != LGP_F16 && a->dtype != LGP_BF16) return LGP_EUNSUPPORTED;
+  if (a->dim % 8 || a->dim > 128) return LGP_EUNSUPPORTED;
+  if (!(a->cap >= 0.f) || !std::isfinite(a->cap) || !std::isfinite(a->scale)) return LGP_EINVAL;
+  // folded rows and rows of tiles are counted in 32 bits
+  const int64_t most = int64_t(1) << 31;
+  if (a->heads > 65536 || d->n_docs >= most / 512 || d->q_rows >= most / a->heads || d->k_rows >= most) return LGP_EUNSUPPORTED;
+  if (d->q_rows * a->heads + 256 * d->n_docs >= most || d->k_rows + 256 * d->n_docs >= most) return LGP_EUNSUPPORTED;
+  if (d->n_docs && (!d->q_offsets || !d->k_offsets)) return LGP_EINVAL;
+  if ((d->q_rows && !a->q) || (d->k_rows && (!a->k || !a->v))) return LGP_EINVAL;
+  if (a->slopes && ((d->q_rows && !d->q_pos) || (d->k_rows && !d->k_pos))) return LGP_EINVAL;
+  if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v)) return LGP_EINVAL;
+  if (a->q_row % 8 || a->q_head % 8 || a->k_row % 8 || a->k_head % 8 || a->v_row % 8 || a->v_head % 8) return LGP_EINVAL;
+  return LGP_OK;
+}
+
+AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
+  AttendParams p = {};
+  p.q = a->q; p.k = a->k; p.v = a->v;
+  p.q_row = a->q_row; p.q_head = a->q_head; p.k_row = a->k_row; p.k_head = a->k_head; p.v_row = a->v_row; p.v_head = a->v_head;
+  p.qs = {d->q_offsets, d->q_lens, d->q_pos, int32_t(d->q_rows)};
+  p.ks = {d->k_offsets, d->k_lens, d->k_pos, int32_t(d->k_rows)};
+  p.n_docs = int32_t(d->n_docs);
+  p.heads = a->heads; p.kv_heads = a->kv_heads; p.group = a->heads / a->kv_heads; p.dim = a->dim;
+  p.scale = a->scale;
+  p.z_mul = (a->cap > 0.f ? a->cap : a->scale) * kLog2e;
+  p.t_mul = a->cap > 0.f ? float(2.0 * double(kLog2e) * a->scale / a->cap) : 0.f;
+  p.slopes = a->slopes;
+  p.splits = 1;
+  return p;
+}
+
+// One wave with 32 keys at a time where documents are short, four with 64 where they are long.  Few tiles over long documents are split over
+// the keys until every CU has a few waves, at no less than 256 keys a part.
+ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
+  const int64_t group = a->heads / a->kv_heads, n = std::max<int64_t>(d->n_docs, 1);
+  ForwardShape f;
+  f.waves = d->q_rows * group <= 32 * n ? 1 : 4;
+  f.tiles = tiles_of(d->q_rows, group, d->n_docs, kForwardRows * f.waves);
+  const int64_t waves = f.tiles * a->kv_heads * f.waves, room = int64_t(compute_units(device)) * 8, keys = d->k_rows / n;
+  f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256, int64_t(256)})));
+  return f;
+}
+
+}  // namespace layer
+}  // namespace lgp
+
+using namespace lgp::layer;
+
+extern "C" {
+
+int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, void* out, void* rest, float* lse, void* workspace,
+               size_t workspace_bytes, void* stream) {
+  if (int st = check_attend(docs, att)) return st;
+  if (docs->q_rows && (!out || !lse || !aligned16(out) || !aligned16(rest))) return LGP_EINVAL;
+  if (int st = use_device(device)) return st;
+  if (docs->q_rows == 0) return LGP_OK;
+  const ForwardShape f = forward_shape(device, docs, att);
+  if (f.tiles * att->kv_heads * f.splits >= int64_t(1) << 31) return LGP_EUNSUPPORTED;
+  AttendParams p = attend_params(docs, att);
+  p.tiles = int32_t(f.tiles);
+  p.splits = f.splits;
+  p.out = out;
+  p.rest = rest;
+  p.lse = lse;
+  if (f.splits > 1) {
+    const size_t rows = size_t(f.splits) * docs->q_rows * att->heads;
+    if (workspace_bytes < rows * (att->dim + 2) * 4) return LGP_ECAPACITY;
+    if (!workspace || !aligned16(workspace)) return LGP_EINVAL;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_ml = p.part_o + rows * att->dim;
+  }
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (att->dtype == LGP_F16) launch<f16>(p, f.waves, att->cap > 0.f, s);
+  else launch<bf16>(p, f.waves, att->cap > 0.f, s);
+  return launched();
+}
+
+}  // extern "C"

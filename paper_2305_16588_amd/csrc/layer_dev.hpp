@@ -1,0 +1,138 @@
+// What the operators of a model layer share: element types, the 32x32x16 matrix instruction and its operand order, documents and
+// their tiles, host helpers of the entry points.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "legion_prep.h"
+
+namespace lgp {
+namespace layer {
+
+using f16 = _Float16;
+using bf16 = __bf16;
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+// The matrix instruction D[32, 32] += A[32, 16] B[16, 32].  Lane l holds of A row l % 32 and of B column l % 32, each at eight places of
+// the sum; of D it holds column l % 32, register r being row 8 * (r / 4) + 4 * (l / 32) + r % 4.  Any order of the sum's places does as
+// long as A and B agree, so registers 8 s .. 8 s + 7 of a D are, rounded, a B operand whose places are rows
+// 16 s + 8 * (j / 4) + 4 * (l / 32) + j % 4: a product is handed to the next one without leaving the registers, and the other operand is
+// read in that order (transposed4 below, two of them).
+template <typename T> struct Elem;
+template <> struct Elem<f16> {
+  typedef f16 x8 __attribute__((ext_vector_type(8)));
+  typedef f16 x4 __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Elem<bf16> {
+  typedef bf16 x8 __attribute__((ext_vector_type(8)));
+  typedef bf16 x4 __attribute__((ext_vector_type(4)));
+  static __device__ __forceinline__ floatx16 mfma(x8 a, x8 b, floatx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <typename T> using vec8 = typename Elem<T>::x8;
+template <typename T> using vec4 = typename Elem<T>::x4;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }     // one ulp, 0 and inf at the ends
+__device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_logf(x); }
+__device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// A tile of rows x D elements of 16 bits in LDS, D 32, 64 or 128: 16-byte chunk c of row r lies at place c ^ swizzle(r) of the row, so that
+// neither the lanes of a wave that read one chunk of 32 rows each, nor those that read four rows transposed, crowd on few banks.
+template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) {
+  constexpr int kChunks = D / 8;
+  const int s = kChunks >= 8 ? row & 7 : (row >> 1) & 3;
+  return row * D + ((chunk ^ s) << 3);
+}
+
+// Operand A or B with the places of the sum running along the rows of a tile: four elements of column (lane % 32) + col0, of rows
+// row0 + 4 * (lane / 32) ... + 3.  Each 16 lanes read four rows of 16 columns, which the LDS hands out transposed.
+template <int D> __device__ __forceinline__ shortx4 transposed4(const void* tile, int row0, int col0, int lane) {
+  const int i = lane & 15;
+  const int row = row0 + 4 * (lane >> 5) + (i >> 2);
+  const int col = col0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+  const short* p = static_cast<const short*>(tile) + chunk_at<D>(row, col >> 3) + (col & 7);
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p);
+}
+template <typename T, int D> __device__ __forceinline__ vec8<T> transposed8(const void* tile, int row0, int col0, int lane) {
+  union { shortx4 s[2]; vec8<T> v; } u;
+  u.s[0] = transposed4<D>(tile, row0, col0, lane);
+  u.s[1] = transposed4<D>(tile, row0 + 8, col0, lane);
+  return u.v;
+}
+
+// Documents: document d owns rows offsets[d] .. offsets[d + 1], the first lens[d] of which hold tokens.  The first begins at row 0 and the
+// last ends at the last row, whatever the array says there; what else makes no sense is clamped, so no row outside is ever touched.
+struct Side {
+  const int32_t* offsets;
+  const int32_t* lens;
+  const int32_t* pos;
+  int32_t rows;
+};
+struct Span { int32_t begin, tokens, owned; };       // first row, rows with a token, rows
+__device__ __forceinline__ int32_t offset_of(const Side& s, int32_t d, int32_t n) {
+  if (d <= 0) return 0;
+  if (d >= n) return s.rows;
+  const int32_t o = s.offsets[d];
+  return o < 0 ? 0 : o > s.rows ? s.rows : o;
+}
+__device__ __forceinline__ Span span_of(const Side& s, int32_t d, int32_t n) {
+  Span x;
+  x.begin = offset_of(s, d, n);
+  const int32_t end = offset_of(s, d + 1, n);
+  x.owned = end > x.begin ? end - x.begin : 0;
+  x.tokens = x.owned;
+  if (s.lens) {
+    const int32_t t = s.lens[d];
+    x.tokens = t < 0 ? 0 : t < x.owned ? t : x.owned;
+  }
+  return x;
+}
+
+// Tiles of `size` rows, found without a list of them: with `fold` rows per token, document d has the tiles from
+// floor(offset * fold / size) + d on, which leaves each at least as many as its rows take, and all of them rows * fold / size + n.  A wave
+// looks for the document of a tile among 64 candidates at a time: three dependent loads for 262 144 documents.
+__device__ __forceinline__ int32_t first_tile(const Side& s, int32_t d, int32_t n, int32_t fold, int32_t size) {
+  return int32_t(int64_t(offset_of(s, d, n)) * fold / size) + d;
+}
+__device__ __forceinline__ int32_t document_of(const Side& s, int32_t n, int32_t fold, int32_t size, int32_t tile, int lane) {
+  int32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int32_t step = (hi - lo + 63) / 64, d = lo + (lane + 1) * step;
+    const bool before = int64_t(lo) + int64_t(lane + 1) * step < hi && first_tile(s, d, n, fold, size) <= tile;
+    lo += step * __popcll(__ballot(before));
+    hi = hi < lo + step ? hi : lo + step;
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+inline int64_t tiles_of(int64_t rows, int64_t fold, int64_t n, int64_t size) { return rows * fold / size + n; }
+
+// Workgroups go to the eight XCDs in turn, and each XCD has an L2 of its own: consecutive pieces of work, which share rows, go to one XCD.
+__device__ __forceinline__ uint32_t piece_of(uint32_t block, uint32_t blocks) {
+  const uint32_t each = blocks / 8, more = blocks % 8, x = block % 8;
+  return x * each + (x < more ? x : more) + block / 8;
+}
+
+inline int use_device(int device) {
+  int n = 0;
+  if (hipGetDeviceCount(&n) != hipSuccess || device < 0 || device >= n || hipSetDevice(device) != hipSuccess) {
+    (void)hipGetLastError();
+    return LGP_EINVAL;
+  }
+  return LGP_OK;
+}
+inline int launched() { return hipGetLastError() == hipSuccess ? LGP_OK : LGP_EHIP; }
+inline int compute_units(int device) {
+  int n = 0;
+  return hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && n > 0 ? n : 256;
+}
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace layer
+}  // namespace lgp
