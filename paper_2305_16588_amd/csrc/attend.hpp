@@ -14,9 +14,13 @@ struct AttendParams {
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;
   Side qs, ks;
   int32_t n_docs, heads, kv_heads, group, dim;
-  // Scores in powers of two: z * log2(e) = capped ? tanh(qk * scale / cap) * cap * log2(e) : qk * scale * log2(e).
+  Divisor per_token;         // by group
+  // Scores in powers of two: z * log2(e) = capped ? tanh(qk * scale / cap) * cap * log2(e) : qk * scale * log2(e), with the magnitude of the
+  // scale: where it is negative, q (by keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the
+  // largest product is the largest score.
   float scale, z_mul;        // z_mul: scale * log2(e), or cap * log2(e)
   float t_mul;               // 2 * log2(e) * scale / cap, so that tanh = 1 - 2 / (exp2(qk * t_mul) + 1)
+  bool negate;
   const float* slopes;
   int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys
   // forward
@@ -32,6 +36,14 @@ struct AttendParams {
 };
 
 template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p) { return *reinterpret_cast<const vec8<T>*>(p); }
+template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool there, bool negate) {
+  union { vec8<T> v; uint32_t w[4]; } u = {};
+  if (there) u.v = load8(p);
+  if (negate)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.w[i] ^= 0x80008000u;
+  return u.v;
+}
 template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
 
 // 2^(z * log2(e)) needs z in powers of two; the tanh of the cap is kept for the backward pass.

@@ -23,11 +23,11 @@ template <> constexpr float kLiftLog2<f16> = 12.f;
 //     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|)),
 // whose three sums per row go to `sums`: so it does not depend on how out was rounded.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
-  __shared__ __align__(16) T lds_k[BN * D];
-  __shared__ __align__(16) T lds_v[BN * D];
-  __shared__ __align__(16) float lds_pos[BIAS ? BN : 4];
+  __shared__ __align__(16) T lds_k[2][BN * D];
+  __shared__ __align__(16) T lds_v[2][BN * D];
+  __shared__ __align__(16) float lds_pos[2][BIAS ? BN : 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
 
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
@@ -48,9 +48,34 @@ __global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p
   const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
   if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
+  int32_t k_begin, k_end;
+  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
+  const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
+  const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  auto stage = [&](int32_t k0, int to) {
+    auto k_of = [&](int r) { return kp + int64_t(k0 + r) * p.k_row; };
+    auto v_of = [&](int r) { return vp + int64_t(k0 + r) * p.v_row; };
+    if (k0 + BN <= k_end) {
+      copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, tid, k_of);
+      copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, tid, v_of);
+    } else {
+      fill_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, k_of);
+      fill_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, v_of);
+    }
+    if constexpr (BIAS) {
+      if (tid < BN) lds_pos[to][tid] = k0 + tid < k_end ? float(p.ks.pos[kd.begin + k0 + tid]) : 0.f;
+    }
+  };
+  if (p.dim < D) {
+    clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
+    clear_tile<T, 2 * BN * D, kThreads>(lds_v[0], tid);
+    __syncthreads();
+  }
+  if (k_begin < k_end) stage(k_begin, 0);
+
   const int32_t row = row0 + 32 * wave + col;
   const bool live = row < qd.tokens * p.group;
-  const int32_t token = qd.begin + row / p.group, head = hk * p.group + row % p.group;
+  const int32_t of_doc = quotient(row, p.per_token), token = qd.begin + of_doc, head = hk * p.group + row - of_doc * p.group;
   const int64_t at_out = int64_t(token) * p.heads + head;
   vec8<T> qf[D / 16], df[D / 16];
   float delta = 0.f;
@@ -58,14 +83,14 @@ __global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p
     const T* q = static_cast<const T*>(p.q) + int64_t(token) * p.q_row + int64_t(head) * p.q_head;
     const T* g = static_cast<const T*>(p.d_out) + at_out * p.dim;
     const T* o = static_cast<const T*>(p.out) + at_out * p.dim;
-    const T* o2 = p.rest ? static_cast<const T*>(p.rest) + at_out * p.dim : nullptr;
+    const T* o2 = static_cast<const T*>(p.rest) + at_out * p.dim;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const int d = 16 * kk + 8 * half;
       const bool there = live && d < p.dim;
-      qf[kk] = there ? load8(q + d) : zero8<T>();
-      df[kk] = there ? load8(g + d) : zero8<T>();
-      const vec8<T> of = there ? load8(o + d) : zero8<T>(), o2f = there && o2 ? load8(o2 + d) : zero8<T>();
+      qf[kk] = load8(q + d, there, p.negate);
+      df[kk] = load8(g + d, there, false);
+      const vec8<T> of = load8(o + d, there, false), o2f = load8(o2 + d, there && p.rest, false);
 #pragma unroll
       for (int i = 0; i < 8; ++i) delta += float(df[kk][i]) * (float(of[i]) + float(o2f[i]));
     }
@@ -85,43 +110,26 @@ __global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p
 
   floatx16 dq[D / 32] = {};
   float sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
-  int32_t k_begin, k_end;
-  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
-  const T* kp = static_cast<const T*>(p.k) + int64_t(hk) * p.k_head;
-  const T* vp = static_cast<const T*>(p.v) + int64_t(hk) * p.v_head;
-
-  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN) {
-    constexpr int kChunks = BN * D / 8;
-#pragma unroll
-    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
-      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
-      if (kChunks % kThreads == 0 || i < kChunks) {
-        const bool there = k0 + r < k_end && d < p.dim;
-        const int64_t key = int64_t(kd.begin) + k0 + r;
-        const vec8<T> kv = there ? load8(kp + key * p.k_row + d) : zero8<T>();
-        const vec8<T> vv = there ? load8(vp + key * p.v_row + d) : zero8<T>();
-        *reinterpret_cast<vec8<T>*>(lds_k + chunk_at<D>(r, d / 8)) = kv;
-        *reinterpret_cast<vec8<T>*>(lds_v + chunk_at<D>(r, d / 8)) = vv;
-      }
-    }
-    if constexpr (BIAS) {
-      for (int i = tid; i < BN; i += kThreads) lds_pos[i] = k0 + i < k_end ? float(p.ks.pos[kd.begin + k0 + i]) : 0.f;
-    }
+  int now = 0;
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
+    loads_done();
     __syncthreads();
-    const bool whole = k0 + BN <= k_end;
+    if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
+    const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
       floatx16 s = {}, g = {};
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], s);
-        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_v + chunk_at<D>(32 * b + col, 2 * kk + half)), df[kk], g);
+        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], s);
+        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_v + chunk_at<D>(32 * b + col, 2 * kk + half)), df[kk], g);
       }
+      const int32_t there = k0 + BN <= k_end ? BN : k_end - k0 - 32 * b - 4 * half;      // places of this block's half that are keys
       vec8<T> uf[2];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         floatx4 kpos = {};
-        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(lds_pos + 32 * b + 8 * r4 + 4 * half);
+        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
@@ -130,8 +138,7 @@ __global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p
             far = fabsf(at - kpos[i]);
             z -= slope * far;
           }
-          float e = exp2_fast(z - lse);
-          if (!whole && k0 + 32 * b + 8 * r4 + 4 * half + i >= k_end) e = 0.f;
+          const float e = 8 * r4 + i < there ? exp2_fast(z - lse) : 0.f;
           if constexpr (BIAS) {
             const float pd = e * g[r];
             sum_pd += pd;
@@ -146,9 +153,8 @@ __global__ __launch_bounds__(64 * NW) void attend_dq_kernel(const AttendParams p
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(transposed8<T, D>(lds_k, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dq[db]);
+        for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(transposed8<T, D>(tile_k, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dq[db]);
     }
-    __syncthreads();
   }
 
   if (row >= qd.owned * p.group) return;
@@ -227,11 +233,11 @@ __global__ __launch_bounds__(64) void slopes_end_kernel(const float* partial, fl
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
-__global__ __launch_bounds__(64 * NW) void attend_dkv_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_dkv_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
-  __shared__ __align__(16) T lds_q[BQ * D];
-  __shared__ __align__(16) T lds_g[BQ * D];
-  __shared__ __align__(16) float lds_row[4][BQ];       // lse, delta, slope, position
+  __shared__ __align__(16) T lds_q[2][BQ * D];
+  __shared__ __align__(16) T lds_g[2][BQ * D];
+  __shared__ __align__(16) float lds_row[2][4][BQ];       // lse, delta, slope, position
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
 
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
@@ -248,6 +254,51 @@ __global__ __launch_bounds__(64 * NW) void attend_dkv_kernel(const AttendParams 
   const int32_t key0 = (tile - first_tile(p.ks, doc, p.n_docs, 1, kKeys)) * kKeys;
   if (key0 < 0 || key0 >= kd.owned) return;
 
+  const int32_t rows = key0 < kd.tokens ? qd.tokens * p.group : 0;
+  const T* qp = static_cast<const T*>(p.q) + int64_t(qd.begin) * p.q_row + int64_t(hk) * p.group * p.q_head;
+  const T* gp = static_cast<const T*>(p.d_out) + (int64_t(qd.begin) * p.heads + int64_t(hk) * p.group) * p.dim;
+  auto stage = [&](int32_t r0, int to) {
+    auto q_of = [&](int r) {
+      const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
+      return qp + int64_t(t) * p.q_row + int64_t(g) * p.q_head;
+    };
+    auto g_of = [&](int r) {
+      const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
+      return gp + (int64_t(t) * p.heads + g) * p.dim;
+    };
+    if (r0 + BQ <= rows) {
+      copy_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, tid, q_of);
+      copy_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, tid, g_of);
+    } else {
+      fill_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, rows - r0, tid, q_of);
+      fill_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, rows - r0, tid, g_of);
+    }
+    for (int i = tid; i < BQ; i += kThreads) {
+      float lse = INFINITY, delta = 0.f, slope = 0.f, pos = 0.f;
+      if (r0 + i < rows) {
+        const uint32_t t = quotient(r0 + i, p.per_token), head = hk * p.group + r0 + i - t * p.group;
+        const int64_t token = qd.begin + int64_t(t);
+        lse = p.lse_in[token * p.heads + head] * kLog2e;
+        if (lse == -INFINITY) lse = INFINITY;
+        delta = p.delta[token * p.heads + head];
+        if constexpr (BIAS) {
+          slope = p.slopes[head] * kLog2e;
+          pos = float(p.qs.pos[token]);
+        }
+      }
+      lds_row[to][0][i] = lse - kLiftLog2<T>;
+      lds_row[to][1][i] = delta;
+      lds_row[to][2][i] = slope;
+      lds_row[to][3][i] = pos;
+    }
+  };
+  if (p.dim < D) {
+    clear_tile<T, 2 * BQ * D, kThreads>(lds_q[0], tid);
+    clear_tile<T, 2 * BQ * D, kThreads>(lds_g[0], tid);
+    __syncthreads();
+  }
+  if (rows > 0) stage(0, 0);
+
   const int32_t key = key0 + 32 * wave + col;
   const bool live = key < kd.tokens;
   const int64_t key_row = int64_t(kd.begin) + key;
@@ -258,64 +309,37 @@ __global__ __launch_bounds__(64 * NW) void attend_dkv_kernel(const AttendParams 
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       const int d = 16 * kk + 8 * half;
-      kf[kk] = live && d < p.dim ? load8(k + d) : zero8<T>();
-      vf[kk] = live && d < p.dim ? load8(v + d) : zero8<T>();
+      kf[kk] = load8(k + d, live && d < p.dim, p.negate);
+      vf[kk] = load8(v + d, live && d < p.dim, false);
     }
   }
   float at = 0.f;
   if constexpr (BIAS) at = live ? float(p.ks.pos[key_row]) : 0.f;
 
   floatx16 dk[D / 32] = {}, dv[D / 32] = {};
-  const int32_t rows = key0 < kd.tokens ? qd.tokens * p.group : 0;
-  for (int32_t r0 = 0; r0 < rows; r0 += BQ) {
-    constexpr int kChunks = BQ * D / 8;
-#pragma unroll
-    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
-      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
-      if (kChunks % kThreads == 0 || i < kChunks) {
-        const bool there = r0 + r < rows && d < p.dim;
-        const int64_t token = qd.begin + (r0 + r) / p.group, head = hk * p.group + (r0 + r) % p.group;
-        const vec8<T> qv = there ? load8(static_cast<const T*>(p.q) + token * p.q_row + head * p.q_head + d) : zero8<T>();
-        const vec8<T> gv = there ? load8(static_cast<const T*>(p.d_out) + (token * p.heads + head) * p.dim + d) : zero8<T>();
-        *reinterpret_cast<vec8<T>*>(lds_q + chunk_at<D>(r, d / 8)) = qv;
-        *reinterpret_cast<vec8<T>*>(lds_g + chunk_at<D>(r, d / 8)) = gv;
-      }
-    }
-    for (int i = tid; i < BQ; i += kThreads) {
-      float lse = INFINITY, delta = 0.f, slope = 0.f, pos = 0.f;
-      if (r0 + i < rows) {
-        const int64_t token = qd.begin + (r0 + i) / p.group, head = hk * p.group + (r0 + i) % p.group;
-        lse = p.lse_in[token * p.heads + head] * kLog2e;
-        if (lse == -INFINITY) lse = INFINITY;
-        delta = p.delta[token * p.heads + head];
-        if constexpr (BIAS) {
-          slope = p.slopes[head] * kLog2e;
-          pos = float(p.qs.pos[token]);
-        }
-      }
-      lds_row[0][i] = lse - kLiftLog2<T>;
-      lds_row[1][i] = delta;
-      lds_row[2][i] = slope;
-      lds_row[3][i] = pos;
-    }
+  int now = 0;
+  for (int32_t r0 = 0; r0 < rows; r0 += BQ, now ^= 1) {
+    loads_done();
     __syncthreads();
+    if (r0 + BQ < rows) stage(r0 + BQ, now ^ 1);
+    const T *tile_q = lds_q[now], *tile_g = lds_g[now];
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
       floatx16 s = {}, g = {};
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_q + chunk_at<D>(32 * b + col, 2 * kk + half)), kf[kk], s);
-        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(lds_g + chunk_at<D>(32 * b + col, 2 * kk + half)), vf[kk], g);
+        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_q + chunk_at<D>(32 * b + col, 2 * kk + half)), kf[kk], s);
+        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_g + chunk_at<D>(32 * b + col, 2 * kk + half)), vf[kk], g);
       }
       vec8<T> pf[2], uf[2];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const int r_at = 32 * b + 8 * r4 + 4 * half;
-        const floatx4 lse = *reinterpret_cast<const floatx4*>(&lds_row[0][r_at]), delta = *reinterpret_cast<const floatx4*>(&lds_row[1][r_at]);
+        const floatx4 lse = *reinterpret_cast<const floatx4*>(&lds_row[now][0][r_at]), delta = *reinterpret_cast<const floatx4*>(&lds_row[now][1][r_at]);
         floatx4 slope = {}, pos = {};
         if constexpr (BIAS) {
-          slope = *reinterpret_cast<const floatx4*>(&lds_row[2][r_at]);
-          pos = *reinterpret_cast<const floatx4*>(&lds_row[3][r_at]);
+          slope = *reinterpret_cast<const floatx4*>(&lds_row[now][2][r_at]);
+          pos = *reinterpret_cast<const floatx4*>(&lds_row[now][3][r_at]);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -333,11 +357,10 @@ __global__ __launch_bounds__(64 * NW) void attend_dkv_kernel(const AttendParams 
       for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          dv[db] = Elem<T>::mfma(transposed8<T, D>(lds_g, 32 * b + 16 * h2, 32 * db, lane), pf[h2], dv[db]);
-          dk[db] = Elem<T>::mfma(transposed8<T, D>(lds_q, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dk[db]);
+          dv[db] = Elem<T>::mfma(transposed8<T, D>(tile_g, 32 * b + 16 * h2, 32 * db, lane), pf[h2], dv[db]);
+          dk[db] = Elem<T>::mfma(transposed8<T, D>(tile_q, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dk[db]);
         }
     }
-    __syncthreads();
   }
 
   if (key >= kd.owned) return;

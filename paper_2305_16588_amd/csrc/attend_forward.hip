@@ -10,14 +10,17 @@ namespace {
 
 // A wave has 32 folded rows, as columns of the transposed scores S^T = K Q^T: every lane then holds scores of one row, so maximum and sum
 // need one exchange between the halves of the wave, and the rounded probabilities are the operand of O^T = V^T P^T as they stand
-// (layer_dev.hpp).  NW waves share the tiles of keys and values in LDS.  D is the head's dimension rounded up to 32, 64 or 128, with zeros.
+// (layer_dev.hpp).  NW waves share the tiles of keys and values in LDS, where the next tile arrives while this one is worked on.  D is the
+// head's dimension rounded up to 32, 64 or 128, with zeros.  Scores are taken against a base that is raised, and sums and results shrunk, only
+// when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.
 // Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
+constexpr float kSlack = 8.f;
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
-  __shared__ __align__(16) T lds_k[BN * D];
-  __shared__ __align__(16) T lds_v[BN * D];
-  __shared__ __align__(16) float lds_pos[BIAS ? BN : 4];
+  __shared__ __align__(16) T lds_k[2][BN * D];
+  __shared__ __align__(16) T lds_v[2][BN * D];
+  __shared__ __align__(16) float lds_pos[2][BIAS ? BN : 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
 
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
@@ -38,17 +41,39 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
   const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
   if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
+  int32_t k_begin, k_end;
+  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
+  const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
+  const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  auto stage = [&](int32_t k0, int to) {
+    auto k_of = [&](int r) { return kp + int64_t(k0 + r) * p.k_row; };
+    auto v_of = [&](int r) { return vp + int64_t(k0 + r) * p.v_row; };
+    if (k0 + BN <= k_end) {
+      copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, tid, k_of);
+      copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, tid, v_of);
+    } else {
+      fill_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, k_of);
+      fill_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, v_of);
+    }
+    if constexpr (BIAS) {
+      if (tid < BN) lds_pos[to][tid] = k0 + tid < k_end ? float(p.ks.pos[kd.begin + k0 + tid]) : 0.f;
+    }
+  };
+  if (p.dim < D) {
+    clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
+    clear_tile<T, 2 * BN * D, kThreads>(lds_v[0], tid);
+    __syncthreads();
+  }
+  if (k_begin < k_end) stage(k_begin, 0);
+
   const int32_t row = row0 + 32 * wave + col;
   const bool live = row < qd.tokens * p.group;
-  const int32_t token = qd.begin + row / p.group, head = hk * p.group + row % p.group;
+  const int32_t of_doc = quotient(row, p.per_token), token = qd.begin + of_doc, head = hk * p.group + row - of_doc * p.group;
   vec8<T> qf[D / 16];
   {
     const T* q = static_cast<const T*>(p.q) + int64_t(token) * p.q_row + int64_t(head) * p.q_head;
 #pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      const int d = 16 * kk + 8 * half;
-      qf[kk] = live && d < p.dim ? load8(q + d) : zero8<T>();
-    }
+    for (int kk = 0; kk < D / 16; ++kk) qf[kk] = load8(q + 16 * kk + 8 * half, live && 16 * kk + 8 * half < p.dim, p.negate);
   }
   float slope = 0.f, at = 0.f;
   if constexpr (BIAS) {
@@ -59,68 +84,61 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
   }
 
   floatx16 o[D / 32] = {};
-  float top = -INFINITY, sum = 0.f;
-  int32_t k_begin, k_end;
-  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
-  const T* kp = static_cast<const T*>(p.k) + int64_t(hk) * p.k_head;
-  const T* vp = static_cast<const T*>(p.v) + int64_t(hk) * p.v_head;
-
-  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN) {
-    constexpr int kChunks = BN * D / 8;
-#pragma unroll
-    for (int c = 0; c < (kChunks + kThreads - 1) / kThreads; ++c) {
-      const int i = c * kThreads + tid, r = i / (D / 8), d = (i % (D / 8)) * 8;
-      if (kChunks % kThreads == 0 || i < kChunks) {
-        const bool there = k0 + r < k_end && d < p.dim;
-        const int64_t key = int64_t(kd.begin) + k0 + r;
-        const vec8<T> kv = there ? load8(kp + key * p.k_row + d) : zero8<T>();
-        const vec8<T> vv = there ? load8(vp + key * p.v_row + d) : zero8<T>();
-        *reinterpret_cast<vec8<T>*>(lds_k + chunk_at<D>(r, d / 8)) = kv;
-        *reinterpret_cast<vec8<T>*>(lds_v + chunk_at<D>(r, d / 8)) = vv;
-      }
-    }
-    if constexpr (BIAS) {
-      for (int i = tid; i < BN; i += kThreads) lds_pos[i] = k0 + i < k_end ? float(p.ks.pos[kd.begin + k0 + i]) : 0.f;
-    }
+  float base = -INFINITY, sum = 0.f;
+  int now = 0;
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
+    loads_done();
     __syncthreads();
+    if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
+    const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 
     floatx16 s[BN / 32];
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
       floatx16 acc = {};
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) {
-        const vec8<T> kf = *reinterpret_cast<const vec8<T>*>(lds_k + chunk_at<D>(32 * b + col, 2 * kk + half));
-        acc = Elem<T>::mfma(kf, qf[kk], acc);
-      }
+      for (int kk = 0; kk < D / 16; ++kk) acc = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], acc);
       s[b] = acc;
     }
-    float most = -INFINITY;
-    const bool whole = k0 + BN <= k_end;
+    if constexpr (CAP || BIAS) {
 #pragma unroll
-    for (int b = 0; b < BN / 32; ++b) {
+      for (int b = 0; b < BN / 32; ++b) {
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        floatx4 kpos = {};
-        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(lds_pos + 32 * b + 8 * r4 + 4 * half);
+        for (int r4 = 0; r4 < 4; ++r4) {
+          floatx4 kpos = {};
+          if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float t, z = score<CAP>(p, s[b][4 * r4 + i], t);
-          if constexpr (BIAS) z -= slope * fabsf(at - kpos[i]);
-          if (!whole && k0 + 32 * b + 8 * r4 + 4 * half + i >= k_end) z = -INFINITY;
-          s[b][4 * r4 + i] = z;
-          most = fmaxf(most, z);
+          for (int i = 0; i < 4; ++i) {
+            float t, z = score<CAP>(p, s[b][4 * r4 + i], t);
+            if constexpr (BIAS) z -= slope * fabsf(at - kpos[i]);
+            s[b][4 * r4 + i] = z;
+          }
         }
       }
     }
-    most = fmaxf(most, other_half(most));
-    const float new_top = fmaxf(top, most);
-    const float base = new_top == -INFINITY ? 0.f : new_top;      // a row whose scores are all -inf keeps a sum of zero
-    const float shrink = exp2_fast(top - base);
-    top = new_top;
-    sum *= shrink;
+    if (k0 + BN > k_end) {
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
+      for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 >= k_end) s[b][r] = -INFINITY;
+    }
+    float most = s[0][0];
+#pragma unroll
+    for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
+    most = fmaxf(most, other_half(most));
+    const float mul = CAP || BIAS ? 1.f : p.z_mul;          // scores that are still to be scaled are scaled with their base
+    most *= mul;
+    if (__any(most > base + kSlack)) {                      // the first tile, but for a row whose scores are all -inf: its sum stays zero
+      const float raised = fmaxf(base, most), shrink = raised == -INFINITY ? 1.f : exp2_fast(base - raised);
+      base = raised;
+      sum *= shrink;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
+    }
+    const float less = base == -INFINITY ? 0.f : base;
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
 #pragma unroll
@@ -128,15 +146,14 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
         vec8<T> pf;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float e = exp2_fast(s[b][8 * h2 + j] - base);
+          const float e = exp2_fast(s[b][8 * h2 + j] * mul - less);
           sum += e;
           pf[j] = T(e);
         }
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(transposed8<T, D>(lds_v, 32 * b + 16 * h2, 32 * db, lane), pf, o[db]);
+        for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(transposed8<T, D>(tile_v, 32 * b + 16 * h2, 32 * db, lane), pf, o[db]);
       }
     }
-    __syncthreads();
   }
 
   sum += other_half(sum);
@@ -157,7 +174,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
       }
     if (half == 0) {
       float* ml = p.part_ml + (int64_t(split) * p.qs.rows * p.heads + at_out) * 2;
-      ml[0] = live ? top : -INFINITY;
+      ml[0] = live ? base : -INFINITY;
       ml[1] = live ? sum : 0.f;
     }
     return;
@@ -182,7 +199,7 @@ __global__ __launch_bounds__(64 * NW) void attend_kernel(const AttendParams p) {
         if (rest) *reinterpret_cast<vec4<T>*>(rest + d) = y;
       }
     }
-  if (half == 0) p.lse[at_out] = live && sum != 0.f ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
+  if (half == 0) p.lse[at_out] = live && sum != 0.f ? (base + log2_fast(sum)) * kLn2 : -INFINITY;
 }
 
 // Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A thread has four elements of a row.
@@ -263,8 +280,11 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   p.n_docs = int32_t(d->n_docs);
   p.heads = a->heads; p.kv_heads = a->kv_heads; p.group = a->heads / a->kv_heads; p.dim = a->dim;
   p.scale = a->scale;
-  p.z_mul = (a->cap > 0.f ? a->cap : a->scale) * kLog2e;
-  p.t_mul = a->cap > 0.f ? float(2.0 * double(kLog2e) * a->scale / a->cap) : 0.f;
+  const float scale = std::fabs(a->scale);
+  p.negate = a->scale < 0.f;
+  p.z_mul = (a->cap > 0.f ? a->cap : std::max(scale, 1e-30f)) * kLog2e;
+  p.t_mul = a->cap > 0.f ? float(2.0 * double(kLog2e) * scale / a->cap) : 0.f;
+  p.per_token = divisor(uint32_t(p.group));
   p.slopes = a->slopes;
   p.splits = 1;
   return p;

@@ -45,11 +45,53 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 
 // A tile of rows x D elements of 16 bits in LDS, D 32, 64 or 128: 16-byte chunk c of row r lies at place c ^ swizzle(r) of the row, so that
 // neither the lanes of a wave that read one chunk of 32 rows each, nor those that read four rows transposed, crowd on few banks.
-template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) {
-  constexpr int kChunks = D / 8;
-  const int s = kChunks >= 8 ? row & 7 : (row >> 1) & 3;
-  return row * D + ((chunk ^ s) << 3);
+template <int D> __device__ __forceinline__ int swizzle(int row) { return D / 8 >= 8 ? row & 7 : (row >> 1) & 3; }
+template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + ((chunk ^ swizzle<D>(row)) << 3); }
+
+// ROWS rows of `dim` elements into such a tile, by the THREADS threads of a workgroup.  `row` gives where row r begins.  copy_tile is for whole
+// tiles and goes past the registers: a wave writes 64 consecutive chunks, and each lane reads the one that belongs there; what lies
+// beyond dim is left as it is, which is zero (clear_tile).  It is done when the wave's loads are (loads_done) and a barrier was passed.
+// fill_tile is for the last rows of a document: rows from `there` on become zeros.
+template <typename T, int D, int ROWS, int THREADS, typename Row>
+__device__ __forceinline__ void copy_tile(T* tile, int dim, int tid, Row row) {
+  static_assert(ROWS * D / 8 % THREADS == 0, "whole waves");
+#pragma unroll
+  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
+    const int at = c * THREADS + tid, r = at / (D / 8), d = ((at % (D / 8)) ^ swizzle<D>(r)) * 8;
+    if (d < dim)
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(row(r) + d),
+                                       (__attribute__((address_space(3))) uint32_t*)(tile + (c * THREADS + (tid & ~63)) * 8), 16, 0, 0);
+  }
 }
+template <typename T, int D, int ROWS, int THREADS, typename Row>
+__device__ __forceinline__ void fill_tile(T* tile, int dim, int there, int tid, Row row) {
+  vec8<T> v[ROWS * D / 8 / THREADS];
+#pragma unroll
+  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
+    const int at = c * THREADS + tid, r = at / (D / 8), d = (at % (D / 8)) * 8;
+    vec8<T> zero = {};
+    v[c] = r < there && d < dim ? *reinterpret_cast<const vec8<T>*>(row(r) + d) : zero;
+  }
+#pragma unroll
+  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
+    const int at = c * THREADS + tid, r = at / (D / 8), d = (at % (D / 8)) * 8;
+    *reinterpret_cast<vec8<T>*>(tile + chunk_at<D>(r, d / 8)) = v[c];
+  }
+}
+template <typename T, int ELEMS, int THREADS> __device__ __forceinline__ void clear_tile(T* tile, int tid) {
+  const vec8<T> zero = {};
+  for (int i = tid; i < ELEMS / 8; i += THREADS) reinterpret_cast<vec8<T>*>(tile)[i] = zero;
+}
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }       // vmcnt(0), the other counters as they are
+
+// Division of numbers below 2^31 by a fixed one.
+struct Divisor { uint32_t by, mul, shift; };
+inline Divisor divisor(uint32_t by) {
+  uint32_t l = 0;
+  while ((1u << l) < by) ++l;
+  return {by, by > 1 ? uint32_t(((uint64_t(1) << (31 + l)) + by - 1) / by) : 0, l ? l - 1 : 0};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor& d) { return d.by == 1 ? n : __umulhi(n, d.mul) >> d.shift; }
 
 // Operand A or B with the places of the sum running along the rows of a tile: four elements of column (lane % 32) + col0, of rows
 // row0 + 4 * (lane / 32) ... + 3.  Each 16 lanes read four rows of 16 columns, which the LDS hands out transposed.
