@@ -65,6 +65,17 @@ __device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, i
 int check_attend(const lgp_documents* d, const lgp_attention* a);
 AttendParams attend_params(const lgp_documents* d, const lgp_attention* a);
 
+// Documents of one query and few keys (attend_single.hip).
+bool single_queries(const lgp_documents* d, const lgp_attention* a);
+void launch_single(const AttendParams& p, const lgp_attention* a, bool backward, hipStream_t s);
+
+// With fp16 a probability below 2^-14 would lose digits, and over 16 000 keys most are: where they are an operand of a product, the backward
+// pass takes them times 2^12, which cannot overflow, and the result times 2^-12.
+template <typename T> constexpr float kLift = 1.f;
+template <> inline constexpr float kLift<f16> = 4096.f;
+template <typename T> constexpr float kLiftLog2 = 0.f;
+template <> inline constexpr float kLiftLog2<f16> = 12.f;
+
 // Launch shapes, chosen on the host by what it knows: rows and documents.
 constexpr int kForwardRows = 32;        // folded rows of a wave
 struct ForwardShape { int waves; int64_t tiles; int splits; };

@@ -9,13 +9,6 @@ namespace lgp {
 namespace layer {
 namespace {
 
-// With fp16 a probability below 2^-14 would lose digits, and over 16 000 keys most are: the second product takes them times 2^12, which
-// cannot overflow, and its result times 2^-12.
-template <typename T> constexpr float kLift = 1.f;
-template <> constexpr float kLift<f16> = 4096.f;
-template <typename T> constexpr float kLiftLog2 = 0.f;
-template <> constexpr float kLiftLog2<f16> = 12.f;
-
 // Gradient of q: with u = scale * q.k, z the score, P = exp(z - lse), dP = d_out . v and delta = d_out . out,
 //     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
 // Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
@@ -393,6 +386,7 @@ struct BackwardShape {
 BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
   BackwardShape b;
   b.q = forward_shape(device, d, a);
+  if (single_queries(d, a)) b.q.splits = 1;
   b.key_waves = d->k_rows <= 32 * std::max<int64_t>(d->n_docs, 1) ? 1 : 4;
   b.key_tiles = tiles_of(d->k_rows, 1, d->n_docs, 32 * b.key_waves);
   const size_t rows = size_t(d->q_rows) * a->heads;
@@ -481,7 +475,8 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
   p.sums = d_slopes ? w + b.sums : nullptr;
   p.part_o = w + b.parts;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
+  if (single_queries(docs, att)) launch_single(p, att, true, s);
+  else if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
   else launch<bf16>(p, b, att->cap > 0.f, s);
   if (d_slopes) {
     slopes_kernel<<<dim3(att->heads, kSlopeGroups), 256, 0, s>>>(p, w + b.partial);

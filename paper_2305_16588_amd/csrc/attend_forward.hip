@@ -315,6 +315,15 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
   if (docs->q_rows && (!out || !lse || !aligned16(out) || !aligned16(rest))) return LGP_EINVAL;
   if (int st = use_device(device)) return st;
   if (docs->q_rows == 0) return LGP_OK;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (single_queries(docs, att)) {
+    AttendParams p = attend_params(docs, att);
+    p.out = out;
+    p.rest = rest;
+    p.lse = lse;
+    launch_single(p, att, false, s);
+    return launched();
+  }
   const ForwardShape f = forward_shape(device, docs, att);
   if (f.tiles * att->kv_heads * f.splits >= int64_t(1) << 31) return LGP_EUNSUPPORTED;
   AttendParams p = attend_params(docs, att);
@@ -330,7 +339,6 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + rows * att->dim;
   }
-  const hipStream_t s = static_cast<hipStream_t>(stream);
   if (att->dtype == LGP_F16) launch<f16>(p, f.waves, att->cap > 0.f, s);
   else launch<bf16>(p, f.waves, att->cap > 0.f, s);
   return launched();

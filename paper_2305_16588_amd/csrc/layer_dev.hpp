@@ -41,6 +41,19 @@ __device__ __forceinline__ float log2_fast(float x) { return __builtin_amdgcn_lo
 __device__ __forceinline__ float rcp_fast(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
 
+// Sum over groups of L lanes, the same in all of them.  Moves within rows of 16 lanes need no trip through LDS.
+template <int CTRL> __device__ __forceinline__ float moved(float x) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
+}
+template <int L> __device__ __forceinline__ float sum_of_lanes(float x) {
+  if constexpr (L >= 2) x += moved<0xb1>(x);        // quad_perm 1 0 3 2
+  if constexpr (L >= 4) x += moved<0x4e>(x);        // quad_perm 2 3 0 1
+  if constexpr (L >= 8) x += moved<0x141>(x);       // row_half_mirror: the other four of eight
+  if constexpr (L >= 16) x += moved<0x140>(x);      // row_mirror: the other eight of sixteen
+  if constexpr (L >= 32) x += __shfl_xor(x, 16, 64);
+  return x;
+}
+
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // A tile of rows x D elements of 16 bits in LDS, D 32, 64 or 128: 16-byte chunk c of row r lies at place c ^ swizzle(r) of the row, so that

@@ -44,12 +44,6 @@ template <> __device__ __forceinline__ void write8<float>(float* p, const float*
   *reinterpret_cast<floatx4*>(p + 4) = floatx4{x[4], x[5], x[6], x[7]};
 }
 
-template <int L> __device__ __forceinline__ float sum_of_lanes(float x) {
-#pragma unroll
-  for (int d = L / 2; d; d >>= 1) x += __shfl_xor(x, d, 64);
-  return x;
-}
-
 // Pair (i, i + rot / 2) turns by the angle of the position (back: the other way).  Lane c of a row has elements 8 c .. 8 c + 7, so the other
 // half of its pairs are a lane's, rot / 16 lanes away.  Every lane of the wave takes part in the exchange.
 template <int L>
