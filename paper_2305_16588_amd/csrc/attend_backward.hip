@@ -45,19 +45,12 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
   const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
   const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  int32_t next_pos = 0;        // as it comes, so that nothing waits for it yet
   auto stage = [&](int32_t k0, int to) {
-    auto k_of = [&](int r) { return kp + int64_t(k0 + r) * p.k_row; };
-    auto v_of = [&](int r) { return vp + int64_t(k0 + r) * p.v_row; };
-    if (k0 + BN <= k_end) {
-      copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, tid, k_of);
-      copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, tid, v_of);
-    } else {
-      fill_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, k_of);
-      fill_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, v_of);
-    }
-    if constexpr (BIAS) {
-      if (tid < BN) lds_pos[to][tid] = k0 + tid < k_end ? float(p.ks.pos[kd.begin + k0 + tid]) : 0.f;
-    }
+    if constexpr (BIAS) next_pos = tid < BN && k0 + tid < k_end ? p.ks.pos[kd.begin + k0 + tid] : 0;
+    const T *k_from = kp + int64_t(k0) * p.k_row, *v_from = vp + int64_t(k0) * p.v_row;
+    copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, [&](int r) { return k_from + r * p.k_row; });
+    copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, [&](int r) { return v_from + r * p.v_row; });
   };
   if (p.dim < D) {
     clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
@@ -106,6 +99,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
   int now = 0;
   for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
     loads_done();
+    if constexpr (BIAS) {
+      if (tid < BN) lds_pos[now][tid] = float(next_pos);
+    }
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
@@ -250,39 +246,36 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
   const int32_t rows = key0 < kd.tokens ? qd.tokens * p.group : 0;
   const T* qp = static_cast<const T*>(p.q) + int64_t(qd.begin) * p.q_row + int64_t(hk) * p.group * p.q_head;
   const T* gp = static_cast<const T*>(p.d_out) + (int64_t(qd.begin) * p.heads + int64_t(hk) * p.group) * p.dim;
+  static_assert(BQ <= kThreads, "a thread has a row");
+  float next[3];               // as they come, so that nothing waits for them yet
+  int32_t next_pos;
   auto stage = [&](int32_t r0, int to) {
-    auto q_of = [&](int r) {
+    next[0] = INFINITY, next[1] = next[2] = 0.f, next_pos = 0;
+    if (tid < BQ && r0 + tid < rows) {
+      const uint32_t t = quotient(r0 + tid, p.per_token), head = hk * p.group + r0 + tid - t * p.group;
+      const int64_t token = qd.begin + int64_t(t);
+      next[0] = p.lse_in[token * p.heads + head];
+      next[1] = p.delta[token * p.heads + head];
+      if constexpr (BIAS) {
+        next[2] = p.slopes[head];
+        next_pos = p.qs.pos[token];
+      }
+    }
+    copy_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, rows - r0, tid, [&](int r) {
       const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
       return qp + int64_t(t) * p.q_row + int64_t(g) * p.q_head;
-    };
-    auto g_of = [&](int r) {
+    });
+    copy_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, rows - r0, tid, [&](int r) {
       const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
       return gp + (int64_t(t) * p.heads + g) * p.dim;
-    };
-    if (r0 + BQ <= rows) {
-      copy_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, tid, q_of);
-      copy_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, tid, g_of);
-    } else {
-      fill_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, rows - r0, tid, q_of);
-      fill_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, rows - r0, tid, g_of);
-    }
-    for (int i = tid; i < BQ; i += kThreads) {
-      float lse = INFINITY, delta = 0.f, slope = 0.f, pos = 0.f;
-      if (r0 + i < rows) {
-        const uint32_t t = quotient(r0 + i, p.per_token), head = hk * p.group + r0 + i - t * p.group;
-        const int64_t token = qd.begin + int64_t(t);
-        lse = p.lse_in[token * p.heads + head] * kLog2e;
-        if (lse == -INFINITY) lse = INFINITY;
-        delta = p.delta[token * p.heads + head];
-        if constexpr (BIAS) {
-          slope = p.slopes[head] * kLog2e;
-          pos = float(p.qs.pos[token]);
-        }
-      }
-      lds_row[to][0][i] = lse - kLiftLog2<T>;
-      lds_row[to][1][i] = delta;
-      lds_row[to][2][i] = slope;
-      lds_row[to][3][i] = pos;
+    });
+  };
+  auto put_rows = [&](int to) {
+    if (tid < BQ) {
+      lds_row[to][0][tid] = (next[0] == -INFINITY ? INFINITY : next[0]) * kLog2e - kLiftLog2<T>;       // no probability where there is no key
+      lds_row[to][1][tid] = next[1];
+      lds_row[to][2][tid] = next[2] * kLog2e;
+      lds_row[to][3][tid] = float(next_pos);
     }
   };
   if (p.dim < D) {
@@ -313,6 +306,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
   int now = 0;
   for (int32_t r0 = 0; r0 < rows; r0 += BQ, now ^= 1) {
     loads_done();
+    put_rows(now);
     __syncthreads();
     if (r0 + BQ < rows) stage(r0 + BQ, now ^ 1);
     const T *tile_q = lds_q[now], *tile_g = lds_g[now];

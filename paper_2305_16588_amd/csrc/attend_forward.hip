@@ -45,19 +45,12 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
   const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
   const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  int32_t next_pos = 0;        // as it comes, so that nothing waits for it yet
   auto stage = [&](int32_t k0, int to) {
-    auto k_of = [&](int r) { return kp + int64_t(k0 + r) * p.k_row; };
-    auto v_of = [&](int r) { return vp + int64_t(k0 + r) * p.v_row; };
-    if (k0 + BN <= k_end) {
-      copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, tid, k_of);
-      copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, tid, v_of);
-    } else {
-      fill_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, k_of);
-      fill_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, v_of);
-    }
-    if constexpr (BIAS) {
-      if (tid < BN) lds_pos[to][tid] = k0 + tid < k_end ? float(p.ks.pos[kd.begin + k0 + tid]) : 0.f;
-    }
+    if constexpr (BIAS) next_pos = tid < BN && k0 + tid < k_end ? p.ks.pos[kd.begin + k0 + tid] : 0;
+    const T *k_from = kp + int64_t(k0) * p.k_row, *v_from = vp + int64_t(k0) * p.v_row;
+    copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, [&](int r) { return k_from + r * p.k_row; });
+    copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, [&](int r) { return v_from + r * p.v_row; });
   };
   if (p.dim < D) {
     clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
@@ -88,6 +81,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   int now = 0;
   for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
     loads_done();
+    if constexpr (BIAS) {
+      if (tid < BN) lds_pos[now][tid] = float(next_pos);
+    }
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];

@@ -61,34 +61,32 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 template <int D> __device__ __forceinline__ int swizzle(int row) { return D / 8 >= 8 ? row & 7 : (row >> 1) & 3; }
 template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + ((chunk ^ swizzle<D>(row)) << 3); }
 
-// ROWS rows of `dim` elements into such a tile, by the THREADS threads of a workgroup.  `row` gives where row r begins.  copy_tile is for whole
-// tiles and goes past the registers: a wave writes 64 consecutive chunks, and each lane reads the one that belongs there; what lies
-// beyond dim is left as it is, which is zero (clear_tile).  It is done when the wave's loads are (loads_done) and a barrier was passed.
-// fill_tile is for the last rows of a document: rows from `there` on become zeros.
+// 16 bytes of each lane go to `lds` + 16 * lane, past the registers.  The compiler would wait for them before the next read of LDS, whichever
+// tile that reads, so it is not told: what arrives may be read when the wave's loads are done (loads_done) and a barrier was passed.
+__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) char*)p)); }
+
+// ROWS rows of `dim` elements into such a tile, by the THREADS threads of a workgroup: `row` gives where row r begins.  A wave writes 64 consecutive
+// chunks, and each lane reads the one that belongs there.  Rows from `there` on become zeros; what lies beyond dim is left as it is,
+// which is zero (clear_tile).
 template <typename T, int D, int ROWS, int THREADS, typename Row>
-__device__ __forceinline__ void copy_tile(T* tile, int dim, int tid, Row row) {
+__device__ __forceinline__ void copy_tile(T* tile, int dim, int there, int tid, Row row) {
   static_assert(ROWS * D / 8 % THREADS == 0, "whole waves");
+  const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(tile) + (tid & ~63) * 16);
 #pragma unroll
   for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
     const int at = c * THREADS + tid, r = at / (D / 8), d = ((at % (D / 8)) ^ swizzle<D>(r)) * 8;
-    if (d < dim)
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) uint32_t*)(row(r) + d),
-                                       (__attribute__((address_space(3))) uint32_t*)(tile + (c * THREADS + (tid & ~63)) * 8), 16, 0, 0);
+    if (r < there && d < dim) copy16(row(r) + d, to + c * THREADS * 16);
   }
-}
-template <typename T, int D, int ROWS, int THREADS, typename Row>
-__device__ __forceinline__ void fill_tile(T* tile, int dim, int there, int tid, Row row) {
-  vec8<T> v[ROWS * D / 8 / THREADS];
+  if (there < ROWS) {
+    const vec8<T> zero = {};
 #pragma unroll
-  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
-    const int at = c * THREADS + tid, r = at / (D / 8), d = (at % (D / 8)) * 8;
-    vec8<T> zero = {};
-    v[c] = r < there && d < dim ? *reinterpret_cast<const vec8<T>*>(row(r) + d) : zero;
-  }
-#pragma unroll
-  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
-    const int at = c * THREADS + tid, r = at / (D / 8), d = (at % (D / 8)) * 8;
-    *reinterpret_cast<vec8<T>*>(tile + chunk_at<D>(r, d / 8)) = v[c];
+    for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
+      const int at = c * THREADS + tid;
+      if (at / (D / 8) >= there) reinterpret_cast<vec8<T>*>(tile)[at] = zero;
+    }
   }
 }
 template <typename T, int ELEMS, int THREADS> __device__ __forceinline__ void clear_tile(T* tile, int tid) {
