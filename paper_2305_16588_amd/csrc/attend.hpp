@@ -15,6 +15,7 @@ struct AttendParams {
   Side qs, ks;
   int32_t n_docs, heads, kv_heads, group, dim;
   Divisor per_token;         // by group
+  int32_t log2_fold;         // by keys: heads of a token that are folded, all of the group or one
   // Scores in powers of two: z * log2(e) = capped ? tanh(qk * scale / cap) * cap * log2(e) : qk * scale * log2(e), with the magnitude of the
   // scale: where it is negative, q (by keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the
   // largest product is the largest score.

@@ -43,14 +43,13 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 
   int32_t k_begin, k_end;
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
-  const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
-  const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  const Rows<T> k_rows = {static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head, p.k_row, 0, 0};
+  const Rows<T> v_rows = {static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head, p.v_row, 0, 0};
   int32_t next_pos = 0;        // as it comes, so that nothing waits for it yet
   auto stage = [&](int32_t k0, int to) {
     if constexpr (BIAS) next_pos = tid < BN && k0 + tid < k_end ? p.ks.pos[kd.begin + k0 + tid] : 0;
-    const T *k_from = kp + int64_t(k0) * p.k_row, *v_from = vp + int64_t(k0) * p.v_row;
-    copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, [&](int r) { return k_from + r * p.k_row; });
-    copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, [&](int r) { return v_from + r * p.v_row; });
+    copy_tile<T, D, BN, kThreads>(lds_k[to], k_rows, k0, p.dim, k_end - k0, tid);
+    copy_tile<T, D, BN, kThreads>(lds_v[to], v_rows, k0, p.dim, k_end - k0, tid);
   };
   if (p.dim < D) {
     clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
@@ -243,17 +242,16 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
   const int32_t key0 = (tile - first_tile(p.ks, doc, p.n_docs, 1, kKeys)) * kKeys;
   if (key0 < 0 || key0 >= kd.owned) return;
 
-  const int32_t rows = key0 < kd.tokens ? qd.tokens * p.group : 0;
-  const T* qp = static_cast<const T*>(p.q) + int64_t(qd.begin) * p.q_row + int64_t(hk) * p.group * p.q_head;
-  const T* gp = static_cast<const T*>(p.d_out) + (int64_t(qd.begin) * p.heads + int64_t(hk) * p.group) * p.dim;
+  // Up to 16 heads of a token, if they divide 16, are folded; otherwise the heads that share this one are gone through one after the other.
+  const int32_t rows = key0 < kd.tokens ? qd.tokens << p.log2_fold : 0;
   static_assert(BQ <= kThreads, "a thread has a row");
   float next[3];               // as they come, so that nothing waits for them yet
   int32_t next_pos;
-  auto stage = [&](int32_t r0, int to) {
+  auto stage = [&](int32_t h0, int32_t r0, int to) {
     next[0] = INFINITY, next[1] = next[2] = 0.f, next_pos = 0;
     if (tid < BQ && r0 + tid < rows) {
-      const uint32_t t = quotient(r0 + tid, p.per_token), head = hk * p.group + r0 + tid - t * p.group;
-      const int64_t token = qd.begin + int64_t(t);
+      const int32_t head = h0 + ((r0 + tid) & ((1 << p.log2_fold) - 1));
+      const int64_t token = qd.begin + ((r0 + tid) >> p.log2_fold);
       next[0] = p.lse_in[token * p.heads + head];
       next[1] = p.delta[token * p.heads + head];
       if constexpr (BIAS) {
@@ -261,14 +259,10 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
         next_pos = p.qs.pos[token];
       }
     }
-    copy_tile<T, D, BQ, kThreads>(lds_q[to], p.dim, rows - r0, tid, [&](int r) {
-      const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
-      return qp + int64_t(t) * p.q_row + int64_t(g) * p.q_head;
-    });
-    copy_tile<T, D, BQ, kThreads>(lds_g[to], p.dim, rows - r0, tid, [&](int r) {
-      const uint32_t t = quotient(r0 + r, p.per_token), g = r0 + r - t * p.group;
-      return gp + (int64_t(t) * p.heads + g) * p.dim;
-    });
+    const Rows<T> q_rows = {static_cast<const T*>(p.q) + int64_t(qd.begin) * p.q_row + int64_t(h0) * p.q_head, p.q_row, p.q_head, p.log2_fold};
+    const Rows<T> g_rows = {static_cast<const T*>(p.d_out) + (int64_t(qd.begin) * p.heads + h0) * p.dim, int64_t(p.heads) * p.dim, p.dim, p.log2_fold};
+    copy_tile<T, D, BQ, kThreads>(lds_q[to], q_rows, r0, p.dim, rows - r0, tid);
+    copy_tile<T, D, BQ, kThreads>(lds_g[to], g_rows, r0, p.dim, rows - r0, tid);
   };
   auto put_rows = [&](int to) {
     if (tid < BQ) {
@@ -283,7 +277,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
     clear_tile<T, 2 * BQ * D, kThreads>(lds_g[0], tid);
     __syncthreads();
   }
-  if (rows > 0) stage(0, 0);
+  if (rows > 0) stage(hk * p.group, 0, 0);
 
   const int32_t key = key0 + 32 * wave + col;
   const bool live = key < kd.tokens;
@@ -304,11 +298,13 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
 
   floatx16 dk[D / 32] = {}, dv[D / 32] = {};
   int now = 0;
-  for (int32_t r0 = 0; r0 < rows; r0 += BQ, now ^= 1) {
+  for (int32_t h0 = hk * p.group, r0 = 0; rows > 0 && h0 < (hk + 1) * p.group; now ^= 1) {
     loads_done();
     put_rows(now);
     __syncthreads();
-    if (r0 + BQ < rows) stage(r0 + BQ, now ^ 1);
+    r0 += BQ;
+    if (r0 >= rows) r0 = 0, h0 += 1 << p.log2_fold;
+    if (h0 < (hk + 1) * p.group) stage(h0, r0, now ^ 1);
     const T *tile_q = lds_q[now], *tile_g = lds_g[now];
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {

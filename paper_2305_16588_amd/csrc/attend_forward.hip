@@ -43,14 +43,13 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
 
   int32_t k_begin, k_end;
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
-  const T* kp = static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head;
-  const T* vp = static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head;
+  const Rows<T> k_rows = {static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head, p.k_row, 0, 0};
+  const Rows<T> v_rows = {static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head, p.v_row, 0, 0};
   int32_t next_pos = 0;        // as it comes, so that nothing waits for it yet
   auto stage = [&](int32_t k0, int to) {
     if constexpr (BIAS) next_pos = tid < BN && k0 + tid < k_end ? p.ks.pos[kd.begin + k0 + tid] : 0;
-    const T *k_from = kp + int64_t(k0) * p.k_row, *v_from = vp + int64_t(k0) * p.v_row;
-    copy_tile<T, D, BN, kThreads>(lds_k[to], p.dim, k_end - k0, tid, [&](int r) { return k_from + r * p.k_row; });
-    copy_tile<T, D, BN, kThreads>(lds_v[to], p.dim, k_end - k0, tid, [&](int r) { return v_from + r * p.v_row; });
+    copy_tile<T, D, BN, kThreads>(lds_k[to], k_rows, k0, p.dim, k_end - k0, tid);
+    copy_tile<T, D, BN, kThreads>(lds_v[to], v_rows, k0, p.dim, k_end - k0, tid);
   };
   if (p.dim < D) {
     clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
@@ -263,6 +262,8 @@ int check_attend(const lgp_documents* d, const lgp_attention* a) {
   if ((d->q_rows && !a->q) || (d->k_rows && (!a->k || !a->v))) return LGP_EINVAL;
   if (a->slopes && ((d->q_rows && !d->q_pos) || (d->k_rows && !d->k_pos))) return LGP_EINVAL;
   if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v)) return LGP_EINVAL;
+  for (int64_t stride : {a->q_row, a->q_head, a->k_row, a->k_head, a->v_row, a->v_head, int64_t(a->heads) * a->dim})
+    if (stride < 0 || stride >= kMostStride) return LGP_EUNSUPPORTED;
   if (a->q_row % 8 || a->q_head % 8 || a->k_row % 8 || a->k_head % 8 || a->v_row % 8 || a->v_head % 8) return LGP_EINVAL;
   return LGP_OK;
 }
@@ -281,6 +282,7 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   p.z_mul = (a->cap > 0.f ? a->cap : std::max(scale, 1e-30f)) * kLog2e;
   p.t_mul = a->cap > 0.f ? float(2.0 * double(kLog2e) * scale / a->cap) : 0.f;
   p.per_token = divisor(uint32_t(p.group));
+  while (16 % p.group == 0 && (1 << p.log2_fold) < p.group) ++p.log2_fold;
   p.slopes = a->slopes;
   p.splits = 1;
   return p;

@@ -19,7 +19,7 @@ template <int L> struct Lanes {
     const int lane = threadIdx.x & 63, slot = lane / L;
     const int64_t unit = int64_t(piece_of(blockIdx.x, gridDim.x)) * 4 + (threadIdx.x >> 6);
     const int32_t chunks = (p.kv_heads + heads_at_once - 1) / heads_at_once;
-    doc = int32_t(unit / chunks);
+    doc = __builtin_amdgcn_readfirstlane(int32_t(unit / chunks));
     c = lane % L;
     head = slot % heads_at_once;
     key = slot / heads_at_once;

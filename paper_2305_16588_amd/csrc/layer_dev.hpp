@@ -56,37 +56,57 @@ template <int L> __device__ __forceinline__ float sum_of_lanes(float x) {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// A tile of rows x D elements of 16 bits in LDS, D 32, 64 or 128: 16-byte chunk c of row r lies at place c ^ swizzle(r) of the row, so that
-// neither the lanes of a wave that read one chunk of 32 rows each, nor those that read four rows transposed, crowd on few banks.
-template <int D> __device__ __forceinline__ int swizzle(int row) { return D / 8 >= 8 ? row & 7 : (row >> 1) & 3; }
+// A tile of rows x D elements of 16 bits in LDS, D 32 to 256: 16-byte chunk c of row r lies at place c ^ swizzle(r) of the row.  256 bytes lie in
+// different banks, so 16 lanes that read the same chunk of 16 rows, and 32 lanes that read 64 bytes of four rows transposed, want different
+// places there: the row's low bits, reversed, do both (for D of 128, chunks of 32 rows 3.6 -> 2.2 ns a wave and CU against the row's low bits
+// as they are, transposed reads 3.5 -> 1.5).
+template <int D> __device__ __forceinline__ int swizzle(int row) { return int(__brev(uint32_t(row)) >> 28) & (D / 8 >= 16 ? 15 : D / 8 - 1); }
 template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) { return row * D + ((chunk ^ swizzle<D>(row)) << 3); }
 
-// 16 bytes of each lane go to `lds` + 16 * lane, past the registers.  The compiler would wait for them before the next read of LDS, whichever
-// tile that reads, so it is not told: what arrives may be read when the wave's loads are done (loads_done) and a barrier was passed.
-__device__ __forceinline__ void copy16(const void* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+// 16 bytes of each lane, `offset` bytes behind `from`, go to `lds` + 16 * lane, past the registers.  The compiler would wait for them before the
+// next read of LDS, whichever tile that reads, so it is not told: what arrives may be read when the wave's loads are done (loads_done) and
+// a barrier was passed.
+__device__ __forceinline__ void copy16(const void* from, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
+template <typename T> __device__ __forceinline__ const T* in_all_lanes(const T* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  return reinterpret_cast<const T*>(uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x)))) | uint64_t(uint32_t(__builtin_amdgcn_readfirstlane(uint32_t(x >> 32)))) << 32);
 }
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) char*)p)); }
 
-// ROWS rows of `dim` elements into such a tile, by the THREADS threads of a workgroup: `row` gives where row r begins.  A wave writes 64 consecutive
-// chunks, and each lane reads the one that belongs there.  Rows from `there` on become zeros; what lies beyond dim is left as it is,
-// which is zero (clear_tile).
-template <typename T, int D, int ROWS, int THREADS, typename Row>
-__device__ __forceinline__ void copy_tile(T* tile, int dim, int there, int tid, Row row) {
-  static_assert(ROWS * D / 8 % THREADS == 0, "whole waves");
+// Rows in memory, `row` elements apart; with fold = 2^log2_fold each is that many rows of a tile, `head` elements apart.  Strides are below
+// 2^24, so that a wave's lanes are less than 2^32 bytes apart.
+constexpr int64_t kMostStride = int64_t(1) << 24;
+template <typename T> struct Rows {
+  const T* from;
+  int64_t row, head;
+  int32_t log2_fold;
+};
+
+// ROWS rows of `dim` elements, from row `first` (a multiple of 16) on, into such a tile, by the THREADS threads of a workgroup.  A wave writes
+// 64 consecutive chunks, and each lane reads the one that belongs there.  Rows from `there` on become zeros; what lies beyond dim is left as
+// it is, which is zero (clear_tile).
+template <typename T, int D, int ROWS, int THREADS>
+__device__ __forceinline__ void copy_tile(T* tile, const Rows<T>& rows, int32_t first, int dim, int there, int tid) {
+  constexpr int kStep = THREADS * 8 / D;         // rows that all threads write at once
+  static_assert(ROWS % kStep == 0, "whole waves");
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(tile) + (tid & ~63) * 16);
+  const int r0 = tid / (D / 8), fold = 1 << rows.log2_fold;
+  const T* from = rows.from + int64_t(first >> rows.log2_fold) * rows.row;
 #pragma unroll
-  for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
-    const int at = c * THREADS + tid, r = at / (D / 8), d = ((at % (D / 8)) ^ swizzle<D>(r)) * 8;
-    if (r < there && d < dim) copy16(row(r) + d, to + c * THREADS * 16);
+  for (int c = 0; c < ROWS / kStep; ++c) {
+    // with 16 rows and more at once the places in a row repeat, and so do the heads of a token
+    const int r = kStep % 16 == 0 ? r0 : c * kStep + r0, d = ((tid % (D / 8)) ^ swizzle<D>(r)) * 8;
+    const uint32_t offset = (uint32_t(r >> rows.log2_fold) * uint32_t(rows.row) + uint32_t(r & (fold - 1)) * uint32_t(rows.head) + d) * sizeof(T);
+    const T* base = in_all_lanes(kStep % 16 == 0 ? from + int64_t(c * kStep >> rows.log2_fold) * rows.row : from);
+    if (c * kStep + r0 < there && d < dim) copy16(base, offset, to + c * THREADS * 16);
   }
   if (there < ROWS) {
     const vec8<T> zero = {};
 #pragma unroll
-    for (int c = 0; c < ROWS * D / 8 / THREADS; ++c) {
-      const int at = c * THREADS + tid;
-      if (at / (D / 8) >= there) reinterpret_cast<vec8<T>*>(tile)[at] = zero;
-    }
+    for (int c = 0; c < ROWS / kStep; ++c)
+      if (c * kStep + r0 >= there) reinterpret_cast<vec8<T>*>(tile)[c * THREADS + tid] = zero;
   }
 }
 template <typename T, int ELEMS, int THREADS> __device__ __forceinline__ void clear_tile(T* tile, int tid) {
@@ -137,12 +157,12 @@ __device__ __forceinline__ int32_t offset_of(const Side& s, int32_t d, int32_t n
 }
 __device__ __forceinline__ Span span_of(const Side& s, int32_t d, int32_t n) {
   Span x;
-  x.begin = offset_of(s, d, n);
-  const int32_t end = offset_of(s, d + 1, n);
+  x.begin = __builtin_amdgcn_readfirstlane(offset_of(s, d, n));         // d is the same in the whole wave
+  const int32_t end = __builtin_amdgcn_readfirstlane(offset_of(s, d + 1, n));
   x.owned = end > x.begin ? end - x.begin : 0;
   x.tokens = x.owned;
   if (s.lens) {
-    const int32_t t = s.lens[d];
+    const int32_t t = __builtin_amdgcn_readfirstlane(s.lens[d]);
     x.tokens = t < 0 ? 0 : t < x.owned ? t : x.owned;
   }
   return x;

@@ -111,96 +111,192 @@ struct GradParams {
   float *dw, *db;                   // [part][out][width] and [part][out]
 };
 
-// dw = dy^T x, a sum over tokens: a workgroup has 128 x 128 of dw and a part of the tokens, its four waves 64 x 64 each.  Both operands are
-// read transposed from LDS.  value * 2^e has at most seven digits, so it is exact in the type of dy, and so are the products: the only
-// rounding is that of the sums in 32 bits.  The workgroups of the first 128 columns add up the bias's gradient as they read dy.
-template <typename T>
-__global__ __launch_bounds__(256) void weight_grad_kernel(const GradParams p) {
-  constexpr int BT = 64, D = 128;
-  __shared__ __align__(16) T lds_y[BT * D];
-  __shared__ __align__(16) T lds_x[BT * D];
+// dw = dy^T x, a sum over tokens: a workgroup has NT x 128 of dw (NT 128 or 256) and a part of the tokens, its eight waves NT / 4 x 64 each.
+// Both operands are read transposed from LDS.  While one tile of kTokens tokens is multiplied, the next is made ready -- its packed values
+// are widened, rows without a token become zeros -- and the one after it is on its way to LDS (DMA: rows of dy are aligned to 16 bytes; else
+// they go through registers).  value * 2^e has at most seven digits, so it is exact in the type of dy, and so are the products: the only
+// rounding is that of the sums in 32 bits.  The workgroups of the first 128 columns add up the bias's gradient.  Columns beyond the
+// operands' ends hold anything, and so do rows and columns of the result that are not written.
+constexpr int kTokens = 32, kAhead = 256;        // of a tile; of which exponents and positions are held
+template <typename T, int NT, bool DMA>
+__global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p) {
+  constexpr int WT = 128, NB = NT / 128, NC = NT / 8, NJ = kTokens * NC / 512;       // NB: blocks of 32 rows of a wave; NC: chunks of eight in a row
+  __shared__ __align__(16) T lds_y[3][kTokens * NT];
+  __shared__ __align__(16) uint8_t lds_raw[3][kTokens * WT];
+  __shared__ __align__(16) T lds_x[2][kTokens * WT];
+  __shared__ uint32_t lds_exps[2][kAhead];
+  __shared__ uint8_t lds_gone[2][kAhead];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
   const int32_t tw = piece % p.tiles_w, tn = piece / p.tiles_w % p.tiles_n, part = piece / p.tiles_w / p.tiles_n;
-  const int32_t w0 = tw * D, n0 = tn * D;
+  const int32_t w0 = tw * WT, n0 = tn * NT;
   const int64_t t_begin = part * p.each, t_end = t_begin + p.each < p.tokens ? t_begin + p.each : p.tokens;
-  floatx16 acc[2][2] = {};
+  const int32_t tokens = int32_t(t_end - t_begin), tiles = (tokens + kTokens - 1) / kTokens;
+  const T* dy = static_cast<const T*>(p.dy) + t_begin * p.dy_row + n0;
+  const int8_t* values = p.values + t_begin * p.pitch + w0;
+  const bool sums = tw == 0 && p.db;
+  const int yc = tid % NC, yr = tid / NC;        // a thread's chunk of dy, and its first row
+  floatx16 acc[NB][2] = {};
   float bias[8] = {};
-  const int c = tid % 16;           // a thread's eight columns
-  for (int64_t t0 = t_begin; t0 < t_end; t0 += BT) {
+
+  vec8<T> held[DMA ? 1 : NJ];
+  auto fetch = [&](int32_t i) {
+    if (i >= tiles) return;
+    const int32_t t0 = i * kTokens;
+    if constexpr (DMA) {
+      copy_tile<T, NT, kTokens, 512>(lds_y[i % 3], Rows<T>{dy, p.dy_row, 0, 0}, t0, p.out - n0, tokens - t0, tid);
+    } else {
 #pragma unroll
-    for (int j = 0; j < BT / 16; ++j) {
-      const int r = tid / 16 + 16 * j;
-      const int64_t t = t0 + r;
-      float y[8] = {};
-      vec8<T> xv = {}, yv;
-      if (t < t_end && (!p.pos || p.pos[t] >= 0)) {
-        const int n = p.out - n0 - 8 * c;
-        if (n > 0) read_any(static_cast<const T*>(p.dy) + t * p.dy_row + n0 + 8 * c, n, y);
-        if (w0 + 8 * c < p.pitch) {
-          union { int8_t b[8]; uint64_t all; } v;
-          v.all = *reinterpret_cast<const uint64_t*>(p.values + t * p.pitch + w0 + 8 * c);
-          const float step = power_of(p.exps[t * p.groups + (w0 + 8 * c) / kGroup]);
+      for (int j = 0; j < NJ; ++j) {
+        const T* src = dy + int64_t(min(t0 + yr + j * (512 / NC), tokens - 1)) * p.dy_row + 8 * yc;
+        const int n = p.out - n0 - 8 * yc;
+        vec8<T> v = {};
+        if (n >= 8) v = *reinterpret_cast<const any8<T>*>(src);
+        else
 #pragma unroll
-          for (int i = 0; i < 8; ++i) xv[i] = T(float(v.b[i]) * step);
-        }
+          for (int k = 0; k < 8; ++k)
+            if (k < n) v[k] = src[k];
+        held[j] = v;
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        yv[i] = T(y[i]);
-        bias[i] += y[i];
-      }
-      *reinterpret_cast<vec8<T>*>(lds_y + chunk_at<D>(r, c)) = yv;
-      *reinterpret_cast<vec8<T>*>(lds_x + chunk_at<D>(r, c)) = xv;
     }
-    __syncthreads();
-#pragma unroll
-    for (int s = 0; s < BT / 16; ++s) {
-      vec8<T> a[2], b[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = transposed8<T, D>(lds_y, 16 * s, 64 * (wave >> 1) + 32 * i, lane);
-        b[i] = transposed8<T, D>(lds_x, 16 * s, 64 * (wave & 1) + 32 * i, lane);
-      }
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = Elem<T>::mfma(a[i], b[j], acc[i][j]);
+    if (tid < kTokens * WT / 16) {
+      const int r = tid / (WT / 16), c = tid % (WT / 16);
+      if (w0 + 16 * c < p.pitch)
+        copy16(values + int64_t(t0) * p.pitch, uint32_t(min(r, tokens - 1 - t0)) * p.pitch + 16 * c,
+               __builtin_amdgcn_readfirstlane(lds_address(lds_raw[i % 3]) + (tid & ~63) * 16));
     }
+  };
+  auto arrived = [&](int32_t i) {        // in this wave: passed on by the next barrier
+    loads_done();
+    if constexpr (!DMA) {
+      if (i < tiles)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) *reinterpret_cast<vec8<T>*>(lds_y[i % 3] + chunk_at<NT>(yr + j * (512 / NC), yc)) = held[j];
+    }
+  };
+  // Exponents of the four groups and the presence of each of the next kAhead tokens, a thread a token.
+  uint32_t exps = 0;
+  int32_t pos = 0;
+  auto look = [&](int32_t block) {
+    const int32_t t = block * kAhead + tid;
+    exps = 0;
+    pos = -1;
+    if (tid < kAhead && t < tokens) {
+      pos = p.pos ? p.pos[t_begin + t] : 0;
+      const uint8_t* e = p.exps + (t_begin + t) * p.groups + w0 / kGroup;
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        if (w0 / kGroup + g < p.groups) exps |= uint32_t(e[g]) << (8 * g);
+    }
+  };
+  auto note = [&](int32_t block) {
+    if (tid < kAhead) {
+      lds_exps[block & 1][tid] = exps;
+      lds_gone[block & 1][tid] = pos < 0;
+    }
+  };
+  auto ready = [&](int32_t i) {
+    if (i >= tiles) return;
+    const int block = i / (kAhead / kTokens) & 1, t0 = i % (kAhead / kTokens) * kTokens;
+    {
+      const int r = tid / (WT / 8), c = tid % (WT / 8);
+      const uint64_t x = *reinterpret_cast<const uint64_t*>(lds_raw[i % 3] + r * WT + 8 * c);
+      const float step = lds_gone[block][t0 + r] ? 0.f : power_of(lds_exps[block][t0 + r] >> (8 * (c / 4)) & 255);
+      vec8<T> v;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = T(float(int8_t(x >> (8 * k))) * step);
+      *reinterpret_cast<vec8<T>*>(lds_x[i & 1] + chunk_at<WT>(r, c)) = v;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int r = yr + j * (512 / NC);
+      vec8<T>* y = reinterpret_cast<vec8<T>*>(lds_y[i % 3] + chunk_at<NT>(r, yc));
+      if (lds_gone[block][t0 + r]) {
+        const vec8<T> zero = {};
+        *y = zero;
+      } else if (sums) {
+        const vec8<T> v = *y;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bias[k] += float(v[k]);
+      }
+    }
+  };
+  if (tiles > 0) {
+    look(0);
+    fetch(0);
+    note(0);
+    arrived(0);
     __syncthreads();
+    fetch(1);
+    ready(0);
+  }
+  for (int32_t i = 0; i < tiles; ++i) {
+    constexpr int kEach = kAhead / kTokens;
+    if (i % kEach == kEach / 2) note(i / kEach + 1);
+    arrived(i + 1);
+    __syncthreads();
+    if (i % kEach == 0) look(i / kEach + 1);
+    fetch(i + 2);
+    ready(i + 1);
+#pragma unroll 1
+    for (int s = 0; s < kTokens / 16; ++s) {
+      vec8<T> a[NB], b[2];
+#pragma unroll
+      for (int k = 0; k < NB; ++k) a[k] = transposed8<T, NT>(lds_y[i % 3], 16 * s, NT / 4 * (wave >> 1) + 32 * k, lane);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) b[k] = transposed8<T, WT>(lds_x[i & 1], 16 * s, 64 * (wave & 1) + 32 * k, lane);
+#pragma unroll
+      for (int k = 0; k < NB; ++k)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[k][j] = Elem<T>::mfma(a[k], b[j], acc[k][j]);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NB; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int n = n0 + 64 * (wave >> 1) + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, w = w0 + 64 * (wave & 1) + 32 * j + (lane & 31);
+        const int n = n0 + NT / 4 * (wave >> 1) + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, w = w0 + 64 * (wave & 1) + 32 * j + (lane & 31);
         if (n < p.out && w < p.width) p.dw[(int64_t(part) * p.out + n) * p.width + w] = acc[i][j][r];
       }
-  if (tw == 0 && p.db) {
-    float* sums = reinterpret_cast<float*>(lds_y);       // [16][128]
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sums[(tid / 16) * D + 8 * c + i] = bias[i];
+  if (sums) {
     __syncthreads();
-    if (tid < D && n0 + tid < p.out) {
+    float* rows = reinterpret_cast<float*>(lds_y);         // [512 / NC][NT]
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rows[yr * NT + 8 * yc + i] = bias[i];
+    __syncthreads();
+    if (tid < NT && n0 + tid < p.out) {
       float s = 0.f;
-      for (int r = 0; r < 16; ++r) s += sums[r * D + tid];
+      for (int r = 0; r < 512 / NC; ++r) s += rows[r * NT + tid];
       p.db[int64_t(part) * p.out + n0 + tid] = s;
     }
   }
 }
 
-// Adds the parts, in their order.
+// Adds the parts: eight lanes of a workgroup's 256 take every eighth part of a value each, and are added in their order.
 __global__ __launch_bounds__(256) void add_parts_kernel(const float* dw_parts, const float* db_parts, int64_t n_dw, int64_t n_db, int32_t parts, float* dw, float* db) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x;
-  const bool is_w = i < n_dw;
-  if (i >= n_dw + n_db) return;
+  __shared__ float lds[8][32];
+  const int at = threadIdx.x & 31, first = threadIdx.x >> 5;
+  const int64_t i = int64_t(blockIdx.x) * 32 + at;
+  const bool is_w = i < n_dw, in = i < n_dw + n_db;
   const float* src = is_w ? dw_parts + i : db_parts + (i - n_dw);
   const int64_t step = is_w ? n_dw : n_db;
   float s = 0.f;
-  for (int32_t k = 0; k < parts; ++k) s += src[k * step];
+  if (in)
+    for (int32_t k = first; k < parts; k += 8) s += src[k * step];
+  lds[first][at] = s;
+  __syncthreads();
+  if (!in || first) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) s += lds[k][at];
   (is_w ? dw[i] : db[i - n_dw]) = s;
+}
+
+template <typename T> void launch_grad(const GradParams& p, int32_t rows, uint32_t blocks, hipStream_t s) {
+  const bool dma = p.out % 8 == 0 && p.dy_row % 8 == 0 && p.dy_row >= 0 && p.dy_row < kMostStride && aligned16(p.dy);
+  if (rows == 128) dma ? weight_grad_kernel<T, 128, true><<<blocks, 512, 0, s>>>(p) : weight_grad_kernel<T, 128, false><<<blocks, 512, 0, s>>>(p);
+  else dma ? weight_grad_kernel<T, 256, true><<<blocks, 512, 0, s>>>(p) : weight_grad_kernel<T, 256, false><<<blocks, 512, 0, s>>>(p);
 }
 
 int check_packed(const lgp_packed* a) {
@@ -224,12 +320,13 @@ PackParams pack_params(const lgp_packed* a, int32_t per_row) {
   return p;
 }
 // Parts of the tokens: two workgroups per CU, of at least 256 tokens each.
-struct GradShape { int32_t tiles_w, tiles_n, parts; int64_t each; size_t bytes; };
+struct GradShape { int32_t rows, tiles_w, tiles_n, parts; int64_t each; size_t bytes; };
 GradShape grad_shape(int device, const lgp_packed* a, int32_t out) {
   GradShape g;
   g.tiles_w = (a->width + 127) / 128;
-  g.tiles_n = (out + 127) / 128;
-  const int64_t tiles = int64_t(g.tiles_w) * g.tiles_n, want = (int64_t(compute_units(device)) * 2 + tiles - 1) / tiles;
+  g.rows = out <= 128 ? 128 : 256;
+  g.tiles_n = (out + g.rows - 1) / g.rows;
+  const int64_t tiles = int64_t(g.tiles_w) * g.tiles_n, want = std::max<int64_t>(1, int64_t(compute_units(device)) * 2 / tiles);
   const int64_t parts = std::max<int64_t>(1, std::min(want, a->tokens / 256));
   g.each = ((a->tokens + parts - 1) / parts + 63) / 64 * 64;
   g.parts = a->tokens ? int32_t((a->tokens + g.each - 1) / g.each) : 1;
@@ -318,11 +415,11 @@ int lgp_packed_weight_grad(int device, const lgp_packed* x, const void* dy, int6
   p.dw = g.parts > 1 ? static_cast<float*>(workspace) : dw;
   p.db = !db ? nullptr : g.parts > 1 ? static_cast<float*>(workspace) + n_dw * g.parts : db;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (dy_dtype == LGP_F16) weight_grad_kernel<f16><<<uint32_t(blocks), 256, 0, s>>>(p);
-  else weight_grad_kernel<bf16><<<uint32_t(blocks), 256, 0, s>>>(p);
+  if (dy_dtype == LGP_F16) launch_grad<f16>(p, g.rows, uint32_t(blocks), s);
+  else launch_grad<bf16>(p, g.rows, uint32_t(blocks), s);
   if (g.parts > 1) {
     const int64_t n_db = db ? out : 0;
-    add_parts_kernel<<<uint32_t((n_dw + n_db + 255) / 256), 256, 0, s>>>(p.dw, p.db, n_dw, n_db, g.parts, dw, db);
+    add_parts_kernel<<<uint32_t((n_dw + n_db + 31) / 32), 256, 0, s>>>(p.dw, p.db, n_dw, n_db, g.parts, dw, db);
   }
   return launched();
 }
