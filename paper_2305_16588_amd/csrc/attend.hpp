@@ -3,6 +3,8 @@
 
 #include "layer_dev.hpp"
 
+#include <type_traits>
+
 namespace lgp {
 namespace layer {
 
@@ -47,13 +49,13 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
 }
 template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
 
-// 2^(z * log2(e)) needs z in powers of two; the tanh of the cap is kept for the backward pass.
-template <bool CAP> __device__ __forceinline__ float score(const AttendParams& p, float qk, float& tanh_out) {
+// A score in powers of two, plus `more`; the tanh of the cap is kept for the backward pass.
+template <bool CAP> __device__ __forceinline__ float score(const AttendParams& p, float qk, float more, float& tanh_out) {
   if constexpr (CAP) {
     tanh_out = 1.f - 2.f * rcp_fast(exp2_fast(qk * p.t_mul) + 1.f);
-    return tanh_out * p.z_mul;
+    return fmaf(tanh_out, p.z_mul, more);
   }
-  return qk * p.z_mul;
+  return fmaf(qk, p.z_mul, more);
 }
 
 // The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys.

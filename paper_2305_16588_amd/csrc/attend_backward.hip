@@ -95,14 +95,16 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 
   floatx16 dq[D / 32] = {};
   float sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
-  int now = 0;
-  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
+  const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
+  auto step = [&](int32_t k0, int now, auto whole) {
+    constexpr bool WHOLE = decltype(whole)::value;
     loads_done();
     if constexpr (BIAS) {
       if (tid < BN) lds_pos[now][tid] = float(next_pos);
     }
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
+    if (idle) return;
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
@@ -121,19 +123,16 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
-          float t = 0.f, z = score<CAP>(p, s[r], t), far = 0.f;
+          float t = 0.f, far = 0.f;
+          if constexpr (BIAS) far = fabsf(at - kpos[i]);
+          const float z = score<CAP>(p, s[r], BIAS ? fmaf(-slope, far, -lse) : -lse, t);
+          const float e = WHOLE || 8 * r4 + i < there ? exp2_fast(z) : 0.f, pd = e * g[r];
           if constexpr (BIAS) {
-            far = fabsf(at - kpos[i]);
-            z -= slope * far;
-          }
-          const float e = 8 * r4 + i < there ? exp2_fast(z - lse) : 0.f;
-          if constexpr (BIAS) {
-            const float pd = e * g[r];
             sum_pd += pd;
-            sum_pf += e * far;
-            sum_pdf += pd * far;
+            sum_pf = fmaf(e, far, sum_pf);
+            sum_pdf = fmaf(pd, far, sum_pdf);
           }
-          float u = e * (g[r] - delta);
+          float u = fmaf(-e, delta, pd);
           if constexpr (CAP) u *= 1.f - t * t;
           uf[r / 8][r % 8] = T(u);
         }
@@ -143,7 +142,13 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(transposed8<T, D>(tile_k, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dq[db]);
     }
+  };
+  int32_t k0 = k_begin;
+  for (; k0 + 2 * BN <= k_end; k0 += 2 * BN) {
+    step(k0, 0, std::true_type());
+    step(k0 + BN, 1, std::true_type());
   }
+  for (int now = 0; k0 < k_end; k0 += BN, ++now) step(k0, now, std::false_type());
 
   if (row >= qd.owned * p.group) return;
   if constexpr (BIAS) {
@@ -297,14 +302,17 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
   if constexpr (BIAS) at = live ? float(p.ks.pos[key_row]) : 0.f;
 
   floatx16 dk[D / 32] = {}, dv[D / 32] = {};
-  int now = 0;
-  for (int32_t h0 = hk * p.group, r0 = 0; rows > 0 && h0 < (hk + 1) * p.group; now ^= 1) {
+  const bool idle = key0 + 32 * wave >= kd.tokens;                   // a wave of keys without tokens only copies
+  int32_t h0 = hk * p.group, r0 = 0;
+  auto step = [&](auto stage_now) {
+    constexpr int now = decltype(stage_now)::value;
     loads_done();
     put_rows(now);
     __syncthreads();
     r0 += BQ;
     if (r0 >= rows) r0 = 0, h0 += 1 << p.log2_fold;
     if (h0 < (hk + 1) * p.group) stage(h0, r0, now ^ 1);
+    if (idle) return;
     const T *tile_q = lds_q[now], *tile_g = lds_g[now];
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
@@ -327,9 +335,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
-          float t = 0.f, z = score<CAP>(p, s[r], t);
-          if constexpr (BIAS) z -= slope[i] * fabsf(at - pos[i]);
-          const float e = exp2_fast(z - lse[i]);             // times kLift
+          float t = 0.f;
+          const float e = exp2_fast(score<CAP>(p, s[r], BIAS ? fmaf(-slope[i], fabsf(at - pos[i]), -lse[i]) : -lse[i], t));             // times kLift
           float u = e * ((g[r] - delta[i]) * (1.f / kLift<T>));
           if constexpr (CAP) u *= 1.f - t * t;
           pf[r / 8][r % 8] = T(e);
@@ -344,6 +351,10 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
           dk[db] = Elem<T>::mfma(transposed8<T, D>(tile_q, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dk[db]);
         }
     }
+  };
+  while (rows > 0 && h0 < (hk + 1) * p.group) {
+    step(std::integral_constant<int, 0>());
+    if (h0 < (hk + 1) * p.group) step(std::integral_constant<int, 1>());
   }
 
   if (key >= kd.owned) return;
@@ -395,7 +406,7 @@ template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams
   const uint32_t blocks = uint32_t(b.q.tiles) * p.kv_heads * p.splits, key_blocks = uint32_t(b.key_tiles) * p.kv_heads;
   if (p.qs.rows) {
     if (b.q.waves == 1) attend_dq_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
-    else attend_dq_kernel<T, D, CAP, BIAS, 4, 64><<<blocks, 256, 0, s>>>(x);
+    else attend_dq_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<blocks, 256, 0, s>>>(x);
   }
   x.tiles = int32_t(b.key_tiles);
   if (p.ks.rows) {

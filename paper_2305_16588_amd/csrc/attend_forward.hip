@@ -12,7 +12,8 @@ namespace {
 // need one exchange between the halves of the wave, and the rounded probabilities are the operand of O^T = V^T P^T as they stand
 // (layer_dev.hpp).  NW waves share the tiles of keys and values in LDS, where the next tile arrives while this one is worked on.  D is the
 // head's dimension rounded up to 32, 64 or 128, with zeros.  Scores are taken against a base that is raised, and sums and results shrunk, only
-// when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.
+// when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.  The
+// two places of a tile are two copies of the loop's body, so that no address is computed in it.
 // Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
 constexpr float kSlack = 8.f;
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
@@ -76,15 +77,18 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   }
 
   floatx16 o[D / 32] = {};
-  float base = -INFINITY, sum = 0.f;
-  int now = 0;
-  for (int32_t k0 = k_begin; k0 < k_end; k0 += BN, now ^= 1) {
+  // Scores are taken relative to `base`; a maximum beyond `limit` raises it: any, until the row has seen a score that is not -inf.
+  float base = 0.f, limit = -3e38f, sum = 0.f;
+  const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
+  auto step = [&](int32_t k0, auto stage_now) {
+    constexpr int now = decltype(stage_now)::value;
     loads_done();
     if constexpr (BIAS) {
       if (tid < BN) lds_pos[now][tid] = float(next_pos);
     }
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
+    if (idle) return;
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 
     floatx16 s[BN / 32];
@@ -95,19 +99,32 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
       for (int kk = 0; kk < D / 16; ++kk) acc = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], acc);
       s[b] = acc;
     }
-    if constexpr (CAP || BIAS) {
+    if (now == 0 && k0 == k_begin) {
+      // The first base is the first tile's maximum, found ahead: scores of a magnitude that leaves no digits for their differences are then
+      // rounded only once the base is taken off, like those of later tiles.
+      float most = -INFINITY;
 #pragma unroll
-      for (int b = 0; b < BN / 32; ++b) {
+      for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-          floatx4 kpos = {};
-          if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
+        for (int r = 0; r < 16; ++r) {
+          const int key = 32 * b + 8 * (r / 4) + 4 * half + r % 4;
+          float t, more = 0.f;
+          if constexpr (BIAS) more = -slope * fabsf(at - lds_pos[now][key]);
+          if (k0 + key < k_end) most = fmaxf(most, score<CAP>(p, s[b][r], more, t));
+        }
+      most = fmaxf(most, other_half(most));
+      if (most > -INFINITY) base = most, limit = kSlack;
+    }
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float t, z = score<CAP>(p, s[b][4 * r4 + i], t);
-            if constexpr (BIAS) z -= slope * fabsf(at - kpos[i]);
-            s[b][4 * r4 + i] = z;
-          }
+    for (int b = 0; b < BN / 32; ++b) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        floatx4 kpos = {};
+        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float t;
+          s[b][4 * r4 + i] = score<CAP>(p, s[b][4 * r4 + i], BIAS ? fmaf(-slope, fabsf(at - kpos[i]), -base) : -base, t);
         }
       }
     }
@@ -124,16 +141,21 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
 #pragma unroll
       for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
     most = fmaxf(most, other_half(most));
-    const float mul = CAP || BIAS ? 1.f : p.z_mul;          // scores that are still to be scaled are scaled with their base
-    most *= mul;
-    if (__any(most > base + kSlack)) {                      // the first tile, but for a row whose scores are all -inf: its sum stays zero
-      const float raised = fmaxf(base, most), shrink = raised == -INFINITY ? 1.f : exp2_fast(base - raised);
-      base = raised;
-      sum *= shrink;
+    if (__any(most > limit)) {
+      const bool raise = most > limit;
+      const float raised = base + most, by = raise ? raised - base : 0.f, shrink = raise ? exp2_fast(-by) : 1.f;
+      base = raise ? raised : base;
+      limit = raise ? kSlack : limit;
+      sum = sum > 0.f ? sum * shrink : sum;          // a first score far below the base of zero has nothing to shrink, and 2^-most is inf
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db) o[db] *= shrink;
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = sum == 0.f ? 0.f : o[db][r] * shrink;
+#pragma unroll
+      for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] -= by;
     }
-    const float less = base == -INFINITY ? 0.f : base;
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
 #pragma unroll
@@ -141,7 +163,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
         vec8<T> pf;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float e = exp2_fast(s[b][8 * h2 + j] * mul - less);
+          const float e = exp2_fast(s[b][8 * h2 + j]);
           sum += e;
           pf[j] = T(e);
         }
@@ -149,6 +171,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
         for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(transposed8<T, D>(tile_v, 32 * b + 16 * h2, 32 * db, lane), pf, o[db]);
       }
     }
+  };
+  for (int32_t k0 = k_begin; k0 < k_end; k0 += 2 * BN) {
+    step(k0, std::integral_constant<int, 0>());
+    if (k0 + BN < k_end) step(k0 + BN, std::integral_constant<int, 1>());
   }
 
   sum += other_half(sum);

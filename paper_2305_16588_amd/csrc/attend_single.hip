@@ -80,8 +80,7 @@ __global__ __launch_bounds__(256) void single_kernel(const AttendParams p, int32
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           float t;
-          z[i][g] = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], q[g])), t);
-          if constexpr (BIAS) z[i][g] -= slope[g] * fabsf(at - far[i]);
+          z[i][g] = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], q[g])), BIAS ? -slope[g] * fabsf(at - far[i]) : 0.f, t);
           if (k0 + i * a.keys_at_once + a.key >= keys) z[i][g] = -INFINITY;
         }
 #pragma unroll
@@ -204,9 +203,9 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
           float dk[8] = {}, dv[8] = {};
 #pragma unroll
           for (int h = 0; h < G; ++h) {
-            float t = 0.f, z = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], x.q[h])), t);
-            if constexpr (BIAS) z -= x.slope[h] * far[i];
-            const float e = key < kd.tokens ? exp2_fast(z - x.lse[h]) : 0.f, dp = sum_of_lanes<L>(dot8<T>(vf[i], x.g[h]));
+            float t = 0.f;
+            const float z = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], x.q[h])), BIAS ? fmaf(-x.slope[h], far[i], -x.lse[h]) : -x.lse[h], t);
+            const float e = key < kd.tokens ? exp2_fast(z) : 0.f, dp = sum_of_lanes<L>(dot8<T>(vf[i], x.g[h]));
             if constexpr (BIAS) {
               pd[h] += e * dp;
               pf[h] += e * far[i];
@@ -263,9 +262,8 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
         x.load(p, a, int64_t(qd.begin) + row);
 #pragma unroll
         for (int h = 0; h < G; ++h) {
-          float t = 0.f, z = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf, x.q[h])), t);
-          if constexpr (BIAS) z -= x.slope[h] * fabsf(x.at - far);
-          const float e = exp2_fast(z - x.lse[h]);
+          float t = 0.f;
+          const float e = exp2_fast(score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf, x.q[h])), BIAS ? fmaf(-x.slope[h], fabsf(x.at - far), -x.lse[h]) : -x.lse[h], t));
           float u = e * (sum_of_lanes<L>(dot8<T>(vf, x.g[h])) - x.delta[h]);
           if constexpr (CAP) u *= 1.f - t * t;
 #pragma unroll
