@@ -95,6 +95,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 
   floatx16 dq[D / 32] = {};
   float sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
+  Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, int now, auto whole) {
     constexpr bool WHOLE = decltype(whole)::value;
@@ -105,14 +106,15 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     if (idle) return;
+    if constexpr (D == 128) at_tile.again();
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
       floatx16 s = {}, g = {};
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], s);
-        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_v + chunk_at<D>(32 * b + col, 2 * kk + half)), df[kk], g);
+        s = Elem<T>::mfma(at_tile.along(tile_k, 32 * b, kk), qf[kk], s);
+        g = Elem<T>::mfma(at_tile.along(tile_v, 32 * b, kk), df[kk], g);
       }
       const int32_t there = k0 + BN <= k_end ? BN : k_end - k0 - 32 * b - 4 * half;      // places of this block's half that are keys
       vec8<T> uf[2];
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(transposed8<T, D>(tile_k, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dq[db]);
+        for (int db = 0; db < D / 32; ++db) dq[db] = Elem<T>::mfma(at_tile.across(tile_k, 32 * b + 16 * h2, 32 * db), uf[h2], dq[db]);
     }
   };
   int32_t k0 = k_begin;
@@ -226,11 +228,14 @@ __global__ __launch_bounds__(64) void slopes_end_kernel(const float* partial, fl
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
-__global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_dkv_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
   __shared__ __align__(16) T lds_q[2][BQ * D];
   __shared__ __align__(16) T lds_g[2][BQ * D];
   __shared__ __align__(16) float lds_row[2][4][BQ];       // lse, delta, slope, position
+  // With heads of 128 the wave's keys, values and both results would be all registers there are: values are read from LDS.
+  constexpr bool kHeld = D < 128 || NW == 1;
+  __shared__ __align__(16) T lds_v[kHeld ? 8 : kKeys * D];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
 
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
@@ -287,7 +292,7 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
   const int32_t key = key0 + 32 * wave + col;
   const bool live = key < kd.tokens;
   const int64_t key_row = int64_t(kd.begin) + key;
-  vec8<T> kf[D / 16], vf[D / 16];
+  vec8<T> kf[D / 16], vf[kHeld ? D / 16 : 1];
   {
     const T* k = static_cast<const T*>(p.k) + key_row * p.k_row + int64_t(hk) * p.k_head;
     const T* v = static_cast<const T*>(p.v) + key_row * p.v_row + int64_t(hk) * p.v_head;
@@ -295,13 +300,16 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
     for (int kk = 0; kk < D / 16; ++kk) {
       const int d = 16 * kk + 8 * half;
       kf[kk] = load8(k + d, live && d < p.dim, p.negate);
-      vf[kk] = load8(v + d, live && d < p.dim, false);
+      const vec8<T> x = load8(v + d, live && d < p.dim, false);
+      if constexpr (kHeld) vf[kk] = x;
+      else *reinterpret_cast<vec8<T>*>(lds_v + chunk_at<D>(32 * wave + col, 2 * kk + half)) = x;
     }
   }
   float at = 0.f;
   if constexpr (BIAS) at = live ? float(p.ks.pos[key_row]) : 0.f;
 
   floatx16 dk[D / 32] = {}, dv[D / 32] = {};
+  Places<T, D> at_tile(lane);
   const bool idle = key0 + 32 * wave >= kd.tokens;                   // a wave of keys without tokens only copies
   int32_t h0 = hk * p.group, r0 = 0;
   auto step = [&](auto stage_now) {
@@ -313,14 +321,16 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
     if (r0 >= rows) r0 = 0, h0 += 1 << p.log2_fold;
     if (h0 < (hk + 1) * p.group) stage(h0, r0, now ^ 1);
     if (idle) return;
+    if constexpr (D == 128) at_tile.again();
     const T *tile_q = lds_q[now], *tile_g = lds_g[now];
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
       floatx16 s = {}, g = {};
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
-        s = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_q + chunk_at<D>(32 * b + col, 2 * kk + half)), kf[kk], s);
-        g = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_g + chunk_at<D>(32 * b + col, 2 * kk + half)), vf[kk], g);
+        s = Elem<T>::mfma(at_tile.along(tile_q, 32 * b, kk), kf[kk], s);
+        g = Elem<T>::mfma(at_tile.along(tile_g, 32 * b, kk),
+                             kHeld ? vf[kHeld ? kk : 0] : at_tile.along(lds_v + 32 * wave * D, 0, kk), g);
       }
       vec8<T> pf[2], uf[2];
 #pragma unroll
@@ -347,8 +357,8 @@ __global__ __launch_bounds__(64 * NW, D == 128 || NW == 1 ? 1 : 2) void attend_d
       for (int h2 = 0; h2 < 2; ++h2)
 #pragma unroll
         for (int db = 0; db < D / 32; ++db) {
-          dv[db] = Elem<T>::mfma(transposed8<T, D>(tile_g, 32 * b + 16 * h2, 32 * db, lane), pf[h2], dv[db]);
-          dk[db] = Elem<T>::mfma(transposed8<T, D>(tile_q, 32 * b + 16 * h2, 32 * db, lane), uf[h2], dk[db]);
+          dv[db] = Elem<T>::mfma(at_tile.across(tile_g, 32 * b + 16 * h2, 32 * db), pf[h2], dv[db]);
+          dk[db] = Elem<T>::mfma(at_tile.across(tile_q, 32 * b + 16 * h2, 32 * db), uf[h2], dk[db]);
         }
     }
   };
@@ -411,7 +421,7 @@ template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams
   x.tiles = int32_t(b.key_tiles);
   if (p.ks.rows) {
     if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<key_blocks, 64, 0, s>>>(x);
-    else attend_dkv_kernel<T, D, CAP, BIAS, 4, 64><<<key_blocks, 256, 0, s>>>(x);
+    else attend_dkv_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<key_blocks, 256, 0, s>>>(x);
   }
 }
 template <typename T, int D> void launch(const AttendParams& p, const BackwardShape& b, bool cap, hipStream_t s) {

@@ -79,6 +79,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   floatx16 o[D / 32] = {};
   // Scores are taken relative to `base`; a maximum beyond `limit` raises it: any, until the row has seen a score that is not -inf.
   float base = 0.f, limit = -3e38f, sum = 0.f;
+  Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, auto stage_now) {
     constexpr int now = decltype(stage_now)::value;
@@ -89,6 +90,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
     __syncthreads();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     if (idle) return;
+    if constexpr (D == 128) at_tile.again();
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 
     floatx16 s[BN / 32];
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
     for (int b = 0; b < BN / 32; ++b) {
       floatx16 acc = {};
 #pragma unroll
-      for (int kk = 0; kk < D / 16; ++kk) acc = Elem<T>::mfma(*reinterpret_cast<const vec8<T>*>(tile_k + chunk_at<D>(32 * b + col, 2 * kk + half)), qf[kk], acc);
+      for (int kk = 0; kk < D / 16; ++kk) acc = Elem<T>::mfma(at_tile.along(tile_k, 32 * b, kk), qf[kk], acc);
       s[b] = acc;
     }
     if (now == 0 && k0 == k_begin) {
@@ -168,7 +170,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
           pf[j] = T(e);
         }
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(transposed8<T, D>(tile_v, 32 * b + 16 * h2, 32 * db, lane), pf, o[db]);
+        for (int db = 0; db < D / 32; ++db) o[db] = Elem<T>::mfma(at_tile.across(tile_v, 32 * b + 16 * h2, 32 * db), pf, o[db]);
       }
     }
   };

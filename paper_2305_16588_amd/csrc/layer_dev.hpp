@@ -21,7 +21,7 @@ typedef short shortx4 __attribute__((ext_vector_type(4)));
 // the sum; of D it holds column l % 32, register r being row 8 * (r / 4) + 4 * (l / 32) + r % 4.  Any order of the sum's places does as
 // long as A and B agree, so registers 8 s .. 8 s + 7 of a D are, rounded, a B operand whose places are rows
 // 16 s + 8 * (j / 4) + 4 * (l / 32) + j % 4: a product is handed to the next one without leaving the registers, and the other operand is
-// read in that order (transposed4 below, two of them).
+// read in that order (Places::across).
 template <typename T> struct Elem;
 template <> struct Elem<f16> {
   typedef f16 x8 __attribute__((ext_vector_type(8)));
@@ -124,21 +124,31 @@ inline Divisor divisor(uint32_t by) {
 }
 __device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor& d) { return d.by == 1 ? n : __umulhi(n, d.mul) >> d.shift; }
 
-// Operand A or B with the places of the sum running along the rows of a tile: four elements of column (lane % 32) + col0, of rows
-// row0 + 4 * (lane / 32) ... + 3.  Each 16 lanes read four rows of 16 columns, which the LDS hands out transposed.
-template <int D> __device__ __forceinline__ shortx4 transposed4(const void* tile, int row0, int col0, int lane) {
-  const int i = lane & 15;
-  const int row = row0 + 4 * (lane >> 5) + (i >> 2);
-  const int col = col0 + 16 * ((lane >> 4) & 1) + 4 * (i & 3);
-  const short* p = static_cast<const short*>(tile) + chunk_at<D>(row, col >> 3) + (col & 7);
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p);
-}
-template <typename T, int D> __device__ __forceinline__ vec8<T> transposed8(const void* tile, int row0, int col0, int lane) {
-  union { shortx4 s[2]; vec8<T> v; } u;
-  u.s[0] = transposed4<D>(tile, row0, col0, lane);
-  u.s[1] = transposed4<D>(tile, row0 + 8, col0, lane);
-  return u.v;
-}
+// Where a lane finds its operands in such tiles.  Both places are those of the first of many, from which the others differ by a few bits or by
+// whole rows: so two registers hold all addresses, if the compiler is kept from taking one for each (again(), once in a loop's body).
+template <typename T, int D> struct Places {
+  int row, col;
+  __device__ __forceinline__ explicit Places(int lane) {
+    const int r = lane & 31, i = lane & 15, r2 = 4 * (lane >> 5) + (i >> 2), c2 = 16 * ((lane >> 4) & 1) + 4 * (i & 3);
+    row = chunk_at<D>(r, lane >> 5);
+    col = chunk_at<D>(r2, c2 >> 3) + (c2 & 7);
+  }
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(row), "+v"(col)); }
+  // The operand whose rows are 32 rows of the tile and whose sum runs along them: elements 16 kk + 8 * (lane / 32) ... + 7 of row row0 + lane % 32.
+  __device__ __forceinline__ vec8<T> along(const T* tile, int row0, int kk) const {
+    return *reinterpret_cast<const vec8<T>*>(tile + row0 * D + (row ^ (kk << 4)));
+  }
+  // The operand whose rows are 32 columns of the tile and whose sum runs along its rows: column col0 + lane % 32 of rows row0 + 4 * (lane / 32) ... + 3
+  // and of those eight further on (row0 a multiple of 16, col0 of 32).  Each 16 lanes read four rows of 16 columns, which the LDS hands out transposed.
+  __device__ __forceinline__ vec8<T> across(const T* tile, int row0, int col0) const {
+    typedef __attribute__((address_space(3))) shortx4* place;
+    union { shortx4 s[2]; vec8<T> v; } u;
+    const int at = col ^ col0;
+    u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + row0 * D + at));
+    u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + (row0 + 8) * D + (at ^ 8)));       // the swizzle of a row eight further on
+    return u.v;
+  }
+};
 
 // Documents: document d owns rows offsets[d] .. offsets[d + 1], the first lens[d] of which hold tokens.  The first begins at row 0 and the
 // last ends at the last row, whatever the array says there; what else makes no sense is clamped, so no row outside is ever touched.

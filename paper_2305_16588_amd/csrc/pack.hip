@@ -138,6 +138,8 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
   const int yc = tid % NC, yr = tid / NC;        // a thread's chunk of dy, and its first row
   floatx16 acc[NB][2] = {};
   float bias[8] = {};
+  const Places<T, NT> at_y(lane);
+  const Places<T, WT> at_x(lane);
 
   vec8<T> held[DMA ? 1 : NJ];
   auto fetch = [&](int32_t i) {
@@ -242,9 +244,9 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
     for (int s = 0; s < kTokens / 16; ++s) {
       vec8<T> a[NB], b[2];
 #pragma unroll
-      for (int k = 0; k < NB; ++k) a[k] = transposed8<T, NT>(lds_y[i % 3], 16 * s, NT / 4 * (wave >> 1) + 32 * k, lane);
+      for (int k = 0; k < NB; ++k) a[k] = at_y.across(lds_y[i % 3], 16 * s, NT / 4 * (wave >> 1) + 32 * k);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) b[k] = transposed8<T, WT>(lds_x[i & 1], 16 * s, 64 * (wave & 1) + 32 * k, lane);
+      for (int k = 0; k < 2; ++k) b[k] = at_x.across(lds_x[i & 1], 16 * s, 64 * (wave & 1) + 32 * k);
 #pragma unroll
       for (int k = 0; k < NB; ++k)
 #pragma unroll
