@@ -25,6 +25,7 @@ struct AttendParams {
   float t_mul;               // 2 * log2(e) * scale / cap, so that tanh = 1 - 2 / (exp2(qk * t_mul) + 1)
   bool negate;
   const float* slopes;
+  float docs_per_tile;
   int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys
   // forward
   void *out, *rest;
@@ -80,6 +81,7 @@ template <typename T> constexpr float kLiftLog2 = 0.f;
 template <> inline constexpr float kLiftLog2<f16> = 12.f;
 
 // Launch shapes, chosen on the host by what it knows: rows and documents.
+constexpr int kMostSplits = 256;        // a thread of join_kernel each
 constexpr int kForwardRows = 32;        // folded rows of a wave
 struct ForwardShape { int waves; int64_t tiles; int splits; };
 ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a);

@@ -36,9 +36,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
     split = piece % p.splits;
     hk = piece / p.splits;
   }
-  const int32_t doc = document_of(p.qs, p.n_docs, p.group, kRows, tile, lane);
-  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
-  const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
+  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, lane);
+  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
+  const int32_t row0 = (tile - doc.first) * kRows;
   if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
   int32_t k_begin, k_end;
@@ -180,49 +180,54 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
     }
 }
 
-// Adds the parts of dq.  A thread has four elements of a row.
+// Adds the parts of dq, like join_kernel.
 template <typename T>
 __global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
-  const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4, all = int64_t(p.qs.rows) * p.heads * p.dim;
-  if (i >= all) return;
+  __shared__ __align__(16) floatx4 sums[8][32];
+  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+  const int64_t row = blockIdx.x, rows = int64_t(p.qs.rows) * p.heads;
   floatx4 x = {};
-  for (int32_t s = 0; s < p.splits; ++s) x += *reinterpret_cast<const floatx4*>(p.part_o + s * all + i);
-  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.dq) + i) = vec4<T>{T(x[0]), T(x[1]), T(x[2]), T(x[3])};
+  if (4 * lane < p.dim)
+#pragma unroll 4
+    for (int32_t s = part; s < p.splits; s += 8) x += *reinterpret_cast<const floatx4*>(p.part_o + (s * rows + row) * p.dim + 4 * lane);
+  sums[part][lane] = x;
+  __syncthreads();
+  if (part || 4 * lane >= p.dim) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) x += sums[k][lane];
+  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.dq) + row * p.dim + 4 * lane) = vec4<T>{T(x[0]), T(x[1]), T(x[2]), T(x[3])};
 }
 
-// Gradient of the slopes from the sums of all rows, in two steps of a fixed order: kSlopeGroups workgroups take every kSlopeGroups-th token
-// of a head, then one adds theirs.
-constexpr int kSlopeGroups = 64;
-__device__ __forceinline__ float workgroup_sum(float x, float* lds) {
-#pragma unroll
-  for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return lds[0] + lds[1] + lds[2] + lds[3];
-}
+// Gradient of the slopes from the sums of all rows, in two steps of a fixed order: kSlopeThreads threads take rows a multiple of the number of
+// heads apart, so that each adds up for one head, then a workgroup adds up what is there of a head.
+constexpr int64_t kSlopeThreads = 65536;
 __global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, float* partial) {
-  __shared__ float lds[4];
-  const int32_t head = blockIdx.x;
-  const int64_t rows = int64_t(p.qs.rows) * p.heads;
+  const int64_t rows = int64_t(p.qs.rows) * p.heads, each = kSlopeThreads / p.heads * p.heads, at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (at >= each) return;
   float x = 0.f;
-  for (int64_t t = int64_t(blockIdx.y) * 256 + threadIdx.x; t < p.qs.rows; t += kSlopeGroups * 256) {
+  for (int64_t r = at; r < rows; r += each) {
     float pd = 0.f, pf = 0.f, pdf = 0.f;
     for (int32_t s = 0; s < p.splits; ++s) {
-      const float* m = p.sums + (s * rows + t * p.heads + head) * 3;
+      const float* m = p.sums + (s * rows + r) * 3;
       pd += m[0];
       pf += m[1];
       pdf += m[2];
     }
     x -= pdf - pd * pf;
   }
-  x = workgroup_sum(x, lds);
-  if (threadIdx.x == 0) partial[head * kSlopeGroups + blockIdx.y] = x;
+  partial[at] = x;
 }
-__global__ __launch_bounds__(64) void slopes_end_kernel(const float* partial, float* out) {
-  float x = partial[blockIdx.x * kSlopeGroups + threadIdx.x];
+__global__ __launch_bounds__(256) void slopes_end_kernel(const float* partial, int32_t heads, float* out) {
+  __shared__ float lds[4];
+  const int32_t each = int32_t(kSlopeThreads) / heads;
+  float x = 0.f;
+#pragma unroll 8
+  for (int32_t i = threadIdx.x; i < each; i += 256) x += partial[int64_t(i) * heads + blockIdx.x];
 #pragma unroll
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
-  if (threadIdx.x == 0) out[blockIdx.x] = x;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
+  __syncthreads();
+  if (threadIdx.x == 0) out[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
@@ -247,9 +252,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
     tile = piece % p.tiles;
     hk = piece / p.tiles;
   }
-  const int32_t doc = document_of(p.ks, p.n_docs, 1, kKeys, tile, lane);
-  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
-  const int32_t key0 = (tile - first_tile(p.ks, doc, p.n_docs, 1, kKeys)) * kKeys;
+  const Found doc = find_tile(p.ks, p.n_docs, p.docs_per_tile, 1, kKeys, tile, lane);
+  const Span kd = doc.span, qd = other_side(p.qs, p.ks, doc, p.n_docs);
+  const int32_t key0 = (tile - doc.first) * kKeys;
   if (key0 < 0 || key0 >= kd.owned) return;
 
   // Up to 16 heads of a token, if they divide 16, are folded; otherwise the heads that share this one are gone through one after the other.
@@ -405,7 +410,7 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
   b.delta = 0;
   b.sums = up(rows);
   b.partial = b.sums + (a->slopes ? up(rows * 3 * b.q.splits) : 0);
-  b.parts = b.partial + (a->slopes ? size_t(a->heads) * kSlopeGroups : 0);
+  b.parts = b.partial + (a->slopes ? size_t(kSlopeThreads) : 0);
   b.bytes = (b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0)) * sizeof(float);
   return b;
 }
@@ -413,12 +418,14 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const BackwardShape& b, hipStream_t s) {
   AttendParams x = p;
   x.tiles = int32_t(b.q.tiles);
+  x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.q.tiles, 1));
   const uint32_t blocks = uint32_t(b.q.tiles) * p.kv_heads * p.splits, key_blocks = uint32_t(b.key_tiles) * p.kv_heads;
   if (p.qs.rows) {
     if (b.q.waves == 1) attend_dq_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
     else attend_dq_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<blocks, 256, 0, s>>>(x);
   }
   x.tiles = int32_t(b.key_tiles);
+  x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.key_tiles, 1));
   if (p.ks.rows) {
     if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<key_blocks, 64, 0, s>>>(x);
     else attend_dkv_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<key_blocks, 256, 0, s>>>(x);
@@ -433,8 +440,7 @@ template <typename T> void launch(const AttendParams& p, const BackwardShape& b,
   else if (p.dim <= 64) launch<T, 64>(p, b, cap, s);
   else launch<T, 128>(p, b, cap, s);
   if (p.splits > 1) {
-    const int64_t threads = int64_t(p.qs.rows) * p.heads * (p.dim / 4);
-    add_kernel<T><<<uint32_t((threads + 255) / 256), 256, 0, s>>>(p);
+    add_kernel<T><<<uint32_t(p.qs.rows * p.heads), 256, 0, s>>>(p);
   }
 }
 
@@ -490,8 +496,8 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
   else if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
   else launch<bf16>(p, b, att->cap > 0.f, s);
   if (d_slopes) {
-    slopes_kernel<<<dim3(att->heads, kSlopeGroups), 256, 0, s>>>(p, w + b.partial);
-    slopes_end_kernel<<<att->heads, 64, 0, s>>>(w + b.partial, d_slopes);
+    slopes_kernel<<<kSlopeThreads / 256, 256, 0, s>>>(p, w + b.partial);
+    slopes_end_kernel<<<att->heads, 256, 0, s>>>(w + b.partial, att->heads, d_slopes);
   }
   return launched();
 }

@@ -37,9 +37,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
     split = piece % p.splits;
     hk = piece / p.splits;
   }
-  const int32_t doc = document_of(p.qs, p.n_docs, p.group, kRows, tile, lane);
-  const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
-  const int32_t row0 = (tile - first_tile(p.qs, doc, p.n_docs, p.group, kRows)) * kRows;
+  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, lane);
+  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
+  const int32_t row0 = (tile - doc.first) * kRows;
   if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
   int32_t k_begin, k_end;
@@ -225,23 +225,39 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   if (half == 0) p.lse[at_out] = live && sum != 0.f ? (base + log2_fast(sum)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A thread has four elements of a row.
+// Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A workgroup has a row, eight groups of 32 lanes a
+// part at a time, a lane four elements.
 template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
-  const int32_t per_row = p.dim / 4;
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, row = i / per_row, rows = int64_t(p.qs.rows) * p.heads;
-  if (row >= rows) return;
-  const int d = int(i % per_row) * 4;
-  float top = -INFINITY;
-  for (int32_t s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_ml[(s * rows + row) * 2]);
-  const float base = top == -INFINITY ? 0.f : top;
+  __shared__ float weight[kMostSplits], high[4], added[4];
+  __shared__ __align__(16) floatx4 sums[8][32];
+  const int tid = threadIdx.x, lane = tid & 31, part = tid >> 5;
+  const int64_t row = blockIdx.x, rows = int64_t(p.qs.rows) * p.heads;
+  const bool in = tid < p.splits;
+  const float top = in ? p.part_ml[(tid * rows + row) * 2] : -INFINITY, mine = in ? p.part_ml[(tid * rows + row) * 2 + 1] : 0.f;
+  float most = top;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+  if ((tid & 63) == 0) high[tid >> 6] = most;
+  __syncthreads();
+  most = fmaxf(fmaxf(high[0], high[1]), fmaxf(high[2], high[3]));
+  const float w = exp2_fast(top - (most == -INFINITY ? 0.f : most));
+  if (in) weight[tid] = w;
+  float sum = in ? w * mine : 0.f;
+#pragma unroll
+  for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, 64);
+  if ((tid & 63) == 0) added[tid >> 6] = sum;
+  __syncthreads();
+  sum = added[0] + added[1] + added[2] + added[3];
   floatx4 o = {};
-  float sum = 0.f;
-  for (int32_t s = 0; s < p.splits; ++s) {
-    const float w = exp2_fast(p.part_ml[(s * rows + row) * 2] - base);
-    sum += w * p.part_ml[(s * rows + row) * 2 + 1];
-    o += w * *reinterpret_cast<const floatx4*>(p.part_o + (s * rows + row) * p.dim + d);
-  }
+  if (4 * lane < p.dim)
+#pragma unroll 4
+    for (int32_t s = part; s < p.splits; s += 8) o += weight[s] * *reinterpret_cast<const floatx4*>(p.part_o + (s * rows + row) * p.dim + 4 * lane);
+  sums[part][lane] = o;
+  __syncthreads();
+  if (part || 4 * lane >= p.dim) return;
+#pragma unroll
+  for (int k = 1; k < 8; ++k) o += sums[k][lane];
   const float inv = sum > 0.f ? 1.f / sum : sum;
   vec4<T> x, y;
 #pragma unroll
@@ -249,9 +265,9 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
     x[j] = T(o[j] * inv);
     y[j] = T(o[j] * inv - float(x[j]));
   }
-  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.out) + row * p.dim + d) = x;
-  if (p.rest) *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.rest) + row * p.dim + d) = y;
-  if (d == 0) p.lse[row] = sum != 0.f ? (top + log2_fast(sum)) * kLn2 : -INFINITY;
+  *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.out) + row * p.dim + 4 * lane) = x;
+  if (p.rest) *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.rest) + row * p.dim + 4 * lane) = y;
+  if (lane == 0) p.lse[row] = sum != 0.f ? (most + log2_fast(sum)) * kLn2 : -INFINITY;
 }
 
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, int waves, hipStream_t s) {
@@ -268,8 +284,7 @@ template <typename T> void launch(const AttendParams& p, int waves, bool cap, hi
   else if (p.dim <= 64) launch<T, 64>(p, waves, cap, s);
   else launch<T, 128>(p, waves, cap, s);
   if (p.splits > 1) {
-    const int64_t threads = int64_t(p.qs.rows) * p.heads * (p.dim / 4);
-    join_kernel<T><<<uint32_t((threads + 255) / 256), 256, 0, s>>>(p);
+    join_kernel<T><<<uint32_t(p.qs.rows * p.heads), 256, 0, s>>>(p);
   }
 }
 
@@ -324,7 +339,7 @@ ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attenti
   f.waves = d->q_rows * group <= 32 * n ? 1 : 4;
   f.tiles = tiles_of(d->q_rows, group, d->n_docs, kForwardRows * f.waves);
   const int64_t waves = f.tiles * a->kv_heads * f.waves, room = int64_t(compute_units(device)) * 8, keys = d->k_rows / n;
-  f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256, int64_t(256)})));
+  f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256, int64_t(kMostSplits)})));
   return f;
 }
 
@@ -354,6 +369,7 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
   if (f.tiles * att->kv_heads * f.splits >= int64_t(1) << 31) return LGP_EUNSUPPORTED;
   AttendParams p = attend_params(docs, att);
   p.tiles = int32_t(f.tiles);
+  p.docs_per_tile = float(p.n_docs) / float(p.tiles);
   p.splits = f.splits;
   p.out = out;
   p.rest = rest;

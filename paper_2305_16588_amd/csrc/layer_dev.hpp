@@ -165,10 +165,10 @@ __device__ __forceinline__ int32_t offset_of(const Side& s, int32_t d, int32_t n
   const int32_t o = s.offsets[d];
   return o < 0 ? 0 : o > s.rows ? s.rows : o;
 }
-__device__ __forceinline__ Span span_of(const Side& s, int32_t d, int32_t n) {
+__device__ __forceinline__ Span span_between(const Side& s, int32_t d, int32_t begin, int32_t end) {       // d is the same in the whole wave
   Span x;
-  x.begin = __builtin_amdgcn_readfirstlane(offset_of(s, d, n));         // d is the same in the whole wave
-  const int32_t end = __builtin_amdgcn_readfirstlane(offset_of(s, d + 1, n));
+  x.begin = __builtin_amdgcn_readfirstlane(begin);
+  end = __builtin_amdgcn_readfirstlane(end);
   x.owned = end > x.begin ? end - x.begin : 0;
   x.tokens = x.owned;
   if (s.lens) {
@@ -177,22 +177,42 @@ __device__ __forceinline__ Span span_of(const Side& s, int32_t d, int32_t n) {
   }
   return x;
 }
+__device__ __forceinline__ Span span_of(const Side& s, int32_t d, int32_t n) { return span_between(s, d, offset_of(s, d, n), offset_of(s, d + 1, n)); }
 
 // Tiles of `size` rows, found without a list of them: with `fold` rows per token, document d has the tiles from
 // floor(offset * fold / size) + d on, which leaves each at least as many as its rows take, and all of them rows * fold / size + n.  A wave
-// looks for the document of a tile among 64 candidates at a time: three dependent loads for 262 144 documents.
-__device__ __forceinline__ int32_t first_tile(const Side& s, int32_t d, int32_t n, int32_t fold, int32_t size) {
-  return int32_t(int64_t(offset_of(s, d, n)) * fold / size) + d;
-}
-__device__ __forceinline__ int32_t document_of(const Side& s, int32_t n, int32_t fold, int32_t size, int32_t tile, int lane) {
-  int32_t lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int32_t step = (hi - lo + 63) / 64, d = lo + (lane + 1) * step;
-    const bool before = int64_t(lo) + int64_t(lane + 1) * step < hi && first_tile(s, d, n, fold, size) <= tile;
-    lo += step * __popcll(__ballot(before));
-    hi = hi < lo + step ? hi : lo + step;
+// looks at 64 documents around where the tile would be if all had as many rows, which also tells where the document begins and ends; if it
+// is not among them, at 64 between the ends of what is left, until it is found.
+__device__ __forceinline__ int32_t first_tile(int32_t offset, int32_t d, int32_t fold, int32_t size) { return int32_t(int64_t(offset) * fold / size) + d; }
+struct Found { int32_t doc, first; Span span; };       // first: its first tile
+__device__ __forceinline__ Found find_tile(const Side& s, int32_t n, float docs_per_tile, int32_t fold, int32_t size, int32_t tile, int lane) {
+  Found f;
+  int32_t lo = int32_t(float(tile) * docs_per_tile) - 31;
+  lo = lo > n - 63 ? n - 63 : lo;
+  lo = lo < 0 ? 0 : lo;
+  int32_t at = lo + lane < n ? lo + lane : n, offset = offset_of(s, at, n);
+  int known = __popcll(__ballot(lo + lane <= n && first_tile(offset, at, fold, size) <= tile));       // of them, begin no later than the tile
+  if (known == 0 || known == 64) {
+    int32_t hi = known ? n : lo;
+    lo = known ? lo + 63 : 0;
+    while (hi - lo > 1) {
+      const int32_t step = (hi - lo + 63) / 64, d = lo + (lane + 1) * step;
+      lo += step * __popcll(__ballot(d < hi && first_tile(offset_of(s, d, n), d, fold, size) <= tile));
+      hi = hi < lo + step ? hi : lo + step;
+    }
+    at = lo + lane < n ? lo + lane : n;
+    offset = offset_of(s, at, n);
+    known = 1;
   }
-  return __builtin_amdgcn_readfirstlane(lo);
+  f.doc = __builtin_amdgcn_readfirstlane(lo + known - 1);
+  const int32_t begin = __builtin_amdgcn_readlane(offset, __builtin_amdgcn_readfirstlane(known - 1));
+  f.first = first_tile(begin, f.doc, fold, size);
+  f.span = span_between(s, f.doc, begin, __builtin_amdgcn_readlane(offset, __builtin_amdgcn_readfirstlane(known & 63)));
+  return f;
+}
+// The same document on the other side, which may be the same rows.
+__device__ __forceinline__ Span other_side(const Side& other, const Side& s, const Found& f, int32_t n) {
+  return other.offsets == s.offsets && other.lens == s.lens && other.rows == s.rows ? f.span : span_of(other, f.doc, n);
 }
 inline int64_t tiles_of(int64_t rows, int64_t fold, int64_t n, int64_t size) { return rows * fold / size + n; }
 
