@@ -83,7 +83,7 @@ template <> inline constexpr float kLiftLog2<f16> = 12.f;
 // Launch shapes, chosen on the host by what it knows: rows and documents.
 constexpr int kMostSplits = 256;        // a thread of join_kernel each
 constexpr int kForwardRows = 32;        // folded rows of a wave
-struct ForwardShape { int waves; int64_t tiles; int splits; };
+struct ForwardShape { int waves, key_waves; int64_t tiles; int splits; };      // waves of rows, and of parts of the keys, in a workgroup
 ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a);
 
 }  // namespace layer

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
   if (p.dim < D) {
     clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
     clear_tile<T, 2 * BN * D, kThreads>(lds_v[0], tid);
-    __syncthreads();
+    tile_ready<(NW > 1)>();
   }
   if (k_begin < k_end) stage(k_begin, 0);
 
@@ -99,11 +99,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, int now, auto whole) {
     constexpr bool WHOLE = decltype(whole)::value;
-    loads_done();
     if constexpr (BIAS) {
       if (tid < BN) lds_pos[now][tid] = float(next_pos);
     }
-    __syncthreads();
+    tile_ready<(NW > 1)>();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     if (idle) return;
     if constexpr (D == 128) at_tile.again();
@@ -290,7 +289,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
   if (p.dim < D) {
     clear_tile<T, 2 * BQ * D, kThreads>(lds_q[0], tid);
     clear_tile<T, 2 * BQ * D, kThreads>(lds_g[0], tid);
-    __syncthreads();
+    tile_ready<(NW > 1)>();
   }
   if (rows > 0) stage(hk * p.group, 0, 0);
 
@@ -319,9 +318,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
   int32_t h0 = hk * p.group, r0 = 0;
   auto step = [&](auto stage_now) {
     constexpr int now = decltype(stage_now)::value;
-    loads_done();
     put_rows(now);
-    __syncthreads();
+    tile_ready<(NW > 1)>();
     r0 += BQ;
     if (r0 >= rows) r0 = 0, h0 += 1 << p.log2_fold;
     if (h0 < (hk + 1) * p.group) stage(h0, r0, now ^ 1);
@@ -402,6 +400,8 @@ struct BackwardShape {
 BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
   BackwardShape b;
   b.q = forward_shape(device, d, a);
+  b.q.splits = std::min(b.q.splits * b.q.key_waves, kMostSplits);        // this kernel's waves take parts of the keys as workgroups of their own
+  if (b.q.key_waves > 1) b.q.splits = int(std::max<int64_t>(1, std::min<int64_t>(b.q.splits, d->k_rows / std::max<int64_t>(d->n_docs, 1) / 256)));
   if (single_queries(d, a)) b.q.splits = 1;
   b.key_waves = d->k_rows <= 32 * std::max<int64_t>(d->n_docs, 1) ? 1 : 4;
   b.key_tiles = tiles_of(d->k_rows, 1, d->n_docs, 32 * b.key_waves);

@@ -15,14 +15,19 @@ namespace {
 // when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.  The
 // two places of a tile are two copies of the loop's body, so that no address is computed in it.
 // Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
+// Where a document has no more rows than a wave (NW 1), KW waves have the same rows and every KW-th tile of the keys each, in tiles of their own,
+// and their results are joined in LDS.
 constexpr float kSlack = 8.f;
-template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const AttendParams p) {
-  constexpr int kThreads = 64 * NW, kRows = 32 * NW;
-  __shared__ __align__(16) T lds_k[2][BN * D];
-  __shared__ __align__(16) T lds_v[2][BN * D];
-  __shared__ __align__(16) float lds_pos[2][BIAS ? BN : 4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
+template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
+__global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(const AttendParams p) {
+  constexpr int kThreads = 64 * NW, kRows = 32 * NW;          // threads that share tiles; rows of a workgroup
+  __shared__ __align__(16) T lds_tiles[KW][2][2][BN * D];     // of keys and values, two places each
+  __shared__ __align__(16) float lds_at[KW][2][BIAS ? BN : 4];
+  const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, tid = threadIdx.x % kThreads, wave = NW > 1 ? threadIdx.x >> 6 : 0;
+  const int part = KW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  auto& lds_k = lds_tiles[part][0];
+  auto& lds_v = lds_tiles[part][1];
+  auto& lds_pos = lds_at[part];
 
   uint32_t piece = piece_of(blockIdx.x, gridDim.x);
   int32_t split = 0, hk, tile;
@@ -43,7 +48,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
   int32_t k_begin, k_end;
-  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
+  part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split * KW + part, p.splits * KW, k_begin, k_end);
   const Rows<T> k_rows = {static_cast<const T*>(p.k) + int64_t(kd.begin) * p.k_row + int64_t(hk) * p.k_head, p.k_row, 0, 0};
   const Rows<T> v_rows = {static_cast<const T*>(p.v) + int64_t(kd.begin) * p.v_row + int64_t(hk) * p.v_head, p.v_row, 0, 0};
   int32_t next_pos = 0;        // as it comes, so that nothing waits for it yet
@@ -53,9 +58,8 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
     copy_tile<T, D, BN, kThreads>(lds_v[to], v_rows, k0, p.dim, k_end - k0, tid);
   };
   if (p.dim < D) {
-    clear_tile<T, 2 * BN * D, kThreads>(lds_k[0], tid);
-    clear_tile<T, 2 * BN * D, kThreads>(lds_v[0], tid);
-    __syncthreads();
+    clear_tile<T, 4 * BN * D, kThreads>(lds_k[0], tid);
+    tile_ready<(NW > 1)>();
   }
   if (k_begin < k_end) stage(k_begin, 0);
 
@@ -83,11 +87,10 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, auto stage_now) {
     constexpr int now = decltype(stage_now)::value;
-    loads_done();
     if constexpr (BIAS) {
       if (tid < BN) lds_pos[now][tid] = float(next_pos);
     }
-    __syncthreads();
+    tile_ready<(NW > 1)>();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     if (idle) return;
     if constexpr (D == 128) at_tile.again();
@@ -180,49 +183,69 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_kernel(const 
   }
 
   sum += other_half(sum);
-  if (row >= qd.owned * p.group) return;
-  const int64_t at_out = int64_t(token) * p.heads + head;
-  if (p.splits > 1) {
-    float* po = p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim;
+  // Results of the waves that share the rows: of every four elements one wave adds up all.
+  float* joined = reinterpret_cast<float*>(lds_tiles);        // [KW][D / 8][64][4]
+  __shared__ float lds_stats[KW > 1 ? KW : 1][2][32];
+  float weight[KW];
+  if constexpr (KW > 1) {
+    if (half == 0) {
+      lds_stats[part][0][col] = sum == 0.f ? -INFINITY : base;
+      lds_stats[part][1][col] = sum;
+    }
+    __syncthreads();                                          // and all are done with their tiles
 #pragma unroll
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        const int d = 32 * db + 8 * r4 + 4 * half;
-        if (d < p.dim) {
-          floatx4 x = {};
-          if (live) x = floatx4{o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]};
-          *reinterpret_cast<floatx4*>(po + d) = x;
-        }
-      }
-    if (half == 0) {
-      float* ml = p.part_ml + (int64_t(split) * p.qs.rows * p.heads + at_out) * 2;
-      ml[0] = live ? base : -INFINITY;
-      ml[1] = live ? sum : 0.f;
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<floatx4*>(joined + ((part * (D / 8) + 4 * db + r4) * 64 + lane) * 4) = floatx4{o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]};
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) top = fmaxf(top, lds_stats[k][0][col]);
+    base = top == -INFINITY ? 0.f : top;
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < KW; ++k) {
+      weight[k] = exp2_fast(lds_stats[k][0][col] - base);
+      sum += weight[k] * lds_stats[k][1][col];
     }
-    return;
+    __syncthreads();
   }
+  if (row >= qd.owned * p.group) return;
+  const int64_t at_out = int64_t(token) * p.heads + head, at_part = int64_t(split) * p.qs.rows * p.heads + at_out;
   const float inv = sum > 0.f ? 1.f / sum : sum;        // zero keys: zeros; NaN stays
-  T* out = static_cast<T*>(p.out) + at_out * p.dim;
-  T* rest = p.rest ? static_cast<T*>(p.rest) + at_out * p.dim : nullptr;
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) {
       const int d = 32 * db + 8 * r4 + 4 * half;
-      if (d < p.dim) {
-        vec4<T> x, y;
+      if ((KW > 1 && (4 * db + r4) % KW != part) || d >= p.dim) continue;
+      floatx4 f = {o[db][4 * r4], o[db][4 * r4 + 1], o[db][4 * r4 + 2], o[db][4 * r4 + 3]};
+      if constexpr (KW > 1) {
+        f = floatx4{};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float f = live ? o[db][4 * r4 + i] * inv : 0.f;
-          x[i] = T(f);
-          y[i] = T(f - float(x[i]));
-        }
-        *reinterpret_cast<vec4<T>*>(out + d) = x;
-        if (rest) *reinterpret_cast<vec4<T>*>(rest + d) = y;
+        for (int k = 0; k < KW; ++k) f += weight[k] * *reinterpret_cast<const floatx4*>(joined + ((k * (D / 8) + 4 * db + r4) * 64 + lane) * 4);
       }
+      if (!live) f = floatx4{};
+      if (p.splits > 1) {
+        *reinterpret_cast<floatx4*>(p.part_o + at_part * p.dim + d) = f;
+        continue;
+      }
+      vec4<T> x, y;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = T(live ? f[i] * inv : 0.f);
+        y[i] = T(live ? f[i] * inv - float(x[i]) : 0.f);
+      }
+      *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.out) + at_out * p.dim + d) = x;
+      if (p.rest) *reinterpret_cast<vec4<T>*>(static_cast<T*>(p.rest) + at_out * p.dim + d) = y;
     }
-  if (half == 0) p.lse[at_out] = live && sum != 0.f ? (base + log2_fast(sum)) * kLn2 : -INFINITY;
+  if (half || part) return;
+  if (p.splits > 1) {
+    p.part_ml[at_part * 2] = live && sum != 0.f ? base : -INFINITY;
+    p.part_ml[at_part * 2 + 1] = live ? sum : 0.f;
+  } else {
+    p.lse[at_out] = live && sum != 0.f ? (base + log2_fast(sum)) * kLn2 : -INFINITY;
+  }
 }
 
 // Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A workgroup has a row, eight groups of 32 lanes a
@@ -270,19 +293,20 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
   if (lane == 0) p.lse[row] = sum != 0.f ? (most + log2_fast(sum)) * kLn2 : -INFINITY;
 }
 
-template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, int waves, hipStream_t s) {
+template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const ForwardShape& f, hipStream_t s) {
   const uint32_t blocks = uint32_t(p.tiles) * p.kv_heads * p.splits;
-  if (waves == 1) attend_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(p);
-  else attend_kernel<T, D, CAP, BIAS, 4, 64><<<blocks, 256, 0, s>>>(p);
+  if (f.waves > 1) attend_kernel<T, D, CAP, BIAS, 4, 1, 64><<<blocks, 256, 0, s>>>(p);
+  else if (f.key_waves > 1) attend_kernel<T, D, CAP, BIAS, 1, 4, 32><<<blocks, 256, 0, s>>>(p);
+  else attend_kernel<T, D, CAP, BIAS, 1, 1, 32><<<blocks, 64, 0, s>>>(p);
 }
-template <typename T, int D> void launch(const AttendParams& p, int waves, bool cap, hipStream_t s) {
-  if (cap) p.slopes ? launch<T, D, true, true>(p, waves, s) : launch<T, D, true, false>(p, waves, s);
-  else p.slopes ? launch<T, D, false, true>(p, waves, s) : launch<T, D, false, false>(p, waves, s);
+template <typename T, int D> void launch(const AttendParams& p, const ForwardShape& f, bool cap, hipStream_t s) {
+  if (cap) p.slopes ? launch<T, D, true, true>(p, f, s) : launch<T, D, true, false>(p, f, s);
+  else p.slopes ? launch<T, D, false, true>(p, f, s) : launch<T, D, false, false>(p, f, s);
 }
-template <typename T> void launch(const AttendParams& p, int waves, bool cap, hipStream_t s) {
-  if (p.dim <= 32) launch<T, 32>(p, waves, cap, s);
-  else if (p.dim <= 64) launch<T, 64>(p, waves, cap, s);
-  else launch<T, 128>(p, waves, cap, s);
+template <typename T> void launch(const AttendParams& p, const ForwardShape& f, bool cap, hipStream_t s) {
+  if (p.dim <= 32) launch<T, 32>(p, f, cap, s);
+  else if (p.dim <= 64) launch<T, 64>(p, f, cap, s);
+  else launch<T, 128>(p, f, cap, s);
   if (p.splits > 1) {
     join_kernel<T><<<uint32_t(p.qs.rows * p.heads), 256, 0, s>>>(p);
   }
@@ -331,15 +355,17 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   return p;
 }
 
-// One wave with 32 keys at a time where documents are short, four with 64 where they are long.  Few tiles over long documents are split over
-// the keys until every CU has a few waves, at no less than 256 keys a part.
+// Where documents have up to 32 folded rows, a wave has them, or four share them where the keys are 64 and more; where they have more, four waves
+// of 32 rows each share the keys.  Few tiles over long documents are split over the keys until every CU has a few waves, at no less than 256
+// keys a part.
 ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
-  const int64_t group = a->heads / a->kv_heads, n = std::max<int64_t>(d->n_docs, 1);
+  const int64_t group = a->heads / a->kv_heads, n = std::max<int64_t>(d->n_docs, 1), keys = d->k_rows / n;
   ForwardShape f;
   f.waves = d->q_rows * group <= 32 * n ? 1 : 4;
+  f.key_waves = f.waves == 1 && keys >= 64 ? 4 : 1;
   f.tiles = tiles_of(d->q_rows, group, d->n_docs, kForwardRows * f.waves);
-  const int64_t waves = f.tiles * a->kv_heads * f.waves, room = int64_t(compute_units(device)) * 8, keys = d->k_rows / n;
-  f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256, int64_t(kMostSplits)})));
+  const int64_t waves = f.tiles * a->kv_heads * f.waves * f.key_waves, room = int64_t(compute_units(device)) * 8;
+  f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256 / f.key_waves, int64_t(kMostSplits)})));
   return f;
 }
 
@@ -381,8 +407,8 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
     p.part_o = static_cast<float*>(workspace);
     p.part_ml = p.part_o + rows * att->dim;
   }
-  if (att->dtype == LGP_F16) launch<f16>(p, f.waves, att->cap > 0.f, s);
-  else launch<bf16>(p, f.waves, att->cap > 0.f, s);
+  if (att->dtype == LGP_F16) launch<f16>(p, f, att->cap > 0.f, s);
+  else launch<bf16>(p, f, att->cap > 0.f, s);
   return launched();
 }
 

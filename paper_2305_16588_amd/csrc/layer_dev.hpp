@@ -115,6 +115,17 @@ template <typename T, int ELEMS, int THREADS> __device__ __forceinline__ void cl
 }
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }       // vmcnt(0), the other counters as they are
 
+// A tile may be read: the copies of all waves that share it are done, and so are everyone's reads of the tile that is overwritten next.
+template <bool SHARED> __device__ __forceinline__ void tile_ready() {
+  if constexpr (SHARED) {
+    loads_done();
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");
+  }
+}
+
 // Division of numbers below 2^31 by a fixed one.
 struct Divisor { uint32_t by, mul, shift; };
 inline Divisor divisor(uint32_t by) {
