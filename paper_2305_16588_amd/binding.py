@@ -53,6 +53,7 @@ class _BlocksOut(C.Structure):
                 ("feat_row", C.c_void_p * (MAX_HOPS + 1))]
 
 
+# Arguments of the layer operators (layer.py packs them itself: a Structure takes microseconds to fill).
 class _Documents(C.Structure):
     _fields_ = [("n_docs", C.c_int64), ("q_rows", C.c_int64), ("k_rows", C.c_int64), ("q_offsets", C.c_void_p), ("k_offsets", C.c_void_p),
                 ("q_lens", C.c_void_p), ("k_lens", C.c_void_p), ("q_pos", C.c_void_p), ("k_pos", C.c_void_p)]
@@ -137,16 +138,16 @@ def load_library():
     L.lgp_get_sample_marks.argtypes = [vp, vp]
     L.lgp_set_profiling.argtypes = [vp, C.c_int]
     L.lgp_get_profile.argtypes = [vp, C.POINTER(Profile)]
-    L.lgp_attend.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), vp, vp, vp, vp, C.c_size_t, vp]
-    L.lgp_attend_workspace.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), C.c_int, vp]
-    L.lgp_attend_backward.argtypes = [C.c_int, C.POINTER(_Documents), C.POINTER(_Attention), vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
-    L.lgp_norm_rotate.argtypes = [C.c_int, C.POINTER(_Heads), vp, vp, vp]
-    L.lgp_norm_rotate_workspace.argtypes = [C.c_int, C.POINTER(_Heads), vp]
-    L.lgp_norm_rotate_backward.argtypes = [C.c_int, C.POINTER(_Heads), vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
-    L.lgp_pack_activations.argtypes = [C.c_int, vp, i64, C.POINTER(_Packed), vp]
-    L.lgp_unpack_activations.argtypes = [C.c_int, C.POINTER(_Packed), vp, vp]
-    L.lgp_packed_weight_grad_workspace.argtypes = [C.c_int, C.POINTER(_Packed), i32, vp]
-    L.lgp_packed_weight_grad.argtypes = [C.c_int, C.POINTER(_Packed), vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_attend.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_attend_workspace.argtypes = [C.c_int, vp, vp, C.c_int, vp]
+    L.lgp_attend_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_norm_rotate.argtypes = [C.c_int, vp, vp, vp, vp]
+    L.lgp_norm_rotate_workspace.argtypes = [C.c_int, vp, vp]
+    L.lgp_norm_rotate_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_pack_activations.argtypes = [C.c_int, vp, i64, vp, vp]
+    L.lgp_unpack_activations.argtypes = [C.c_int, vp, vp, vp]
+    L.lgp_packed_weight_grad_workspace.argtypes = [C.c_int, vp, i32, vp]
+    L.lgp_packed_weight_grad.argtypes = [C.c_int, vp, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
     L.lgp_strerror.argtypes = [C.c_int]
     L.lgp_strerror.restype = C.c_char_p
     L.lgp_last_error.argtypes = [vp]

@@ -234,8 +234,11 @@ __device__ __forceinline__ uint32_t piece_of(uint32_t block, uint32_t blocks) {
 }
 
 inline int use_device(int device) {
-  int n = 0;
-  if (hipGetDeviceCount(&n) != hipSuccess || device < 0 || device >= n || hipSetDevice(device) != hipSuccess) {
+  static const int devices = [] {
+    int n = 0;
+    return hipGetDeviceCount(&n) == hipSuccess ? n : 0;
+  }();
+  if (device < 0 || device >= devices || hipSetDevice(device) != hipSuccess) {
     (void)hipGetLastError();
     return LGP_EINVAL;
   }

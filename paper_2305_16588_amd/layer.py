@@ -7,18 +7,29 @@ that the kernels run on.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
 from .binding import LegionPrepError, _Attention, _Documents, _Heads, _Packed, _raw_stream, load_library
 
 _DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-_EINVAL = -1
+_EINVAL, _ECAPACITY = -1, -3
 
 
-def _want(ok, text: str):
-    if not ok:
-        raise LegionPrepError(_EINVAL, text)
+def _packer(structure):
+    """struct.pack for a ctypes structure."""
+    code = {C.c_void_p: "P", C.c_int64: "q", C.c_int32: "i", C.c_float: "f"}
+    form = struct.Struct("@" + "".join(code[kind] for _, kind in structure._fields_) + "0P")
+    assert form.size == C.sizeof(structure)
+    return form.pack
+
+
+_documents, _attention_of, _heads, _packed = (_packer(x) for x in (_Documents, _Attention, _Heads, _Packed))
+
+
+def _bad(text: str) -> LegionPrepError:
+    return LegionPrepError(_EINVAL, text)
 
 
 def _ok(st: int):
@@ -26,53 +37,68 @@ def _ok(st: int):
         raise LegionPrepError(st, load_library().lgp_strerror(st).decode())
 
 
-class _On:
-    """The stream a call runs on, which is also the one that its results are allocated for."""
+class _Here:
+    """The current stream, where results are allocated as they are."""
+    __slots__ = ("ptr",)
 
-    def __init__(self, device: torch.device, stream):
-        self.index = device.index
-        self.other = None
-        if stream is not None:
-            self.ptr = stream.cuda_stream
-            self.other = torch.cuda.stream(stream)
-        elif _raw_stream is not None:
-            self.ptr = _raw_stream(self.index)
-        else:
-            self.ptr = torch.cuda.current_stream(device).cuda_stream
+    def __init__(self, index: int):
+        self.ptr = torch.cuda.current_stream(index).cuda_stream if _raw_stream is None else _raw_stream(index)
 
     def __enter__(self):
-        if self.other is not None:
-            self.other.__enter__()
-        return self
+        return self.ptr
 
     def __exit__(self, *exc):
-        if self.other is not None:
-            self.other.__exit__(*exc)
+        pass
+
+
+class _There:
+    """Another stream, which results are allocated for."""
+    __slots__ = ("stream", "context")
+
+    def __init__(self, stream):
+        self.stream, self.context = stream, torch.cuda.stream(stream)
+
+    def __enter__(self):
+        self.context.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        self.context.__exit__(*exc)
+
+
+def _on(index: int, stream):
+    return _Here(index) if stream is None else _There(stream)
 
 
 def _ptr(t):
-    return None if t is None else t.data_ptr()
+    return 0 if t is None else t.data_ptr()
 
 
-def _ints(t, n: int, device, name: str):
-    """An optional int32 vector of n entries."""
-    if t is not None:
-        _want(t.dtype == torch.int32 and t.is_cuda and t.device == device and t.is_contiguous() and t.numel() == n,
-              f"{name}: {n} contiguous int32 entries on {device}")
+def _ints(t, n: int, index: int, name: str):
+    """The address of an optional int32 vector of n entries."""
+    if t is None:
+        return 0
+    if t.dtype is not torch.int32 or t.get_device() != index or t.numel() != n or not t.is_contiguous():
+        raise _bad(f"{name}: {n} contiguous int32 entries on cuda:{index}")
+    return t.data_ptr()
 
 
-def _heads_of(t, name: str, dtype, device):
-    """A [rows, heads, dim] tensor whose heads can be read 16 bytes at a time; its strides."""
-    _want(t.dim() == 3 and t.dtype == dtype and t.device == device, f"{name}: [rows, heads, dim], {dtype}, on {device}")
+def _heads_of(t, name: str, dtype, index: int):
+    """The address and the strides of a [rows, heads, dim] tensor whose heads can be read 16 bytes at a time."""
+    if t.dim() != 3 or t.dtype is not dtype or t.get_device() != index:
+        raise _bad(f"{name}: [rows, heads, dim], {dtype}, on cuda:{index}")
     row, head, one = t.stride()
-    if t.numel():
-        _want(one == 1 and row % 8 == 0 and head % 8 == 0 and t.data_ptr() % 16 == 0,
-              f"{name}: elements of a head side by side, strides in multiples of 8, aligned to 16 bytes")
-    return row, head
+    at = t.data_ptr()
+    if one != 1 or row % 8 or head % 8 or at % 16:
+        if t.numel():
+            raise _bad(f"{name}: elements of a head side by side, strides in multiples of 8, aligned to 16 bytes")
+        row = head = 0
+    return at, row, head
 
 
-def _like(t, shape, name: str, dtype, device):
-    _want(tuple(t.shape) == tuple(shape) and t.dtype == dtype and t.device == device, f"{name}: {list(shape)}, {dtype}, on {device}")
+def _like(t, shape, name: str, dtype, index: int):
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise _bad(f"{name}: {list(shape)}, {dtype}, on cuda:{index}")
     t = t.contiguous()
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
@@ -84,40 +110,39 @@ class Documents:
 
     def __init__(self, q_offsets, k_offsets, q_lens=None, k_lens=None, q_pos=None, k_pos=None):
         n = q_offsets.numel() - 1
-        dev = q_offsets.device
-        _want(n >= 0 and dev.type == "cuda", "q_offsets: one entry at least, on a GPU")
-        _ints(q_offsets, n + 1, dev, "q_offsets")
-        _ints(k_offsets, n + 1, dev, "k_offsets")
-        _ints(q_lens, n, dev, "q_lens")
-        _ints(k_lens, n, dev, "k_lens")
-        self.device, self.q_pos, self.k_pos = dev, q_pos, k_pos
+        index = q_offsets.get_device()
+        if n < 0 or index < 0:
+            raise _bad("q_offsets: one entry at least, on a GPU")
+        self.index, self.q_pos, self.k_pos = index, q_pos, k_pos
         self._keep = (q_offsets, k_offsets, q_lens, k_lens)
-        self.c = _Documents(n, 0, 0, q_offsets.data_ptr(), k_offsets.data_ptr(), _ptr(q_lens), _ptr(k_lens), _ptr(q_pos), _ptr(k_pos))
+        self._n = n
+        self._at = (_ints(q_offsets, n + 1, index, "q_offsets"), _ints(k_offsets, n + 1, index, "k_offsets"), _ints(q_lens, n, index, "q_lens"),
+                    _ints(k_lens, n, index, "k_lens"))
 
-    def _rows(self, q_rows: int, k_rows: int):
-        _ints(self.q_pos, q_rows, self.device, "q_pos")
-        _ints(self.k_pos, k_rows, self.device, "k_pos")
-        self.c.q_rows, self.c.k_rows = q_rows, k_rows
-        return self.c
+    def _rows(self, q_rows: int, k_rows: int) -> bytes:
+        return _documents(self._n, q_rows, k_rows, *self._at, _ints(self.q_pos, q_rows, self.index, "q_pos"), _ints(self.k_pos, k_rows, self.index, "k_pos"))
 
 
 def _attention(q, k, v, docs: Documents, slopes, cap: float, scale):
-    dev = docs.device
-    strides = _heads_of(q, "q", q.dtype, dev) + _heads_of(k, "k", q.dtype, dev) + _heads_of(v, "v", q.dtype, dev)
-    heads, dim = q.shape[1:]
-    _want(k.shape == v.shape and k.shape[2] == dim and k.shape[1] > 0 and heads > 0 and heads % k.shape[1] == 0,
-          "k and v: [rows, kv_heads, dim] with a kv_heads that divides the heads of q")
-    _want(q.dtype in (torch.float16, torch.bfloat16), "q, k and v: float16 or bfloat16")
+    index, dtype = docs.index, q.dtype
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise _bad("q, k and v: float16 or bfloat16")
+    (qp, q_row, q_head), (kp, k_row, k_head), (vp, v_row, v_head) = _heads_of(q, "q", dtype, index), _heads_of(k, "k", dtype, index), _heads_of(v, "v", dtype, index)
+    (q_rows, heads, dim), (k_rows, kv_heads, k_dim) = q.shape, k.shape
+    if k.shape != v.shape or k_dim != dim or not kv_heads or not heads or heads % kv_heads:
+        raise _bad("k and v: [rows, kv_heads, dim] with a kv_heads that divides the heads of q")
     if slopes is not None:
-        _want(slopes.dtype == torch.float32 and slopes.device == dev and slopes.is_contiguous() and slopes.numel() == heads, "slopes: float32[heads]")
-        _want((docs.q_pos is not None or not q.shape[0]) and (docs.k_pos is not None or not k.shape[0]), "slopes need positions of queries and keys")
-    return docs._rows(q.shape[0], k.shape[0]), _Attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), *strides, heads, k.shape[1], dim, _DTYPE[q.dtype],
-                                                          dim ** -0.5 if scale is None else scale, cap, _ptr(slopes))
+        if slopes.dtype is not torch.float32 or slopes.get_device() != index or slopes.numel() != heads or not slopes.is_contiguous():
+            raise _bad("slopes: float32[heads]")
+        if (docs.q_pos is None and q_rows) or (docs.k_pos is None and k_rows):
+            raise _bad("slopes need positions of queries and keys")
+    return docs._rows(q_rows, k_rows), _attention_of(qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, heads, kv_heads, dim, _DTYPE[dtype],
+                                                      dim ** -0.5 if scale is None else scale, cap, _ptr(slopes))
 
 
-def _workspace(on: _On, device, query, *args):
+def _workspace(index: int, device, query, *args):
     size = C.c_size_t()
-    _ok(query(on.index, *args, C.byref(size)))
+    _ok(query(index, *args, C.byref(size)))
     return (torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None), size.value
 
 
@@ -130,12 +155,16 @@ def attend(q, k, v, docs: Documents, slopes=None, cap: float = 0.0, scale: float
     without tokens get zeros and -inf.  rest: also return what the rounding of out took off, for attend_backward."""
     L = load_library()
     d, a = _attention(q, k, v, docs, slopes, cap, scale)
-    with _On(docs.device, stream) as on:
-        out = torch.empty(q.shape, dtype=q.dtype, device=docs.device)
+    device = q.device
+    with _on(docs.index, stream) as on:
+        out = torch.empty(q.shape, dtype=q.dtype, device=device)
         left = torch.empty_like(out) if rest else None
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=docs.device)
-        w, size = _workspace(on, docs.device, L.lgp_attend_workspace, C.byref(d), C.byref(a), 0)
-        _ok(L.lgp_attend(on.index, C.byref(d), C.byref(a), out.data_ptr(), _ptr(left), lse.data_ptr(), _ptr(w), size, on.ptr))
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=device)
+        st = L.lgp_attend(docs.index, d, a, out.data_ptr(), _ptr(left), lse.data_ptr(), 0, 0, on)
+        if st == _ECAPACITY:                    # nothing was launched: few calls want a workspace
+            w, size = _workspace(docs.index, device, L.lgp_attend_workspace, d, a, 0)
+            st = L.lgp_attend(docs.index, d, a, out.data_ptr(), _ptr(left), lse.data_ptr(), _ptr(w), size, on)
+        _ok(st)
     return out, lse, left
 
 
@@ -143,43 +172,51 @@ def attend_backward(d_out, q, k, v, out, lse, docs: Documents, rest=None, slopes
     """Gradients (dq, dk, dv, d_slopes) of attend by its inputs, from that of out and from what attend returned; d_slopes is None without slopes."""
     L = load_library()
     d, a = _attention(q, k, v, docs, slopes, cap, scale)
-    dev = docs.device
-    with _On(dev, stream) as on:
-        d_out, out = _like(d_out, q.shape, "d_out", q.dtype, dev), _like(out, q.shape, "out", q.dtype, dev)
-        rest = None if rest is None else _like(rest, q.shape, "rest", q.dtype, dev)
-        lse = _like(lse, q.shape[:2], "lse", torch.float32, dev)
+    index, dev = docs.index, q.device
+    with _on(index, stream) as on:
+        d_out, out = _like(d_out, q.shape, "d_out", q.dtype, index), _like(out, q.shape, "out", q.dtype, index)
+        rest = None if rest is None else _like(rest, q.shape, "rest", q.dtype, index)
+        lse = _like(lse, q.shape[:2], "lse", torch.float32, index)
         dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
         d_slopes = None if slopes is None else torch.empty_like(slopes)
-        w, size = _workspace(on, dev, L.lgp_attend_workspace, C.byref(d), C.byref(a), 1)
-        _ok(L.lgp_attend_backward(on.index, C.byref(d), C.byref(a), d_out.data_ptr(), out.data_ptr(), _ptr(rest), lse.data_ptr(), dq.data_ptr(),
-                                  dk.data_ptr(), dv.data_ptr(), _ptr(d_slopes), _ptr(w), size, on.ptr))
+        w, size = _workspace(index, dev, L.lgp_attend_workspace, d, a, 1)
+        _ok(L.lgp_attend_backward(index, d, a, d_out.data_ptr(), out.data_ptr(), _ptr(rest), lse.data_ptr(), dq.data_ptr(),
+                                  dk.data_ptr(), dv.data_ptr(), _ptr(d_slopes), _ptr(w), size, on))
     return dq, dk, dv, d_slopes
 
 
 def rotation_table(positions: int, rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """float32[positions, rot]: cosines, then sines, of position * base^(-2 i / rot), computed in 64 bits."""
-    _want(positions > 0 and rot > 0 and rot % 16 == 0, "rot: a multiple of 16")
+    if positions < 1 or rot < 1 or rot % 16:
+        raise _bad("positions: one at least; rot: a multiple of 16")
     angle = torch.arange(positions, dtype=torch.float64)[:, None] * float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
     return torch.cat([angle.cos(), angle.sin()], 1).float().to(device)
 
 
+def _weight(w, name: str, dim: int, index: int):
+    at = w.data_ptr()
+    if w.dtype is not torch.float32 or w.get_device() != index or w.numel() != dim or not w.is_contiguous() or at % 16:
+        raise _bad(f"{name}: float32[dim], aligned to 16 bytes")
+    return at
+
+
 def _norm(q, k, q_weight, k_weight, pos, table, eps: float):
-    dev, dtype = q.device, q.dtype
-    _want(dtype in _DTYPE, "q and k: float32, float16 or bfloat16")
-    strides = _heads_of(q, "q", dtype, dev) + _heads_of(k, "k", dtype, dev)
-    tokens, heads, dim = q.shape
-    _want(k.shape[0] == tokens and k.shape[2] == dim, "k: [tokens, kv_heads, dim], as many tokens and elements as q")
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        _want(w.dtype == torch.float32 and w.device == dev and w.is_contiguous() and w.numel() == dim and w.data_ptr() % 16 == 0,
-              f"{name}: float32[dim], aligned to 16 bytes")
-    _ints(pos, tokens, dev, "pos")
+    index, dtype = q.get_device(), q.dtype
+    if dtype not in _DTYPE or index < 0:
+        raise _bad("q and k: float32, float16 or bfloat16, on a GPU")
+    (qp, q_row, q_head), (kp, k_row, k_head) = _heads_of(q, "q", dtype, index), _heads_of(k, "k", dtype, index)
+    (tokens, heads, dim), (k_tokens, kv_heads, k_dim) = q.shape, k.shape
+    if k_tokens != tokens or k_dim != dim:
+        raise _bad("k: [tokens, kv_heads, dim], as many tokens and elements as q")
     rot = n_pos = 0
+    at = 0
     if table is not None:
-        _want(table.dtype == torch.float32 and table.device == dev and table.is_contiguous() and table.dim() == 2 and table.data_ptr() % 16 == 0 and
-              pos is not None, "table: float32[positions, rot], aligned to 16 bytes, and pos with it")
+        at = table.data_ptr()
+        if table.dim() != 2 or table.dtype is not torch.float32 or table.get_device() != index or not table.is_contiguous() or at % 16 or pos is None:
+            raise _bad("table: float32[positions, rot], aligned to 16 bytes, and pos with it")
         n_pos, rot = table.shape
-    return dev, _Heads(q.data_ptr(), k.data_ptr(), *strides, tokens, heads, k.shape[1], dim, _DTYPE[dtype], q_weight.data_ptr(),
-                       k_weight.data_ptr(), _ptr(pos), rot, n_pos, _ptr(table), eps)
+    return index, _heads(qp, kp, q_row, q_head, k_row, k_head, tokens, heads, kv_heads, dim, _DTYPE[dtype], _weight(q_weight, "q_weight", dim, index),
+                         _weight(k_weight, "k_weight", dim, index), _ints(pos, tokens, index, "pos"), rot, n_pos, at, eps)
 
 
 def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-6, stream=None):
@@ -187,24 +224,26 @@ def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-
     table.shape[1] elements by the token's position (rotation_table); new tensors (q, k), rows end to end.  dim: a multiple of 8 up to 256.
     Rows of a negative pos have no token and become zeros; those of a position beyond the table become NaN."""
     L = load_library()
-    dev, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
-    with _On(dev, stream) as on:
+    index, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
+    dev = q.device
+    with _on(index, stream) as on:
         q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
-        _ok(L.lgp_norm_rotate(on.index, C.byref(h), q_out.data_ptr(), k_out.data_ptr(), on.ptr))
+        _ok(L.lgp_norm_rotate(index, h, q_out.data_ptr(), k_out.data_ptr(), on))
     return q_out, k_out
 
 
 def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-6, stream=None):
     """Gradients (dq, dk, dq_weight, dk_weight) of norm_rotate, from those of its results; the other arguments are what it was given."""
     L = load_library()
-    dev, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
-    with _On(dev, stream) as on:
-        dq_out, dk_out = _like(dq_out, q.shape, "dq_out", q.dtype, dev), _like(dk_out, k.shape, "dk_out", k.dtype, dev)
+    index, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
+    dev = q.device
+    with _on(index, stream) as on:
+        dq_out, dk_out = _like(dq_out, q.shape, "dq_out", q.dtype, index), _like(dk_out, k.shape, "dk_out", k.dtype, index)
         dq, dk = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
         dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
-        w, size = _workspace(on, dev, L.lgp_norm_rotate_workspace, C.byref(h))
-        _ok(L.lgp_norm_rotate_backward(on.index, C.byref(h), dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqw.data_ptr(),
-                                       dkw.data_ptr(), _ptr(w), size, on.ptr))
+        w, size = _workspace(index, dev, L.lgp_norm_rotate_workspace, h)
+        _ok(L.lgp_norm_rotate_backward(index, h, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqw.data_ptr(),
+                                       dkw.data_ptr(), _ptr(w), size, on))
     return dq, dk, dqw, dkw
 
 
@@ -212,14 +251,20 @@ class PackedActivations:
     """Activations in 8 bits: values (int8[tokens, width rounded up to 16]) times 2^(exps - 127) (uint8[tokens, groups of 32])."""
 
     def __init__(self, values, exps, width: int, dtype, pos=None):
-        _want(values.dim() == 2 and values.dtype == torch.int8 and values.is_contiguous() and values.is_cuda and values.data_ptr() % 16 == 0 and width > 0 and
-              values.shape[1] == (width + 15) // 16 * 16, "values: contiguous int8[tokens, width rounded up to 16], on a GPU")
-        _want(exps.dtype == torch.uint8 and exps.is_contiguous() and exps.device == values.device and
-              tuple(exps.shape) == (values.shape[0], (width + 31) // 32), "exps: contiguous uint8[tokens, (width + 31) / 32]")
-        _want(dtype in _DTYPE, "dtype: float32, float16 or bfloat16")
-        _ints(pos, values.shape[0], values.device, "pos")
-        self.values, self.exps, self.width, self.dtype, self.pos = values, exps, int(width), dtype, pos
-        self.c = _Packed(values.shape[0], width, _DTYPE[dtype], values.data_ptr(), exps.data_ptr(), _ptr(pos))
+        index = values.get_device()
+        if (index < 0 or values.dim() != 2 or values.dtype is not torch.int8 or width < 1 or values.shape[1] != (width + 15) // 16 * 16 or
+                not values.is_contiguous() or values.data_ptr() % 16):
+            raise _bad("values: contiguous int8[tokens, width rounded up to 16], on a GPU, aligned to 16 bytes")
+        if exps.dtype is not torch.uint8 or exps.get_device() != index or exps.shape != (values.shape[0], (width + 31) // 32) or not exps.is_contiguous():
+            raise _bad("exps: contiguous uint8[tokens, (width + 31) / 32]")
+        if dtype not in _DTYPE:
+            raise _bad("dtype: float32, float16 or bfloat16")
+        self._set(values, exps, int(width), dtype, pos, index, _ints(pos, values.shape[0], index, "pos"))
+
+    def _set(self, values, exps, width, dtype, pos, index, pos_ptr):
+        self.values, self.exps, self.width, self.dtype, self.pos, self.index = values, exps, width, dtype, pos, index
+        self.c = _packed(values.shape[0], width, _DTYPE[dtype], values.data_ptr(), exps.data_ptr(), pos_ptr)
+        return self
 
     @property
     def shape(self):
@@ -227,32 +272,35 @@ class PackedActivations:
 
 
 def _rows2(t, name: str):
-    _want(t.dim() == 2 and t.is_cuda and (t.stride(1) == 1 or t.shape[1] == 1 or t.numel() == 0), f"{name}: [tokens, width] on a GPU, values of a row side by side")
-    return t.stride(0)
+    row, one = t.stride() if t.dim() == 2 else (0, 0)
+    if t.get_device() < 0 or t.dim() != 2 or (one != 1 and t.shape[1] != 1 and t.numel()):
+        raise _bad(f"{name}: [tokens, width] on a GPU, values of a row side by side")
+    return row
 
 
 def pack_activations(x, pos=None, stream=None) -> PackedActivations:
     """x [tokens, width] (float32, float16 or bfloat16, values of a row side by side) in 8 bits: 32 values of a row share a power of two.  Rows of a
     negative pos (int32[tokens]) hold no token: they are not read and packed as zeros."""
     L = load_library()
-    row = _rows2(x, "x")
-    _want(x.dtype in _DTYPE and x.shape[1] > 0, "x: float32, float16 or bfloat16, one value in a row at least")
+    row, index, dtype, device = _rows2(x, "x"), x.get_device(), x.dtype, x.device
     tokens, width = x.shape
-    _ints(pos, tokens, x.device, "pos")
-    with _On(x.device, stream) as on:
-        values = torch.empty((tokens, (width + 15) // 16 * 16), dtype=torch.int8, device=x.device)
-        exps = torch.empty((tokens, (width + 31) // 32), dtype=torch.uint8, device=x.device)
-        packed = PackedActivations(values, exps, width, x.dtype, pos)
-        _ok(L.lgp_pack_activations(on.index, x.data_ptr(), row, C.byref(packed.c), on.ptr))
+    if dtype not in _DTYPE or width < 1:
+        raise _bad("x: float32, float16 or bfloat16, one value in a row at least")
+    pos_ptr = _ints(pos, tokens, index, "pos")
+    with _on(index, stream) as on:
+        values = torch.empty((tokens, (width + 15) // 16 * 16), dtype=torch.int8, device=device)
+        exps = torch.empty((tokens, (width + 31) // 32), dtype=torch.uint8, device=device)
+        packed = PackedActivations.__new__(PackedActivations)._set(values, exps, width, dtype, pos, index, pos_ptr)
+        _ok(L.lgp_pack_activations(index, x.data_ptr(), row, packed.c, on))
     return packed
 
 
 def unpack_activations(packed: PackedActivations, stream=None) -> torch.Tensor:
     """The values that `packed` stands for, in the type that came."""
     L = load_library()
-    with _On(packed.values.device, stream) as on:
+    with _on(packed.index, stream) as on:
         x = torch.empty(packed.shape, dtype=packed.dtype, device=packed.values.device)
-        _ok(L.lgp_unpack_activations(on.index, C.byref(packed.c), x.data_ptr(), on.ptr))
+        _ok(L.lgp_unpack_activations(packed.index, packed.c, x.data_ptr(), on))
     return x
 
 
@@ -260,14 +308,15 @@ def packed_weight_grad(packed: PackedActivations, dy, bias: bool = True, stream=
     """(dw, db) of a linear layer y = x W^T + b whose input was packed: float32[out, width] and float32[out] (None if bias is False), from dy [tokens,
     out] in bfloat16, or in float16 if x was."""
     L = load_library()
-    row = _rows2(dy, "dy")
-    _want(dy.shape[0] == packed.shape[0] and dy.shape[1] > 0 and dy.device == packed.values.device, "dy: [tokens, out], where the packed rows are")
-    _want(dy.dtype == torch.bfloat16 or (dy.dtype == torch.float16 and packed.dtype == torch.float16),
-          "dy: bfloat16, or float16 with activations that came in float16")
-    out = dy.shape[1]
-    with _On(dy.device, stream) as on:
-        dw = torch.empty((out, packed.width), dtype=torch.float32, device=dy.device)
-        db = torch.empty(out, dtype=torch.float32, device=dy.device) if bias else None
-        w, size = _workspace(on, dy.device, L.lgp_packed_weight_grad_workspace, C.byref(packed.c), out)
-        _ok(L.lgp_packed_weight_grad(on.index, C.byref(packed.c), dy.data_ptr(), row, _DTYPE[dy.dtype], out, dw.data_ptr(), _ptr(db), _ptr(w), size, on.ptr))
+    row, index, device = _rows2(dy, "dy"), packed.index, dy.device
+    tokens, out = dy.shape
+    if tokens != packed.values.shape[0] or out < 1 or dy.get_device() != index:
+        raise _bad("dy: [tokens, out], where the packed rows are")
+    if dy.dtype is not torch.bfloat16 and (dy.dtype is not torch.float16 or packed.dtype is not torch.float16):
+        raise _bad("dy: bfloat16, or float16 with activations that came in float16")
+    with _on(index, stream) as on:
+        dw = torch.empty((out, packed.width), dtype=torch.float32, device=device)
+        db = torch.empty(out, dtype=torch.float32, device=device) if bias else None
+        w, size = _workspace(index, device, L.lgp_packed_weight_grad_workspace, packed.c, out)
+        _ok(L.lgp_packed_weight_grad(index, packed.c, dy.data_ptr(), row, _DTYPE[dy.dtype], out, dw.data_ptr(), _ptr(db), _ptr(w), size, on))
     return dw, db

@@ -77,7 +77,7 @@ def check(got, ref, what=""):
 
 def head_norm(x, w, pos, table, eps, d_out=None):
     """RMS norm, weights and rotation of x [tokens, heads, dim]; {name: (value, bound)}."""
-    u, tiny = UNIT[x.dtype], TINY[x.dtype]
+    u, tiny = UNIT[x.dtype], TINY.get(x.dtype, 0.0)
     D = x.shape[2]
     rot = 0 if table is None else table.shape[1]
     live = torch.ones(x.shape[0], dtype=torch.bool, device=x.device) if pos is None else pos >= 0
