@@ -17,10 +17,11 @@ struct NormParams {
   const int32_t* pos;
   const float* table;        // [n_pos][rot]: cosines, then sines
   float eps;
+  int32_t log2_side;         // 2^log2_side heads side by side
+  bool apart;                // forward: queries and keys in workgroups of their own, where there are few
   void *q_out, *k_out;       // [tokens][heads][dim] and [tokens][kv_heads][dim]; backward: the gradients of q and k
   const void *dq, *dk;       // backward: like q_out and k_out
-  float* partial;            // backward: [workgroup of q, then of k][dim]
-  int32_t q_groups;          // backward: workgroups of q
+  float* partial;            // backward: [workgroup][2][dim]
 };
 
 template <typename T> __device__ __forceinline__ void read8(const T* p, float* x) {
@@ -45,141 +46,174 @@ template <> __device__ __forceinline__ void write8<float>(float* p, const float*
 }
 
 // Pair (i, i + rot / 2) turns by the angle of the position (back: the other way).  Lane c of a row has elements 8 c .. 8 c + 7, so the other
-// half of its pairs are a lane's, rot / 16 lanes away.  Every lane of the wave takes part in the exchange.
-template <int L>
-__device__ __forceinline__ void rotate(const NormParams& p, float* y, int c, int lane, int32_t pos, bool live, bool back) {
-  if (p.rot == 0) return;
-  const int lanes = p.rot / 16;
-  const bool in = c < 2 * lanes, low = c < lanes;
-  const int from = in ? (low ? lane + lanes : lane - lanes) : lane;
-  float z[8];
+// half of its pairs are a lane's, rot / 16 lanes away.  A token's cosines and sines are read once for all its heads.  Every lane of the wave takes
+// part in the exchange.
+struct Turn {
+  float co[8], si[8];         // sines with the sign of the lane's half
+  int from;                   // the lane of the other half
+  bool in;
+  __device__ __forceinline__ Turn(const NormParams& p, int c, int lane, int32_t pos, bool known, bool back) {
+    const int lanes = p.rot / 16;
+    const bool low = c < lanes;
+    in = c < 2 * lanes && known;
+    from = c < 2 * lanes ? (low ? lane + lanes : lane - lanes) : lane;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) z[i] = __shfl(y[i], from, 64);
-  if (!in || !live) return;
-  const float* t = p.table + int64_t(pos) * p.rot + 8 * (low ? c : c - lanes);
-  float co[8], si[8];
-  read8(t, co);
-  read8(t + p.rot / 2, si);
+    for (int i = 0; i < 8; ++i) co[i] = 1.f, si[i] = 0.f;
+    if (in) {
+      const float* t = p.table + int64_t(pos) * p.rot + 8 * (low ? c : c - lanes);
+      read8(t, co);
+      read8(t + p.rot / 2, si);
+      if (low != back)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = y[i] * co[i] + (low == back ? si[i] : -si[i]) * z[i];
-}
+        for (int i = 0; i < 8; ++i) si[i] = -si[i];
+    }
+  }
+  __device__ __forceinline__ void operator()(float* y) const {
+    float z[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i] = __shfl(y[i], from, 64);
+    if (!in) return;          // not even times zero: what is not turned may be infinite
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = y[i] * co[i] + si[i] * z[i];
+  }
+};
 
-// L lanes of a row of up to 8 L elements; 64 / L rows of a wave.
+// L lanes of a head, 2^log2_side heads of a token side by side (heads_side), so that a wave's loads are whole lines; a lane has eight
+// elements of every so many heads, kAtOnce of them on their way at a time.
+constexpr int kAtOnce = 4;
 template <typename T, int L>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormParams p) {
-  const int lane = threadIdx.x & 63, c = lane % L;
-  const uint32_t per_token = p.heads + p.kv_heads;
-  const int64_t row = (int64_t(blockIdx.x) * 256 + threadIdx.x) / L, rows = p.tokens * per_token;
-  const bool in = row < rows;
-  const int64_t token = in ? row / per_token : 0;
-  const int32_t h = in ? int32_t(row - token * per_token) : 0;
-  const bool is_q = h < p.heads, mine = 8 * c < p.dim;
+  const int lane = threadIdx.x & 63, c = lane % L, side = 1 << p.log2_side, first = lane / L & (side - 1);
+  const int64_t at = (int64_t(blockIdx.x) * (256 / L) + threadIdx.x / L) >> p.log2_side, token = at < p.tokens ? at : p.tokens - 1;       // the last ones again
+  const bool mine = 8 * c < p.dim;
   const int32_t pos = p.pos ? p.pos[token] : 0;
-  const bool live = in && pos >= 0, known = p.rot == 0 || pos < p.n_pos;
-  float x[8] = {}, sum = 0.f;
-  if (live && mine) {
-    const T* src = is_q ? static_cast<const T*>(p.q) + token * p.q_row + h * p.q_head : static_cast<const T*>(p.k) + token * p.k_row + (h - p.heads) * p.k_head;
-    read8(src + 8 * c, x);
-  }
+  const bool live = pos >= 0, known = p.rot == 0 || pos < p.n_pos;
+  const Turn turn(p, c, lane, pos, live && known, false);
+  auto rows = [&](const T* src, int64_t stride, int32_t heads, const float* weights, T* dst) {
+    float w[8] = {};
+    if (mine && heads) read8(weights + 8 * c, w);
+    for (int32_t h0 = 0; h0 < heads; h0 += kAtOnce << p.log2_side) {
+      float x[kAtOnce][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-  sum = sum_of_lanes<L>(sum);
-  const float r = 1.f / sqrtf(sum / float(p.dim) + p.eps);
-  const float* w = is_q ? p.q_weight : p.k_weight;
-  if (mine) {
-    float wt[8];
-    read8(w + 8 * c, wt);
+      for (int j = 0; j < kAtOnce; ++j) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] *= r * wt[i];
-  }
-  rotate<L>(p, x, c, lane, pos, live && known, false);
-  if (!in || !mine) return;
-  if (!live || !known) {
+        for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+        const int32_t h = h0 + j * side + first;
+        if (live && mine && h < heads) read8(src + h * stride + 8 * c, x[j]);
+      }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = live ? NAN : 0.f;
-  }
-  T* dst = is_q ? static_cast<T*>(p.q_out) + (token * p.heads + h) * p.dim : static_cast<T*>(p.k_out) + (token * p.kv_heads + h - p.heads) * p.dim;
-  write8(dst + 8 * c, x);
+      for (int j = 0; j < kAtOnce; ++j) {
+        const int32_t h = h0 + j * side + first;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += x[j][i] * x[j][i];
+        const float r = known ? 1.f / sqrtf(sum_of_lanes<L>(sum) / float(p.dim) + p.eps) : NAN;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[j][i] *= r * w[i];
+        if (p.rot) turn(x[j]);
+        if (!mine || h >= heads || at >= p.tokens) continue;
+        if (!live)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[j][i] = 0.f;
+        write8(dst + int64_t(h) * p.dim + 8 * c, x[j]);
+      }
+    }
+  };
+  if (blockIdx.y == 0) rows(static_cast<const T*>(p.q) + token * p.q_row, p.q_head, p.heads, p.q_weight, static_cast<T*>(p.q_out) + token * p.heads * p.dim);
+  if (blockIdx.y == gridDim.y - 1)
+    rows(static_cast<const T*>(p.k) + token * p.k_row, p.k_head, p.kv_heads, p.k_weight, static_cast<T*>(p.k_out) + token * p.kv_heads * p.dim);
 }
 
 // Backward, with n = x r, r = 1 / sqrt(mean(x^2) + eps) and g = w * (dy turned back):  dx = r (g - n mean(g n)),  dw = sum over rows of n * (dy
-// turned back).  A workgroup takes rows of queries or of keys, so that a lane adds up the gradient of its own eight weights in registers;
-// its groups of lanes are added in LDS and all workgroups in a second kernel, in a fixed order.
+// turned back).  Lanes as in the forward kernel, which go on to further tokens: a lane adds up the gradients of its own eight weights of queries
+// and of keys in registers; the lanes of a workgroup are added in LDS and all workgroups in a second kernel, in a fixed order.
 template <typename T, int L>
 __global__ __launch_bounds__(256) void norm_rotate_backward_kernel(const NormParams p) {
-  constexpr int kRows = 256 / L;
-  __shared__ float lds[kRows][8 * L + 1];
-  const int lane = threadIdx.x & 63, c = lane % L, group = threadIdx.x / L;
-  const bool is_q = int32_t(blockIdx.x) < p.q_groups, mine = 8 * c < p.dim;
-  const int32_t heads = is_q ? p.heads : p.kv_heads, block = is_q ? blockIdx.x : blockIdx.x - p.q_groups;
-  const int32_t blocks = is_q ? p.q_groups : gridDim.x - p.q_groups;
-  const int64_t rows = p.tokens * heads, row_stride = is_q ? p.q_row : p.k_row, head_stride = is_q ? p.q_head : p.k_head;
-  const T* src = static_cast<const T*>(is_q ? p.q : p.k);
-  const T* grad = static_cast<const T*>(is_q ? p.dq : p.dk);
-  T* dst = static_cast<T*>(is_q ? p.q_out : p.k_out);
-  float w[8] = {}, dw[8] = {};
-  if (mine) read8((is_q ? p.q_weight : p.k_weight) + 8 * c, w);
-  for (int64_t row0 = int64_t(block) * kRows; row0 < rows; row0 += int64_t(blocks) * kRows) {
-    const int64_t row = row0 + group;
-    const bool in = row < rows;
-    const int64_t token = in ? row / heads : 0;
-    const int32_t h = in ? int32_t(row - token * heads) : 0;
+  constexpr int kGroups = 256 / L, kPairs = 2;           // heads of a lane on their way at a time
+  __shared__ float lds[kGroups][8 * L + 1];
+  const int lane = threadIdx.x & 63, c = lane % L, group = threadIdx.x / L, side = 1 << p.log2_side, first = group & (side - 1);
+  const int tokens = kGroups >> p.log2_side;             // at a time
+  const bool mine = 8 * c < p.dim;
+  float dwq[8] = {}, dwk[8] = {};
+  for (int64_t token0 = int64_t(blockIdx.x) * tokens; token0 < p.tokens; token0 += int64_t(gridDim.x) * tokens) {
+    const int64_t at = token0 + (group >> p.log2_side), token = at < p.tokens ? at : p.tokens - 1;
+    const bool in = at < p.tokens;
     const int32_t pos = p.pos ? p.pos[token] : 0;
     const bool live = in && pos >= 0, known = p.rot == 0 || pos < p.n_pos;
-    float x[8] = {}, g[8] = {}, sum = 0.f, dot = 0.f;
-    if (live && mine) {
-      read8(src + token * row_stride + h * head_stride + 8 * c, x);
-      read8(grad + row * p.dim + 8 * c, g);
-    }
+    const Turn turn(p, c, lane, pos, live && known, true);
+    auto rows = [&](const T* src, int64_t stride, const T* grad, int32_t heads, const float* weights, T* dst, float* dw) {
+      float w[8] = {};
+      if (mine && heads) read8(weights + 8 * c, w);
+      for (int32_t h0 = 0; h0 < heads; h0 += kPairs << p.log2_side) {
+        float x[kPairs][8], g[kPairs][8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += x[i] * x[i];
-    sum = sum_of_lanes<L>(sum);
-    const float r = 1.f / sqrtf(sum / float(p.dim) + p.eps);
-    rotate<L>(p, g, c, lane, pos, live && known, true);
-    if (live && !known) {
+        for (int j = 0; j < kPairs; ++j) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[i] = NAN;
-    }
+          for (int i = 0; i < 8; ++i) x[j][i] = g[j][i] = 0.f;
+          const int32_t h = h0 + j * side + first;
+          if (live && mine && h < heads) {
+            read8(src + h * stride + 8 * c, x[j]);
+            read8(grad + int64_t(h) * p.dim + 8 * c, g[j]);
+          }
+        }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      x[i] *= r;
-      dw[i] += g[i] * x[i];
-      g[i] *= w[i];
-      dot += g[i] * x[i];
-    }
-    dot = sum_of_lanes<L>(dot) / float(p.dim);
+        for (int j = 0; j < kPairs; ++j) {
+          const int32_t h = h0 + j * side + first;
+          float sum = 0.f, dot = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = r * (g[i] - x[i] * dot);
-    if (in && mine) {
-      if (!live) {
+          for (int i = 0; i < 8; ++i) sum += x[j][i] * x[j][i];
+          const float r = 1.f / sqrtf(sum_of_lanes<L>(sum) / float(p.dim) + p.eps);
+          if (p.rot) turn(g[j]);
+          if (live && !known && h < heads)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) g[i] = 0.f;
+            for (int i = 0; i < 8; ++i) g[j][i] = NAN;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[j][i] *= r;
+            dw[i] += g[j][i] * x[j][i];
+            g[j][i] *= w[i];
+            dot += g[j][i] * x[j][i];
+          }
+          dot = sum_of_lanes<L>(dot) / float(p.dim);
+          if (!in || !mine || h >= heads) continue;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) g[j][i] = live ? r * (g[j][i] - x[j][i] * dot) : 0.f;
+          write8(dst + int64_t(h) * p.dim + 8 * c, g[j]);
+        }
       }
-      write8(dst + row * p.dim + 8 * c, g);
-    }
+    };
+    rows(static_cast<const T*>(p.q) + token * p.q_row, p.q_head, static_cast<const T*>(p.dq) + token * p.heads * p.dim, p.heads, p.q_weight,
+         static_cast<T*>(p.q_out) + token * p.heads * p.dim, dwq);
+    rows(static_cast<const T*>(p.k) + token * p.k_row, p.k_head, static_cast<const T*>(p.dk) + token * p.kv_heads * p.dim, p.kv_heads, p.k_weight,
+         static_cast<T*>(p.k_out) + token * p.kv_heads * p.dim, dwk);
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) lds[group][8 * c + i] = dw[i];
-  __syncthreads();
-  for (int d = threadIdx.x; d < p.dim; d += 256) {
-    float s = 0.f;
-    for (int g = 0; g < kRows; ++g) s += lds[g][d];
-    p.partial[int64_t(blockIdx.x) * p.dim + d] = s;
+  for (int of_k = 0; of_k < 2; ++of_k) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) lds[group][8 * c + i] = of_k ? dwk[i] : dwq[i];
+    __syncthreads();
+    for (int d = threadIdx.x; d < p.dim; d += 256) {
+      float s = 0.f;
+      for (int g = 0; g < kGroups; ++g) s += lds[g][d];
+      p.partial[(int64_t(blockIdx.x) * 2 + of_k) * p.dim + d] = s;
+    }
   }
 }
 
 // Sum of the workgroups' weight gradients: a workgroup per weight of queries (y = 0) and keys.
-__global__ __launch_bounds__(256) void weights_kernel(const float* partial, int32_t dim, int32_t q_groups, int32_t k_groups, float* q, float* k) {
+__global__ __launch_bounds__(256) void weights_kernel(const float* partial, int32_t dim, int32_t groups, float* q, float* k) {
   __shared__ float lds[4];
-  const int32_t d = blockIdx.x, groups = blockIdx.y ? k_groups : q_groups;
-  const float* src = partial + (blockIdx.y ? int64_t(q_groups) * dim : 0);
+  const int32_t d = blockIdx.x;
+  float* out = blockIdx.y ? k : q;
+  if (!out) return;
   float s = 0.f;
-  for (int32_t g = threadIdx.x; g < groups; g += 256) s += src[int64_t(g) * dim + d];
+  for (int32_t g = threadIdx.x; g < groups; g += 256) s += partial[(int64_t(g) * 2 + blockIdx.y) * dim + d];
 #pragma unroll
   for (int i = 32; i; i >>= 1) s += __shfl_xor(s, i, 64);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  if (threadIdx.x == 0) (blockIdx.y ? k : q)[d] = lds[0] + lds[1] + lds[2] + lds[3];
+  if (threadIdx.x == 0) out[d] = lds[0] + lds[1] + lds[2] + lds[3];
 }
 
 int lanes_of(int32_t dim) {
@@ -187,9 +221,19 @@ int lanes_of(int32_t dim) {
   while (8 * l < dim) l *= 2;
   return l;
 }
+// Heads side by side.  Where there are too few tokens to fill the GPU, as many as a wave holds.  Else one in the forward pass, which then reads a
+// token's angles least often, and in the backward pass, which reads and writes more, as many as make 16 lanes, 256 bytes of 16-bit elements (282624
+// tokens, 8 + 8 heads of 32: forward 120 us, with four side by side 146; backward 193, with four 173).  Never more than there are heads.
+bool few_tokens(int device, const lgp_heads* h) { return h->tokens * 16 < int64_t(compute_units(device)) * 512; }
+int32_t heads_side(int device, const lgp_heads* h, bool backward) {
+  const int l = lanes_of(h->dim), most = few_tokens(device, h) ? 64 : backward ? 16 : l;
+  int side = 0;
+  while ((l << side) < most && (1 << side) < std::max(h->heads, h->kv_heads)) ++side;
+  return side;
+}
 template <typename T> void forward(const NormParams& p, hipStream_t s) {
   const int l = lanes_of(p.dim);
-  const uint32_t blocks = uint32_t((p.tokens * (p.heads + p.kv_heads) * l + 255) / 256);
+  const dim3 blocks(uint32_t(((p.tokens * l << p.log2_side) + 255) / 256), p.apart ? 2 : 1);
   switch (l) {
     case 1: norm_rotate_kernel<T, 1><<<blocks, 256, 0, s>>>(p); break;
     case 2: norm_rotate_kernel<T, 2><<<blocks, 256, 0, s>>>(p); break;
@@ -215,7 +259,7 @@ int check_norm(const lgp_heads* h) {
   if (h->tokens < 0 || h->heads < 0 || h->kv_heads < 0 || h->heads + h->kv_heads < 1 || h->dim < 1 || h->rot < 0 || h->rot > h->dim) return LGP_EINVAL;
   if (h->dtype != LGP_F32 && h->dtype != LGP_F16 && h->dtype != LGP_BF16) return LGP_EUNSUPPORTED;
   if (h->dim % 8 || h->dim > 256 || h->rot % 16) return LGP_EUNSUPPORTED;
-  if (h->heads > 65536 || h->kv_heads > 65536 || h->tokens >= (int64_t(1) << 36) / (h->heads + h->kv_heads)) return LGP_EUNSUPPORTED;   // workgroups below 2^31
+  if (h->heads > 65536 || h->kv_heads > 65536 || h->tokens >= int64_t(1) << 33) return LGP_EUNSUPPORTED;       // workgroups below 2^31
   if (h->tokens && ((h->heads && !h->q) || (h->kv_heads && !h->k))) return LGP_EINVAL;
   if ((h->heads && !h->q_weight) || (h->kv_heads && !h->k_weight)) return LGP_EINVAL;
   if (h->rot && (!h->table || h->n_pos < 1 || (h->tokens && !h->pos))) return LGP_EINVAL;
@@ -230,14 +274,10 @@ NormParams norm_params(const lgp_heads* h) {
   p.q_weight = h->q_weight; p.k_weight = h->k_weight; p.pos = h->pos; p.table = h->table; p.eps = h->eps;
   return p;
 }
-// Workgroups of the backward kernel that take queries and keys: at most four per CU, shared by the rows there are of each.
-void backward_groups(int device, const lgp_heads* h, int32_t* q, int32_t* k) {
-  const int64_t rows = 256 / lanes_of(h->dim), most = int64_t(compute_units(device)) * 4, all = std::max<int64_t>(1, h->heads + h->kv_heads);
-  auto groups = [&](int64_t heads) {
-    return heads == 0 ? 0 : int32_t(std::max<int64_t>(1, std::min((h->tokens * heads + rows - 1) / rows, most * heads / all)));
-  };
-  *q = groups(h->heads);
-  *k = groups(h->kv_heads);
+// Workgroups of the backward kernel: at most four per CU.
+int32_t backward_groups(int device, const lgp_heads* h) {
+  const int64_t tokens = std::max(1, 256 / lanes_of(h->dim) >> heads_side(device, h, true));
+  return int32_t(std::max<int64_t>(1, std::min((h->tokens + tokens - 1) / tokens, int64_t(compute_units(device)) * 4)));
 }
 
 }  // namespace
@@ -255,6 +295,8 @@ int lgp_norm_rotate(int device, const lgp_heads* in, void* q_out, void* k_out, v
   if (int st = use_device(device)) return st;
   if (in->tokens == 0) return LGP_OK;
   NormParams p = norm_params(in);
+  p.log2_side = heads_side(device, in, false);
+  p.apart = few_tokens(device, in);
   p.q_out = q_out;
   p.k_out = k_out;
   const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -268,9 +310,7 @@ int lgp_norm_rotate_workspace(int device, const lgp_heads* in, size_t* bytes) {
   if (!bytes) return LGP_EINVAL;
   *bytes = 0;
   if (int st = check_norm(in)) return st;
-  int32_t q, k;
-  backward_groups(device, in, &q, &k);
-  *bytes = size_t(q + k) * in->dim * sizeof(float);
+  *bytes = size_t(backward_groups(device, in)) * 2 * in->dim * sizeof(float);
   return LGP_OK;
 }
 
@@ -282,23 +322,20 @@ int lgp_norm_rotate_backward(int device, const lgp_heads* in, const void* dq_out
   if (!aligned16(dq_out) || !aligned16(dk_out) || !aligned16(dq) || !aligned16(dk)) return LGP_EINVAL;
   if (int st = use_device(device)) return st;
   NormParams p = norm_params(in);
-  int32_t q, k;
-  backward_groups(device, in, &q, &k);
-  if (workspace_bytes < size_t(q + k) * in->dim * sizeof(float)) return LGP_ECAPACITY;
+  p.log2_side = heads_side(device, in, true);
+  const int32_t groups = backward_groups(device, in);
+  if (workspace_bytes < size_t(groups) * 2 * in->dim * sizeof(float)) return LGP_ECAPACITY;
   if (!workspace || !aligned16(workspace)) return LGP_EINVAL;
   p.dq = dq_out;
   p.dk = dk_out;
   p.q_out = dq;
   p.k_out = dk;
   p.partial = static_cast<float*>(workspace);
-  p.q_groups = q;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (in->dtype == LGP_F32) backward<float>(p, q + k, s);
-  else if (in->dtype == LGP_F16) backward<f16>(p, q + k, s);
-  else backward<bf16>(p, q + k, s);
-  // without heads of one kind there are no workgroups of it, and nothing of it to write
-  if (in->heads && in->kv_heads) weights_kernel<<<dim3(in->dim, 2), 256, 0, s>>>(p.partial, in->dim, q, k, dq_weight, dk_weight);
-  else weights_kernel<<<dim3(in->dim, 1), 256, 0, s>>>(p.partial, in->dim, q + k, 0, in->heads ? dq_weight : dk_weight, nullptr);
+  if (in->dtype == LGP_F32) backward<float>(p, groups, s);
+  else if (in->dtype == LGP_F16) backward<f16>(p, groups, s);
+  else backward<bf16>(p, groups, s);
+  weights_kernel<<<dim3(in->dim, 2), 256, 0, s>>>(p.partial, in->dim, groups, in->heads ? dq_weight : nullptr, in->kv_heads ? dk_weight : nullptr);
   return launched();
 }
 
