@@ -22,7 +22,7 @@ struct AttendParams {
   // scale: where it is negative, q (by keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the
   // largest product is the largest score.
   float scale, z_mul;        // z_mul: scale * log2(e), or cap * log2(e)
-  float t_mul;               // 2 * log2(e) * scale / cap, so that tanh = 1 - 2 / (exp2(qk * t_mul) + 1)
+  float t_mul;               // scale / cap
   bool negate;
   const float* slopes;
   float docs_per_tile;
@@ -36,7 +36,7 @@ struct AttendParams {
   const float* lse_in;
   void *dq, *dk, *dv;
   float* delta;              // [q_rows][heads]: d_out . out
-  float* sums;               // [split][q_rows][heads][3], if the gradient of the slopes is wanted: see attend_dq_kernel
+  floatx4* sums;             // [split][q_rows][heads], if the gradient of the slopes is wanted: see attend_dq_kernel
 };
 
 template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p) { return *reinterpret_cast<const vec8<T>*>(p); }
@@ -50,14 +50,34 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
 }
 template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
 
-// A score in powers of two, plus `more`; the tanh of the cap is kept for the backward pass.
-template <bool CAP> __device__ __forceinline__ float score(const AttendParams& p, float qk, float more, float& tanh_out) {
-  if constexpr (CAP) {
-    tanh_out = 1.f - 2.f * rcp_fast(exp2_fast(qk * p.t_mul) + 1.f);
-    return fmaf(tanh_out, p.z_mul, more);
-  }
-  return fmaf(qk, p.z_mul, more);
+// tanh(x) for the cap of the scores.  Up to kNear it is x + x^3 (c0 + c1 x^2 + c2 x^4 + c3 x^6), fitted by least squares of the relative error,
+// reweighted until even: 1e-7 with its roundings, and it is where capped scores mostly are.  Beyond, 1 - 2 / (e^2x + 1), which near zero would be
+// 1e-7 off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.
+constexpr float kNear = 0.55f;
+__device__ __forceinline__ float tanh_near(float x) {
+  const float u = x * x;
+  return fmaf(fmaf(fmaf(fmaf(0.016437582671642303f, u, -0.05267181620001793f), u, 0.13320724666118622f), u, -0.3333294689655304f) * u, x, x);
 }
+__device__ __forceinline__ float tanh_of(float x) {
+  const float far = 1.f - 2.f * rcp_fast(exp2_fast(x * (2.f * kLog2e)) + 1.f);
+  return fabsf(x) <= kNear ? tanh_near(x) : far;
+}
+// Products q.k become tanh(q.k * scale / cap) where scores are capped, and stay as they are where not; times z_mul they are scores in powers of two.
+template <bool CAP> __device__ __forceinline__ void cap(const AttendParams& p, floatx16& s) {
+  if constexpr (CAP) {
+    float most = 0.f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+    if (__any(most * p.t_mul > kNear)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = tanh_of(s[r] * p.t_mul);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = tanh_near(s[r] * p.t_mul);
+    }
+  }
+}
+template <bool CAP> __device__ __forceinline__ float capped(const AttendParams& p, float s) { return CAP ? tanh_of(s * p.t_mul) : s; }
 
 // The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys.
 __device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, int32_t splits, int32_t& begin, int32_t& end) {

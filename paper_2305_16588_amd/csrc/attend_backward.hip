@@ -13,10 +13,10 @@ namespace {
 //     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
 // Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
 // delta is taken from out and what its rounding took off.  The slope of a head has the gradient
-//     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|)),
-// whose three sums per row go to `sums`: so it does not depend on how out was rounded.
+//     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|) / sum_j P) / sum_j P,
+// whose four sums per row go to `sums`: so it depends neither on how out was rounded nor on the rounding of lse.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 2) void attend_dq_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
   __shared__ __align__(16) T lds_k[2][BN * D];
   __shared__ __align__(16) T lds_v[2][BN * D];
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
   }
 
   floatx16 dq[D / 32] = {};
-  float sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
+  float sum_p = 0.f, sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, int now, auto whole) {
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
     tile_ready<(NW > 1)>();
     if (k0 + BN < k_end) stage(k0 + BN, now ^ 1);
     if (idle) return;
-    if constexpr (D == 128) at_tile.again();
+    at_tile.again();
     const T *tile_k = lds_k[now], *tile_v = lds_v[now];
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
@@ -116,6 +116,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
         g = Elem<T>::mfma(at_tile.along(tile_v, 32 * b, kk), df[kk], g);
       }
       const int32_t there = k0 + BN <= k_end ? BN : k_end - k0 - 32 * b - 4 * half;      // places of this block's half that are keys
+      cap<CAP>(p, s);
       vec8<T> uf[2];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
@@ -124,17 +125,18 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
-          float t = 0.f, far = 0.f;
+          float far = 0.f;
           if constexpr (BIAS) far = fabsf(at - kpos[i]);
-          const float z = score<CAP>(p, s[r], BIAS ? fmaf(-slope, far, -lse) : -lse, t);
+          const float z = fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope, far, -lse) : -lse);
           const float e = WHOLE || 8 * r4 + i < there ? exp2_fast(z) : 0.f, pd = e * g[r];
           if constexpr (BIAS) {
+            sum_p += e;
             sum_pd += pd;
             sum_pf = fmaf(e, far, sum_pf);
             sum_pdf = fmaf(pd, far, sum_pdf);
           }
           float u = fmaf(-e, delta, pd);
-          if constexpr (CAP) u *= 1.f - t * t;
+          if constexpr (CAP) u = fmaf(-u * s[r], s[r], u);
           uf[r / 8][r % 8] = T(u);
         }
       }
@@ -153,15 +155,11 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dq_kernel(con
 
   if (row >= qd.owned * p.group) return;
   if constexpr (BIAS) {
+    sum_p += other_half(sum_p);
     sum_pd += other_half(sum_pd);
     sum_pf += other_half(sum_pf);
     sum_pdf += other_half(sum_pdf);
-    if (p.sums && half == 0) {
-      float* x = p.sums + (int64_t(split) * p.qs.rows * p.heads + at_out) * 3;
-      x[0] = live ? sum_pd : 0.f;
-      x[1] = live ? sum_pf : 0.f;
-      x[2] = live ? sum_pdf : 0.f;
-    }
+    if (p.sums && half == 0) p.sums[int64_t(split) * p.qs.rows * p.heads + at_out] = live ? floatx4{sum_p, sum_pd, sum_pf, sum_pdf} : floatx4{};
   }
   float* part = p.splits > 1 ? p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim : nullptr;
   T* out = static_cast<T*>(p.dq) + at_out * p.dim;
@@ -205,14 +203,10 @@ __global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, float
   if (at >= each) return;
   float x = 0.f;
   for (int64_t r = at; r < rows; r += each) {
-    float pd = 0.f, pf = 0.f, pdf = 0.f;
-    for (int32_t s = 0; s < p.splits; ++s) {
-      const float* m = p.sums + (s * rows + r) * 3;
-      pd += m[0];
-      pf += m[1];
-      pdf += m[2];
-    }
-    x -= pdf - pd * pf;
+    floatx4 m = {};
+    for (int32_t s = 0; s < p.splits; ++s) m += p.sums[s * rows + r];
+    const float inv = m[0] != 0.f ? 1.f / m[0] : 0.f;
+    x -= (m[3] - m[1] * m[2] * inv) * inv;
   }
   partial[at] = x;
 }
@@ -232,7 +226,7 @@ __global__ __launch_bounds__(256) void slopes_end_kernel(const float* partial, i
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 2) void attend_dkv_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
   __shared__ __align__(16) T lds_q[2][BQ * D];
   __shared__ __align__(16) T lds_g[2][BQ * D];
@@ -324,7 +318,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
     if (r0 >= rows) r0 = 0, h0 += 1 << p.log2_fold;
     if (h0 < (hk + 1) * p.group) stage(h0, r0, now ^ 1);
     if (idle) return;
-    if constexpr (D == 128) at_tile.again();
+    at_tile.again();
     const T *tile_q = lds_q[now], *tile_g = lds_g[now];
 #pragma unroll
     for (int b = 0; b < BQ / 32; ++b) {
@@ -335,6 +329,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
         g = Elem<T>::mfma(at_tile.along(tile_g, 32 * b, kk),
                              kHeld ? vf[kHeld ? kk : 0] : at_tile.along(lds_v + 32 * wave * D, 0, kk), g);
       }
+      cap<CAP>(p, s);
       vec8<T> pf[2], uf[2];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
@@ -348,10 +343,9 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : 2) void attend_dkv_kernel(co
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
-          float t = 0.f;
-          const float e = exp2_fast(score<CAP>(p, s[r], BIAS ? fmaf(-slope[i], fabsf(at - pos[i]), -lse[i]) : -lse[i], t));             // times kLift
+          const float e = exp2_fast(fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope[i], fabsf(at - pos[i]), -lse[i]) : -lse[i]));             // times kLift
           float u = e * ((g[r] - delta[i]) * (1.f / kLift<T>));
-          if constexpr (CAP) u *= 1.f - t * t;
+          if constexpr (CAP) u = fmaf(-u * s[r], s[r], u);
           pf[r / 8][r % 8] = T(e);
           uf[r / 8][r % 8] = T(u);
         }
@@ -409,7 +403,7 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
   auto up = [](size_t x) { return (x + 3) / 4 * 4; };
   b.delta = 0;
   b.sums = up(rows);
-  b.partial = b.sums + (a->slopes ? up(rows * 3 * b.q.splits) : 0);
+  b.partial = b.sums + (a->slopes ? rows * 4 * b.q.splits : 0);
   b.parts = b.partial + (a->slopes ? size_t(kSlopeThreads) : 0);
   b.bytes = (b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0)) * sizeof(float);
   return b;
@@ -422,13 +416,13 @@ template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams
   const uint32_t blocks = uint32_t(b.q.tiles) * p.kv_heads * p.splits, key_blocks = uint32_t(b.key_tiles) * p.kv_heads;
   if (p.qs.rows) {
     if (b.q.waves == 1) attend_dq_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
-    else attend_dq_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<blocks, 256, 0, s>>>(x);
+    else attend_dq_kernel<T, D, CAP, BIAS, 4, 32><<<blocks, 256, 0, s>>>(x);
   }
   x.tiles = int32_t(b.key_tiles);
   x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.key_tiles, 1));
   if (p.ks.rows) {
     if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<key_blocks, 64, 0, s>>>(x);
-    else attend_dkv_kernel<T, D, CAP, BIAS, 4, D == 128 ? 32 : 64><<<key_blocks, 256, 0, s>>>(x);
+    else attend_dkv_kernel<T, D, CAP, BIAS, 4, 32><<<key_blocks, 256, 0, s>>>(x);
   }
 }
 template <typename T, int D> void launch(const AttendParams& p, const BackwardShape& b, bool cap, hipStream_t s) {
@@ -489,7 +483,7 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
   p.dk = dk;
   p.dv = dv;
   p.delta = w + b.delta;
-  p.sums = d_slopes ? w + b.sums : nullptr;
+  p.sums = d_slopes ? reinterpret_cast<floatx4*>(w + b.sums) : nullptr;
   p.part_o = w + b.parts;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (single_queries(docs, att)) launch_single(p, att, true, s);

@@ -102,6 +102,7 @@ __global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(c
       floatx16 acc = {};
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) acc = Elem<T>::mfma(at_tile.along(tile_k, 32 * b, kk), qf[kk], acc);
+      cap<CAP>(p, acc);
       s[b] = acc;
     }
     if (now == 0 && k0 == k_begin) {
@@ -113,9 +114,9 @@ __global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(c
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = 32 * b + 8 * (r / 4) + 4 * half + r % 4;
-          float t, more = 0.f;
+          float more = 0.f;
           if constexpr (BIAS) more = -slope * fabsf(at - lds_pos[now][key]);
-          if (k0 + key < k_end) most = fmaxf(most, score<CAP>(p, s[b][r], more, t));
+          if (k0 + key < k_end) most = fmaxf(most, fmaf(s[b][r], p.z_mul, more));
         }
       most = fmaxf(most, other_half(most));
       if (most > -INFINITY) base = most, limit = kSlack;
@@ -128,8 +129,7 @@ __global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(c
         if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float t;
-          s[b][4 * r4 + i] = score<CAP>(p, s[b][4 * r4 + i], BIAS ? fmaf(-slope, fabsf(at - kpos[i]), -base) : -base, t);
+          s[b][4 * r4 + i] = fmaf(s[b][4 * r4 + i], p.z_mul, BIAS ? fmaf(-slope, fabsf(at - kpos[i]), -base) : -base);
         }
       }
     }
@@ -347,7 +347,7 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   const float scale = std::fabs(a->scale);
   p.negate = a->scale < 0.f;
   p.z_mul = (a->cap > 0.f ? a->cap : std::max(scale, 1e-30f)) * kLog2e;
-  p.t_mul = a->cap > 0.f ? float(2.0 * double(kLog2e) * scale / a->cap) : 0.f;
+  p.t_mul = a->cap > 0.f ? scale / a->cap : 0.f;
   p.per_token = divisor(uint32_t(p.group));
   while (16 % p.group == 0 && (1 << p.log2_fold) < p.group) ++p.log2_fold;
   p.slopes = a->slopes;

@@ -79,8 +79,7 @@ __global__ __launch_bounds__(256) void single_kernel(const AttendParams p, int32
       for (int i = 0; i < kSteps; ++i)
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          float t;
-          z[i][g] = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], q[g])), BIAS ? -slope[g] * fabsf(at - far[i]) : 0.f, t);
+          z[i][g] = fmaf(capped<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], q[g]))), p.z_mul, BIAS ? -slope[g] * fabsf(at - far[i]) : 0.f);
           if (k0 + i * a.keys_at_once + a.key >= keys) z[i][g] = -INFINITY;
         }
 #pragma unroll
@@ -181,7 +180,8 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
   for (int32_t row = 0; row < qd.owned; ++row) {
     const int64_t token = int64_t(qd.begin) + row;
     const bool live = row < qd.tokens;
-    float dq[G][8] = {}, pd[G] = {}, pf[G] = {}, pdf[G] = {};
+    float dq[G][8] = {};
+    floatx4 sums[G] = {};
     if (live) {
       Query<T, L, G, BIAS> x;
       x.load(p, a, token);
@@ -203,13 +203,10 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
           float dk[8] = {}, dv[8] = {};
 #pragma unroll
           for (int h = 0; h < G; ++h) {
-            float t = 0.f;
-            const float z = score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], x.q[h])), BIAS ? fmaf(-x.slope[h], far[i], -x.lse[h]) : -x.lse[h], t);
+            const float t = capped<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], x.q[h]))), z = fmaf(t, p.z_mul, BIAS ? fmaf(-x.slope[h], far[i], -x.lse[h]) : -x.lse[h]);
             const float e = key < kd.tokens ? exp2_fast(z) : 0.f, dp = sum_of_lanes<L>(dot8<T>(vf[i], x.g[h]));
             if constexpr (BIAS) {
-              pd[h] += e * dp;
-              pf[h] += e * far[i];
-              pdf[h] += e * dp * far[i];
+              sums[h] += floatx4{e, e * dp, e * far[i], e * dp * far[i]};
             }
             float u = e * (dp - x.delta[h]);
             if constexpr (CAP) u *= 1.f - t * t;
@@ -226,15 +223,15 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
     }
 #pragma unroll
     for (int h = 0; h < G; ++h) {
-      float o[8] = {}, s[3] = {};
+      float o[8] = {};
+      floatx4 s = {};
       for (int k = 0; k < a.keys_at_once; ++k) {
         const int from = a.twin(k, heads_at_once);
 #pragma unroll
         for (int j = 0; j < 8; ++j) o[j] += __shfl(dq[h][j], from, 64);
         if constexpr (BIAS) {
-          s[0] += __shfl(pd[h], from, 64);
-          s[1] += __shfl(pf[h], from, 64);
-          s[2] += __shfl(pdf[h], from, 64);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] += __shfl(sums[h][j], from, 64);
         }
       }
       if (!a.in || a.key != 0) continue;
@@ -244,8 +241,7 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
       for (int j = 0; j < 8; ++j) x[j] = T(o[j] * p.scale);
       *reinterpret_cast<vec8<T>*>(static_cast<T*>(p.dq) + at_out * p.dim + 8 * a.c) = x;
       if constexpr (BIAS) {
-        if (p.sums && a.c == 0)
-          for (int j = 0; j < 3; ++j) p.sums[at_out * 3 + j] = s[j];
+        if (p.sums && a.c == 0) p.sums[at_out] = s;
       }
     }
   }
@@ -262,8 +258,8 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
         x.load(p, a, int64_t(qd.begin) + row);
 #pragma unroll
         for (int h = 0; h < G; ++h) {
-          float t = 0.f;
-          const float e = exp2_fast(score<CAP>(p, sum_of_lanes<L>(dot8<T>(kf, x.q[h])), BIAS ? fmaf(-x.slope[h], fabsf(x.at - far), -x.lse[h]) : -x.lse[h], t));
+          const float t = capped<CAP>(p, sum_of_lanes<L>(dot8<T>(kf, x.q[h])));
+          const float e = exp2_fast(fmaf(t, p.z_mul, BIAS ? fmaf(-x.slope[h], fabsf(x.at - far), -x.lse[h]) : -x.lse[h]));
           float u = e * (sum_of_lanes<L>(dot8<T>(vf, x.g[h])) - x.delta[h]);
           if constexpr (CAP) u *= 1.f - t * t;
 #pragma unroll

@@ -90,12 +90,14 @@ template <typename T> struct Rows {
 template <typename T, int D, int ROWS, int THREADS>
 __device__ __forceinline__ void copy_tile(T* tile, const Rows<T>& rows, int32_t first, int dim, int there, int tid) {
   constexpr int kStep = THREADS * 8 / D;         // rows that all threads write at once
-  static_assert(ROWS % kStep == 0, "whole waves");
+  static_assert(ROWS % kStep == 0 || kStep % ROWS == 0, "whole waves");
   const uint32_t to = __builtin_amdgcn_readfirstlane(lds_address(tile) + (tid & ~63) * 16);
   const int r0 = tid / (D / 8), fold = 1 << rows.log2_fold;
   const T* from = rows.from + int64_t(first >> rows.log2_fold) * rows.row;
+  if (kStep > ROWS && r0 >= ROWS) return;        // more threads than chunks
+  constexpr int kSteps = kStep > ROWS ? 1 : ROWS / kStep;
 #pragma unroll
-  for (int c = 0; c < ROWS / kStep; ++c) {
+  for (int c = 0; c < kSteps; ++c) {
     // with 16 rows and more at once the places in a row repeat, and so do the heads of a token
     const int r = kStep % 16 == 0 ? r0 : c * kStep + r0, d = ((tid % (D / 8)) ^ swizzle<D>(r)) * 8;
     const uint32_t offset = (uint32_t(r >> rows.log2_fold) * uint32_t(rows.row) + uint32_t(r & (fold - 1)) * uint32_t(rows.head) + d) * sizeof(T);
@@ -105,7 +107,7 @@ __device__ __forceinline__ void copy_tile(T* tile, const Rows<T>& rows, int32_t 
   if (there < ROWS) {
     const vec8<T> zero = {};
 #pragma unroll
-    for (int c = 0; c < ROWS / kStep; ++c)
+    for (int c = 0; c < kSteps; ++c)
       if (c * kStep + r0 >= there) reinterpret_cast<vec8<T>*>(tile)[c * THREADS + tid] = zero;
   }
 }
