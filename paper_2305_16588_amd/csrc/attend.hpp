@@ -101,6 +101,10 @@ template <typename T> constexpr float kLiftLog2 = 0.f;
 template <> inline constexpr float kLiftLog2<f16> = 12.f;
 
 // Launch shapes, chosen on the host by what it knows: rows and documents.
+// Whether a workgroup is one wave of 32 rows, which waits for no other but has its tiles to itself: documents of up to 32 rows, and with heads of up
+// to 32, whose tiles are small, of up to 320 (1024 documents of 276 rows, half of them with tokens, heads of 32: forward 295 us with four waves, 281
+// with one, gradients of q 336 and 303, of k and v 321 and 312; 256 of 916 folded rows, heads of 64: forward 198 and 284).
+inline bool one_wave(int64_t rows, int64_t docs, int32_t dim) { return rows <= (dim <= 32 ? 320 : 32) * docs; }
 constexpr int kMostSplits = 256;        // a thread of join_kernel each
 constexpr int kForwardRows = 32;        // folded rows of a wave
 struct ForwardShape { int waves, key_waves; int64_t tiles; int splits; };      // waves of rows, and of parts of the keys, in a workgroup

@@ -397,7 +397,7 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
   b.q.splits = std::min(b.q.splits * b.q.key_waves, kMostSplits);        // this kernel's waves take parts of the keys as workgroups of their own
   if (b.q.key_waves > 1) b.q.splits = int(std::max<int64_t>(1, std::min<int64_t>(b.q.splits, d->k_rows / std::max<int64_t>(d->n_docs, 1) / 256)));
   if (single_queries(d, a)) b.q.splits = 1;
-  b.key_waves = d->k_rows <= 32 * std::max<int64_t>(d->n_docs, 1) ? 1 : 4;
+  b.key_waves = one_wave(d->k_rows, std::max<int64_t>(d->n_docs, 1), a->dim) ? 1 : 4;
   b.key_tiles = tiles_of(d->k_rows, 1, d->n_docs, 32 * b.key_waves);
   const size_t rows = size_t(d->q_rows) * a->heads;
   auto up = [](size_t x) { return (x + 3) / 4 * 4; };

@@ -356,13 +356,13 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
 }
 
 // Where documents have up to 32 folded rows, a wave has them, or four share them where the keys are 64 and more; where they have more, four waves
-// of 32 rows each share the keys.  Few tiles over long documents are split over the keys until every CU has a few waves, at no less than 256
+// of 32 rows each share the keys, or are on their own where tiles are small and documents of a few waves leave others idle.  Few tiles over long documents are split over the keys until every CU has a few waves, at no less than 256
 // keys a part.
 ForwardShape forward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
   const int64_t group = a->heads / a->kv_heads, n = std::max<int64_t>(d->n_docs, 1), keys = d->k_rows / n;
   ForwardShape f;
-  f.waves = d->q_rows * group <= 32 * n ? 1 : 4;
-  f.key_waves = f.waves == 1 && keys >= 64 ? 4 : 1;
+  f.waves = one_wave(d->q_rows * group, n, a->dim) ? 1 : 4;
+  f.key_waves = d->q_rows * group <= 32 * n && keys >= 64 ? 4 : 1;
   f.tiles = tiles_of(d->q_rows, group, d->n_docs, kForwardRows * f.waves);
   const int64_t waves = f.tiles * a->kv_heads * f.waves * f.key_waves, room = int64_t(compute_units(device)) * 8;
   f.splits = int(std::max<int64_t>(1, std::min({room / std::max<int64_t>(waves, 1), keys / 256 / f.key_waves, int64_t(kMostSplits)})));
