@@ -18,11 +18,10 @@ struct AttendParams {
   int32_t n_docs, heads, kv_heads, group, dim;
   Divisor per_token;         // by group
   int32_t log2_fold;         // by keys: heads of a token that are folded, all of the group or one
-  // Scores in powers of two: z * log2(e) = capped ? tanh(qk * scale / cap) * cap * log2(e) : qk * scale * log2(e), with the magnitude of the
-  // scale: where it is negative, q (by keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the
-  // largest product is the largest score.
-  float scale, z_mul;        // z_mul: scale * log2(e), or cap * log2(e)
-  float t_mul;               // scale / cap
+  // Scores in powers of two: the product qk, capped, times z_mul = scale * log2(e), with the magnitude of the scale: where it is negative, q (by
+  // keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the largest product is the largest score.
+  float scale, z_mul;
+  float t_mul, t_inv, tanh_c[4];         // scale / cap and its inverse, and kTanh with its powers: see capped_near
   bool negate;
   const float* slopes;
   float docs_per_tile;
@@ -50,19 +49,20 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
 }
 template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
 
-// tanh(x) for the cap of the scores.  Up to kNear it is x + x^3 (c0 + c1 x^2 + c2 x^4 + c3 x^6), fitted by least squares of the relative error,
-// reweighted until even: 1e-7 with its roundings, and it is where capped scores mostly are.  Beyond, 1 - 2 / (e^2x + 1), which near zero would be
-// 1e-7 off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.
+// The cap: a product qk becomes tanh(x) / t_mul with x = qk * t_mul, which is qk where the cap is far.  Up to x = kNear that is
+// qk (1 + c0 x^2 + c1 x^4 + c2 x^6 + c3 x^8), fitted by least squares of the relative error, reweighted until even: 1e-7 with its roundings, and it
+// is where capped scores mostly are; the powers of t_mul are in the coefficients.  Beyond, tanh(x) = 1 - 2 / (e^2x + 1), which near zero would be 1e-7
+// off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.
 constexpr float kNear = 0.55f;
-__device__ __forceinline__ float tanh_near(float x) {
-  const float u = x * x;
-  return fmaf(fmaf(fmaf(fmaf(0.016437582671642303f, u, -0.05267181620001793f), u, 0.13320724666118622f), u, -0.3333294689655304f) * u, x, x);
+constexpr float kTanh[4] = {-0.3333294689655304f, 0.13320724666118622f, -0.05267181620001793f, 0.016437582671642303f};
+__device__ __forceinline__ float capped_near(const AttendParams& p, float s) {
+  const float w = s * s;
+  return s * fmaf(fmaf(fmaf(fmaf(p.tanh_c[3], w, p.tanh_c[2]), w, p.tanh_c[1]), w, p.tanh_c[0]), w, 1.f);
 }
-__device__ __forceinline__ float tanh_of(float x) {
-  const float far = 1.f - 2.f * rcp_fast(exp2_fast(x * (2.f * kLog2e)) + 1.f);
-  return fabsf(x) <= kNear ? tanh_near(x) : far;
+__device__ __forceinline__ float capped_any(const AttendParams& p, float s) {
+  const float x = s * p.t_mul, far = (1.f - 2.f * rcp_fast(exp2_fast(x * (2.f * kLog2e)) + 1.f)) * p.t_inv;
+  return fabsf(x) <= kNear ? capped_near(p, s) : far;
 }
-// Products q.k become tanh(q.k * scale / cap) where scores are capped, and stay as they are where not; times z_mul they are scores in powers of two.
 template <bool CAP> __device__ __forceinline__ void cap(const AttendParams& p, floatx16& s) {
   if constexpr (CAP) {
     float most = 0.f;
@@ -70,14 +70,22 @@ template <bool CAP> __device__ __forceinline__ void cap(const AttendParams& p, f
     for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
     if (__any(most * p.t_mul > kNear)) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = tanh_of(s[r] * p.t_mul);
+      for (int r = 0; r < 16; ++r) s[r] = capped_any(p, s[r]);
     } else {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = tanh_near(s[r] * p.t_mul);
+      for (int r = 0; r < 16; ++r) s[r] = capped_near(p, s[r]);
     }
   }
 }
-template <bool CAP> __device__ __forceinline__ float capped(const AttendParams& p, float s) { return CAP ? tanh_of(s * p.t_mul) : s; }
+template <bool CAP> __device__ __forceinline__ float capped(const AttendParams& p, float s) { return CAP ? capped_any(p, s) : s; }
+// u times the cap's derivative, 1 - tanh^2, from the capped product.
+template <bool CAP> __device__ __forceinline__ float through_cap(const AttendParams& p, float u, float s) {
+  if constexpr (CAP) {
+    const float t = s * p.t_mul;
+    return fmaf(-u * t, t, u);
+  }
+  return u;
+}
 
 // The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys.
 __device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, int32_t splits, int32_t& begin, int32_t& end) {

@@ -136,7 +136,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 
             sum_pdf = fmaf(pd, far, sum_pdf);
           }
           float u = fmaf(-e, delta, pd);
-          if constexpr (CAP) u = fmaf(-u * s[r], s[r], u);
+          u = through_cap<CAP>(p, u, s[r]);
           uf[r / 8][r % 8] = T(u);
         }
       }
@@ -345,7 +345,7 @@ __global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 
           const int r = 4 * r4 + i;
           const float e = exp2_fast(fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope[i], fabsf(at - pos[i]), -lse[i]) : -lse[i]));             // times kLift
           float u = e * ((g[r] - delta[i]) * (1.f / kLift<T>));
-          if constexpr (CAP) u = fmaf(-u * s[r], s[r], u);
+          u = through_cap<CAP>(p, u, s[r]);
           pf[r / 8][r % 8] = T(e);
           uf[r / 8][r % 8] = T(u);
         }

@@ -81,7 +81,7 @@ __global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(c
   }
 
   floatx16 o[D / 32] = {};
-  // Scores are taken relative to `base`; a maximum beyond `limit` raises it: any, until the row has seen a score that is not -inf.
+  // Scores are taken relative to `base`; a maximum beyond `limit` raises it: any, until the row has seen a score that is not infinite.
   float base = 0.f, limit = -3e38f, sum = 0.f;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
@@ -106,20 +106,12 @@ __global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(c
       s[b] = acc;
     }
     if (now == 0 && k0 == k_begin) {
-      // The first base is the first tile's maximum, found ahead: scores of a magnitude that leaves no digits for their differences are then
-      // rounded only once the base is taken off, like those of later tiles.
-      float most = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < BN / 32; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int key = 32 * b + 8 * (r / 4) + 4 * half + r % 4;
-          float more = 0.f;
-          if constexpr (BIAS) more = -slope * fabsf(at - lds_pos[now][key]);
-          if (k0 + key < k_end) most = fmaxf(most, fmaf(s[b][r], p.z_mul, more));
-        }
-      most = fmaxf(most, other_half(most));
-      if (most > -INFINITY) base = most, limit = kSlack;
+      // The first base is the score of the first key, unless that is infinite: scores of a magnitude that leaves no digits for their differences are
+      // then rounded only once the base is taken off.
+      float more = 0.f;
+      if constexpr (BIAS) more = -slope * fabsf(at - lds_pos[now][0]);
+      const float z = __shfl(fmaf(s[0][0], p.z_mul, more), col, 64);
+      if (fabsf(z) < INFINITY) base = z, limit = kSlack;
     }
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
@@ -346,8 +338,11 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   p.scale = a->scale;
   const float scale = std::fabs(a->scale);
   p.negate = a->scale < 0.f;
-  p.z_mul = (a->cap > 0.f ? a->cap : std::max(scale, 1e-30f)) * kLog2e;
+  p.z_mul = std::max(scale, 1e-30f) * kLog2e;
   p.t_mul = a->cap > 0.f ? scale / a->cap : 0.f;
+  p.t_inv = p.t_mul > 0.f ? 1.f / p.t_mul : 0.f;
+  double power = 1.0;
+  for (int i = 0; i < 4; ++i) p.tanh_c[i] = float(kTanh[i] * (power *= double(p.t_mul) * p.t_mul));
   p.per_token = divisor(uint32_t(p.group));
   while (16 % p.group == 0 && (1 << p.log2_fold) < p.group) ++p.log2_fold;
   p.slopes = a->slopes;

@@ -209,7 +209,7 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
               sums[h] += floatx4{e, e * dp, e * far[i], e * dp * far[i]};
             }
             float u = e * (dp - x.delta[h]);
-            if constexpr (CAP) u *= 1.f - t * t;
+            u = through_cap<CAP>(p, u, t);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
               dq[h][j] += u * float(kf[i][j]);
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
           const float t = capped<CAP>(p, sum_of_lanes<L>(dot8<T>(kf, x.q[h])));
           const float e = exp2_fast(fmaf(t, p.z_mul, BIAS ? fmaf(-x.slope[h], fabsf(x.at - far), -x.lse[h]) : -x.lse[h]));
           float u = e * (sum_of_lanes<L>(dot8<T>(vf, x.g[h])) - x.delta[h]);
-          if constexpr (CAP) u *= 1.f - t * t;
+          u = through_cap<CAP>(p, u, t);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
             dk[j] += u * back * x.q[h][j];

@@ -103,6 +103,11 @@ def _like(t, shape, name: str, dtype, index: int):
     return t if t.data_ptr() % 16 == 0 else t.clone()
 
 
+def _new(t):
+    """A tensor like t, rows end to end."""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 class Documents:
     """Which rows of queries and of keys belong together.  Document d owns rows offsets[d] .. offsets[d + 1] (int32[n + 1], the first 0, the last
     the number of rows); the first lens[d] of them hold tokens (None: all).  q_pos and k_pos (int32, by row) are needed where scores fall
@@ -157,8 +162,8 @@ def attend(q, k, v, docs: Documents, slopes=None, cap: float = 0.0, scale: float
     d, a = _attention(q, k, v, docs, slopes, cap, scale)
     device = q.device
     with _on(docs.index, stream) as on:
-        out = torch.empty(q.shape, dtype=q.dtype, device=device)
-        left = torch.empty_like(out) if rest else None
+        out = _new(q)
+        left = _new(q) if rest else None
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=device)
         st = L.lgp_attend(docs.index, d, a, out.data_ptr(), _ptr(left), lse.data_ptr(), 0, 0, on)
         if st == _ECAPACITY:                    # nothing was launched: few calls want a workspace
@@ -177,7 +182,7 @@ def attend_backward(d_out, q, k, v, out, lse, docs: Documents, rest=None, slopes
         d_out, out = _like(d_out, q.shape, "d_out", q.dtype, index), _like(out, q.shape, "out", q.dtype, index)
         rest = None if rest is None else _like(rest, q.shape, "rest", q.dtype, index)
         lse = _like(lse, q.shape[:2], "lse", torch.float32, index)
-        dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v))
+        dq, dk, dv = _new(q), _new(k), _new(v)
         d_slopes = None if slopes is None else torch.empty_like(slopes)
         w, size = _workspace(index, dev, L.lgp_attend_workspace, d, a, 1)
         _ok(L.lgp_attend_backward(index, d, a, d_out.data_ptr(), out.data_ptr(), _ptr(rest), lse.data_ptr(), dq.data_ptr(),
@@ -225,9 +230,8 @@ def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-
     Rows of a negative pos have no token and become zeros; those of a position beyond the table become NaN."""
     L = load_library()
     index, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
-    dev = q.device
     with _on(index, stream) as on:
-        q_out, k_out = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
+        q_out, k_out = _new(q), _new(k)
         _ok(L.lgp_norm_rotate(index, h, q_out.data_ptr(), k_out.data_ptr(), on))
     return q_out, k_out
 
@@ -239,7 +243,7 @@ def norm_rotate_backward(dq_out, dk_out, q, k, q_weight, k_weight, pos=None, tab
     dev = q.device
     with _on(index, stream) as on:
         dq_out, dk_out = _like(dq_out, q.shape, "dq_out", q.dtype, index), _like(dk_out, k.shape, "dk_out", k.dtype, index)
-        dq, dk = torch.empty(q.shape, dtype=q.dtype, device=dev), torch.empty(k.shape, dtype=k.dtype, device=dev)
+        dq, dk = _new(q), _new(k)
         dqw, dkw = torch.empty_like(q_weight), torch.empty_like(k_weight)
         w, size = _workspace(index, dev, L.lgp_norm_rotate_workspace, h)
         _ok(L.lgp_norm_rotate_backward(index, h, dq_out.data_ptr(), dk_out.data_ptr(), dq.data_ptr(), dk.data_ptr(), dqw.data_ptr(),
