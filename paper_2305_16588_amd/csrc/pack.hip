@@ -2,6 +2,7 @@
 #include "layer_dev.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace lgp {
 namespace layer {
@@ -142,11 +143,11 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
   const Places<T, WT> at_x(lane);
 
   vec8<T> held[DMA ? 1 : NJ];
-  auto fetch = [&](int32_t i) {
+  auto fetch = [&](int32_t i, int to) {
     if (i >= tiles) return;
     const int32_t t0 = i * kTokens;
     if constexpr (DMA) {
-      copy_tile<T, NT, kTokens, 512>(lds_y[i % 3], Rows<T>{dy, p.dy_row, 0, 0}, t0, p.out - n0, tokens - t0, tid);
+      copy_tile<T, NT, kTokens, 512>(lds_y[to], Rows<T>{dy, p.dy_row, 0, 0}, t0, p.out - n0, tokens - t0, tid);
     } else {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
@@ -165,15 +166,15 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
       const int r = tid / (WT / 16), c = tid % (WT / 16);
       if (w0 + 16 * c < p.pitch)
         copy16(values + int64_t(t0) * p.pitch, uint32_t(min(r, tokens - 1 - t0)) * p.pitch + 16 * c,
-               __builtin_amdgcn_readfirstlane(lds_address(lds_raw[i % 3]) + (tid & ~63) * 16));
+               __builtin_amdgcn_readfirstlane(lds_address(lds_raw[to]) + (tid & ~63) * 16));
     }
   };
-  auto arrived = [&](int32_t i) {        // in this wave: passed on by the next barrier
+  auto arrived = [&](int32_t i, int at) {        // in this wave: passed on by the next barrier
     loads_done();
     if constexpr (!DMA) {
       if (i < tiles)
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) *reinterpret_cast<vec8<T>*>(lds_y[i % 3] + chunk_at<NT>(yr + j * (512 / NC), yc)) = held[j];
+        for (int j = 0; j < NJ; ++j) *reinterpret_cast<vec8<T>*>(lds_y[at] + chunk_at<NT>(yr + j * (512 / NC), yc)) = held[j];
     }
   };
   // Exponents of the four groups and the presence of each of the next kAhead tokens, a thread a token.
@@ -197,22 +198,22 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
       lds_gone[block & 1][tid] = pos < 0;
     }
   };
-  auto ready = [&](int32_t i) {
+  auto ready = [&](int32_t i, int at, int to) {
     if (i >= tiles) return;
     const int block = i / (kAhead / kTokens) & 1, t0 = i % (kAhead / kTokens) * kTokens;
     {
       const int r = tid / (WT / 8), c = tid % (WT / 8);
-      const uint64_t x = *reinterpret_cast<const uint64_t*>(lds_raw[i % 3] + r * WT + 8 * c);
+      const uint64_t x = *reinterpret_cast<const uint64_t*>(lds_raw[at] + r * WT + 8 * c) ^ 0x8080808080808080ull;       // plus 128: bytes without a sign
       const float step = lds_gone[block][t0 + r] ? 0.f : power_of(lds_exps[block][t0 + r] >> (8 * (c / 4)) & 255);
       vec8<T> v;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = T(float(int8_t(x >> (8 * k))) * step);
-      *reinterpret_cast<vec8<T>*>(lds_x[i & 1] + chunk_at<WT>(r, c)) = v;
+      for (int k = 0; k < 8; ++k) v[k] = T(fmaf(float(uint8_t(x >> (8 * k))), step, -128.f * step));
+      *reinterpret_cast<vec8<T>*>(lds_x[to] + chunk_at<WT>(r, c)) = v;
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const int r = yr + j * (512 / NC);
-      vec8<T>* y = reinterpret_cast<vec8<T>*>(lds_y[i % 3] + chunk_at<NT>(r, yc));
+      vec8<T>* y = reinterpret_cast<vec8<T>*>(lds_y[at] + chunk_at<NT>(r, yc));
       if (lds_gone[block][t0 + r]) {
         const vec8<T> zero = {};
         *y = zero;
@@ -225,33 +226,41 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
   };
   if (tiles > 0) {
     look(0);
-    fetch(0);
+    fetch(0, 0);
     note(0);
-    arrived(0);
+    arrived(0, 0);
     __syncthreads();
-    fetch(1);
-    ready(0);
+    fetch(1, 1);
+    ready(0, 0, 0);
   }
-  for (int32_t i = 0; i < tiles; ++i) {
-    constexpr int kEach = kAhead / kTokens;
+  auto step = [&](int32_t i, auto of_six) {
+    constexpr int y_at = decltype(of_six)::value % 3, x_at = decltype(of_six)::value % 2, kEach = kAhead / kTokens;
     if (i % kEach == kEach / 2) note(i / kEach + 1);
-    arrived(i + 1);
+    arrived(i + 1, (y_at + 1) % 3);
     __syncthreads();
     if (i % kEach == 0) look(i / kEach + 1);
-    fetch(i + 2);
-    ready(i + 1);
-#pragma unroll 1
+    fetch(i + 2, (y_at + 2) % 3);
+    ready(i + 1, (y_at + 1) % 3, x_at ^ 1);
+#pragma unroll
     for (int s = 0; s < kTokens / 16; ++s) {
       vec8<T> a[NB], b[2];
 #pragma unroll
-      for (int k = 0; k < NB; ++k) a[k] = at_y.across(lds_y[i % 3], 16 * s, NT / 4 * (wave >> 1) + 32 * k);
+      for (int k = 0; k < NB; ++k) a[k] = at_y.across(lds_y[y_at], 16 * s, NT / 4 * (wave >> 1) + 32 * k);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) b[k] = at_x.across(lds_x[i & 1], 16 * s, 64 * (wave & 1) + 32 * k);
+      for (int k = 0; k < 2; ++k) b[k] = at_x.across(lds_x[x_at], 16 * s, 64 * (wave & 1) + 32 * k);
 #pragma unroll
       for (int k = 0; k < NB; ++k)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[k][j] = Elem<T>::mfma(a[k], b[j], acc[k][j]);
     }
+  };
+  for (int32_t i = 0; i < tiles; i += 6) {       // places of tiles are constants in each of six copies
+    step(i, std::integral_constant<int, 0>());
+    if (i + 1 < tiles) step(i + 1, std::integral_constant<int, 1>());
+    if (i + 2 < tiles) step(i + 2, std::integral_constant<int, 2>());
+    if (i + 3 < tiles) step(i + 3, std::integral_constant<int, 3>());
+    if (i + 4 < tiles) step(i + 4, std::integral_constant<int, 4>());
+    if (i + 5 < tiles) step(i + 5, std::integral_constant<int, 5>());
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i)
