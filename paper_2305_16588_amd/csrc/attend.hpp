@@ -108,6 +108,9 @@ template <> inline constexpr float kLift<f16> = 4096.f;
 template <typename T> constexpr float kLiftLog2 = 0.f;
 template <> inline constexpr float kLiftLog2<f16> = 12.f;
 
+// Waves per SIMD that the kernels' registers are to leave room for: as many as their tiles in LDS do.
+constexpr int waves_per_simd(int dim, int waves) { return dim == 32 ? 4 : dim == 64 ? (waves == 1 ? 2 : 3) : waves == 1 ? 1 : 2; }
+
 // Launch shapes, chosen on the host by what it knows: rows and documents.
 // Whether a workgroup is one wave of 32 rows, which waits for no other but has its tiles to itself: documents of up to 32 rows, and with heads of up
 // to 32, whose tiles are small, of up to 320 (1024 documents of 276 rows, half of them with tokens, heads of 32: forward 295 us with four waves, 281

@@ -16,7 +16,7 @@ namespace {
 //     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|) / sum_j P) / sum_j P,
 // whose four sums per row go to `sums`: so it depends neither on how out was rounded nor on the rounding of lse.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 2) void attend_dq_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
   __shared__ __align__(16) T lds_k[2][BN * D];
   __shared__ __align__(16) T lds_v[2][BN * D];
@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
 
 // Gradient of the slopes from the sums of all rows, in two steps of a fixed order: kSlopeThreads threads take rows a multiple of the number of
 // heads apart, so that each adds up for one head, then a workgroup adds up what is there of a head.
-constexpr int64_t kSlopeThreads = 65536;
+constexpr int64_t kSlopeThreads = 131072;
 __global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, float* partial) {
   const int64_t rows = int64_t(p.qs.rows) * p.heads, each = kSlopeThreads / p.heads * p.heads, at = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (at >= each) return;
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(256) void slopes_end_kernel(const float* partial, i
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
-__global__ __launch_bounds__(64 * NW, NW == 1 ? 1 : D == 32 ? 4 : D == 64 ? 3 : 2) void attend_dkv_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
   __shared__ __align__(16) T lds_q[2][BQ * D];
   __shared__ __align__(16) T lds_g[2][BQ * D];

@@ -19,7 +19,7 @@ namespace {
 // and their results are joined in LDS.
 constexpr float kSlack = 8.f;
 template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
-__global__ __launch_bounds__(64 * NW * KW, NW == 1 ? 1 : 2) void attend_kernel(const AttendParams p) {
+__global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;          // threads that share tiles; rows of a workgroup
   __shared__ __align__(16) T lds_tiles[KW][2][2][BN * D];     // of keys and values, two places each
   __shared__ __align__(16) float lds_at[KW][2][BIAS ? BN : 4];
