@@ -67,7 +67,7 @@ template <int D> __device__ __forceinline__ int chunk_at(int row, int chunk) { r
 // next read of LDS, whichever tile that reads, so it is not told: what arrives may be read when the wave's loads are done (loads_done) and
 // a barrier was passed.
 __device__ __forceinline__ void copy16(const void* from, uint32_t offset, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");       // m0 is never held across statements
 }
 template <typename T> __device__ __forceinline__ const T* in_all_lanes(const T* p) {
   const uint64_t x = reinterpret_cast<uint64_t>(p);

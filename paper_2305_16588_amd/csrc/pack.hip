@@ -313,7 +313,7 @@ template <typename T> void launch_grad(const GradParams& p, int32_t rows, uint32
 int check_packed(const lgp_packed* a) {
   if (!a || a->tokens < 0 || a->width < 1) return LGP_EINVAL;
   if (a->dtype != LGP_F32 && a->dtype != LGP_F16 && a->dtype != LGP_BF16) return LGP_EUNSUPPORTED;
-  if (a->width > (1 << 20) || a->tokens >= (int64_t(1) << 40)) return LGP_EUNSUPPORTED;
+  if (a->width > (1 << 20) || a->tokens >= int64_t(1) << 31) return LGP_EUNSUPPORTED;
   if (a->tokens && (!a->values || !a->exps)) return LGP_EINVAL;
   return aligned16(a->values) ? LGP_OK : LGP_EINVAL;
 }
