@@ -117,6 +117,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
       }
       const int32_t there = k0 + BN <= k_end ? BN : k_end - k0 - 32 * b - 4 * half;      // places of this block's half that are keys
       cap<CAP>(p, s);
+      floatx4 of_tile = {};             // sums of sums: a lane's 16 scores first, for the digits of long ones
       vec8<T> uf[2];
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
@@ -130,15 +131,21 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
           const float z = fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope, far, -lse) : -lse);
           const float e = WHOLE || 8 * r4 + i < there ? exp2_fast(z) : 0.f, pd = e * g[r];
           if constexpr (BIAS) {
-            sum_p += e;
-            sum_pd += pd;
-            sum_pf = fmaf(e, far, sum_pf);
-            sum_pdf = fmaf(pd, far, sum_pdf);
+            of_tile[0] += e;
+            of_tile[1] += pd;
+            of_tile[2] = fmaf(e, far, of_tile[2]);
+            of_tile[3] = fmaf(pd, far, of_tile[3]);
           }
           float u = fmaf(-e, delta, pd);
           u = through_cap<CAP>(p, u, s[r]);
           uf[r / 8][r % 8] = T(u);
         }
+      }
+      if constexpr (BIAS) {
+        sum_p += of_tile[0];
+        sum_pd += of_tile[1];
+        sum_pf += of_tile[2];
+        sum_pdf += of_tile[3];
       }
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
