@@ -14,8 +14,7 @@ namespace {
 // Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
 // delta is taken from out and what its rounding took off.  The slope of a head has the gradient
 //     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|) / sum_j P) / sum_j P,
-// whose four sums per row go to `sums`: so it depends neither on how out was rounded nor on the rounding of lse.  Distances are taken relative to
-// that of the document's middle key, which changes nothing of this but the digits that the difference loses where most keys are as far.
+// whose four sums per row go to `sums`: so it depends neither on how out was rounded nor on the rounding of lse.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
 __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
@@ -83,15 +82,13 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
   }
   delta += other_half(delta);
   float lse = INFINITY;           // no probability where there is no token or no key
-  float slope = 0.f, at = 0.f, mid = 0.f;
+  float slope = 0.f, at = 0.f;
   if (live) {
     lse = p.lse_in[at_out] * kLog2e;
     if (lse == -INFINITY) lse = INFINITY;
     if constexpr (BIAS) {
       slope = p.slopes[head] * kLog2e;
       at = float(p.qs.pos[token]);
-      if (kd.tokens > 0) mid = fabsf(at - float(p.ks.pos[kd.begin + kd.tokens / 2]));
-      lse += slope * mid;
     }
     if (split == 0 && half == 0) p.delta[at_out] = delta;
   }
@@ -130,7 +127,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
           float far = 0.f;
-          if constexpr (BIAS) far = fabsf(at - kpos[i]) - mid;
+          if constexpr (BIAS) far = fabsf(at - kpos[i]);
           const float z = fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope, far, -lse) : -lse);
           const float e = WHOLE || 8 * r4 + i < there ? exp2_fast(z) : 0.f, pd = e * g[r];
           if constexpr (BIAS) {

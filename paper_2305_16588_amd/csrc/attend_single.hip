@@ -185,12 +185,6 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
     if (live) {
       Query<T, L, G, BIAS> x;
       x.load(p, a, token);
-      float mid = 0.f;             // distances relative to that of the middle key: see attend_dq_kernel
-      if constexpr (BIAS) {
-        if (kd.tokens > 0) mid = fabsf(x.at - float(p.ks.pos[kd.begin + kd.tokens / 2]));
-#pragma unroll
-        for (int h = 0; h < G; ++h) x.lse[h] += x.slope[h] * mid;
-      }
       for (int32_t k0 = 0; k0 < kd.tokens; k0 += kSteps * a.keys_at_once) {
         vec8<T> kf[kSteps], vf[kSteps];
         float far[kSteps] = {};
@@ -201,7 +195,7 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
           const int64_t key_row = int64_t(kd.begin) + key;
           kf[i] = load8(kp + key_row * p.k_row, there, false);
           vf[i] = load8(vp + key_row * p.v_row, there, false);
-          if constexpr (BIAS) far[i] = there ? fabsf(x.at - float(p.ks.pos[key_row])) - mid : 0.f;
+          if constexpr (BIAS) far[i] = there ? fabsf(x.at - float(p.ks.pos[key_row])) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
