@@ -13,8 +13,8 @@ namespace {
 //     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
 // Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
 // delta is taken from out and what its rounding took off.  The slope of a head has the gradient
-//     - sum dS |distance| = - sum_rows (sum_j P dP |distance| - (sum_j P dP) (sum_j P |distance|) / sum_j P) / sum_j P,
-// whose four sums per row go to `sums`: so it depends neither on how out was rounded nor on the rounding of lse.
+//     - sum dS |distance| = - sum_rows (sum_j dS |distance| - (sum_j dS) (sum_j P |distance|) / sum_j P) / sum_j P,
+// whose four sums per row go to `sums`: the second term is what the rounding of out and of lse left in dS, so the gradient depends on neither.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
 __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
   constexpr int kThreads = 64 * NW, kRows = 32 * NW;
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
   }
 
   floatx16 dq[D / 32] = {};
-  float sum_p = 0.f, sum_pd = 0.f, sum_pf = 0.f, sum_pdf = 0.f;
+  float sum_p = 0.f, sum_s = 0.f, sum_pf = 0.f, sum_sf = 0.f;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, int now, auto whole) {
@@ -130,22 +130,22 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
           if constexpr (BIAS) far = fabsf(at - kpos[i]);
           const float z = fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope, far, -lse) : -lse);
           const float e = WHOLE || 8 * r4 + i < there ? exp2_fast(z) : 0.f, pd = e * g[r];
+          float u = fmaf(-e, delta, pd);
           if constexpr (BIAS) {
             of_tile[0] += e;
-            of_tile[1] += pd;
+            of_tile[1] += u;
             of_tile[2] = fmaf(e, far, of_tile[2]);
-            of_tile[3] = fmaf(pd, far, of_tile[3]);
+            of_tile[3] = fmaf(u, far, of_tile[3]);
           }
-          float u = fmaf(-e, delta, pd);
           u = through_cap<CAP>(p, u, s[r]);
           uf[r / 8][r % 8] = T(u);
         }
       }
       if constexpr (BIAS) {
         sum_p += of_tile[0];
-        sum_pd += of_tile[1];
+        sum_s += of_tile[1];
         sum_pf += of_tile[2];
-        sum_pdf += of_tile[3];
+        sum_sf += of_tile[3];
       }
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
@@ -163,10 +163,10 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
   if (row >= qd.owned * p.group) return;
   if constexpr (BIAS) {
     sum_p += other_half(sum_p);
-    sum_pd += other_half(sum_pd);
+    sum_s += other_half(sum_s);
     sum_pf += other_half(sum_pf);
-    sum_pdf += other_half(sum_pdf);
-    if (p.sums && half == 0) p.sums[int64_t(split) * p.qs.rows * p.heads + at_out] = live ? floatx4{sum_p, sum_pd, sum_pf, sum_pdf} : floatx4{};
+    sum_sf += other_half(sum_sf);
+    if (p.sums && half == 0) p.sums[int64_t(split) * p.qs.rows * p.heads + at_out] = live ? floatx4{sum_p, sum_s, sum_pf, sum_sf} : floatx4{};
   }
   float* part = p.splits > 1 ? p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim : nullptr;
   T* out = static_cast<T*>(p.dq) + at_out * p.dim;

@@ -205,10 +205,8 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
           for (int h = 0; h < G; ++h) {
             const float t = capped<CAP>(p, sum_of_lanes<L>(dot8<T>(kf[i], x.q[h]))), z = fmaf(t, p.z_mul, BIAS ? fmaf(-x.slope[h], far[i], -x.lse[h]) : -x.lse[h]);
             const float e = key < kd.tokens ? exp2_fast(z) : 0.f, dp = sum_of_lanes<L>(dot8<T>(vf[i], x.g[h]));
-            if constexpr (BIAS) {
-              sums[h] += floatx4{e, e * dp, e * far[i], e * dp * far[i]};
-            }
             float u = e * (dp - x.delta[h]);
+            if constexpr (BIAS) sums[h] += floatx4{e, u, e * far[i], u * far[i]};
             u = through_cap<CAP>(p, u, t);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
