@@ -47,7 +47,6 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
     for (int i = 0; i < 4; ++i) u.w[i] ^= 0x80008000u;
   return u.v;
 }
-template <typename T> __device__ __forceinline__ vec8<T> zero8() { vec8<T> z = {}; return z; }
 
 // The cap: a product qk becomes tanh(x) / t_mul with x = qk * t_mul, which is qk where the cap is far.  Up to x = kNear that is
 // qk (1 + c0 x^2 + c1 x^4 + c2 x^6 + c3 x^8), fitted by least squares of the relative error, reweighted until even: 1e-7 with its roundings, and it

