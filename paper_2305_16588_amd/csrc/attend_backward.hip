@@ -205,32 +205,36 @@ __global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
 }
 
 // Gradient of the slopes from the sums of all rows, in two steps of a fixed order: kSlopeThreads threads take rows a multiple of the number of
-// heads apart, so that each adds up for one head, then a workgroup adds up what is there of a head.  Measured: 282 624 rows
-// of 8 heads, 9 us each.
+// heads apart, so that each adds up for one head, then a workgroup adds up what is there of a head.  Rows may cancel down to a small part of
+// what one of them has, so they are added in 64 bits.  Measured: 282 624 rows of 8 heads, 9 and 5 us.
 constexpr int64_t kSlopeThreads = 131072;
-__global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, float* partial) {
+__global__ __launch_bounds__(256) void slopes_kernel(const AttendParams p, double* partial) {
   const int64_t rows = int64_t(p.qs.rows) * p.heads, each = kSlopeThreads / p.heads * p.heads, at = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (at >= each) return;
-  float x = 0.f;
+  double x = 0.;
   for (int64_t r = at; r < rows; r += each) {
     floatx4 m = {};
     for (int32_t s = 0; s < p.splits; ++s) m += p.sums[s * rows + r];
     const float inv = m[0] != 0.f ? 1.f / m[0] : 0.f;
-    x -= (m[3] - m[1] * m[2] * inv) * inv;
+    x -= double((m[3] - m[1] * m[2] * inv) * inv);
   }
-  partial[at] = x;
+  partial[at % p.heads * (each / p.heads) + at / p.heads] = x;       // of a head side by side
 }
-__global__ __launch_bounds__(256) void slopes_end_kernel(const float* partial, int32_t heads, float* out) {
-  __shared__ float lds[4];
+constexpr int kEndThreads = 1024;
+__global__ __launch_bounds__(kEndThreads) void slopes_end_kernel(const double* partial, int32_t heads, float* out) {
+  __shared__ double lds[kEndThreads / 64];
   const int32_t each = int32_t(kSlopeThreads) / heads;
-  float x = 0.f;
+  double x = 0.;
 #pragma unroll 8
-  for (int32_t i = threadIdx.x; i < each; i += 256) x += partial[int64_t(i) * heads + blockIdx.x];
+  for (int32_t i = threadIdx.x; i < each; i += kEndThreads) x += partial[int64_t(blockIdx.x) * each + i];
 #pragma unroll
   for (int d = 32; d; d >>= 1) x += __shfl_xor(x, d, 64);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = x;
   __syncthreads();
-  if (threadIdx.x == 0) out[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
+  if (threadIdx.x) return;
+#pragma unroll
+  for (int k = 1; k < kEndThreads / 64; ++k) x += lds[k];
+  out[blockIdx.x] = float(x);
 }
 
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
@@ -416,7 +420,7 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
   b.delta = 0;
   b.sums = up(rows);
   b.partial = b.sums + (a->slopes ? rows * 4 * b.q.splits : 0);
-  b.parts = b.partial + (a->slopes ? size_t(kSlopeThreads) : 0);
+  b.parts = b.partial + (a->slopes ? 2 * size_t(kSlopeThreads) : 0);
   b.bytes = (b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0)) * sizeof(float);
   return b;
 }
@@ -502,8 +506,9 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
   else if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
   else launch<bf16>(p, b, att->cap > 0.f, s);
   if (d_slopes) {
-    slopes_kernel<<<kSlopeThreads / 256, 256, 0, s>>>(p, w + b.partial);
-    slopes_end_kernel<<<att->heads, 256, 0, s>>>(w + b.partial, att->heads, d_slopes);
+    double* partial = reinterpret_cast<double*>(w + b.partial);      // after the sums, so aligned to 16 bytes like them
+    slopes_kernel<<<kSlopeThreads / 256, 256, 0, s>>>(p, partial);
+    slopes_end_kernel<<<att->heads, kEndThreads, 0, s>>>(partial, att->heads, d_slopes);
   }
   return launched();
 }
