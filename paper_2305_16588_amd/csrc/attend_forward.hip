@@ -142,15 +142,17 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
       for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
     most = fmaxf(most, other_half(most));
     if (__any(most > limit)) {
+      // A row that has no base yet has nothing either, and 2^-by is inf where its first score is far below zero.  The row's state decides, not its sum:
+      // a lane's sum is that of half of the keys so far, while its results are those of all.
       const bool raise = most > limit;
-      const float raised = base + most, by = raise ? raised - base : 0.f, shrink = raise ? exp2_fast(-by) : 1.f;
+      const float raised = base + most, by = raise ? raised - base : 0.f, shrink = raise && limit == kSlack ? exp2_fast(-by) : 1.f;
       base = raise ? raised : base;
       limit = raise ? kSlack : limit;
-      sum = sum > 0.f ? sum * shrink : sum;          // a first score far below the base of zero has nothing to shrink, and 2^-most is inf
+      sum *= shrink;
 #pragma unroll
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[db][r] = sum == 0.f ? 0.f : o[db][r] * shrink;
+        for (int r = 0; r < 16; ++r) o[db][r] *= shrink;
 #pragma unroll
       for (int b = 0; b < BN / 32; ++b)
 #pragma unroll

@@ -1,0 +1,66 @@
+"""Operators of a model layer at the ends of their ranges, against their definitions in 64 bits (tests/layer_common.py)."""
+import math
+
+import pytest
+import torch
+
+import layer_common as ref
+from test_gpu_9_layer import BF16, F16, draw, lgp, make_docs
+
+pytestmark = pytest.mark.gpu
+
+
+def alone(q, k, v, info, keep, **kw):
+    """The definition over the keys that `keep` marks: the others have no weight at all, so the documents are as if they did not hold them."""
+    at = torch.cat([torch.zeros(1, dtype=torch.long), keep.cpu().long().cumsum(0)])
+    spans = [(qo, qn, int(at[ko]), int(at[ko + kn] - at[ko])) for qo, qn, ko, kn in info["spans"]]
+    return ref.attention(q, k[keep], v[keep], dict(spans=spans, q_pos=info["q_pos"], k_pos=info["k_pos"][keep]), **kw)
+
+
+# lengths that choose four waves of rows, four waves of keys, and one wave by itself; three tiles of keys and more each
+SHAPES = [([300], [333]), ([20, 9], [200, 150]), ([40] * 5, [50] * 5)]
+
+
+@pytest.mark.parametrize("q_owned,k_owned", SHAPES)
+@pytest.mark.parametrize("dtype,dim", [(BF16, 32), (F16, 64), (BF16, 128)])
+@pytest.mark.parametrize("nats", [60, 100, 300])
+def test_scores_that_spread_widely(nats, dtype, dim, q_owned, k_owned):
+    """Most keys of a row weigh nothing, and rows find their largest score in different tiles.  Probabilities below 2^-126 are zeros."""
+    L = lgp()
+    docs, info = make_docs(q_owned, k_owned)
+    Tq, Tk = sum(q_owned), sum(k_owned)
+    for heads, bias in ((2, False), (4, True)):
+        q, k, v, g = (draw((t, h, dim), dtype, 1 + i, nats ** 0.5 if i < 2 else 1.0) for i, (t, h) in enumerate(((Tq, heads), (Tk, 2), (Tk, 2), (Tq, heads))))
+        slopes = torch.linspace(0.05, 0.6, heads, device="cuda") if bias else None
+        out, lse, rest = L.attend(q, k, v, docs, slopes=slopes, rest=True)
+        got = L.attend_backward(g, q, k, v, out, lse, docs, rest=rest, slopes=slopes)
+        want = ref.attention(q, k, v, info, g, slopes)
+        for x, name in zip((out, lse, *got[:3]), ("out", "lse", "dq", "dk", "dv")):
+            value, bound = want[name]
+            ref.check(x, (value, bound + 2.0 ** -110), name)
+
+
+@pytest.mark.parametrize("half", [0, 1])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("q_rows,keys,late", [(70, 128, 100), (20, 400, 100), (20, 60, 50)])
+def test_keys_that_weigh_nothing_in_every_other_four(q_rows, keys, late, dtype, half):
+    """Four of eight keys lie 150 below the others, or have a score of -inf; one of a later tile is above all, so that some rows take a new base and
+    all of them keep what they have."""
+    L = lgp()
+    at = torch.arange(keys, device="cuda")
+    near = (at % 8 // 4 == half) & (at < late // 2)
+    for low in (-150.0, -math.inf):
+        score = torch.where(near, 5.40625, low)
+        if half == 0:
+            score[0] = 0.0                                     # the first base: the others are not far enough above for another
+        score[late] = 5.8125 if half == 0 else 12.0
+        q, k = torch.zeros((q_rows, 2, 64), device="cuda", dtype=dtype), torch.zeros((keys, 2, 64), device="cuda", dtype=dtype)
+        q[:, :, 0] = 8.0
+        q[1::2, :, 0] = 4.0                                    # in these rows the late key is not far above
+        k[:, :, 0] = score[:, None].to(dtype)
+        v = draw((keys, 2, 64), dtype, 3)
+        docs, info = make_docs([q_rows], [keys])
+        out, lse, _ = L.attend(q, k, v, docs, scale=0.125)
+        want = alone(q, k, v, info, score > -math.inf, scale=0.125)
+        ref.check(out, want["out"], f"out, {low}")
+        ref.check(lse, want["lse"], f"lse, {low}")
