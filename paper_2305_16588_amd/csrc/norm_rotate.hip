@@ -164,7 +164,9 @@ __global__ __launch_bounds__(256) void norm_rotate_backward_kernel(const NormPar
           float sum = 0.f, dot = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) sum += x[j][i] * x[j][i];
-          const float r = 1.f / sqrtf(sum_of_lanes<L>(sum) / float(p.dim) + p.eps);
+          // no norm where there is no head or no token: with an eps of zero it would be infinite, and its product with their zeros NaN
+          sum = sum_of_lanes<L>(sum);
+          const float r = live && h < heads ? 1.f / sqrtf(sum / float(p.dim) + p.eps) : 0.f;
           if (p.rot) turn(g[j]);
           if (live && !known && h < heads)
 #pragma unroll

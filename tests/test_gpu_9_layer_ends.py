@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import layer_common as ref
-from test_gpu_9_layer import BF16, F16, draw, lgp, make_docs
+from test_gpu_9_layer import BF16, F16, F32, draw, lgp, make_docs
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,24 @@ def test_keys_that_weigh_nothing_in_every_other_four(q_rows, keys, late, dtype, 
         want = alone(q, k, v, info, score > -math.inf, scale=0.125)
         ref.check(out, want["out"], f"out, {low}")
         ref.check(lse, want["lse"], f"lse, {low}")
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("tokens,heads,kv_heads,dim", [(1, 1, 1, 64), (5, 3, 1, 32), (1001, 5, 2, 128), (257, 1, 3, 40)])
+def test_head_norms_without_eps(tokens, heads, kv_heads, dim, dtype):
+    """Neither rows without a token nor places beyond the heads or the tokens are divided by a norm of zero."""
+    L = lgp()
+    q, k = draw((tokens, heads, dim), dtype, 1), draw((tokens, kv_heads, dim), dtype, 2)
+    gq, gk = draw(q.shape, dtype, 3), draw(k.shape, dtype, 4)
+    w = draw((dim,), F32, 5)
+    pos, table = torch.arange(tokens, device="cuda", dtype=torch.int32), L.rotation_table(2000, 32)
+    pos[1::3] = -1
+    live = pos >= 0
+    out = L.norm_rotate(q, k, w, w, pos, table, eps=0.0)
+    back = L.norm_rotate_backward(gq, gk, q, k, w, w, pos, table, eps=0.0)
+    for i, (x, g) in enumerate(((q, gq), (k, gk))):
+        want = ref.head_norm(x[live], w, pos[live], table, 0.0, g[live])
+        ref.check(out[i][live], want["out"], "out")
+        ref.check(back[i][live], want["dx"], "dx")
+        ref.check(back[2 + i], want["dw"], "dw")
+        assert (out[i][~live] == 0).all() and (back[i][~live] == 0).all()
