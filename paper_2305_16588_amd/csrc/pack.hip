@@ -211,7 +211,7 @@ __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p)
       const float step = lds_gone[block][t0 + r] ? 0.f : power_of(lds_exps[block][t0 + r] >> (8 * (c / 4)) & 255);
       vec8<T> v;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = T(fmaf(float(uint8_t(x >> (8 * k))), step, -128.f * step));
+      for (int k = 0; k < 8; ++k) v[k] = T((float(uint8_t(x >> (8 * k))) - 128.f) * step);        // not less 128 steps: those may be infinite
       *reinterpret_cast<vec8<T>*>(lds_x[to] + chunk_at<WT>(r, c)) = v;
     }
 #pragma unroll

@@ -85,3 +85,17 @@ def test_head_norms_without_eps(tokens, heads, kv_heads, dim, dtype):
         ref.check(back[i][live], want["dx"], "dx")
         ref.check(back[2 + i], want["dw"], "dw")
         assert (out[i][~live] == 0).all() and (back[i][~live] == 0).all()
+
+
+@pytest.mark.parametrize("x_dtype", [BF16, F32])
+def test_weight_gradient_of_the_largest_activations(x_dtype):
+    L = lgp()
+    x = draw((70, 96), F32, 1)
+    x[3, 32:64] *= 2.0 ** 126
+    x[5, 0], x[6, 95] = torch.finfo(x_dtype).max, -torch.finfo(x_dtype).max
+    dy = draw((70, 40), F32, 2, 2.0 ** -20).bfloat16()
+    p = L.pack_activations(x.to(x_dtype))
+    dw, _ = L.packed_weight_grad(p, dy)
+    X, Y = L.unpack_activations(p).double(), dy.double()
+    assert torch.isfinite(X).all()
+    ref.check(dw, (Y.T @ X, 2.0 ** -24 * 72 * Y.abs().T @ X.abs()), "dw")
