@@ -12,7 +12,8 @@ namespace {
 // need one exchange between the halves of the wave, and the rounded probabilities are the operand of O^T = V^T P^T as they stand
 // (layer_dev.hpp).  NW waves share the tiles of keys and values in LDS, where the next tile arrives while this one is worked on.  D is the
 // head's dimension rounded up to 32, 64 or 128, with zeros.  Scores are taken against a base that is raised, and sums and results shrunk, only
-// when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.  The
+// when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.  The base is
+// settled before anything is taken off: a difference from a base that a tile leaves far behind would be rounded at the size of that distance.  The
 // two places of a tile are two copies of the loop's body, so that no address is computed in it.
 // Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
 // Where a document has no more rows than a wave (NW 1), KW waves have the same rows and every KW-th tile of the keys each, in tiles of their own,
@@ -88,6 +89,8 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
   float base = 0.f, limit = -3e38f, sum = 0.f;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
+  // How far a score is above x, rounded once: without a bias from the product.
+  auto above = [&](float score, float x) { return BIAS ? score - x : fmaf(score, p.z_mul, -x); };
   auto step = [&](int32_t k0, auto stage_now) {
     constexpr int now = decltype(stage_now)::value;
     if constexpr (BIAS) {
@@ -108,25 +111,15 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
       cap<CAP>(p, acc);
       s[b] = acc;
     }
-    if (now == 0 && k0 == k_begin) {
-      // The first base is the score of the first key, unless that is infinite: scores of a magnitude that leaves no digits for their differences are
-      // then rounded only once the base is taken off.
-      float more = 0.f;
-      if constexpr (BIAS) more = -slope * fabsf(at - lds_pos[now][0]);
-      const float z = __shfl(fmaf(s[0][0], p.z_mul, more), col, 64);
-      if (fabsf(z) < INFINITY) base = z, limit = kSlack;
-    }
+    if constexpr (BIAS) {
 #pragma unroll
-    for (int b = 0; b < BN / 32; ++b) {
+      for (int b = 0; b < BN / 32; ++b)
 #pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4) {
-        floatx4 kpos = {};
-        if constexpr (BIAS) kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const floatx4 kpos = *reinterpret_cast<const floatx4*>(&lds_pos[now][32 * b + 8 * r4 + 4 * half]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          s[b][4 * r4 + i] = fmaf(s[b][4 * r4 + i], p.z_mul, BIAS ? fmaf(-slope, fabsf(at - kpos[i]), -base) : -base);
+          for (int i = 0; i < 4; ++i) s[b][4 * r4 + i] = fmaf(s[b][4 * r4 + i], p.z_mul, -slope * fabsf(at - kpos[i]));
         }
-      }
     }
     if (k0 + BN > k_end) {
 #pragma unroll
@@ -141,11 +134,13 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
 #pragma unroll
       for (int r = 0; r < 16; ++r) most = fmaxf(most, s[b][r]);
     most = fmaxf(most, other_half(most));
-    if (__any(most > limit)) {
+    if (__any(above(most, base) > limit)) {
       // A row that has no base yet has nothing either, and 2^-by is inf where its first score is far below zero.  The row's state decides, not its sum:
       // a lane's sum is that of half of the keys so far, while its results are those of all.
-      const bool raise = most > limit;
-      const float raised = base + most, by = raise ? raised - base : 0.f, shrink = raise && limit == kSlack ? exp2_fast(-by) : 1.f;
+      const bool raise = above(most, base) > limit;
+      float raised = BIAS ? most : most * p.z_mul;
+      if (above(most, raised) > kSlack) raised = nextafterf(raised, INFINITY);       // beyond 2^27, where a place is more than that
+      const float shrink = raise && limit == kSlack ? exp2_fast(base - raised) : 1.f;
       base = raise ? raised : base;
       limit = raise ? kSlack : limit;
       sum *= shrink;
@@ -153,10 +148,6 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[db][r] *= shrink;
-#pragma unroll
-      for (int b = 0; b < BN / 32; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[b][r] -= by;
     }
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {
@@ -165,7 +156,7 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
         vec8<T> pf;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float e = exp2_fast(s[b][8 * h2 + j]);
+          const float e = exp2_fast(above(s[b][8 * h2 + j], base));
           sum += e;
           pf[j] = T(e);
         }

@@ -99,3 +99,33 @@ def test_weight_gradient_of_the_largest_activations(x_dtype):
     X, Y = L.unpack_activations(p).double(), dy.double()
     assert torch.isfinite(X).all()
     ref.check(dw, (Y.T @ X, 2.0 ** -24 * 72 * Y.abs().T @ X.abs()), "dw")
+
+
+@pytest.mark.parametrize("q_owned,k_owned", SHAPES)
+@pytest.mark.parametrize("far", [1e4, 1e6, 2.0 ** 24])
+def test_keys_far_below_cost_the_others_no_digits(far, q_owned, k_owned):
+    """A first key, or all keys of the first tiles, far below the rest, by their distance or by their product: in 64 bits they weigh nothing, and the
+    others are as exact as without them."""
+    L = lgp()
+    Tq, Tk = sum(q_owned), sum(k_owned)
+    q, k, v = draw((Tq, 4, 64), BF16, 1), draw((Tk, 2, 64), BF16, 2), draw((Tk, 2, 64), BF16, 3)
+    for below in (1, min(k_owned) - 12):
+        docs, info = make_docs(q_owned, k_owned)
+        keep = torch.ones(Tk, dtype=torch.bool, device="cuda")
+        for s in info["spans"]:
+            keep[s[2]:s[2] + below] = False
+        info["k_pos"][~keep] = int(far)                    # what docs holds too
+        slopes = torch.linspace(1.0, 1.3, 4, device="cuda")
+        out, lse, _ = L.attend(q, k, v, docs, slopes=slopes)
+        want = alone(q, k, v, info, keep, slopes=slopes)
+        ref.check(out, want["out"], "out, by distance")
+        ref.check(lse, want["lse"], "lse, by distance")
+        info["k_pos"].clamp_(max=7)
+        k2, q2 = k.clone(), q.clone()
+        q2[..., 0], k2[..., 0] = 1.0, 0.0
+        k2[~keep] = 0
+        k2[~keep, :, 0] = -8 * far
+        out, lse, _ = L.attend(q2, k2, v, docs)
+        want = alone(q2, k2, v, info, keep)
+        ref.check(out, want["out"], "out, by product")
+        ref.check(lse, want["lse"], "lse, by product")
