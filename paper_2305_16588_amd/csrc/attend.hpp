@@ -86,11 +86,12 @@ template <bool CAP> __device__ __forceinline__ float through_cap(const AttendPar
   return u;
 }
 
-// The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys.
-__device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, int32_t splits, int32_t& begin, int32_t& end) {
-  const int32_t tiles = (keys + size - 1) / size, each = (tiles + splits - 1) / splits;
-  begin = s * each * size < keys ? s * each * size : keys;
-  end = (s + 1) * each * size < keys ? (s + 1) * each * size : keys;
+// The part of a document's keys that split s of `splits` takes: whole tiles of `size` keys, at most 256.  Counted in tiles: all parts together may be
+// as many keys more than there are as to pass 2^31.
+__host__ __device__ __forceinline__ void part_of(int32_t keys, int32_t size, int32_t s, int32_t splits, int32_t& begin, int32_t& end) {
+  const int32_t tiles = (keys + size - 1) / size, each = (tiles + splits - 1) / splits, first = s * each, last = first + each;
+  begin = first < tiles ? first * size : keys;
+  end = last < tiles ? last * size : keys;
 }
 
 int check_attend(const lgp_documents* d, const lgp_attention* a);
