@@ -11,7 +11,8 @@ namespace {
 
 // Gradient of q: with u = scale * q.k, z the score, P = exp(z - lse), dP = d_out . v and delta = d_out . out,
 //     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
-// Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product.
+// Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product, as k itself is; with
+// fp16 it is lifted first (kLiftFirst).
 // delta is taken from out and what its rounding took off.  The slope of a head has the gradient
 //     - sum dS |distance| = - sum_rows (sum_j dS |distance| - (sum_j dS) (sum_j P |distance|) / sum_j P) / sum_j P,
 // whose four sums per row go to `sums`: the second term is what the rounding of out and of lse left in dS, so the gradient depends on neither.
@@ -97,6 +98,9 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
 
   floatx16 dq[D / 32] = {};
   float sum_p = 0.f, sum_s = 0.f, sum_pf = 0.f, sum_sf = 0.f;
+  constexpr bool kLifts = std::is_same<T, f16>::value;
+  float lift = kLifts ? kLiftFirst : 1.f;        // of the probabilities, so of dU and of all four sums
+  if constexpr (kLifts) lse -= kLiftFirstLog2;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
   auto step = [&](int32_t k0, int now, auto whole) {
@@ -140,7 +144,8 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
             of_tile[3] = fmaf(u, far, of_tile[3]);
           }
           u = through_cap<CAP>(p, u, s[r]);
-          uf[r / 8][r % 8] = T(u);
+          if constexpr (kLifts) s[r] = u;
+          else uf[r / 8][r % 8] = T(u);
         }
       }
       if constexpr (BIAS) {
@@ -148,6 +153,27 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
         sum_s += of_tile[1];
         sum_pf += of_tile[2];
         sum_sf += of_tile[3];
+      }
+      if constexpr (kLifts) {
+        float most = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+        if (__any(most > kLiftedMost)) {
+          most = fmaxf(most, other_half(most));
+          const int by_log2 = most > kLiftedMost ? lower_log2(most) : 0;
+          const float by = __builtin_amdgcn_ldexpf(1.f, by_log2);
+          lift *= by;
+          lse -= float(by_log2);
+          sum_p *= by, sum_s *= by, sum_pf *= by, sum_sf *= by;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= by;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[db][r] *= by;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) uf[r / 8][r % 8] = T(s[r]);
       }
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
@@ -168,7 +194,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
     sum_s += other_half(sum_s);
     sum_pf += other_half(sum_pf);
     sum_sf += other_half(sum_sf);
-    if (p.sums && half == 0) p.sums[int64_t(split) * p.qs.rows * p.heads + at_out] = live ? floatx4{sum_p, sum_s, sum_pf, sum_sf} : floatx4{};
+    if (p.sums && half == 0) p.sums[int64_t(split) * p.qs.rows * p.heads + at_out] = live ? floatx4{sum_p, sum_s, sum_pf, sum_sf} * (1.f / lift) : floatx4{};
   }
   float* part = p.splits > 1 ? p.part_o + (int64_t(split) * p.qs.rows * p.heads + at_out) * p.dim : nullptr;
   T* out = static_cast<T*>(p.dq) + at_out * p.dim;
@@ -179,7 +205,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
       const int d = 32 * db + 8 * r4 + 4 * half;
       if (d < p.dim) {
         floatx4 x = {};
-        if (live) x = floatx4{dq[db][4 * r4], dq[db][4 * r4 + 1], dq[db][4 * r4 + 2], dq[db][4 * r4 + 3]} * p.scale;
+        if (live) x = floatx4{dq[db][4 * r4], dq[db][4 * r4 + 1], dq[db][4 * r4 + 2], dq[db][4 * r4 + 3]} * (p.scale / lift);
         if (part) *reinterpret_cast<floatx4*>(part + d) = x;
         else *reinterpret_cast<vec4<T>*>(out + d) = vec4<T>{T(x[0]), T(x[1]), T(x[2]), T(x[3])};
       }
@@ -323,6 +349,8 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
   if constexpr (BIAS) at = live ? float(p.ks.pos[key_row]) : 0.f;
 
   floatx16 dk[D / 32] = {}, dv[D / 32] = {};
+  constexpr bool kLifts = std::is_same<T, f16>::value;
+  float lift = (kLifts ? kLiftFirst : 1.f) / kLift<T>;        // of dU, less that of the probabilities
   Places<T, D> at_tile(lane);
   const bool idle = key0 + 32 * wave >= kd.tokens;                   // a wave of keys without tokens only copies
   int32_t h0 = hk * p.group, r0 = 0;
@@ -360,11 +388,30 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
         for (int i = 0; i < 4; ++i) {
           const int r = 4 * r4 + i;
           const float e = exp2_fast(fmaf(s[r], p.z_mul, BIAS ? fmaf(-slope[i], fabsf(at - pos[i]), -lse[i]) : -lse[i]));             // times kLift
-          float u = e * ((g[r] - delta[i]) * (1.f / kLift<T>));
+          float u = e * ((g[r] - delta[i]) * lift);
           u = through_cap<CAP>(p, u, s[r]);
           pf[r / 8][r % 8] = T(e);
-          uf[r / 8][r % 8] = T(u);
+          if constexpr (kLifts) s[r] = u;
+          else uf[r / 8][r % 8] = T(u);
         }
+      }
+      if constexpr (kLifts) {
+        float most = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
+        if (__any(most > kLiftedMost)) {
+          most = fmaxf(most, other_half(most));
+          const float by = __builtin_amdgcn_ldexpf(1.f, most > kLiftedMost ? lower_log2(most) : 0);
+          lift *= by;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= by;
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dk[db][r] *= by;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) uf[r / 8][r % 8] = T(s[r]);
       }
 #pragma unroll
       for (int h2 = 0; h2 < 2; ++h2)
@@ -392,7 +439,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
         vec4<T> x, y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[i] = T(live ? dk[db][4 * r4 + i] * p.scale : 0.f);
+          x[i] = T(live ? dk[db][4 * r4 + i] * (p.scale / (lift * kLift<T>)) : 0.f);
           y[i] = T(live ? dv[db][4 * r4 + i] * (1.f / kLift<T>) : 0.f);
         }
         *reinterpret_cast<vec4<T>*>(dk_out + d) = x;

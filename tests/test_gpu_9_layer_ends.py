@@ -129,3 +129,51 @@ def test_keys_far_below_cost_the_others_no_digits(far, q_owned, k_owned):
         want = alone(q2, k2, v, info, keep)
         ref.check(out, want["out"], "out, by product")
         ref.check(lse, want["lse"], "lse, by product")
+
+
+def off(got, want):
+    """Relative error in the 2-norm, and what rounding the exact result costs of it."""
+    return float((got.double() - want).norm() / want.norm()), float((want.to(got.dtype).double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("size", [1.0, 1e-2, 1e-3, 1e-4])
+@pytest.mark.parametrize("dim,rows", [(64, 300), (128, 40), (32, 33)])
+def test_small_gradients_in_fp16(dim, rows, size):
+    """dU = P (dP - delta) is far smaller than d_out over thousands of keys, and is rounded for the products that make dq and dk.  Beside the rounding
+    of the result there are those of dU, of the probabilities in out (through delta) and of delta's sum, each at most a unit of the terms of the sum
+    and at random: together less than four units."""
+    L = lgp()
+    keys = 6000
+    docs, info = make_docs([rows], [keys])
+    v, g = draw((keys, 2, dim), F16, 3), draw((rows, 2, dim), F32, 4, size).half()
+    scale = 30 * dim ** -0.5
+    for q_size, k_size in ((1 / 30, 1.0), (1.0, 1 / 30)):     # so that dq, and then dk, is not among the smallest numbers itself
+        q, k = draw((rows, 2, dim), F16, 1, q_size), draw((keys, 2, dim), F16, 2, k_size)
+        out, lse, rest = L.attend(q, k, v, docs, scale=scale, rest=True)
+        got = L.attend_backward(g, q, k, v, out, lse, docs, rest=rest, scale=scale)
+        want = ref.attention(q, k, v, info, g, scale=scale)
+        for x, name in zip(got, ("dq", "dk", "dv")):
+            err, own = off(x, want[name][0])
+            assert err <= own + 4 * ref.UNIT[F16], f"{name}: {err:.3g}, rounding alone {own:.3g}"
+
+
+@pytest.mark.parametrize("dim,rows", [(64, 300), (128, 40), (32, 33)])
+def test_large_gradients_in_fp16(dim, rows):
+    """dU beyond the largest number of fp16, where dq, dk and dv are not, in some rows and in some tiles of the keys only."""
+    L = lgp()
+    keys = 200
+    docs, info = make_docs([rows], [keys])
+    q, k, v = draw((rows, 2, dim), F16, 1, 0.01), draw((keys, 2, dim), F16, 2, 0.01), draw((keys, 2, dim), F16, 3, 0.5)
+    v[100:] *= 400
+    g = draw((rows, 2, dim), F32, 4, 8000.0)
+    g[::3] *= 1e-4
+    g = g.half()
+    out, lse, rest = L.attend(q, k, v, docs, rest=True)
+    got = L.attend_backward(g, q, k, v, out, lse, docs, rest=rest)
+    want = ref.attention(q, k, v, info, g)
+    P = torch.softmax(q[:, 0].double() @ k[:, 0].double().T * dim ** -0.5, 1)
+    dP = g[:, 0].double() @ v[:, 0].double().T
+    assert (P * (dP - (P * dP).sum(1, keepdim=True))).abs().max() > 2 * 65504
+    for x, name in zip(got, ("dq", "dk", "dv")):
+        err, own = off(x, want[name][0])
+        assert err <= own + 4 * ref.UNIT[F16], f"{name}: {err:.3g}, rounding alone {own:.3g}"
