@@ -25,7 +25,8 @@ struct AttendParams {
   bool negate;
   const float* slopes;
   float docs_per_tile;
-  int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys
+  int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys; attend_single.hip: workgroups with documents,
+                             // and before them those that list the large ones
   // forward
   void *out, *rest;
   float* lse;
@@ -35,7 +36,9 @@ struct AttendParams {
   const float* lse_in;
   void *dq, *dk, *dv;
   float* delta;              // [q_rows][heads]: d_out . out
-  floatx4* sums;             // [split][q_rows][heads], if the gradient of the slopes is wanted: see attend_dq_kernel
+  floatx4* sums;             // [split][q_rows][heads], if the gradient of the slopes is wanted: see dq_rows
+  // documents of one query on average: those that are not left to single waves, see each_large
+  int32_t *n_large, *large;  // [survey] and [survey][kSurvey], or NULL: there can be none
 };
 
 template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p) { return *reinterpret_cast<const vec8<T>*>(p); }
@@ -97,9 +100,62 @@ __host__ __device__ __forceinline__ void part_of(int32_t keys, int32_t size, int
 int check_attend(const lgp_documents* d, const lgp_attention* a);
 AttendParams attend_params(const lgp_documents* d, const lgp_attention* a);
 
-// Documents of one query and few keys (attend_single.hip).
+// Documents of one query and few keys on average (attend_single.hip).  The host knows no more of them; one that has many of both, or very many keys,
+// would be one wave's work and take as long as its pairs one after the other.  So a wave takes documents of up to kLargePairs pairs, and while these
+// are gone through, waves of the same launch list the others, kSurvey documents each.  A second launch goes through the lists: a workgroup
+// counts all their tiles, 64 documents at a time, and takes every so many-th one.  Measured: 122 880 documents of up to 10 keys, none of them large:
+// 5 us for each of the three second launches of a training step of 595.  2000 documents, bf16, heads 8/8 of 64: one of them 2000 rows and the others
+// empty, forward 32 us and backward 130; one of them a query over 60 000 keys, 384 and 1162, one workgroup for each head.
+constexpr int kLargePairs = 512, kSurvey = 512, kLargeGroups = 512;       // workgroups of the second launch
 bool single_queries(const lgp_documents* d, const lgp_attention* a);
+inline int64_t surveys(const lgp_documents* d) {       // none if all rows together are no large document
+  const int64_t q = d->q_rows > 1 ? d->q_rows : 1, k = d->k_rows > 1 ? d->k_rows : 1;
+  return q > kLargePairs || k > kLargePairs || q * k > kLargePairs ? (d->n_docs + kSurvey - 1) / kSurvey : 0;
+}
+inline size_t survey_bytes(const lgp_documents* d) { return (size_t(surveys(d)) * (1 + kSurvey) * sizeof(int32_t) + 15) / 16 * 16; }
+inline void set_survey(AttendParams& p, const lgp_documents* d, void* at) {
+  const int64_t n = surveys(d);
+  p.n_large = n ? static_cast<int32_t*>(at) : nullptr;
+  p.large = n ? p.n_large + n : nullptr;
+}
 void launch_single(const AttendParams& p, const lgp_attention* a, bool backward, hipStream_t s);
+void launch_large(const AttendParams& p, const lgp_attention* a, hipStream_t s);       // of the forward pass
+__device__ __forceinline__ bool is_large(int32_t q_owned, int32_t k_owned) {
+  return int64_t(q_owned > 1 ? q_owned : 1) * (k_owned > 1 ? k_owned : 1) > kLargePairs;
+}
+__device__ __forceinline__ int32_t owned_of(const Side& s, int32_t d, int32_t n) {
+  const int32_t begin = offset_of(s, d, n), end = offset_of(s, d + 1, n);
+  return end > begin ? end - begin : 0;
+}
+// tiles(rows of queries, of keys) is what a document has of them; work(document, tile) is called by all waves of a workgroup alike.
+template <typename Tiles, typename Work> __device__ __forceinline__ void each_large(const AttendParams& p, Tiles tiles, Work work) {
+  const int lane = threadIdx.x & 63;
+  const int32_t n = (p.n_docs + kSurvey - 1) / kSurvey;
+  int32_t next = blockIdx.x;               // this workgroup's next tile, counted from the first of the documents that are looked at
+  for (int32_t s0 = 0; s0 < n; s0 += 64) {
+    const int32_t count = s0 + lane < n ? p.n_large[s0 + lane] : 0;
+    for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
+      const int of = __builtin_ctzll(some);
+      const int32_t listed = __builtin_amdgcn_readlane(count, of);
+      for (int32_t i0 = 0; i0 < listed; i0 += 64) {
+        const int32_t doc = i0 + lane < listed ? p.large[int64_t(s0 + of) * kSurvey + i0 + lane] : -1;
+        int32_t upto = doc >= 0 ? tiles(owned_of(p.qs, doc, p.n_docs), owned_of(p.ks, doc, p.n_docs)) : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+          const int32_t before = __shfl_up(upto, d, 64);
+          if (lane >= d) upto += before;
+        }
+        const int32_t all = __builtin_amdgcn_readlane(upto, 63);
+        for (; next < all; next += gridDim.x) {
+          const int l = __popcll(__ballot(upto <= next));
+          work(__builtin_amdgcn_readlane(doc, l), next - (l ? __builtin_amdgcn_readlane(upto, l - 1) : 0));
+          __syncthreads();                 // the next one has the same LDS
+        }
+        next -= all;
+      }
+    }
+  }
+}
 
 // With fp16 a probability below 2^-14 would lose digits, and over 16 000 keys most are: where they are an operand of a product, the backward
 // pass takes them times 2^12, which cannot overflow, and the result times 2^-12.

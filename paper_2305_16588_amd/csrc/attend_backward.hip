@@ -19,30 +19,12 @@ namespace {
 // Measured: 4 documents of 8192 tokens, heads 8/4 of 128, bf16, bias: 1662 us, 0.99 PFLOP/s, matrix instructions 49 % and vector instructions 61 %
 // of the cycles; 1024 documents of 276 rows, heads 8/8 of 32, cap and bias: 282 us, vector instructions 88 %.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
-__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
-  constexpr int kThreads = 64 * NW, kRows = 32 * NW;
+__device__ __forceinline__ void dq_rows(const AttendParams& p, int32_t hk, int32_t split, int32_t row0, const Span qd, const Span kd) {
+  constexpr int kThreads = 64 * NW;
   __shared__ __align__(16) T lds_k[2][BN * D];
   __shared__ __align__(16) T lds_v[2][BN * D];
   __shared__ __align__(16) float lds_pos[2][BIAS ? BN : 4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
-
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
-  int32_t split = 0, hk, tile;
-  if constexpr (NW == 1) {
-    hk = piece % p.kv_heads;
-    piece /= p.kv_heads;
-    split = piece % p.splits;
-    tile = piece / p.splits;
-  } else {
-    tile = piece % p.tiles;
-    piece /= p.tiles;
-    split = piece % p.splits;
-    hk = piece / p.splits;
-  }
-  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, lane);
-  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
-  const int32_t row0 = (tile - doc.first) * kRows;
-  if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
   int32_t k_begin, k_end;
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split, p.splits, k_begin, k_end);
@@ -212,6 +194,38 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
     }
 }
 
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
+__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
+  constexpr int kRows = 32 * NW;
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t split = 0, hk, tile;
+  if constexpr (NW == 1) {
+    hk = piece % p.kv_heads;
+    piece /= p.kv_heads;
+    split = piece % p.splits;
+    tile = piece / p.splits;
+  } else {
+    tile = piece % p.tiles;
+    piece /= p.tiles;
+    split = piece % p.splits;
+    hk = piece / p.splits;
+  }
+  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, threadIdx.x & 63);
+  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
+  const int32_t row0 = (tile - doc.first) * kRows;
+  if (row0 < 0 || row0 >= qd.owned * p.group) return;
+  dq_rows<T, D, CAP, BIAS, NW, BN>(p, hk, split, row0, qd, kd);
+}
+
+// Large documents among those of one query on average: here, and of k and v below.
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, waves_per_simd(D, 4)) void attend_dq_large_kernel(const AttendParams p) {
+  each_large(p, [&](int32_t q, int32_t) { return (q * p.group + 127) / 128 * p.kv_heads; },
+             [&](int32_t doc, int32_t tile) {
+               dq_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, 0, tile / p.kv_heads * 128, span_of(p.qs, doc, p.n_docs), span_of(p.ks, doc, p.n_docs));
+             });
+}
+
 // Adds the parts of dq, like join_kernel, and in its time.
 template <typename T>
 __global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
@@ -268,7 +282,7 @@ __global__ __launch_bounds__(kEndThreads) void slopes_end_kernel(const double* p
 // Measured, at the sizes of attend_dq_kernel: 2200 us, 1.00 PFLOP/s, matrix instructions 45 % of the cycles of two waves per SIMD that wait for each
 // other's tiles; 303 us, vector instructions 69 %.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
-__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_kernel(const AttendParams p) {
+__device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int32_t key0, const Span kd, const Span qd) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
   __shared__ __align__(16) T lds_q[2][BQ * D];
   __shared__ __align__(16) T lds_g[2][BQ * D];
@@ -277,20 +291,6 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
   constexpr bool kHeld = D < 128 || NW == 1;
   __shared__ __align__(16) T lds_v[kHeld ? 8 : kKeys * D];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 31, half = lane >> 5;
-
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
-  int32_t hk, tile;
-  if constexpr (NW == 1) {
-    hk = piece % p.kv_heads;
-    tile = piece / p.kv_heads;
-  } else {
-    tile = piece % p.tiles;
-    hk = piece / p.tiles;
-  }
-  const Found doc = find_tile(p.ks, p.n_docs, p.docs_per_tile, 1, kKeys, tile, lane);
-  const Span kd = doc.span, qd = other_side(p.qs, p.ks, doc, p.n_docs);
-  const int32_t key0 = (tile - doc.first) * kKeys;
-  if (key0 < 0 || key0 >= kd.owned) return;
 
   // Up to 16 heads of a token, if they divide 16, are folded; otherwise the heads that share this one are gone through one after the other.
   const int32_t rows = key0 < kd.tokens ? qd.tokens << p.log2_fold : 0;
@@ -448,11 +448,38 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
     }
 }
 
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
+__global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_kernel(const AttendParams p) {
+  constexpr int kKeys = 32 * NW;
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t hk, tile;
+  if constexpr (NW == 1) {
+    hk = piece % p.kv_heads;
+    tile = piece / p.kv_heads;
+  } else {
+    tile = piece % p.tiles;
+    hk = piece / p.tiles;
+  }
+  const Found doc = find_tile(p.ks, p.n_docs, p.docs_per_tile, 1, kKeys, tile, threadIdx.x & 63);
+  const Span kd = doc.span, qd = other_side(p.qs, p.ks, doc, p.n_docs);
+  const int32_t key0 = (tile - doc.first) * kKeys;
+  if (key0 < 0 || key0 >= kd.owned) return;
+  dkv_rows<T, D, CAP, BIAS, NW, BQ>(p, hk, key0, kd, qd);
+}
+
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, waves_per_simd(D, 4)) void attend_dkv_large_kernel(const AttendParams p) {
+  each_large(p, [&](int32_t, int32_t k) { return (k + 127) / 128 * p.kv_heads; },
+             [&](int32_t doc, int32_t tile) {
+               dkv_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, tile / p.kv_heads * 128, span_of(p.ks, doc, p.n_docs), span_of(p.qs, doc, p.n_docs));
+             });
+}
+
 struct BackwardShape {
   ForwardShape q;             // of the kernel by queries
   int key_waves;              // of the kernel by keys
   int64_t key_tiles;
-  size_t delta, sums, parts, partial, bytes;      // offsets into the workspace, in floats; all of it, in bytes
+  size_t delta, sums, parts, partial, survey, bytes;      // offsets into the workspace, in floats; all of it, in bytes
 };
 BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_attention* a) {
   BackwardShape b;
@@ -468,11 +495,17 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
   b.sums = up(rows);
   b.partial = b.sums + (a->slopes ? rows * 4 * b.q.splits : 0);
   b.parts = b.partial + (a->slopes ? 2 * size_t(kSlopeThreads) : 0);
-  b.bytes = (b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0)) * sizeof(float);
+  b.survey = b.parts + (b.q.splits > 1 ? rows * a->dim * b.q.splits : 0);
+  b.bytes = b.survey * sizeof(float) + (single_queries(d, a) ? survey_bytes(d) : 0);
   return b;
 }
 
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const BackwardShape& b, hipStream_t s) {
+  if (p.n_large) {
+    attend_dq_large_kernel<T, D, CAP, BIAS><<<kLargeGroups, 256, 0, s>>>(p);
+    attend_dkv_large_kernel<T, D, CAP, BIAS><<<kLargeGroups, 256, 0, s>>>(p);
+    return;
+  }
   AttendParams x = p;
   x.tiles = int32_t(b.q.tiles);
   x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.q.tiles, 1));
@@ -517,7 +550,8 @@ int lgp_attend_workspace(int device, const lgp_documents* docs, const lgp_attent
     *bytes = backward_shape(device, docs, att).bytes;
   } else {
     const ForwardShape f = forward_shape(device, docs, att);
-    if (f.splits > 1) *bytes = size_t(f.splits) * docs->q_rows * att->heads * (att->dim + 2) * sizeof(float);
+    if (single_queries(docs, att)) *bytes = survey_bytes(docs);
+    else if (f.splits > 1) *bytes = size_t(f.splits) * docs->q_rows * att->heads * (att->dim + 2) * sizeof(float);
   }
   return LGP_OK;
 }
@@ -549,9 +583,12 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
   p.sums = d_slopes ? reinterpret_cast<floatx4*>(w + b.sums) : nullptr;
   p.part_o = w + b.parts;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (single_queries(docs, att)) launch_single(p, att, true, s);
-  else if (att->dtype == LGP_F16) launch<f16>(p, b, att->cap > 0.f, s);
-  else launch<bf16>(p, b, att->cap > 0.f, s);
+  const bool single = single_queries(docs, att);
+  if (single) {
+    set_survey(p, docs, w + b.survey);
+    launch_single(p, att, true, s);
+  }
+  if (!single || p.n_large) att->dtype == LGP_F16 ? launch<f16>(p, b, att->cap > 0.f, s) : launch<bf16>(p, b, att->cap > 0.f, s);
   if (d_slopes) {
     double* partial = reinterpret_cast<double*>(w + b.partial);      // after the sums, so aligned to 16 bytes like them
     slopes_kernel<<<kSlopeThreads / 256, 256, 0, s>>>(p, partial);

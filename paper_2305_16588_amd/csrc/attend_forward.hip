@@ -23,8 +23,8 @@ namespace {
 // queries over 50 001 keys each, heads 16/2 of 128: 158 us, bound by bytes, 5.2 TB/s.
 constexpr float kSlack = 8.f;
 template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
-__global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_kernel(const AttendParams p) {
-  constexpr int kThreads = 64 * NW, kRows = 32 * NW;          // threads that share tiles; rows of a workgroup
+__device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, int32_t split, int32_t row0, const Span qd, const Span kd) {
+  constexpr int kThreads = 64 * NW;                           // that share tiles
   __shared__ __align__(16) T lds_tiles[KW][2][2][BN * D];     // of keys and values, two places each
   __shared__ __align__(16) float lds_at[KW][2][BIAS ? BN : 4];
   const int lane = threadIdx.x & 63, col = lane & 31, half = lane >> 5, tid = threadIdx.x % kThreads, wave = NW > 1 ? threadIdx.x >> 6 : 0;
@@ -32,24 +32,6 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
   auto& lds_k = lds_tiles[part][0];
   auto& lds_v = lds_tiles[part][1];
   auto& lds_pos = lds_at[part];
-
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
-  int32_t split = 0, hk, tile;
-  if constexpr (NW == 1) {          // short documents: the heads of a token lie side by side in memory
-    hk = piece % p.kv_heads;
-    piece /= p.kv_heads;
-    split = piece % p.splits;
-    tile = piece / p.splits;
-  } else {                          // long ones: the tiles that share keys one after the other
-    tile = piece % p.tiles;
-    piece /= p.tiles;
-    split = piece % p.splits;
-    hk = piece / p.splits;
-  }
-  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, lane);
-  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
-  const int32_t row0 = (tile - doc.first) * kRows;
-  if (row0 < 0 || row0 >= qd.owned * p.group) return;
 
   int32_t k_begin, k_end;
   part_of(row0 < qd.tokens * p.group ? kd.tokens : 0, BN, split * KW + part, p.splits * KW, k_begin, k_end);
@@ -236,6 +218,38 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
   }
 }
 
+template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
+__global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_kernel(const AttendParams p) {
+  constexpr int kRows = 32 * NW;
+  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  int32_t split = 0, hk, tile;
+  if constexpr (NW == 1) {          // short documents: the heads of a token lie side by side in memory
+    hk = piece % p.kv_heads;
+    piece /= p.kv_heads;
+    split = piece % p.splits;
+    tile = piece / p.splits;
+  } else {                          // long ones: the tiles that share keys one after the other
+    tile = piece % p.tiles;
+    piece /= p.tiles;
+    split = piece % p.splits;
+    hk = piece / p.splits;
+  }
+  const Found doc = find_tile(p.qs, p.n_docs, p.docs_per_tile, p.group, kRows, tile, threadIdx.x & 63);
+  const Span qd = doc.span, kd = other_side(p.ks, p.qs, doc, p.n_docs);
+  const int32_t row0 = (tile - doc.first) * kRows;
+  if (row0 < 0 || row0 >= qd.owned * p.group) return;
+  attend_rows<T, D, CAP, BIAS, NW, KW, BN>(p, hk, split, row0, qd, kd);
+}
+
+// Large documents among those of one query on average, by four waves that share their keys.
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(256, waves_per_simd(D, 1)) void attend_large_kernel(const AttendParams p) {
+  each_large(p, [&](int32_t q, int32_t) { return (q * p.group + 31) / 32 * p.kv_heads; },
+             [&](int32_t doc, int32_t tile) {
+               attend_rows<T, D, CAP, BIAS, 1, 4, 32>(p, tile % p.kv_heads, 0, tile / p.kv_heads * 32, span_of(p.qs, doc, p.n_docs), span_of(p.ks, doc, p.n_docs));
+             });
+}
+
 // Joins the parts of a query: out = sum_s 2^(top_s - top) o_s / sum_s 2^(top_s - top) sum_s.  A workgroup has a row, eight groups of 32 lanes a
 // part at a time, a lane four elements.  Measured: 256 rows of 128 in 30 parts: 5 us, of which a launch is most.
 template <typename T>
@@ -282,6 +296,10 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
 }
 
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const ForwardShape& f, hipStream_t s) {
+  if (p.n_large) {
+    attend_large_kernel<T, D, CAP, BIAS><<<uint32_t(f.tiles), 256, 0, s>>>(p);
+    return;
+  }
   const uint32_t blocks = uint32_t(p.tiles) * p.kv_heads * p.splits;
   if (f.waves > 1) attend_kernel<T, D, CAP, BIAS, 4, 1, 64><<<blocks, 256, 0, s>>>(p);
   else if (f.key_waves > 1) attend_kernel<T, D, CAP, BIAS, 1, 4, 32><<<blocks, 256, 0, s>>>(p);
@@ -301,6 +319,12 @@ template <typename T> void launch(const AttendParams& p, const ForwardShape& f, 
 }
 
 }  // namespace
+
+void launch_large(const AttendParams& p, const lgp_attention* a, hipStream_t s) {
+  const ForwardShape f = {1, 4, kLargeGroups, 1};
+  if (a->dtype == LGP_F16) launch<f16>(p, f, a->cap > 0.f, s);
+  else launch<bf16>(p, f, a->cap > 0.f, s);
+}
 
 int check_attend(const lgp_documents* d, const lgp_attention* a) {
   if (!d || !a) return LGP_EINVAL;
@@ -379,7 +403,11 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
     p.out = out;
     p.rest = rest;
     p.lse = lse;
+    if (workspace_bytes < survey_bytes(docs)) return LGP_ECAPACITY;
+    if (surveys(docs) && (!workspace || !aligned16(workspace))) return LGP_EINVAL;
+    set_survey(p, docs, workspace);
     launch_single(p, att, false, s);
+    if (p.n_large) launch_large(p, att, s);
     return launched();
   }
   const ForwardShape f = forward_shape(device, docs, att);

@@ -18,7 +18,7 @@ template <int L> struct Lanes {
   int32_t doc, hk;
   __device__ __forceinline__ Lanes(const AttendParams& p, int32_t heads_at_once) {
     const int lane = threadIdx.x & 63, slot = lane / L;
-    const int64_t unit = int64_t(piece_of(blockIdx.x, gridDim.x)) * 4 + (threadIdx.x >> 6);
+    const int64_t unit = int64_t(piece_of(blockIdx.x - p.splits, p.tiles)) * 4 + (threadIdx.x >> 6);
     const int32_t chunks = (p.kv_heads + heads_at_once - 1) / heads_at_once;
     doc = __builtin_amdgcn_readfirstlane(int32_t(unit / chunks));
     c = lane % L;
@@ -45,11 +45,37 @@ template <typename T> __device__ __forceinline__ void widen(vec8<T> a, float* x)
 
 constexpr int kSteps = 4;       // keys that a lane has in flight
 
+// The first workgroups of a launch: a wave lists the large ones of kSurvey documents, in their order.
+__device__ __forceinline__ void survey(const AttendParams& p) {
+  constexpr int kAtOnce = 8;           // loads of so many documents of a lane are on their way together
+  const int lane = threadIdx.x & 63;
+  const int32_t at = blockIdx.x * 4 + (threadIdx.x >> 6), d0 = at * kSurvey;
+  if (d0 >= p.n_docs) return;
+  int32_t n = 0;
+  for (int32_t d1 = d0; d1 < d0 + kSurvey; d1 += 64 * kAtOnce) {
+    bool large[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int32_t d = d1 + 64 * i + lane;          // beyond the last one: no rows
+      large[i] = is_large(owned_of(p.qs, d, p.n_docs), owned_of(p.ks, d, p.n_docs));
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const uint64_t all = __ballot(large[i]);
+      if (large[i]) p.large[d0 + n + __popcll(all & ((uint64_t(1) << lane) - 1))] = d1 + 64 * i + lane;
+      n += __popcll(all);
+    }
+  }
+  if (lane == 0) p.n_large[at] = n;
+}
+
 template <typename T, int L, int G, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void single_kernel(const AttendParams p, int32_t heads_at_once) {
+  if (blockIdx.x < uint32_t(p.splits)) return survey(p);
   const Lanes<L> a(p, heads_at_once);
   if (a.doc >= p.n_docs) return;
   const Span qd = span_of(p.qs, a.doc, p.n_docs), kd = span_of(p.ks, a.doc, p.n_docs);
+  if (is_large(qd.owned, kd.owned)) return;
   const T* kp = static_cast<const T*>(p.k) + int64_t(a.hk) * p.k_head + 8 * a.c;
   const T* vp = static_cast<const T*>(p.v) + int64_t(a.hk) * p.v_head + 8 * a.c;
   for (int32_t row = 0; row < qd.owned; ++row) {
@@ -160,9 +186,11 @@ template <typename T, int L, int G, bool BIAS> struct Query {
 
 template <typename T, int L, int G, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams p, int32_t heads_at_once) {
+  if (blockIdx.x < uint32_t(p.splits)) return survey(p);
   const Lanes<L> a(p, heads_at_once);
   if (a.doc >= p.n_docs) return;
   const Span qd = span_of(p.qs, a.doc, p.n_docs), kd = span_of(p.ks, a.doc, p.n_docs);
+  if (is_large(qd.owned, kd.owned)) return;
   const T* kp = static_cast<const T*>(p.k) + int64_t(a.hk) * p.k_head + 8 * a.c;
   const T* vp = static_cast<const T*>(p.v) + int64_t(a.hk) * p.v_head + 8 * a.c;
   const float back = fabsf(p.scale);        // q was negated as it was read where the scale is negative
@@ -275,9 +303,12 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
 
 template <typename T, int L, int G, bool CAP, bool BIAS> void launch(const AttendParams& p, bool backward, hipStream_t s) {
   const int32_t at_once = std::min(p.kv_heads, 64 / L), chunks = (p.kv_heads + at_once - 1) / at_once;
-  const uint32_t blocks = uint32_t((int64_t(p.n_docs) * chunks + 3) / 4);
-  if (backward) single_backward_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(p, at_once);
-  else single_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(p, at_once);
+  AttendParams x = p;
+  x.tiles = int32_t((int64_t(p.n_docs) * chunks + 3) / 4);
+  x.splits = p.n_large ? (p.n_docs + 4 * kSurvey - 1) / (4 * kSurvey) : 0;
+  const uint32_t blocks = uint32_t(x.splits) + uint32_t(x.tiles);
+  if (backward) single_backward_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
+  else single_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
 }
 template <typename T, int L, int G> void launch(const AttendParams& p, bool cap, bool backward, hipStream_t s) {
   if (cap) p.slopes ? launch<T, L, G, true, true>(p, backward, s) : launch<T, L, G, true, false>(p, backward, s);

@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import layer_common as ref
-from test_gpu_9_layer import BF16, F16, F32, draw, lgp, make_docs
+from test_gpu_9_layer import BF16, F16, F32, draw, lgp, make_docs, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -177,3 +177,65 @@ def test_large_gradients_in_fp16(dim, rows):
     for x, name in zip(got, ("dq", "dk", "dv")):
         err, own = off(x, want[name][0])
         assert err <= own + 4 * ref.UNIT[F16], f"{name}: {err:.3g}, rounding alone {own:.3g}"
+
+
+def milliseconds(f):
+    f()
+    a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    a.record()
+    f()
+    b.record()
+    b.synchronize()
+    return a.elapsed_time(b)
+
+
+@pytest.mark.parametrize("dtype,dim,heads,kv_heads", [(F16, 32, 4, 4), (BF16, 64, 4, 2), (BF16, 128, 3, 3)])
+@pytest.mark.parametrize("large", [{700: (2000, 2000)}, {0: (1, 60_000), 1999: (300, 900)}, {d: (30, 40 + d % 50) for d in range(0, 1990, 37)},
+                                   {5: (1, 513), 6: (2, 256), 7: (2, 257), 1500: (1900, 0), 1501: (0, 5000)}])
+def test_large_documents_among_many_small_ones(large, dtype, dim, heads, kv_heads):
+    """One query and few keys on average.  What has many of both is not one wave's work: a quarter of a second is ten times what the slowest of these
+    cases takes, and a hundredth of four million pairs one after the other."""
+    n = 2000
+    rng = torch.Generator().manual_seed(1)
+    small = torch.randint(0, 9, (n,), generator=rng).tolist()
+    rest = n - sum(q for q, _ in large.values())               # queries that are left for the others
+    q_owned, k_owned = [0] * n, list(small)
+    for d, (q, k) in large.items():
+        q_owned[d], k_owned[d] = q, k
+    for d in range(n):
+        if d not in large and rest > 0:
+            q_owned[d], rest = 1, rest - 1
+    q_tokens = [max(0, q - 3) if q > 50 else q for q in q_owned]
+    docs, info = make_docs(q_owned, k_owned, q_tokens, [max(0, k - 5) if k > 50 else k for k in k_owned])
+    run_attention(docs, info, heads, kv_heads, dim, dtype, 20.0, True)
+    out, lse, dq, dk, dv, _ = run_attention(docs, info, heads, kv_heads, dim, dtype)
+    L = lgp()
+    q, k, g = (torch.zeros((t, h, dim), dtype=dtype, device="cuda") for t, h in ((sum(q_owned), heads), (sum(k_owned), kv_heads), (sum(q_owned), heads)))
+    assert milliseconds(lambda: L.attend_backward(g, q, k, k, *L.attend(q, k, k, docs)[:2], docs)) < 250
+
+
+def test_large_documents_in_graphs_and_twice():
+    L = lgp()
+    owned = [1] * 500
+    owned[13], owned[400] = 90, 70
+    for d in range(20, 180):
+        owned[d] = 0
+    docs, _ = make_docs(owned, [k + 9 for k in owned])
+    Tq, Tk = sum(owned), sum(owned) + 9 * 500
+    q, k, v, g = draw((Tq, 4, 64), BF16, 1), draw((Tk, 2, 64), BF16, 2), draw((Tk, 2, 64), BF16, 3), draw((Tq, 4, 64), BF16, 4)
+    slopes = torch.full((4,), 0.1, device="cuda")
+
+    def step():
+        out, lse, rest = L.attend(q, k, v, docs, slopes=slopes, cap=30.0, rest=True)
+        return [out, lse, rest, *L.attend_backward(g, q, k, v, out, lse, docs, rest=rest, slopes=slopes, cap=30.0)]
+
+    want = step()
+    assert all(torch.equal(a, b) for a, b in zip(step(), want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for r in range(3):
+        q.copy_(draw((Tq, 4, 64), BF16, 10 + r))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step())), f"replay {r}"
