@@ -22,6 +22,7 @@ struct AttendParams {
   // keys: k) is negated as it is read.  z_mul is then positive (a scale of zero is taken as 1e-30), and the largest product is the largest score.
   float scale, z_mul;
   float t_mul, t_inv, tanh_c[4];         // scale / cap and its inverse, and kTanh with its powers: see capped_near
+  float near;                // up to which product capped_near holds; negative where the powers leave the range of fp32
   bool negate;
   const float* slopes;
   float docs_per_tile;
@@ -54,7 +55,8 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
 // The cap: a product qk becomes tanh(x) / t_mul with x = qk * t_mul, which is qk where the cap is far.  Up to x = kNear that is
 // qk (1 + c0 x^2 + c1 x^4 + c2 x^6 + c3 x^8), fitted by least squares of the relative error, reweighted until even: 1e-7 with its roundings, and it
 // is where capped scores mostly are; the powers of t_mul are in the coefficients.  Beyond, tanh(x) = 1 - 2 / (e^2x + 1), which near zero would be 1e-7
-// off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.
+// off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.  Where the powers of t_mul leave the range of
+// fp32 -- products of millions below a cap of a million, caps of millionths -- all go the other way, which takes x first.
 constexpr float kNear = 0.55f;
 constexpr float kTanh[4] = {-0.3333294689655304f, 0.13320724666118622f, -0.05267181620001793f, 0.016437582671642303f};
 __device__ __forceinline__ float capped_near(const AttendParams& p, float s) {
@@ -62,15 +64,15 @@ __device__ __forceinline__ float capped_near(const AttendParams& p, float s) {
   return s * fmaf(fmaf(fmaf(fmaf(p.tanh_c[3], w, p.tanh_c[2]), w, p.tanh_c[1]), w, p.tanh_c[0]), w, 1.f);
 }
 __device__ __forceinline__ float capped_any(const AttendParams& p, float s) {
-  const float x = s * p.t_mul, far = (1.f - 2.f * rcp_fast(exp2_fast(x * (2.f * kLog2e)) + 1.f)) * p.t_inv;
-  return fabsf(x) <= kNear ? capped_near(p, s) : far;
+  const float x = s * p.t_mul, w = x * x, far = (1.f - 2.f * rcp_fast(exp2_fast(x * (2.f * kLog2e)) + 1.f)) * p.t_inv;
+  return fabsf(x) <= kNear ? s * fmaf(fmaf(fmaf(fmaf(kTanh[3], w, kTanh[2]), w, kTanh[1]), w, kTanh[0]), w, 1.f) : far;
 }
 template <bool CAP> __device__ __forceinline__ void cap(const AttendParams& p, floatx16& s) {
   if constexpr (CAP) {
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(s[r]));
-    if (__any(most * p.t_mul > kNear)) {
+    if (__any(most > p.near)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = capped_any(p, s[r]);
     } else {

@@ -359,8 +359,9 @@ AttendParams attend_params(const lgp_documents* d, const lgp_attention* a) {
   const float scale = std::fabs(a->scale);
   p.negate = a->scale < 0.f;
   p.z_mul = std::max(scale, 1e-30f) * kLog2e;
-  p.t_mul = a->cap > 0.f ? scale / a->cap : 0.f;
+  p.t_mul = a->cap > 0.f ? std::min(scale / a->cap, 1e38f) : 0.f;
   p.t_inv = p.t_mul > 0.f ? 1.f / p.t_mul : 0.f;
+  p.near = p.t_mul == 0.f || (p.t_mul >= 0x1p-12f && p.t_mul <= 0x1p12f) ? kNear / p.t_mul : -1.f;
   double power = 1.0;
   for (int i = 0; i < 4; ++i) p.tanh_c[i] = float(kTanh[i] * (power *= double(p.t_mul) * p.t_mul));
   p.per_token = divisor(uint32_t(p.group));

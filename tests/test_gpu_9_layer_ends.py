@@ -239,3 +239,24 @@ def test_large_documents_in_graphs_and_twice():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, step())), f"replay {r}"
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("cap,q_size,k_size,scale", [(1e6, 100.0, 1000.0, 1.0), (2e5, 30.0, 300.0, 1.0), (1e-6, 1.0, 1.0, 0.125), (1e-30, 1.0, 1.0, 0.125),
+                                                     (1e-44, 1.0, 1.0, 0.125), (1e30, 1.0, 1.0, 0.125), (30.0, 1.0, 1.0, 0.0), (30.0, 1.0, 1.0, 1e-12)])
+@pytest.mark.parametrize("q_owned,k_owned", [([70], [130]), ([1] * 20, [9] * 20)])
+def test_caps_of_every_size(q_owned, k_owned, cap, q_size, k_size, scale, dtype):
+    """The cap's tanh is a polynomial in the product where scores are near, with powers of scale / cap as coefficients.  Rows of zeros among the queries."""
+    L = lgp()
+    Tq, Tk = sum(q_owned), sum(k_owned)
+    docs, info = make_docs(q_owned, k_owned)
+    q, k, v, g = draw((Tq, 2, 32), dtype, 1, q_size), draw((Tk, 2, 32), dtype, 2, k_size), draw((Tk, 2, 32), dtype, 3), draw((Tq, 2, 32), dtype, 4)
+    q[::4] = 0
+    out, lse, rest = L.attend(q, k, v, docs, cap=cap, scale=scale, rest=True)
+    got = L.attend_backward(g, q, k, v, out, lse, docs, rest=rest, cap=cap, scale=scale)
+    want = ref.attention(q, k, v, info, g, cap=cap, scale=scale)
+    ref.check(out, want["out"], "out")
+    ref.check(lse, want["lse"], "lse")
+    for x, name in zip(got, ("dq", "dk", "dv")):
+        value, bound = want[name]
+        ref.check(x, (value, bound + 2.0 ** -110), name)
