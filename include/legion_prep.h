@@ -411,7 +411,7 @@ typedef struct {
 } lgp_documents;
 
 /* Queries, keys and values.  Strides are in elements, between rows and between heads; elements of a head are consecutive.  Strides are
- * multiples of 8 below 2^24 and pointers of 16 bytes.  heads is a multiple of kv_heads: consecutive heads / kv_heads query heads share a key head. */
+ * multiples of 8, between rows below 2^24 and between query heads below 2^26, and pointers of 16 bytes.  heads is a multiple of kv_heads: consecutive heads / kv_heads query heads share a key head. */
 typedef struct {
   const void *q, *k, *v;
   int64_t q_row, q_head, k_row, k_head, v_row, v_head;

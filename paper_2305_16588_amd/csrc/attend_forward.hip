@@ -341,8 +341,12 @@ int check_attend(const lgp_documents* d, const lgp_attention* a) {
   if ((d->q_rows && !a->q) || (d->k_rows && (!a->k || !a->v))) return LGP_EINVAL;
   if (a->slopes && ((d->q_rows && !d->q_pos) || (d->k_rows && !d->k_pos))) return LGP_EINVAL;
   if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v)) return LGP_EINVAL;
-  for (int64_t stride : {a->q_row, a->q_head, a->k_row, a->k_head, a->v_row, a->v_head, int64_t(a->heads) * a->dim})
+  // rows of tiles lie less than 2^32 bytes apart (copy_tile), and so do the query heads that are folded into them; key heads are told apart in 64 bits
+  for (int64_t stride : {a->q_row, a->k_row, a->v_row, int64_t(a->heads) * a->dim})
     if (stride < 0 || stride >= kMostStride) return LGP_EUNSUPPORTED;
+  if (a->q_head < 0 || a->q_head >= 4 * kMostStride) return LGP_EUNSUPPORTED;
+  for (int64_t stride : {a->k_head, a->v_head})
+    if (stride < 0 || stride >= int64_t(1) << 40) return LGP_EUNSUPPORTED;
   if (a->q_row % 8 || a->q_head % 8 || a->k_row % 8 || a->k_head % 8 || a->v_row % 8 || a->v_head % 8) return LGP_EINVAL;
   return LGP_OK;
 }

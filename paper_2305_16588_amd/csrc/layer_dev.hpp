@@ -76,7 +76,7 @@ template <typename T> __device__ __forceinline__ const T* in_all_lanes(const T* 
 __device__ __forceinline__ uint32_t lds_address(const void* p) { return uint32_t(uintptr_t((const __attribute__((address_space(3))) char*)p)); }
 
 // Rows in memory, `row` elements apart; with fold = 2^log2_fold each is that many rows of a tile, `head` elements apart.  Strides are below
-// 2^24, so that a wave's lanes are less than 2^32 bytes apart.
+// 2^24, and those of up to 16 heads below 2^26, so that the 32 rows that a wave's lanes are in lie less than 2^32 bytes apart.
 constexpr int64_t kMostStride = int64_t(1) << 24;
 template <typename T> struct Rows {
   const T* from;

@@ -88,7 +88,12 @@ def _heads_of(t, name: str, dtype, index: int):
     if t.dim() != 3 or t.dtype is not dtype or t.get_device() != index:
         raise _bad(f"{name}: [rows, heads, dim], {dtype}, on cuda:{index}")
     row, head, one = t.stride()
+    rows, heads, _ = t.shape
     at = t.data_ptr()
+    if rows < 2:              # the stride of a single row or head says nothing
+        row = 0
+    if heads < 2:
+        head = 0
     if one != 1 or row % 8 or head % 8 or at % 16:
         if t.numel():
             raise _bad(f"{name}: elements of a head side by side, strides in multiples of 8, aligned to 16 bytes")

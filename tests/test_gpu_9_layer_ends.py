@@ -260,3 +260,35 @@ def test_caps_of_every_size(q_owned, k_owned, cap, q_size, k_size, scale, dtype)
     for x, name in zip(got, ("dq", "dk", "dv")):
         value, bound = want[name]
         ref.check(x, (value, bound + 2.0 ** -110), name)
+
+
+@pytest.mark.parametrize("heads,kv_heads", [(4, 2), (16, 1), (3, 1), (2, 2)])
+def test_heads_before_rows_in_long_lists(heads, kv_heads):
+    """As lists that are kept by head have them: a head begins as far behind the one before as a long list is."""
+    L = lgp()
+
+    def by_head(t, apart):
+        store = torch.empty((t.shape[1] - 1) * apart + t.shape[0] * t.shape[2], dtype=t.dtype, device="cuda")
+        x = store.as_strided(t.shape, (t.shape[2], apart, 1))
+        return x.copy_(t)
+
+    for owned in ([290, 10], [1] * 300):
+        docs, info = make_docs(owned, owned)
+        q, k, v, g = (draw((300, h, 64), BF16, i) for i, h in enumerate((heads, kv_heads, kv_heads, heads)))
+        far = (by_head(q, (1 << 25) + 64), by_head(k, (1 << 28) + 8), by_head(v, 1 << 24))
+        near = L.attend(q, k, v, docs)[:2]
+        assert all(torch.equal(a, b) for a, b in zip(L.attend(*far, docs), near))
+        assert all(torch.equal(a, b) for a, b in zip(L.attend_backward(g, *far, *near, docs)[:3], L.attend_backward(g, q, k, v, *near, docs)[:3]))
+
+
+def test_strides_of_a_single_row_or_head_say_nothing():
+    L = lgp()
+    docs, _ = make_docs([1], [1])
+    x = draw((1, 3, 64), F16, 1)
+    want = L.attend(x, x[:, :1], x[:, :1], docs)[:2]
+    store = torch.empty(1 << 12, dtype=F16, device="cuda")
+    for row in (77, 1 << 30):
+        q, k = store.as_strided((1, 3, 64), (row, 64, 1)).copy_(x), store.as_strided((1, 1, 64), (row, 13, 1), 1024).copy_(x[:, :1])
+        assert all(torch.equal(a, b) for a, b in zip(L.attend(q, k, k, docs), want))
+        w = torch.ones(64, device="cuda")
+        assert all(torch.equal(a, b) for a, b in zip(L.norm_rotate(q, k, w, w), L.norm_rotate(x, x[:, :1], w, w)))
