@@ -67,7 +67,11 @@ class _There:
 
 
 def _on(index: int, stream):
-    return _Here(index) if stream is None else _There(stream)
+    if stream is None:
+        return _Here(index)
+    if stream.device_index != index:
+        raise _bad(f"stream: of cuda:{index}, where the arguments are")
+    return _There(stream)
 
 
 def _ptr(t):
@@ -146,8 +150,12 @@ def _attention(q, k, v, docs: Documents, slopes, cap: float, scale):
             raise _bad("slopes: float32[heads]")
         if (docs.q_pos is None and q_rows) or (docs.k_pos is None and k_rows):
             raise _bad("slopes need positions of queries and keys")
-    return docs._rows(q_rows, k_rows), _attention_of(qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, heads, kv_heads, dim, _DTYPE[dtype],
-                                                      dim ** -0.5 if scale is None else scale, cap, _ptr(slopes))
+    rows = docs._rows(q_rows, k_rows)
+    try:
+        return rows, _attention_of(qp, kp, vp, q_row, q_head, k_row, k_head, v_row, v_head, heads, kv_heads, dim, _DTYPE[dtype],
+                                   dim ** -0.5 if scale is None else scale, cap, _ptr(slopes))
+    except (OverflowError, struct.error):
+        raise _bad("scale and cap: numbers that float32 holds") from None
 
 
 def _workspace(index: int, device, query, *args):
@@ -225,8 +233,12 @@ def _norm(q, k, q_weight, k_weight, pos, table, eps: float):
         if table.dim() != 2 or table.dtype is not torch.float32 or table.get_device() != index or not table.is_contiguous() or at % 16 or pos is None:
             raise _bad("table: float32[positions, rot], aligned to 16 bytes, and pos with it")
         n_pos, rot = table.shape
-    return index, _heads(qp, kp, q_row, q_head, k_row, k_head, tokens, heads, kv_heads, dim, _DTYPE[dtype], _weight(q_weight, "q_weight", dim, index),
-                         _weight(k_weight, "k_weight", dim, index), _ints(pos, tokens, index, "pos"), rot, n_pos, at, eps)
+    args = (qp, kp, q_row, q_head, k_row, k_head, tokens, heads, kv_heads, dim, _DTYPE[dtype], _weight(q_weight, "q_weight", dim, index),
+            _weight(k_weight, "k_weight", dim, index), _ints(pos, tokens, index, "pos"), rot, n_pos, at)
+    try:
+        return index, _heads(*args, eps)
+    except (OverflowError, struct.error):
+        raise _bad("eps: a number that float32 holds") from None
 
 
 def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-6, stream=None):

@@ -1,5 +1,6 @@
 """Operators of a model layer at the ends of their ranges, against their definitions in 64 bits (tests/layer_common.py)."""
 import math
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -292,3 +293,16 @@ def test_strides_of_a_single_row_or_head_say_nothing():
         assert all(torch.equal(a, b) for a, b in zip(L.attend(q, k, k, docs), want))
         w = torch.ones(64, device="cuda")
         assert all(torch.equal(a, b) for a, b in zip(L.norm_rotate(q, k, w, w), L.norm_rotate(x, x[:, :1], w, w)))
+
+
+def test_numbers_and_streams_that_do_not_fit_are_refused():
+    L = lgp()
+    docs, _ = make_docs([4], [4])
+    q, w = draw((4, 2, 64), F16, 1), torch.ones(64, device="cuda")
+    x = torch.ones((4, 8), device="cuda")
+    elsewhere = SimpleNamespace(device_index=1, cuda_stream=0)
+    for f in (lambda: L.attend(q, q, q, docs, cap=1e39), lambda: L.attend(q, q, q, docs, scale=-1e300), lambda: L.attend(q, q, q, docs, scale="1"),
+              lambda: L.norm_rotate(q, q, w, w, eps=1e39), lambda: L.attend(q, q, q, docs, stream=elsewhere), lambda: L.norm_rotate(q, q, w, w, stream=elsewhere),
+              lambda: L.pack_activations(x, stream=elsewhere)):
+        with pytest.raises(L.LegionPrepError):
+            f()
