@@ -2,7 +2,8 @@
 held in 8 bits (argument checks and marshalling only; the kernels are the library's).
 
 Arguments that make no sense raise LegionPrepError before anything is launched.  Results and workspaces are allocated for the stream
-that the kernels run on.
+that the kernels run on.  attend and norm_rotate are differentiable: where a gradient is wanted of an input, their results carry it.  Packed
+activations are what a backward pass keeps, and no gradient passes through them.
 """
 from __future__ import annotations
 
@@ -10,6 +11,7 @@ import ctypes as C
 import struct
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from .binding import LegionPrepError, _Attention, _Documents, _Heads, _Packed, _raw_stream, load_library
 
@@ -164,13 +166,35 @@ def _workspace(index: int, device, query, *args):
     return (torch.empty(size.value, dtype=torch.uint8, device=device) if size.value else None), size.value
 
 
+class _Attend(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, slopes, docs, cap, scale):
+        out, lse, rest = attend(q, k, v, docs, slopes=slopes, cap=cap, scale=scale, rest=True)
+        ctx.save_for_backward(q, k, v, slopes, out, lse, rest)
+        ctx.mark_non_differentiable(lse, rest)
+        ctx.of = docs, cap, scale
+        return out, lse, rest
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_out, *_):
+        q, k, v, slopes, out, lse, rest = ctx.saved_tensors
+        docs, cap, scale = ctx.of
+        return *attend_backward(d_out, q, k, v, out, lse, docs, rest=rest, slopes=slopes, cap=cap, scale=scale), None, None, None
+
+
 def attend(q, k, v, docs: Documents, slopes=None, cap: float = 0.0, scale: float | None = None, rest: bool = False, stream=None):
     """Attention of every query to the keys of its document; (out, lse, rest).
 
     q [q_rows, heads, dim], k and v [k_rows, kv_heads, dim]: float16 or bfloat16, dim a multiple of 8 up to 128.  Scores are scale * q.k
     (dim^-1/2 by default), capped as cap * tanh(. / cap) where cap > 0, less slopes[head] * |q_pos - k_pos| where slopes (float32[heads]) are
     given.  out is like q, end to end; lse (float32[q_rows, heads]) is the logarithm of the sum of exp(score).  Queries without keys and rows
-    without tokens get zeros and -inf.  rest: also return what the rounding of out took off, for attend_backward."""
+    without tokens get zeros and -inf.  rest: also return what the rounding of out took off, for attend_backward.  Gradients pass through out, not
+    through lse or rest."""
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad)):
+        with _on(docs.index, stream):
+            out, lse, left = _Attend.apply(q, k, v, slopes, docs, cap, scale)
+        return out, lse, left if rest else None
     L = load_library()
     d, a = _attention(q, k, v, docs, slopes, cap, scale)
     device = q.device
@@ -241,10 +265,26 @@ def _norm(q, k, q_weight, k_weight, pos, table, eps: float):
         raise _bad("eps: a number that float32 holds") from None
 
 
+class _NormRotate(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, pos, table, eps):
+        ctx.save_for_backward(q, k, q_weight, k_weight, pos, table)
+        ctx.eps = eps
+        return norm_rotate(q, k, q_weight, k_weight, pos, table, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        return *norm_rotate_backward(dq_out, dk_out, *ctx.saved_tensors, eps=ctx.eps), None, None, None
+
+
 def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-6, stream=None):
     """RMS norm of every head of q [tokens, heads, dim] and k [tokens, kv_heads, dim] with weights (float32[dim]), and the rotation of its first
     table.shape[1] elements by the token's position (rotation_table); new tensors (q, k), rows end to end.  dim: a multiple of 8 up to 256.
     Rows of a negative pos have no token and become zeros; those of a position beyond the table become NaN."""
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad):
+        with _on(q.get_device(), stream):
+            return _NormRotate.apply(q, k, q_weight, k_weight, pos, table, eps)
     L = load_library()
     index, h = _norm(q, k, q_weight, k_weight, pos, table, eps)
     with _on(index, stream) as on:

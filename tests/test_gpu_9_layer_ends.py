@@ -306,3 +306,33 @@ def test_numbers_and_streams_that_do_not_fit_are_refused():
               lambda: L.pack_activations(x, stream=elsewhere)):
         with pytest.raises(L.LegionPrepError):
             f()
+
+
+@pytest.mark.parametrize("side", [False, True])
+def test_gradients_pass_through_the_operators(side):
+    """What autograd makes of attend and norm_rotate is what their backward calls return, on the current stream and on another."""
+    L = lgp()
+    docs, info = make_docs([40, 1, 200], [40, 1, 200], [33, 1, 200], [33, 1, 200])
+    qkv = draw((241, 8, 64), BF16, 1).requires_grad_()
+    wq, wk, slopes = (draw((n,), F32, 2 + i).abs().requires_grad_() for i, n in enumerate((64, 64, 4)))
+    pos, table = torch.arange(241, device="cuda", dtype=torch.int32), L.rotation_table(300, 32)
+    g = draw((241, 4, 64), BF16, 5)
+    stream = torch.cuda.Stream() if side else None
+    if side:
+        stream.wait_stream(torch.cuda.current_stream())
+    q, k = L.norm_rotate(qkv[:, :4], qkv[:, 4:6], wq, wk, pos, table, stream=stream)
+    out, lse, rest = L.attend(q, k, qkv[:, 6:], docs, slopes=slopes, cap=20.0, stream=stream)
+    assert out.requires_grad and not lse.requires_grad and rest is None
+    if side:
+        torch.cuda.current_stream().wait_stream(stream)
+    out.backward(g)
+    torch.cuda.synchronize()
+    with torch.no_grad():
+        args = (qkv[:, :4], qkv[:, 4:6], wq, wk, pos, table)
+        q2, k2 = L.norm_rotate(*args)
+        out2, lse2, rest2 = L.attend(q2, k2, qkv[:, 6:], docs, slopes=slopes, cap=20.0, rest=True)
+        assert not out2.requires_grad and torch.equal(out2, out) and torch.equal(lse2, lse)
+        dq, dk, dv, ds = L.attend_backward(g, q2, k2, qkv[:, 6:], out2, lse2, docs, rest=rest2, slopes=slopes, cap=20.0)
+        dq, dk, dwq, dwk = L.norm_rotate_backward(dq, dk, *args)
+    assert torch.equal(qkv.grad, torch.cat([dq, dk, dv], 1)) and torch.equal(slopes.grad, ds) and torch.equal(wq.grad, dwq) and torch.equal(wk.grad, dwk)
+    assert not L.unpack_activations(L.pack_activations(qkv.flatten(1))).requires_grad
