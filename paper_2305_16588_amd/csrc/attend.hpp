@@ -26,6 +26,7 @@ struct AttendParams {
   bool negate;
   const float* slopes;
   float docs_per_tile;
+  uint32_t first;            // workgroups of launches before this one
   int32_t tiles, splits;     // tiles of queries per key head (backward by keys: of keys); parts of the keys; attend_single.hip: workgroups with documents,
                              // and before them those that list the large ones
   // forward

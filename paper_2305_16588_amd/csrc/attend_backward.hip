@@ -197,7 +197,7 @@ __device__ __forceinline__ void dq_rows(const AttendParams& p, int32_t hk, int32
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
 __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kernel(const AttendParams p) {
   constexpr int kRows = 32 * NW;
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  uint32_t piece = p.first + piece_of(blockIdx.x, gridDim.x);
   int32_t split = 0, hk, tile;
   if constexpr (NW == 1) {
     hk = piece % p.kv_heads;
@@ -451,7 +451,7 @@ __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int3
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
 __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_kernel(const AttendParams p) {
   constexpr int kKeys = 32 * NW;
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  uint32_t piece = p.first + piece_of(blockIdx.x, gridDim.x);
   int32_t hk, tile;
   if constexpr (NW == 1) {
     hk = piece % p.kv_heads;
@@ -509,17 +509,18 @@ template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams
   AttendParams x = p;
   x.tiles = int32_t(b.q.tiles);
   x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.q.tiles, 1));
-  const uint32_t blocks = uint32_t(b.q.tiles) * p.kv_heads * p.splits, key_blocks = uint32_t(b.key_tiles) * p.kv_heads;
-  if (p.qs.rows) {
+  if (p.qs.rows) in_launches(b.q.tiles * p.kv_heads * p.splits, 64 * b.q.waves, [&](uint32_t first, uint32_t blocks) {
+    x.first = first;
     if (b.q.waves == 1) attend_dq_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
     else attend_dq_kernel<T, D, CAP, BIAS, 4, 32><<<blocks, 256, 0, s>>>(x);
-  }
+  });
   x.tiles = int32_t(b.key_tiles);
   x.docs_per_tile = float(p.n_docs) / float(std::max<int64_t>(b.key_tiles, 1));
-  if (p.ks.rows) {
-    if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<key_blocks, 64, 0, s>>>(x);
-    else attend_dkv_kernel<T, D, CAP, BIAS, 4, 32><<<key_blocks, 256, 0, s>>>(x);
-  }
+  if (p.ks.rows) in_launches(b.key_tiles * p.kv_heads, 64 * b.key_waves, [&](uint32_t first, uint32_t blocks) {
+    x.first = first;
+    if (b.key_waves == 1) attend_dkv_kernel<T, D, CAP, BIAS, 1, 32><<<blocks, 64, 0, s>>>(x);
+    else attend_dkv_kernel<T, D, CAP, BIAS, 4, 32><<<blocks, 256, 0, s>>>(x);
+  });
 }
 template <typename T, int D> void launch(const AttendParams& p, const BackwardShape& b, bool cap, hipStream_t s) {
   if (cap) p.slopes ? launch<T, D, true, true>(p, b, s) : launch<T, D, true, false>(p, b, s);

@@ -221,7 +221,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, i
 template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
 __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_kernel(const AttendParams p) {
   constexpr int kRows = 32 * NW;
-  uint32_t piece = piece_of(blockIdx.x, gridDim.x);
+  uint32_t piece = p.first + piece_of(blockIdx.x, gridDim.x);
   int32_t split = 0, hk, tile;
   if constexpr (NW == 1) {          // short documents: the heads of a token lie side by side in memory
     hk = piece % p.kv_heads;
@@ -300,10 +300,13 @@ template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams
     attend_large_kernel<T, D, CAP, BIAS><<<uint32_t(f.tiles), 256, 0, s>>>(p);
     return;
   }
-  const uint32_t blocks = uint32_t(p.tiles) * p.kv_heads * p.splits;
-  if (f.waves > 1) attend_kernel<T, D, CAP, BIAS, 4, 1, 64><<<blocks, 256, 0, s>>>(p);
-  else if (f.key_waves > 1) attend_kernel<T, D, CAP, BIAS, 1, 4, 32><<<blocks, 256, 0, s>>>(p);
-  else attend_kernel<T, D, CAP, BIAS, 1, 1, 32><<<blocks, 64, 0, s>>>(p);
+  in_launches(int64_t(p.tiles) * p.kv_heads * p.splits, 64 * f.waves * f.key_waves, [&](uint32_t first, uint32_t blocks) {
+    AttendParams x = p;
+    x.first = first;
+    if (f.waves > 1) attend_kernel<T, D, CAP, BIAS, 4, 1, 64><<<blocks, 256, 0, s>>>(x);
+    else if (f.key_waves > 1) attend_kernel<T, D, CAP, BIAS, 1, 4, 32><<<blocks, 256, 0, s>>>(x);
+    else attend_kernel<T, D, CAP, BIAS, 1, 1, 32><<<blocks, 64, 0, s>>>(x);
+  });
 }
 template <typename T, int D> void launch(const AttendParams& p, const ForwardShape& f, bool cap, hipStream_t s) {
   if (cap) p.slopes ? launch<T, D, true, true>(p, f, s) : launch<T, D, true, false>(p, f, s);

@@ -18,7 +18,7 @@ template <int L> struct Lanes {
   int32_t doc, hk;
   __device__ __forceinline__ Lanes(const AttendParams& p, int32_t heads_at_once) {
     const int lane = threadIdx.x & 63, slot = lane / L;
-    const int64_t unit = int64_t(piece_of(blockIdx.x - p.splits, p.tiles)) * 4 + (threadIdx.x >> 6);
+    const int64_t unit = (int64_t(p.first) + piece_of(blockIdx.x - p.splits, p.tiles)) * 4 + (threadIdx.x >> 6);
     const int32_t chunks = (p.kv_heads + heads_at_once - 1) / heads_at_once;
     doc = __builtin_amdgcn_readfirstlane(int32_t(unit / chunks));
     c = lane % L;
@@ -303,12 +303,15 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
 
 template <typename T, int L, int G, bool CAP, bool BIAS> void launch(const AttendParams& p, bool backward, hipStream_t s) {
   const int32_t at_once = std::min(p.kv_heads, 64 / L), chunks = (p.kv_heads + at_once - 1) / at_once;
-  AttendParams x = p;
-  x.tiles = int32_t((int64_t(p.n_docs) * chunks + 3) / 4);
-  x.splits = p.n_large ? (p.n_docs + 4 * kSurvey - 1) / (4 * kSurvey) : 0;
-  const uint32_t blocks = uint32_t(x.splits) + uint32_t(x.tiles);
-  if (backward) single_backward_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
-  else single_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
+  in_launches((int64_t(p.n_docs) * chunks + 3) / 4, 256, [&](uint32_t first, uint32_t groups) {
+    AttendParams x = p;
+    x.first = first;
+    x.tiles = int32_t(groups);
+    x.splits = p.n_large && !first ? (p.n_docs + 4 * kSurvey - 1) / (4 * kSurvey) : 0;
+    const uint32_t blocks = uint32_t(x.splits) + groups;
+    if (backward) single_backward_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
+    else single_kernel<T, L, G, CAP, BIAS><<<blocks, 256, 0, s>>>(x, at_once);
+  });
 }
 template <typename T, int L, int G> void launch(const AttendParams& p, bool cap, bool backward, hipStream_t s) {
   if (cap) p.slopes ? launch<T, L, G, true, true>(p, backward, s) : launch<T, L, G, true, false>(p, backward, s);

@@ -246,6 +246,11 @@ inline int use_device(int device) {
   }
   return LGP_OK;
 }
+// A launch has less than 2^32 threads, and what is beyond is dropped without an error: f(first workgroup, workgroups) for as many launches as it takes.
+template <typename F> void in_launches(int64_t groups, int64_t threads, F f) {
+  const int64_t most = (int64_t(1) << 31) / threads;
+  for (int64_t g = 0; g < groups; g += most) f(uint32_t(g), uint32_t(groups - g < most ? groups - g : most));
+}
 inline int launched() { return hipGetLastError() == hipSuccess ? LGP_OK : LGP_EHIP; }
 inline int compute_units(int device) {
   int n = 0;

@@ -235,17 +235,28 @@ int32_t heads_side(int device, const lgp_heads* h, bool backward) {
   while ((l << side) < most && (1 << side) < std::max(h->heads, h->kv_heads)) ++side;
   return side;
 }
-template <typename T> void forward(const NormParams& p, hipStream_t s) {
-  const int l = lanes_of(p.dim);
-  const dim3 blocks(uint32_t(((p.tokens * l << p.log2_side) + 255) / 256), p.apart ? 2 : 1);
-  switch (l) {
-    case 1: norm_rotate_kernel<T, 1><<<blocks, 256, 0, s>>>(p); break;
-    case 2: norm_rotate_kernel<T, 2><<<blocks, 256, 0, s>>>(p); break;
-    case 4: norm_rotate_kernel<T, 4><<<blocks, 256, 0, s>>>(p); break;
-    case 8: norm_rotate_kernel<T, 8><<<blocks, 256, 0, s>>>(p); break;
-    case 16: norm_rotate_kernel<T, 16><<<blocks, 256, 0, s>>>(p); break;
-    default: norm_rotate_kernel<T, 32><<<blocks, 256, 0, s>>>(p); break;
-  }
+template <typename T> void forward(const NormParams& whole, hipStream_t s) {
+  const int l = lanes_of(whole.dim);
+  const int64_t per_group = std::max(1, 256 / l >> whole.log2_side);        // tokens
+  in_launches((whole.tokens + per_group - 1) / per_group, 256, [&](uint32_t first, uint32_t groups) {
+    const int64_t t0 = first * per_group;
+    NormParams p = whole;
+    p.tokens = std::min(whole.tokens - t0, groups * per_group);
+    p.q = static_cast<const T*>(whole.q) + t0 * whole.q_row;
+    p.k = static_cast<const T*>(whole.k) + t0 * whole.k_row;
+    p.q_out = static_cast<T*>(whole.q_out) + t0 * whole.heads * whole.dim;
+    p.k_out = static_cast<T*>(whole.k_out) + t0 * whole.kv_heads * whole.dim;
+    if (whole.pos) p.pos = whole.pos + t0;
+    const dim3 blocks(groups, p.apart ? 2 : 1);
+    switch (l) {
+      case 1: norm_rotate_kernel<T, 1><<<blocks, 256, 0, s>>>(p); break;
+      case 2: norm_rotate_kernel<T, 2><<<blocks, 256, 0, s>>>(p); break;
+      case 4: norm_rotate_kernel<T, 4><<<blocks, 256, 0, s>>>(p); break;
+      case 8: norm_rotate_kernel<T, 8><<<blocks, 256, 0, s>>>(p); break;
+      case 16: norm_rotate_kernel<T, 16><<<blocks, 256, 0, s>>>(p); break;
+      default: norm_rotate_kernel<T, 32><<<blocks, 256, 0, s>>>(p); break;
+    }
+  });
 }
 template <typename T> void backward(const NormParams& p, uint32_t blocks, hipStream_t s) {
   switch (lanes_of(p.dim)) {
@@ -263,7 +274,7 @@ int check_norm(const lgp_heads* h) {
   if (h->tokens < 0 || h->heads < 0 || h->kv_heads < 0 || h->heads + h->kv_heads < 1 || h->dim < 1 || h->rot < 0 || h->rot > h->dim) return LGP_EINVAL;
   if (h->dtype != LGP_F32 && h->dtype != LGP_F16 && h->dtype != LGP_BF16) return LGP_EUNSUPPORTED;
   if (h->dim % 8 || h->dim > 256 || h->rot % 16) return LGP_EUNSUPPORTED;
-  if (h->heads > 65536 || h->kv_heads > 65536 || h->tokens >= int64_t(1) << 33) return LGP_EUNSUPPORTED;       // workgroups below 2^31
+  if (h->heads > 65536 || h->kv_heads > 65536 || h->tokens >= int64_t(1) << 33) return LGP_EUNSUPPORTED;
   if (h->tokens && ((h->heads && !h->q) || (h->kv_heads && !h->k))) return LGP_EINVAL;
   if ((h->heads && !h->q_weight) || (h->kv_heads && !h->k_weight)) return LGP_EINVAL;
   if (h->rot && (!h->table || h->n_pos < 1 || (h->tokens && !h->pos))) return LGP_EINVAL;

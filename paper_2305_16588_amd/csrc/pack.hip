@@ -333,6 +333,7 @@ PackParams pack_params(const lgp_packed* a, int32_t per_row) {
   p.values = a->values;
   p.exps = a->exps;
   p.rows_each = std::max<int32_t>(1, 1024 / per_row);      // about four rounds of 256 lanes
+  while (p.tokens / p.rows_each >= int64_t(1) << 23) p.rows_each *= 2;       // a launch has less than 2^32 threads
   return p;
 }
 // Parts of the tokens: two workgroups per CU, of at least 256 tokens each.

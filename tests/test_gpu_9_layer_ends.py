@@ -336,3 +336,60 @@ def test_gradients_pass_through_the_operators(side):
         dq, dk, dwq, dwk = L.norm_rotate_backward(dq, dk, *args)
     assert torch.equal(qkv.grad, torch.cat([dq, dk, dv], 1)) and torch.equal(slopes.grad, ds) and torch.equal(wq.grad, dwq) and torch.equal(wk.grad, dwk)
     assert not L.unpack_activations(L.pack_activations(qkv.flatten(1))).requires_grad
+
+
+@pytest.fixture
+def room():
+    """Most of the GPU's memory."""
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_head_norms_of_more_rows_than_a_launch_has_threads(room):
+    """134 million rows of 32 lanes each; all but two of them are one row in memory."""
+    L = lgp()
+    T, at = (1 << 27) + 5, (1 << 26) + 3
+    rows = draw((2, 1, 256), F16, 1)
+    q, none = rows[:1].expand(T, 1, 256), torch.empty((T, 0, 256), dtype=F16, device="cuda")
+    w = draw((256,), F32, 2)
+    pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+    pos[at], pos[T - 1] = 7, -1
+    table = L.rotation_table(8, 64)
+    out = L.norm_rotate(q, none, w, w, pos, table)[0]
+    want = L.norm_rotate(rows[:1].expand(3, 1, 256).contiguous(), none[:3], w, w, pos[[0, at, T - 1]], table)[0]
+    assert torch.equal(out[[0, at, T - 1]], want)
+    out[at], out[T - 1] = want[0], want[0]
+    assert all((part == want[0]).all() for part in out.split(1 << 24))
+
+
+def test_packing_of_more_rows_than_a_launch_has_threads(room):
+    L = lgp()
+    T = (1 << 31) - 1                                           # 147 GB of results
+    x = draw((1, 64), F16, 1)
+    p = L.pack_activations(x.expand(T, 64))
+    want = L.pack_activations(x)
+    for got, one in ((p.values, want.values), (p.exps, want.exps)):
+        assert all((part == one).all() for part in got.split(1 << 26))
+
+
+def test_documents_of_more_tiles_than_a_launch_has_threads(room):
+    """2.2 million documents of two rows, 32 heads: a wave each for 75 million tiles."""
+    L = lgp()
+    n, H, D = 2_200_000, 32, 8
+    offs = torch.arange(n + 1, dtype=torch.int32, device="cuda") * 2
+    docs = L.Documents(offs, offs)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, d_out = (torch.randn((2 * n, H, D), generator=g, device="cuda", dtype=F16) for _ in range(4))
+    out, lse, rest = L.attend(q, k, v, docs, rest=True)
+    got = out, *L.attend_backward(d_out, q, k, v, out, lse, docs, rest=rest)[:3]
+    for d in (0, n // 2, n - 50_000):
+        rows = slice(2 * d, 2 * d + 100_000)
+        a, b, c, e = (t[rows].view(-1, 2, H, D).float().transpose(1, 2) for t in (q, k, v, d_out))
+        P = torch.softmax((a[:, :, :, None] * b[:, :, None]).sum(-1) * D ** -0.5, 3)                # [documents, H, 2, 2]
+        o = (P[..., None] * c[:, :, None]).sum(3)
+        dS = P * ((e[:, :, :, None] * c[:, :, None]).sum(-1) - (e * o).sum(-1, keepdim=True)) * D ** -0.5
+        want = o, (dS[..., None] * b[:, :, None]).sum(3), (dS[..., None] * a[:, :, :, None]).sum(2), (P[..., None] * e[:, :, :, None]).sum(2)
+        for x, y, name in zip(got, want, ("out", "dq", "dk", "dv")):
+            # terms of up to 40, a few units each
+            assert (x[rows].view(-1, 2, H, D).float().transpose(1, 2) - y).abs().max() < 40 * 4 * ref.UNIT[F16], f"{name}, document {d}"
