@@ -168,9 +168,9 @@ template <typename T> constexpr float kLiftLog2 = 0.f;
 template <> inline constexpr float kLiftLog2<f16> = 12.f;
 
 // dU has no such bound on either side: it is as small as the gradients of a mean over a batch and the probabilities together, or as large as those of
-// a loss that was scaled up.  With fp16 it is taken times a power of two for each column of a product: 2^64 at first, and lowered, with what has been
-// added up, when one comes out beyond kLiftedMost.
-constexpr float kLiftFirstLog2 = 64.f, kLiftFirst = 0x1p64f, kLiftedMost = 32768.f;
+// a loss that was scaled up.  With fp16 it is taken times a power of two for each column of a product: 2^48 at first, and lowered, with what has been
+// added up, when one comes out beyond kLiftedMost.  (Of numbers of fp16 the largest dU is 2^39, times a distance of 2^24 in the sums for the slopes.)
+constexpr float kLiftFirstLog2 = 48.f, kLiftFirst = 0x1p48f, kLiftedMost = 32768.f;
 // By what power of two: `most` then is 512 to 1024, which leaves room for larger ones.
 __device__ __forceinline__ int lower_log2(float most) { return 10 - __builtin_amdgcn_frexp_expf(most); }
 

@@ -180,6 +180,19 @@ def test_large_gradients_in_fp16(dim, rows):
         assert err <= own + 4 * ref.UNIT[F16], f"{name}: {err:.3g}, rounding alone {own:.3g}"
 
 
+def test_the_largest_gradients_in_fp16_over_long_distances():
+    """The sums for the slopes' gradient hold dU times distances of up to 2^24."""
+    L = lgp()
+    docs, info = make_docs([64], [128])
+    info["k_pos"].copy_(torch.arange(128, device="cuda") * (1 << 17))
+    q, k, v = draw((64, 2, 64), F16, 1, 0.1), draw((128, 2, 64), F16, 2, 0.1), draw((128, 2, 64), F16, 3, 60.0)
+    g = draw((64, 2, 64), F32, 4, 12000.0).half()
+    slopes = torch.full((2,), 1e-7, device="cuda")
+    out, lse, rest = L.attend(q, k, v, docs, slopes=slopes, rest=True)
+    ds = L.attend_backward(g, q, k, v, out, lse, docs, rest=rest, slopes=slopes)[3]
+    ref.check(ds, ref.attention(q, k, v, info, g, slopes)["d_slopes"], "d_slopes")
+
+
 def milliseconds(f):
     f()
     a, b = (torch.cuda.Event(enable_timing=True) for _ in range(2))
@@ -240,6 +253,17 @@ def test_large_documents_in_graphs_and_twice():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, step())), f"replay {r}"
+
+
+def test_many_large_documents_in_a_row():
+    """More than a wave lists and goes through at once, at the ends of a long list of documents."""
+    n = 40_000
+    q_owned, k_owned = [0] * n, [2] * n
+    for d in [*range(100), 511, 512, 513, 20_000, *range(n - 90, n)]:
+        q_owned[d], k_owned[d] = 23, 24
+    q_owned[30_000], q_owned[30_001] = 1, 1
+    docs, info = make_docs(q_owned, k_owned)
+    run_attention(docs, info, 2, 1, 32, F16, 20.0, True)
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
