@@ -56,7 +56,8 @@ template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p, bool 
 // The cap: a product qk becomes tanh(x) / t_mul with x = qk * t_mul, which is qk where the cap is far.  Up to x = kNear that is
 // qk (1 + c0 x^2 + c1 x^4 + c2 x^6 + c3 x^8), fitted by least squares of the relative error, reweighted until even: 1e-7 with its roundings, and it
 // is where capped scores mostly are; the powers of t_mul are in the coefficients.  Beyond, tanh(x) = 1 - 2 / (e^2x + 1), which near zero would be 1e-7
-// off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.  Where the powers of t_mul leave the range of
+// off in absolute terms, times the cap.  Scores of a tile go the short way together, if none is beyond.  Cap 30, scores of about 1, 4 and 16: 1024
+// documents of 276, heads 8/8 of 32, 331, 342 and 437 us forward; 128 of 916, heads of 64, 428, 453 and 628.  Where the powers of t_mul leave the range of
 // fp32 -- products of millions below a cap of a million, caps of millionths -- all go the other way, which takes x first.
 constexpr float kNear = 0.55f;
 constexpr float kTanh[4] = {-0.3333294689655304f, 0.13320724666118622f, -0.05267181620001793f, 0.016437582671642303f};
@@ -179,8 +180,11 @@ constexpr int waves_per_simd(int dim, int waves) { return dim == 32 ? 4 : dim ==
 
 // Launch shapes, chosen on the host by what it knows: rows and documents.
 // Whether a workgroup is one wave of 32 rows, which waits for no other but has its tiles to itself: documents of up to 32 rows, and with heads of up
-// to 32, whose tiles are small, of up to 320 (1024 documents of 276 rows, half of them with tokens, heads of 32: forward 295 us with four waves, 281
-// with one, gradients of q 336 and 303, of k and v 321 and 312; 256 of 916 folded rows, heads of 64: forward 198 and 284).
+// to 32, whose tiles are small, of up to 320.  Four waves and one, us forward / backward, bf16, heads 8/8 of 32, half of the rows without a token: with cap
+// and bias, 4000 documents of 100 rows 279 / 785 and 209 / 626, 1050 of 276 239 / 618 and 216 / 552, 781 of 320 188 / 546 and 188 / 506, 320 of 500
+// 144 / 414 and 148 / 421; without, 245 / 617 and 199 / 551, 176 / 471 and 184 / 476, 153 / 408 and 167 / 432, 95 / 282 and 105 / 314.  With all rows full
+// and neither cap nor bias four waves are ahead from 100 rows on (297 / 861 and 325 / 891; at 320 234 / 651 and 293 / 728), which the host cannot tell.
+// 256 documents of 916 folded rows, heads of 64: forward 198 and 284.
 inline bool one_wave(int64_t rows, int64_t docs, int32_t dim) { return rows <= (dim <= 32 ? 320 : 32) * docs; }
 constexpr int kMostSplits = 256;        // a thread of join_kernel each
 constexpr int kForwardRows = 32;        // folded rows of a wave

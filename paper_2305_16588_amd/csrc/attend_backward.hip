@@ -13,11 +13,11 @@ namespace {
 //     dS = P (dP - delta),  dU = dS (1 - tanh^2),  dq = scale * sum_j dU k_j.
 // Everything is transposed, as in the forward kernel: columns are folded rows.  dU is rounded to the type of k for the last product, as k itself is; with
 // fp16 it is lifted first (kLiftFirst).
-// delta is taken from out and what its rounding took off.  The slope of a head has the gradient
+// delta is taken from out and what its rounding took off, so it has the rounding of the probabilities that made out and not that of out.  The slope of a head has the gradient
 //     - sum dS |distance| = - sum_rows (sum_j dS |distance| - (sum_j dS) (sum_j P |distance|) / sum_j P) / sum_j P,
 // whose four sums per row go to `sums`: the second term is what the rounding of out and of lse left in dS, so the gradient depends on neither.
-// Measured: 4 documents of 8192 tokens, heads 8/4 of 128, bf16, bias: 1662 us, 0.99 PFLOP/s, matrix instructions 49 % and vector instructions 61 %
-// of the cycles; 1024 documents of 276 rows, heads 8/8 of 32, cap and bias: 282 us, vector instructions 88 %.
+// Measured: 4 documents of 8192 tokens, heads 8/4 of 128, bf16, bias: 1595 to 1640 us, 1.02 PFLOP/s, matrix instructions 49 % and vector instructions
+// 61 % of the cycles; 1024 documents of 276 rows, heads 8/8 of 32, cap and bias: 270 us, vector instructions 86 %.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BN>
 __device__ __forceinline__ void dq_rows(const AttendParams& p, int32_t hk, int32_t split, int32_t row0, const Span qd, const Span kd) {
   constexpr int kThreads = 64 * NW;
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(kEndThreads) void slopes_end_kernel(const double* p
 
 // Gradients of k and v: a wave has 32 keys as columns and walks over the folded rows of their document, BQ at a time, in LDS.
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
-// Measured, at the sizes of attend_dq_kernel: 2200 us, 1.00 PFLOP/s, matrix instructions 45 % of the cycles of two waves per SIMD that wait for each
-// other's tiles; 303 us, vector instructions 69 %.
+// Measured, at the sizes of attend_dq_kernel: 2115 to 2180 us, 1.02 PFLOP/s, matrix instructions 45 % of the cycles of two waves per SIMD that wait for each
+// other's tiles; 304 us, vector instructions 66 %.
 template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
 __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int32_t key0, const Span kd, const Span qd) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;

@@ -15,12 +15,14 @@ namespace {
 // when a row's maximum has outgrown it by 2^kSlack: after the first tiles that is rare, and it would be a quarter of the arithmetic.  The base is
 // settled before anything is taken off: a difference from a base that a tile leaves far behind would be rounded at the size of that distance.  The
 // two places of a tile are two copies of the loop's body, so that no address is computed in it.
-// Probabilities are rounded to the type of v for the second product, as the values themselves are; their sum is taken before.
+// Probabilities are rounded to the type of v for the second product, as the values themselves are: 32 bits there would want the fp32 matrix
+// instructions, at a fraction of the rate.  Their sum is taken before, which lse wants; dividing by the sum of the rounded ones instead was level in error and 1 to 4 % dearer.  Error
+// in the 2-norm of bf16 results 0.0024 where one rounding at the end has 0.0017, of fp16 2.9e-4 and 2.1e-4.
 // Where a document has no more rows than a wave (NW 1), KW waves have the same rows and every KW-th tile of the keys each, in tiles of their own,
 // and their results are joined in LDS.
-// Measured: 4 documents of 8192 tokens, heads 8/4 of 128, bf16, bias: 1285 us, 0.86 PFLOP/s, bound by matrix and vector instructions (40 and 61 % of
-// the cycles); 1024 documents of 276 rows, heads 8/8 of 32, cap and bias: 260 us, bound by the vector instructions of cap, bias and exponent; 16
-// queries over 50 001 keys each, heads 16/2 of 128: 158 us, bound by bytes, 5.2 TB/s.
+// Measured: 4 documents of 8192 tokens, heads 8/4 of 128, bf16, bias: 1220 to 1250 us, 0.89 PFLOP/s, bound by matrix and vector instructions (41 and
+// 60 % of the cycles); 1024 documents of 276 rows, heads 8/8 of 32, cap and bias: 260 us, bound by the vector instructions of cap, bias and exponent
+// (70 %); 256 of 916, heads 4/2 of 64, cap: 158 us, likewise (88 %); 16 queries over 50 001 keys each, heads 16/2 of 128: 159 us, bound by bytes, 5.2 TB/s.
 constexpr float kSlack = 8.f;
 template <typename T, int D, bool CAP, bool BIAS, int NW, int KW, int BN>
 __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, int32_t split, int32_t row0, const Span qd, const Span kd) {

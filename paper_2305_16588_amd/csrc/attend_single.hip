@@ -2,7 +2,7 @@
 // one row in 32 to work on and a wave per head little to read; here a wave takes all heads of a document, reads every key and value row once
 // and end to end, and computes in fp32 lanes.  Both passes are bound by those bytes: the backward pass has one query per key, so the gradients of
 // its row of k and v are ready as it is read and everything is read once and written once.  Measured: 122 880 documents of up to 10 keys, 8 heads
-// of 32, fp16: 183 us forward, 403 backward, where the bytes take 577 together at the rate of a copy.
+// of 32, fp16: 186 us forward, 399 backward, where the bytes take 577 together at the rate of a copy.
 #include "attend.hpp"
 
 #include <algorithm>
@@ -330,6 +330,10 @@ template <typename T> void launch(const AttendParams& p, bool cap, bool backward
 
 }  // namespace
 
+// Up to two heads of a key head (a lane holds a query and a result for each of them) and 64 keys on average.  These kernels and the tiled ones, us
+// forward / backward, fp16: heads 8/4 of 64, 78 125 documents of 10 keys 189 / 374 and 705 / 1769, 12 207 of 64 157 / 343 and 409 / 826; still ahead
+// beyond, by less, 3051 of 256 144 / 334 and 168 / 690.  With four heads of a key head the tiled ones take 254 / 671 for 122 880 documents of 10 keys, heads
+// 8/2 of 32, where these take 174 / 340 with heads 8/4.
 bool single_queries(const lgp_documents* d, const lgp_attention* a) {
   return d->n_docs > 0 && a->heads <= 2 * a->kv_heads && d->q_rows <= d->n_docs && d->k_rows <= 64 * d->n_docs;
 }

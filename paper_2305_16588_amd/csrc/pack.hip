@@ -120,8 +120,8 @@ struct GradParams {
 // they go through registers).  value * 2^e has at most seven digits, so it is exact in the type of dy, and so are the products: the only
 // rounding is that of the sums in 32 bits.  The workgroups of the first 128 columns add up the bias's gradient.  Columns beyond the
 // operands' ends hold anything, and so do rows and columns of the result that are not written.  Measured, with 256 columns of dy: 400 000 rows of
-// 1024 values, fp16: 373 to 386 us, 0.55 PFLOP/s; 1 000 003 of 256, bf16, 30 % without a token: 211 to 216 us.  Bound by the widening and LDS beside
-// the matrix instructions, which have a third of the cycles.
+// 1024 values, fp16: 373 to 386 us, 0.55 PFLOP/s; 1 000 003 of 256, bf16, 30 % without a token: 211 to 216 us.  No unit is full: matrix instructions have
+// 34 and 30 % of the cycles, vector ones 40 and 41, LDS instructions are issued in 21 and 19; the rest are waits, for a tile at its barrier among them.
 constexpr int kTokens = 32, kAhead = 256;        // of a tile; of which exponents and positions are held
 template <typename T, int NT, bool DMA>
 __global__ __launch_bounds__(512, 4) void weight_grad_kernel(const GradParams p) {
