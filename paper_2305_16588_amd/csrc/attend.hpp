@@ -135,7 +135,7 @@ __device__ __forceinline__ int32_t owned_of(const Side& s, int32_t d, int32_t n)
 template <typename Tiles, typename Work> __device__ __forceinline__ void each_large(const AttendParams& p, Tiles tiles, Work work) {
   const int lane = threadIdx.x & 63;
   const int32_t n = (p.n_docs + kSurvey - 1) / kSurvey;
-  int32_t next = blockIdx.x;               // this workgroup's next tile, counted from the first of the documents that are looked at
+  int64_t next = blockIdx.x;               // this workgroup's next tile, counted from the first of the documents that are looked at
   for (int32_t s0 = 0; s0 < n; s0 += 64) {
     const int32_t count = s0 + lane < n ? p.n_large[s0 + lane] : 0;
     for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
@@ -143,16 +143,18 @@ template <typename Tiles, typename Work> __device__ __forceinline__ void each_la
       const int32_t listed = __builtin_amdgcn_readlane(count, of);
       for (int32_t i0 = 0; i0 < listed; i0 += 64) {
         const int32_t doc = i0 + lane < listed ? p.large[int64_t(s0 + of) * kSurvey + i0 + lane] : -1;
-        int32_t upto = doc >= 0 ? tiles(owned_of(p.qs, doc, p.n_docs), owned_of(p.ks, doc, p.n_docs)) : 0;
+        // in 64 bits: where offsets make no sense, every document may have all rows
+        int64_t upto = doc >= 0 ? tiles(owned_of(p.qs, doc, p.n_docs), owned_of(p.ks, doc, p.n_docs)) : 0;
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
-          const int32_t before = __shfl_up(upto, d, 64);
+          const int64_t before = __shfl_up(upto, d, 64);
           if (lane >= d) upto += before;
         }
-        const int32_t all = __builtin_amdgcn_readlane(upto, 63);
+        const int64_t all = __shfl(upto, 63, 64);
         for (; next < all; next += gridDim.x) {
           const int l = __popcll(__ballot(upto <= next));
-          work(__builtin_amdgcn_readlane(doc, l), next - (l ? __builtin_amdgcn_readlane(upto, l - 1) : 0));
+          const int64_t first = l ? __shfl(upto, l - 1, 64) : 0;
+          work(__builtin_amdgcn_readlane(doc, l), __builtin_amdgcn_readfirstlane(int32_t(next - first)));
           __syncthreads();                 // the next one has the same LDS
         }
         next -= all;

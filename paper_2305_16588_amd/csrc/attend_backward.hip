@@ -219,7 +219,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
 
 // Large documents among those of one query on average: here, and of k and v below.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, waves_per_simd(D, 4)) void attend_dq_large_kernel(const AttendParams p) {
+__global__ __launch_bounds__(256, 2) void attend_dq_large_kernel(const AttendParams p) {
   each_large(p, [&](int32_t q, int32_t) { return (q * p.group + 127) / 128 * p.kv_heads; },
              [&](int32_t doc, int32_t tile) {
                dq_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, 0, tile / p.kv_heads * 128, span_of(p.qs, doc, p.n_docs), span_of(p.ks, doc, p.n_docs));
@@ -468,7 +468,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
 }
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, waves_per_simd(D, 4)) void attend_dkv_large_kernel(const AttendParams p) {
+__global__ __launch_bounds__(256, 2) void attend_dkv_large_kernel(const AttendParams p) {
   each_large(p, [&](int32_t, int32_t k) { return (k + 127) / 128 * p.kv_heads; },
              [&](int32_t doc, int32_t tile) {
                dkv_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, tile / p.kv_heads * 128, span_of(p.ks, doc, p.n_docs), span_of(p.qs, doc, p.n_docs));

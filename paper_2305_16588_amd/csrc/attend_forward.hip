@@ -245,7 +245,7 @@ __global__ __launch_bounds__(64 * NW * KW, waves_per_simd(D, NW)) void attend_ke
 
 // Large documents among those of one query on average, by four waves that share their keys.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, waves_per_simd(D, 1)) void attend_large_kernel(const AttendParams p) {
+__global__ __launch_bounds__(256, waves_per_simd(D < 64 ? 64 : D, 1)) void attend_large_kernel(const AttendParams p) {
   each_large(p, [&](int32_t q, int32_t) { return (q * p.group + 31) / 32 * p.kv_heads; },
              [&](int32_t doc, int32_t tile) {
                attend_rows<T, D, CAP, BIAS, 1, 4, 32>(p, tile % p.kv_heads, 0, tile / p.kv_heads * 32, span_of(p.qs, doc, p.n_docs), span_of(p.ks, doc, p.n_docs));
