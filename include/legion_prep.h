@@ -438,7 +438,9 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
 int lgp_attend_workspace(int device, const lgp_documents* docs, const lgp_attention* att, int backward, size_t* bytes);
 
 /* Gradients of lgp_attend by q, k and v (dq [q_rows, heads, dim], dk and dv [k_rows, kv_heads, dim]: rows end to end, zeros where no token
- * is) and by the slopes (float[heads], NULL if not wanted), from d_out, which lies like out, and from what lgp_attend wrote.  rest may be NULL. */
+ * is) and by the slopes (float[heads], NULL if not wanted), from d_out, which lies like out, and from what lgp_attend wrote.  rest may be NULL.
+ * Probabilities are exp(score - lse) again, so a row's have a common relative error of 2^-23 of its lse: less than the rounding of the results up to an
+ * lse of 10^4, where all keys are that far below zero or above. */
 int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attention* att, const void* d_out, const void* out, const void* rest,
                         const float* lse, void* dq, void* dk, void* dv, float* d_slopes, void* workspace, size_t workspace_bytes, void* stream);
 

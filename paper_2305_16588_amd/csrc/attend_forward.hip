@@ -73,8 +73,10 @@ __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, i
   float base = 0.f, limit = -3e38f, sum = 0.f;
   Places<T, D> at_tile(lane);
   const bool idle = row0 + 32 * wave >= qd.tokens * p.group;         // a wave of rows without tokens only copies
-  // How far a score is above x, rounded once: without a bias from the product.
-  auto above = [&](float score, float x) { return BIAS ? score - x : fmaf(score, p.z_mul, -x); };
+  // How far a score is above x, rounded once: without a bias from the product.  Only where a base passes 2^24, whose places are more than one, products
+  // are made scores first: the largest is the base to the last digit then.
+  float mul = p.z_mul;
+  auto above = [&](float score, float x) { return BIAS ? score - x : fmaf(score, mul, -x); };
   auto step = [&](int32_t k0, auto stage_now) {
     constexpr int now = decltype(stage_now)::value;
     if constexpr (BIAS) {
@@ -105,6 +107,13 @@ __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, i
           for (int i = 0; i < 4; ++i) s[b][4 * r4 + i] = fmaf(s[b][4 * r4 + i], p.z_mul, -slope * fabsf(at - kpos[i]));
         }
     }
+    auto make_scores = [&] {
+#pragma unroll
+      for (int b = 0; b < BN / 32; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[b][r] *= p.z_mul;
+    };
+    if (!BIAS && mul != p.z_mul) make_scores();
     if (k0 + BN > k_end) {
 #pragma unroll
       for (int b = 0; b < BN / 32; ++b)
@@ -122,9 +131,7 @@ __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, i
       // A row that has no base yet has nothing either, and 2^-by is inf where its first score is far below zero.  The row's state decides, not its sum:
       // a lane's sum is that of half of the keys so far, while its results are those of all.
       const bool raise = above(most, base) > limit;
-      float raised = BIAS ? most : most * p.z_mul;
-      if (above(most, raised) > kSlack) raised = nextafterf(raised, INFINITY);       // beyond 2^27, where a place is more than that
-      const float shrink = raise && limit == kSlack ? exp2_fast(base - raised) : 1.f;
+      const float raised = BIAS ? most : most * mul, shrink = raise && limit == kSlack ? exp2_fast(base - raised) : 1.f;
       base = raise ? raised : base;
       limit = raise ? kSlack : limit;
       sum *= shrink;
@@ -132,6 +139,10 @@ __device__ __forceinline__ void attend_rows(const AttendParams& p, int32_t hk, i
       for (int db = 0; db < D / 32; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[db][r] *= shrink;
+      if (!BIAS && mul == p.z_mul && __any(fabsf(base) > 0x1p24f)) {
+        make_scores();
+        mul = 1.f;
+      }
     }
 #pragma unroll
     for (int b = 0; b < BN / 32; ++b) {

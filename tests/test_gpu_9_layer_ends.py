@@ -417,3 +417,30 @@ def test_documents_of_more_tiles_than_a_launch_has_threads(room):
         for x, y, name in zip(got, want, ("out", "dq", "dk", "dv")):
             # terms of up to 40, a few units each
             assert (x[rows].view(-1, 2, H, D).float().transpose(1, 2) - y).abs().max() < 40 * 4 * ref.UNIT[F16], f"{name}, document {d}"
+
+
+@pytest.mark.parametrize("q_owned,k_owned", [*SHAPES, ([1] * 60, [9] * 60)])
+@pytest.mark.parametrize("dtype,size", [(F16, 1.2e4), (BF16, 1e9), (BF16, 1e-9)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_scores_of_every_magnitude(bias, dtype, size, q_owned, k_owned):
+    """Beyond 2^24 a score's place is more than the distance that a weight is lost over: a row's result is the value of its largest score, where that is
+    larger by more than the rounding of the sums."""
+    L = lgp()
+    docs, info = make_docs(q_owned, k_owned)
+    Tq, Tk = sum(q_owned), sum(k_owned)
+    q, k, v = draw((Tq, 2, 128), dtype, 1, size), draw((Tk, 2, 128), dtype, 2, size), draw((Tk, 2, 128), dtype, 3)
+    slopes = torch.full((2,), 0.1, device="cuda") if bias else None
+    out, lse, _ = L.attend(q, k, v, docs, slopes=slopes, scale=1.0)
+    assert torch.isfinite(out).all()
+    want = ref.attention(q, k, v, info, None, slopes, scale=1.0)
+    if size < 1:
+        ref.check(out, want["out"], "out")
+        ref.check(lse, want["lse"], "lse")
+        return
+    for qo, qn, ko, kn in info["spans"]:
+        z = torch.matmul(q[qo:qo + qn].double().transpose(0, 1), k[ko:ko + kn].double().permute(1, 2, 0).contiguous())          # [heads, queries, keys]
+        top = z.topk(2, 2)
+        clear = ((top.values[..., 0] - top.values[..., 1]) > 2.0 ** -20 * 128 * float(z.abs().max())).t()
+        best = torch.stack([v[ko:ko + kn, h][top.indices[h, :, 0]] for h in range(2)], 1)
+        assert clear.float().mean() > 0.9 and torch.equal(out[qo:qo + qn][clear], best[clear])
+        assert ((lse[qo:qo + qn].double() / top.values[..., 0].t() - 1).abs()[clear] < 2.0 ** -17).all()
