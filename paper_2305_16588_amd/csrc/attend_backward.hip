@@ -530,7 +530,7 @@ template <typename T> void launch(const AttendParams& p, const BackwardShape& b,
   if (p.dim <= 32) launch<T, 32>(p, b, cap, s);
   else if (p.dim <= 64) launch<T, 64>(p, b, cap, s);
   else launch<T, 128>(p, b, cap, s);
-  if (p.splits > 1) {
+  if (p.splits > 1 && p.qs.rows) {
     add_kernel<T><<<uint32_t(p.qs.rows * p.heads), 256, 0, s>>>(p);
   }
 }

@@ -444,3 +444,12 @@ def test_scores_of_every_magnitude(bias, dtype, size, q_owned, k_owned):
         best = torch.stack([v[ko:ko + kn, h][top.indices[h, :, 0]] for h in range(2)], 1)
         assert clear.float().mean() > 0.9 and torch.equal(out[qo:qo + qn][clear], best[clear])
         assert ((lse[qo:qo + qn].double() / top.values[..., 0].t() - 1).abs()[clear] < 2.0 ** -17).all()
+
+
+@pytest.mark.parametrize("q_owned,k_owned", [([0], [1500]), ([0, 0], [9000, 2000]), ([0] * 50, [700] * 50)])
+def test_keys_without_any_queries(q_owned, k_owned):
+    """As many keys as are split where queries are few, and none of them."""
+    docs, info = make_docs(q_owned, k_owned)
+    for heads, kv_heads in ((2, 2), (8, 2)):
+        _, _, _, dk, dv, ds = run_attention(docs, info, heads, kv_heads, 64, F16, 0.0, True)
+        assert (dk == 0).all() and (dv == 0).all() and (ds == 0).all()
