@@ -491,8 +491,8 @@ int lgp_pack_activations(int device, const void* x, int64_t x_row, const lgp_pac
 int lgp_unpack_activations(int device, const lgp_packed* in, void* x, void* stream);
 
 /* Gradients of a linear layer y = x W^T + b from its packed input: dw [out, width] = sum over tokens of dy^T x and db [out] = sum of dy (NULL:
- * not wanted), both fp32, added up in fp32 from exact products.  dy: fp16 or bf16, dy_row elements from row to row; fp16 only if x came in
- * fp16. */
+ * not wanted), both fp32, added up in fp32 from exact products (with fp16, a product with a factor below 2^-14 is exact to 2^-37 of the other one).  dy:
+ * fp16 or bf16, dy_row elements from row to row; fp16 only if x came in fp16. */
 int lgp_packed_weight_grad_workspace(int device, const lgp_packed* x, int32_t out, size_t* bytes);
 int lgp_packed_weight_grad(int device, const lgp_packed* x, const void* dy, int64_t dy_row, int32_t dy_dtype, int32_t out, float* dw, float* db,
                            void* workspace, size_t workspace_bytes, void* stream);
