@@ -429,8 +429,8 @@ typedef struct {
  * rows end to end.  A query without keys, and a row without a token, gets zeros and an lse of -inf.  rest (NULL, or like out) receives
  * what the rounding of out took off: d_out . out then has no rounding of out in it in the backward pass, only that of the probabilities
  * (which are rounded to the type of v for their product with it).
- * Few queries over long documents are split over the keys and joined, in `workspace` (lgp_attend_workspace); where documents have one query and up to
- * 64 keys on average, the large ones among them are listed there. */
+ * Few queries over long documents are split over the keys and joined, in `workspace` (lgp_attend_workspace); where many documents have one query
+ * and up to 64 keys on average, the large ones among them are listed there. */
 int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, void* out, void* rest, float* lse, void* workspace,
                size_t workspace_bytes, void* stream);
 

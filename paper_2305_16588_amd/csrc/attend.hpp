@@ -40,7 +40,9 @@ struct AttendParams {
   float* delta;              // [q_rows][heads]: d_out . out
   floatx4* sums;             // [split][q_rows][heads], if the gradient of the slopes is wanted: see dq_rows
   // documents of one query on average: those that are not left to single waves, see each_large
-  int32_t *n_large, *large;  // [survey] and [survey][kSurvey], or NULL: there can be none
+  bool any_large;            // there can be some
+  int32_t* n_large;          // [survey], or NULL: documents are few
+  uint16_t* large;           // [survey][kSurvey]: counted from the survey's first document
 };
 
 template <typename T> __device__ __forceinline__ vec8<T> load8(const T* p) { return *reinterpret_cast<const vec8<T>*>(p); }
@@ -105,44 +107,80 @@ int check_attend(const lgp_documents* d, const lgp_attention* a);
 AttendParams attend_params(const lgp_documents* d, const lgp_attention* a);
 
 // Documents of one query and few keys on average (attend_single.hip).  The host knows no more of them; one that has many of both, or very many keys,
-// would be one wave's work and take as long as its pairs one after the other.  So a wave takes documents of up to kLargePairs pairs, and while these
-// are gone through, waves of the same launch list the others, kSurvey documents each.  A second launch goes through the lists: a workgroup
-// counts all their tiles, 64 documents at a time, and takes every so many-th one.  Measured: 122 880 documents of up to 10 keys, none of them large:
-// 5 us for each of the three second launches of a training step of 595.  2000 documents, bf16, heads 8/8 of 64: one of them 2000 rows and the others
-// empty, forward 32 us and backward 130; one of them a query over 60 000 keys, 384 and 1162, one workgroup for each head.
-constexpr int kLargePairs = 512, kSurvey = 512, kLargeGroups = 512;       // workgroups of the second launch
+// would be one wave's work and take as long as its pairs one after the other.  So waves leave documents of more than kLargePairs pairs, if there can be
+// any of more than kFewPairs, and a second launch of the tiled kernels goes through these: a workgroup counts all their tiles, 64 documents at a time,
+// and takes every so many-th one.  Up to kOwnSurveys * kSurvey documents are looked through by every workgroup of it; of more, waves of the first
+// launch list the large ones, kSurvey documents each (8192 documents, us a training step: looked through 61, listed 51 to 53).  Measured where none
+// is large: a launch of 5 us, 3 for the host; 1024 documents of up to 10 keys, heads 8/8 of 32, forward 12.9 -> 16.3, trained 31 -> 37.5; 122 880 trained
+// 582 -> 592.  2000 documents, bf16, heads 8/8 of 64: one of them 2000 rows and the others empty, forward 40 and backward 100; one of them a query over
+// 60 000 keys, 390 and 1240, one workgroup for each head.
+constexpr int kLargePairs = 512, kFewPairs = 2048, kSurvey = 512, kOwnSurveys = 8, kLargeGroups = 256;       // kLargeGroups: workgroups of the second launch
 bool single_queries(const lgp_documents* d, const lgp_attention* a);
-inline int64_t surveys(const lgp_documents* d) {       // none if all rows together are no large document
+inline bool any_large(const lgp_documents* d) {
   const int64_t q = d->q_rows > 1 ? d->q_rows : 1, k = d->k_rows > 1 ? d->k_rows : 1;
-  return q > kLargePairs || k > kLargePairs || q * k > kLargePairs ? (d->n_docs + kSurvey - 1) / kSurvey : 0;
+  return q > kFewPairs || k > kFewPairs || q * k > kFewPairs;
 }
-inline size_t survey_bytes(const lgp_documents* d) { return (size_t(surveys(d)) * (1 + kSurvey) * sizeof(int32_t) + 15) / 16 * 16; }
+inline int64_t surveys(const lgp_documents* d) { return any_large(d) && d->n_docs > kOwnSurveys * kSurvey ? (d->n_docs + kSurvey - 1) / kSurvey : 0; }
+inline size_t survey_bytes(const lgp_documents* d) { return (size_t(surveys(d)) * (sizeof(int32_t) + kSurvey * sizeof(uint16_t)) + 15) / 16 * 16; }
 inline void set_survey(AttendParams& p, const lgp_documents* d, void* at) {
   const int64_t n = surveys(d);
+  p.any_large = any_large(d);
   p.n_large = n ? static_cast<int32_t*>(at) : nullptr;
-  p.large = n ? p.n_large + n : nullptr;
+  p.large = n ? reinterpret_cast<uint16_t*>(p.n_large + n) : nullptr;
 }
 void launch_single(const AttendParams& p, const lgp_attention* a, bool backward, hipStream_t s);
 void launch_large(const AttendParams& p, const lgp_attention* a, hipStream_t s);       // of the forward pass
 __device__ __forceinline__ bool is_large(int32_t q_owned, int32_t k_owned) {
   return int64_t(q_owned > 1 ? q_owned : 1) * (k_owned > 1 ? k_owned : 1) > kLargePairs;
 }
+// Rows of document d as span_of has them, none beyond the last one; without a branch, so that loads do not wait for each other.
 __device__ __forceinline__ int32_t owned_of(const Side& s, int32_t d, int32_t n) {
-  const int32_t begin = offset_of(s, d, n), end = offset_of(s, d + 1, n);
-  return end > begin ? end - begin : 0;
+  const int32_t a = d < n ? d : n, b = d < n ? d + 1 : n;
+  int32_t begin = s.offsets[a], end = s.offsets[b];
+  begin = a == 0 ? 0 : a == n ? s.rows : min(max(begin, 0), s.rows);
+  end = b == n ? s.rows : min(max(end, 0), s.rows);
+  return max(end - begin, 0);
 }
-// tiles(rows of queries, of keys) is what a document has of them; work(document, tile) is called by all waves of a workgroup alike.
+// A wave lists the large ones of kSurvey documents, in their order, and counts them.
+__device__ __forceinline__ void list_large(const AttendParams& p, int32_t survey, uint16_t* docs, int32_t* count) {
+  constexpr int kAtOnce = kSurvey / 64;        // loads of a lane's documents are on their way together
+  const int lane = threadIdx.x & 63;
+  const int32_t d0 = survey * kSurvey + lane;
+  bool large[kAtOnce];
+#pragma unroll
+  for (int i = 0; i < kAtOnce; ++i)            // beyond the last one: no rows
+    large[i] = is_large(owned_of(p.qs, d0 + 64 * i, p.n_docs), owned_of(p.ks, d0 + 64 * i, p.n_docs));
+  int32_t n = 0;
+#pragma unroll
+  for (int i = 0; i < kAtOnce; ++i) {
+    const uint64_t all = __ballot(large[i]);
+    if (large[i]) docs[n + __popcll(all & ((uint64_t(1) << lane) - 1))] = uint16_t(64 * i + lane);
+    n += __popcll(all);
+  }
+  if (lane == 0) *count = n;
+}
+// tiles(rows of queries, of keys) is what a document has of them; work(document, tile) is called by all waves of a workgroup of 256 alike.
 template <typename Tiles, typename Work> __device__ __forceinline__ void each_large(const AttendParams& p, Tiles tiles, Work work) {
+  __shared__ int32_t own_n[kOwnSurveys];
+  __shared__ uint16_t own[kOwnSurveys * kSurvey];
   const int lane = threadIdx.x & 63;
   const int32_t n = (p.n_docs + kSurvey - 1) / kSurvey;
+  const int32_t* counts = p.n_large;
+  const uint16_t* docs = p.large;
+  if (!counts) {
+    for (int32_t at = threadIdx.x >> 6; at < n; at += 4) list_large(p, at, own + at * kSurvey, own_n + at);
+    __syncthreads();
+    counts = own_n;
+    docs = own;
+  }
   int64_t next = blockIdx.x;               // this workgroup's next tile, counted from the first of the documents that are looked at
   for (int32_t s0 = 0; s0 < n; s0 += 64) {
-    const int32_t count = s0 + lane < n ? p.n_large[s0 + lane] : 0;
+    const int32_t count = s0 + lane < n ? counts[s0 + lane] : 0;
     for (uint64_t some = __ballot(count > 0); some; some &= some - 1) {
       const int of = __builtin_ctzll(some);
       const int32_t listed = __builtin_amdgcn_readlane(count, of);
       for (int32_t i0 = 0; i0 < listed; i0 += 64) {
-        const int32_t doc = i0 + lane < listed ? p.large[int64_t(s0 + of) * kSurvey + i0 + lane] : -1;
+        const int32_t doc = i0 + lane < listed ? (s0 + of) * kSurvey + docs[int64_t(s0 + of) * kSurvey + i0 + lane] : -1;
         // in 64 bits: where offsets make no sense, every document may have all rows
         int64_t upto = doc >= 0 ? tiles(owned_of(p.qs, doc, p.n_docs), owned_of(p.ks, doc, p.n_docs)) : 0;
 #pragma unroll

@@ -217,15 +217,6 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dq_kern
   dq_rows<T, D, CAP, BIAS, NW, BN>(p, hk, split, row0, qd, kd);
 }
 
-// Large documents among those of one query on average: here, and of k and v below.
-template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attend_dq_large_kernel(const AttendParams p) {
-  each_large(p, [&](int32_t q, int32_t) { return (q * p.group + 127) / 128 * p.kv_heads; },
-             [&](int32_t doc, int32_t tile) {
-               dq_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, 0, tile / p.kv_heads * 128, span_of(p.qs, doc, p.n_docs), span_of(p.ks, doc, p.n_docs));
-             });
-}
-
 // Adds the parts of dq, like join_kernel, and in its time.
 template <typename T>
 __global__ __launch_bounds__(256) void add_kernel(const AttendParams p) {
@@ -281,7 +272,8 @@ __global__ __launch_bounds__(kEndThreads) void slopes_end_kernel(const double* p
 //     dv_j = sum_i P_ij d_out_i,   dk_j = scale * sum_i dU_ij q_i.
 // Measured, at the sizes of attend_dq_kernel: 2115 to 2180 us, 1.02 PFLOP/s, matrix instructions 45 % of the cycles of two waves per SIMD that wait for each
 // other's tiles; 304 us, vector instructions 66 %.
-template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ>
+// DELTA: delta is not there yet; eight threads take that of a row from d_out, out and rest.
+template <typename T, int D, bool CAP, bool BIAS, int NW, int BQ, bool DELTA = false>
 __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int32_t key0, const Span kd, const Span qd) {
   constexpr int kThreads = 64 * NW, kKeys = 32 * NW;
   __shared__ __align__(16) T lds_q[2][BQ * D];
@@ -294,7 +286,9 @@ __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int3
 
   // Up to 16 heads of a token, if they divide 16, are folded; otherwise the heads that share this one are gone through one after the other.
   const int32_t rows = key0 < kd.tokens ? qd.tokens << p.log2_fold : 0;
-  static_assert(BQ <= kThreads, "a thread has a row");
+  static_assert(BQ <= kThreads && (!DELTA || 8 * BQ == kThreads), "a thread has a row, or eight");
+  constexpr int kChunks = DELTA ? (D + 63) / 64 : 1;
+  vec8<T> of_g[kChunks], of_o[kChunks], of_rest[kChunks];
   float next[3];               // as they come, so that nothing waits for them yet
   int32_t next_pos;
   auto stage = [&](int32_t h0, int32_t r0, int to) {
@@ -303,10 +297,22 @@ __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int3
       const int32_t head = h0 + ((r0 + tid) & ((1 << p.log2_fold) - 1));
       const int64_t token = qd.begin + ((r0 + tid) >> p.log2_fold);
       next[0] = p.lse_in[token * p.heads + head];
-      next[1] = p.delta[token * p.heads + head];
+      if constexpr (!DELTA) next[1] = p.delta[token * p.heads + head];
       if constexpr (BIAS) {
         next[2] = p.slopes[head];
         next_pos = p.qs.pos[token];
+      }
+    }
+    if constexpr (DELTA) {
+      const int32_t r = r0 + tid / 8;
+      const int64_t d0 = ((qd.begin + int64_t(r >> p.log2_fold)) * p.heads + h0 + (r & ((1 << p.log2_fold) - 1))) * p.dim;
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j) {
+        const int d = 8 * (tid % 8 + 8 * j);
+        const bool there = r < rows && d < p.dim;
+        of_g[j] = load8(static_cast<const T*>(p.d_out) + d0 + d, there, false);
+        of_o[j] = load8(static_cast<const T*>(p.out) + d0 + d, there, false);
+        of_rest[j] = load8(static_cast<const T*>(p.rest) + d0 + d, there && p.rest, false);
       }
     }
     const Rows<T> q_rows = {static_cast<const T*>(p.q) + int64_t(qd.begin) * p.q_row + int64_t(h0) * p.q_head, p.q_row, p.q_head, p.log2_fold};
@@ -317,9 +323,18 @@ __device__ __forceinline__ void dkv_rows(const AttendParams& p, int32_t hk, int3
   auto put_rows = [&](int to) {
     if (tid < BQ) {
       lds_row[to][0][tid] = (next[0] == -INFINITY ? INFINITY : next[0]) * kLog2e - kLiftLog2<T>;       // no probability where there is no key
-      lds_row[to][1][tid] = next[1];
+      if constexpr (!DELTA) lds_row[to][1][tid] = next[1];
       lds_row[to][2][tid] = next[2] * kLog2e;
       lds_row[to][3][tid] = float(next_pos);
+    }
+    if constexpr (DELTA) {
+      float delta = 0.f;
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta += float(of_g[j][i]) * (float(of_o[j][i]) + float(of_rest[j][i]));
+      delta = sum_of_lanes<8>(delta);
+      if (tid % 8 == 0) lds_row[to][1][tid / 8] = delta;
     }
   };
   if (p.dim < D) {
@@ -467,11 +482,15 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
   dkv_rows<T, D, CAP, BIAS, NW, BQ>(p, hk, key0, kd, qd);
 }
 
+// Large documents among those of one query on average.  Tiles of queries and of keys are taken side by side, so the latter take delta themselves.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attend_dkv_large_kernel(const AttendParams p) {
-  each_large(p, [&](int32_t, int32_t k) { return (k + 127) / 128 * p.kv_heads; },
+__global__ __launch_bounds__(256, 2) void attend_backward_large_kernel(const AttendParams p) {
+  each_large(p, [&](int32_t q, int32_t k) { return ((q * p.group + 127) / 128 + (k + 127) / 128) * p.kv_heads; },
              [&](int32_t doc, int32_t tile) {
-               dkv_rows<T, D, CAP, BIAS, 4, 32>(p, tile % p.kv_heads, tile / p.kv_heads * 128, span_of(p.ks, doc, p.n_docs), span_of(p.qs, doc, p.n_docs));
+               const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
+               const int32_t hk = tile % p.kv_heads, at = tile / p.kv_heads, of_q = (qd.owned * p.group + 127) / 128;
+               if (at < of_q) dq_rows<T, D, CAP, BIAS, 4, 32>(p, hk, 0, at * 128, qd, kd);
+               else dkv_rows<T, D, CAP, BIAS, 4, 32, true>(p, hk, (at - of_q) * 128, kd, qd);
              });
 }
 
@@ -501,9 +520,8 @@ BackwardShape backward_shape(int device, const lgp_documents* d, const lgp_atten
 }
 
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const BackwardShape& b, hipStream_t s) {
-  if (p.n_large) {
-    attend_dq_large_kernel<T, D, CAP, BIAS><<<kLargeGroups, 256, 0, s>>>(p);
-    attend_dkv_large_kernel<T, D, CAP, BIAS><<<kLargeGroups, 256, 0, s>>>(p);
+  if (p.any_large) {
+    attend_backward_large_kernel<T, D, CAP, BIAS><<<kLargeGroups, 256, 0, s>>>(p);
     return;
   }
   AttendParams x = p;
@@ -589,7 +607,7 @@ int lgp_attend_backward(int device, const lgp_documents* docs, const lgp_attenti
     set_survey(p, docs, w + b.survey);
     launch_single(p, att, true, s);
   }
-  if (!single || p.n_large) att->dtype == LGP_F16 ? launch<f16>(p, b, att->cap > 0.f, s) : launch<bf16>(p, b, att->cap > 0.f, s);
+  if (!single || p.any_large) att->dtype == LGP_F16 ? launch<f16>(p, b, att->cap > 0.f, s) : launch<bf16>(p, b, att->cap > 0.f, s);
   if (d_slopes) {
     double* partial = reinterpret_cast<double*>(w + b.partial);      // after the sums, so aligned to 16 bytes like them
     slopes_kernel<<<kSlopeThreads / 256, 256, 0, s>>>(p, partial);

@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256) void join_kernel(const AttendParams p) {
 }
 
 template <typename T, int D, bool CAP, bool BIAS> void launch(const AttendParams& p, const ForwardShape& f, hipStream_t s) {
-  if (p.n_large) {
+  if (p.any_large) {
     attend_large_kernel<T, D, CAP, BIAS><<<uint32_t(f.tiles), 256, 0, s>>>(p);
     return;
   }
@@ -428,7 +428,7 @@ int lgp_attend(int device, const lgp_documents* docs, const lgp_attention* att, 
     if (surveys(docs) && (!workspace || !aligned16(workspace))) return LGP_EINVAL;
     set_survey(p, docs, workspace);
     launch_single(p, att, false, s);
-    if (p.n_large) launch_large(p, att, s);
+    if (p.any_large) launch_large(p, att, s);
     return launched();
   }
   const ForwardShape f = forward_shape(device, docs, att);

@@ -45,28 +45,10 @@ template <typename T> __device__ __forceinline__ void widen(vec8<T> a, float* x)
 
 constexpr int kSteps = 4;       // keys that a lane has in flight
 
-// The first workgroups of a launch: a wave lists the large ones of kSurvey documents, in their order.
+// The first workgroups of a launch.
 __device__ __forceinline__ void survey(const AttendParams& p) {
-  constexpr int kAtOnce = 8;           // loads of so many documents of a lane are on their way together
-  const int lane = threadIdx.x & 63;
-  const int32_t at = blockIdx.x * 4 + (threadIdx.x >> 6), d0 = at * kSurvey;
-  if (d0 >= p.n_docs) return;
-  int32_t n = 0;
-  for (int32_t d1 = d0; d1 < d0 + kSurvey; d1 += 64 * kAtOnce) {
-    bool large[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const int32_t d = d1 + 64 * i + lane;          // beyond the last one: no rows
-      large[i] = is_large(owned_of(p.qs, d, p.n_docs), owned_of(p.ks, d, p.n_docs));
-    }
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      const uint64_t all = __ballot(large[i]);
-      if (large[i]) p.large[d0 + n + __popcll(all & ((uint64_t(1) << lane) - 1))] = d1 + 64 * i + lane;
-      n += __popcll(all);
-    }
-  }
-  if (lane == 0) p.n_large[at] = n;
+  const int32_t at = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at * kSurvey < p.n_docs) list_large(p, at, p.large + int64_t(at) * kSurvey, p.n_large + at);
 }
 
 template <typename T, int L, int G, bool CAP, bool BIAS>
@@ -75,7 +57,7 @@ __global__ __launch_bounds__(256) void single_kernel(const AttendParams p, int32
   const Lanes<L> a(p, heads_at_once);
   if (a.doc >= p.n_docs) return;
   const Span qd = span_of(p.qs, a.doc, p.n_docs), kd = span_of(p.ks, a.doc, p.n_docs);
-  if (is_large(qd.owned, kd.owned)) return;
+  if (p.any_large && is_large(qd.owned, kd.owned)) return;
   const T* kp = static_cast<const T*>(p.k) + int64_t(a.hk) * p.k_head + 8 * a.c;
   const T* vp = static_cast<const T*>(p.v) + int64_t(a.hk) * p.v_head + 8 * a.c;
   for (int32_t row = 0; row < qd.owned; ++row) {
@@ -190,7 +172,7 @@ __global__ __launch_bounds__(256) void single_backward_kernel(const AttendParams
   const Lanes<L> a(p, heads_at_once);
   if (a.doc >= p.n_docs) return;
   const Span qd = span_of(p.qs, a.doc, p.n_docs), kd = span_of(p.ks, a.doc, p.n_docs);
-  if (is_large(qd.owned, kd.owned)) return;
+  if (p.any_large && is_large(qd.owned, kd.owned)) return;
   const T* kp = static_cast<const T*>(p.k) + int64_t(a.hk) * p.k_head + 8 * a.c;
   const T* vp = static_cast<const T*>(p.v) + int64_t(a.hk) * p.v_head + 8 * a.c;
   const float back = fabsf(p.scale);        // q was negated as it was read where the scale is negative
