@@ -484,7 +484,7 @@ __global__ __launch_bounds__(64 * NW, waves_per_simd(D, NW)) void attend_dkv_ker
 
 // Large documents among those of one query on average.  Tiles of queries and of keys are taken side by side, so the latter take delta themselves.
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, 2) void attend_backward_large_kernel(const AttendParams p) {
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_backward_large_kernel(const AttendParams p) {
   each_large(p, [&](int32_t q, int32_t k) { return ((q * p.group + 127) / 128 + (k + 127) / 128) * p.kv_heads; },
              [&](int32_t doc, int32_t tile) {
                const Span qd = span_of(p.qs, doc, p.n_docs), kd = span_of(p.ks, doc, p.n_docs);
