@@ -17,6 +17,7 @@ from .binding import LegionPrepError, _Attention, _Documents, _Heads, _Packed, _
 
 _DTYPE = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _EINVAL, _ECAPACITY = -1, -3
+_LARGE = 1 << 24              # strides from here on are looked at more closely
 
 
 def _packer(structure):
@@ -94,16 +95,14 @@ def _heads_of(t, name: str, dtype, index: int):
     if t.dim() != 3 or t.dtype is not dtype or t.get_device() != index:
         raise _bad(f"{name}: [rows, heads, dim], {dtype}, on cuda:{index}")
     row, head, one = t.stride()
-    rows, heads, _ = t.shape
     at = t.data_ptr()
-    if rows < 2:              # the stride of a single row or head says nothing
-        row = 0
-    if heads < 2:
-        head = 0
-    if one != 1 or row % 8 or head % 8 or at % 16:
-        if t.numel():
+    if one != 1 or row % 8 or head % 8 or at % 16 or row >= _LARGE or head >= _LARGE:
+        rows, heads, _ = t.shape
+        row, head = row if rows > 1 else 0, head if heads > 1 else 0          # the stride of a single row or head says nothing
+        if t.numel() and (one != 1 or row % 8 or head % 8 or at % 16):
             raise _bad(f"{name}: elements of a head side by side, strides in multiples of 8, aligned to 16 bytes")
-        row = head = 0
+        if not t.numel():
+            row = head = 0
     return at, row, head
 
 
@@ -191,7 +190,7 @@ def attend(q, k, v, docs: Documents, slopes=None, cap: float = 0.0, scale: float
     given.  out is like q, end to end; lse (float32[q_rows, heads]) is the logarithm of the sum of exp(score).  Queries without keys and rows
     without tokens get zeros and -inf.  rest: also return what the rounding of out took off, for attend_backward.  Gradients pass through out, not
     through lse or rest."""
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad)):
+    if (q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad)) and torch.is_grad_enabled():
         with _on(docs.index, stream):
             out, lse, left = _Attend.apply(q, k, v, slopes, docs, cap, scale)
         return out, lse, left if rest else None
@@ -257,10 +256,9 @@ def _norm(q, k, q_weight, k_weight, pos, table, eps: float):
         if table.dim() != 2 or table.dtype is not torch.float32 or table.get_device() != index or not table.is_contiguous() or at % 16 or pos is None:
             raise _bad("table: float32[positions, rot], aligned to 16 bytes, and pos with it")
         n_pos, rot = table.shape
-    args = (qp, kp, q_row, q_head, k_row, k_head, tokens, heads, kv_heads, dim, _DTYPE[dtype], _weight(q_weight, "q_weight", dim, index),
-            _weight(k_weight, "k_weight", dim, index), _ints(pos, tokens, index, "pos"), rot, n_pos, at)
+    wq, wk, positions = _weight(q_weight, "q_weight", dim, index), _weight(k_weight, "k_weight", dim, index), _ints(pos, tokens, index, "pos")
     try:
-        return index, _heads(*args, eps)
+        return index, _heads(qp, kp, q_row, q_head, k_row, k_head, tokens, heads, kv_heads, dim, _DTYPE[dtype], wq, wk, positions, rot, n_pos, at, eps)
     except (OverflowError, struct.error):
         raise _bad("eps: a number that float32 holds") from None
 
@@ -282,7 +280,7 @@ def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-
     """RMS norm of every head of q [tokens, heads, dim] and k [tokens, kv_heads, dim] with weights (float32[dim]), and the rotation of its first
     table.shape[1] elements by the token's position (rotation_table); new tensors (q, k), rows end to end.  dim: a multiple of 8 up to 256.
     Rows of a negative pos have no token and become zeros; those of a position beyond the table become NaN."""
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad):
+    if (q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad) and torch.is_grad_enabled():
         with _on(q.get_device(), stream):
             return _NormRotate.apply(q, k, q_weight, k_weight, pos, table, eps)
     L = load_library()
