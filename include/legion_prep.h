@@ -497,6 +497,67 @@ int lgp_packed_weight_grad_workspace(int device, const lgp_packed* x, int32_t ou
 int lgp_packed_weight_grad(int device, const lgp_packed* x, const void* dy, int64_t dy_row, int32_t dy_dtype, int32_t out, float* dw, float* db,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- What a layer has around its attention ----
+ * As above: no context, all arrays [device] unless they say otherwise, only `stream` orders the calls, results do not change from run to run. */
+
+/* Rows that a branch of a layer is added to, and the norm of the sum.  Strides are in elements, between rows; the elements of a row are consecutive
+ * and need no alignment beyond their own. */
+typedef struct {
+  const void* x;                        /* the branch; not read by the backward pass                         */
+  const void* residual;                 /* what it is added to, or NULL: nothing is; backward: the sum       */
+  int64_t x_row, residual_row;
+  int64_t tokens;
+  int32_t width;                        /* 1 to 16384                                                        */
+  int32_t dtype;                        /* LGP_F32, LGP_F16 or LGP_BF16: of x, the norm's result, its gradient, dx */
+  int32_t stream_dtype;                 /* of the residual, the sum and their gradients: dtype or LGP_F32    */
+  const float* weight;                  /* float[width]                                                      */
+  const int32_t* pos;                   /* tokens entries, or NULL; a negative one: there is no token in this
+                                           row, it is not read and its results are zeros                     */
+  float eps;
+} lgp_residual;
+
+/* Rows in 8-bit integers: value = values * scales[row]. */
+typedef struct {
+  int64_t tokens;
+  int32_t width;
+  int8_t* values;                       /* [tokens][width rounded up to 16], zeros behind width, aligned to 16 bytes */
+  float* scales;                        /* [tokens]                                                          */
+  const int32_t* pos;                   /* as above                                                          */
+} lgp_rows8;
+
+/* total = x + residual, rounded to the type of the residual, and y = total * weight / sqrt(mean(total^2) + eps), of the rounded total.  Both are [tokens,
+ * width], rows end to end.  Without a residual, total is x itself and not written (it may be NULL), and the types have to be the same. */
+int lgp_add_norm(int device, const lgp_residual* in, void* y, void* total, void* stream);
+
+/* The same with y in 8 bits, from its 32-bit value: scale = max |y| / 127, at least 2^-126, and values = y / scale, rounded to even.  A row with an infinity or a
+ * NaN has a scale of NaN.  out->pos is not read: in->pos says where tokens are. */
+int lgp_add_norm_rows8(int device, const lgp_residual* in, const lgp_rows8* out, void* total, void* stream);
+
+/* Gradients of lgp_add_norm, from those of y (dy [tokens, width] in dtype) and of the total (d_total, in stream_dtype, or NULL where nothing else uses it), rows end to
+ * end: d_residual = d_total + r (g - n mean(g n)) with n = total r, g = dy weight; dx is the same in the type of x, and NULL where both types are the same; d_weight
+ * (float[width]) is the sum of dy n. */
+int lgp_add_norm_workspace(int device, const lgp_residual* in, size_t* bytes);
+int lgp_add_norm_backward(int device, const lgp_residual* in, const void* dy, const void* d_total, void* dx, void* d_residual, float* d_weight, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* Rows of x (dtype, x_row elements from row to row, any alignment; up to 16384 wide) in 8 bits, by the same rule. */
+int lgp_pack_rows8(int device, const void* x, int64_t x_row, int32_t dtype, const lgp_rows8* out, void* stream);
+
+/* A gradient: n consecutive elements, aligned to one.  out: where the scaled ones go; out = grad: they stay where they are. */
+typedef struct {
+  const void* grad;
+  void* out;
+  int64_t n;
+  int64_t dtype;                        /* LGP_F32, LGP_F16 or LGP_BF16                                      */
+} lgp_gradient;
+
+/* The norm over all n gradients (list is [host]; n up to 65536), the root of the sum of their elements' squares in 64 bits, as a float; and out = grad * min(1, most / norm), rounded once.
+ * Where that factor is 1 elements that stay are neither read again nor written, and nothing is launched for them with a `most` of infinity.  Where the norm is no finite
+ * float they are left as they are, and copied where they go elsewhere.  Ranges that are written may not overlap others; both calls of a pair may share a workspace if
+ * the stream orders them. */
+int lgp_clip_gradients_workspace(int device, size_t* bytes);
+int lgp_clip_gradients(int device, const lgp_gradient* list, int64_t n, double most, float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 const char* lgp_strerror(int status);
 const char* lgp_last_error(const lgp_ctx* ctx); /* text of the last failure on this context */
 

@@ -77,6 +77,19 @@ class _Packed(C.Structure):
                 ("pos", C.c_void_p)]
 
 
+class _Residual(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("residual", C.c_void_p), ("x_row", C.c_int64), ("residual_row", C.c_int64), ("tokens", C.c_int64), ("width", C.c_int32),
+                ("dtype", C.c_int32), ("stream_dtype", C.c_int32), ("weight", C.c_void_p), ("pos", C.c_void_p), ("eps", C.c_float)]
+
+
+class _Rows8(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("width", C.c_int32), ("values", C.c_void_p), ("scales", C.c_void_p), ("pos", C.c_void_p)]
+
+
+class _Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int64)]
+
+
 class Profile(C.Structure):
     _fields_ = [("n_sample", C.c_int64), ("n_partition", C.c_int64), ("n_hit", C.c_int64), ("n_miss", C.c_int64),
                 ("ms_sample", C.c_double), ("ms_partition", C.c_double), ("ms_hit", C.c_double),
@@ -89,6 +102,8 @@ EXPORTS = ["lgp_host_alloc", "lgp_host_free", "lgp_shuffle_tablet", "lgp_create"
            "lgp_sample_khop", "lgp_sample_extract", "lgp_build_blocks", "lgp_gather_features", "lgp_gather_features_static", "lgp_set_overlap", "lgp_workspace_bytes", "lgp_check", "lgp_set_wait_polls", "lgp_get_sample_marks", "lgp_set_profiling", "lgp_get_profile",
            "lgp_attend", "lgp_attend_workspace", "lgp_attend_backward", "lgp_norm_rotate", "lgp_norm_rotate_workspace", "lgp_norm_rotate_backward",
            "lgp_pack_activations", "lgp_unpack_activations", "lgp_packed_weight_grad_workspace", "lgp_packed_weight_grad",
+           "lgp_add_norm", "lgp_add_norm_rows8", "lgp_add_norm_workspace", "lgp_add_norm_backward", "lgp_pack_rows8", "lgp_clip_gradients_workspace",
+           "lgp_clip_gradients",
            "lgp_strerror", "lgp_last_error"]
 
 _lib = None
@@ -148,6 +163,13 @@ def load_library():
     L.lgp_unpack_activations.argtypes = [C.c_int, vp, vp, vp]
     L.lgp_packed_weight_grad_workspace.argtypes = [C.c_int, vp, i32, vp]
     L.lgp_packed_weight_grad.argtypes = [C.c_int, vp, vp, i64, i32, i32, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_add_norm.argtypes = [C.c_int, vp, vp, vp, vp]
+    L.lgp_add_norm_rows8.argtypes = [C.c_int, vp, vp, vp, vp]
+    L.lgp_add_norm_workspace.argtypes = [C.c_int, vp, vp]
+    L.lgp_add_norm_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_pack_rows8.argtypes = [C.c_int, vp, i64, i32, vp, vp]
+    L.lgp_clip_gradients_workspace.argtypes = [C.c_int, vp]
+    L.lgp_clip_gradients.argtypes = [C.c_int, vp, i64, C.c_double, vp, vp, C.c_size_t, vp]
     L.lgp_strerror.argtypes = [C.c_int]
     L.lgp_strerror.restype = C.c_char_p
     L.lgp_last_error.argtypes = [vp]

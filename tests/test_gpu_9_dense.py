@@ -1,0 +1,368 @@
+"""What a layer has around its attention, against its definitions in 64 bits (tests/dense_common.py), at the sizes, masks and layouts where it can go
+wrong; streams, captured graphs and runs that are repeated bit by bit."""
+import math
+
+import pytest
+import torch
+
+import dense_common as ref
+from layer_common import UNIT, check
+
+pytestmark = pytest.mark.gpu
+
+F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
+TYPES = [(F32, F32), (F16, F16), (BF16, BF16), (F16, F32), (BF16, F32)]
+
+
+def lgp():
+    import paper_2305_16588_amd
+    return paper_2305_16588_amd
+
+
+def draw(shape, dtype, seed, size=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return (torch.randn(shape, generator=g, device="cuda") * size).to(dtype)
+
+
+def slots(tokens, seed, share=0.3):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.where(torch.rand(tokens, generator=g, device="cuda") < share, -1, torch.arange(tokens, device="cuda")).to(torch.int32)
+
+
+def strided(t, more=3):
+    """The same rows further apart, at an odd place."""
+    wide = torch.full((t.shape[0], t.shape[1] + more), math.nan, dtype=t.dtype, device=t.device)
+    wide[:, 1:1 + t.shape[1]] = t
+    return wide[:, 1:1 + t.shape[1]]
+
+
+def same(a, b):
+    return torch.equal(torch.nan_to_num(a.float(), nan=7.0), torch.nan_to_num(b.float(), nan=7.0))
+
+
+def run_norm(tokens, width, dtype, stream, pos=None, seed=1, adds=True, apart=False, eps=1e-6, later=True):
+    L = lgp()
+    x, w = draw((tokens, width), dtype, seed), 1 + draw((width,), F32, seed + 1, 0.3)
+    res = draw((tokens, width), stream, seed + 2, 2.0) if adds else None
+    dy, dt = draw((tokens, width), dtype, seed + 3), draw((tokens, width), stream, seed + 4) if later else None
+    if pos is not None:
+        for t in (x, res, dy, dt):
+            if t is not None:
+                t[pos < 0] = math.nan
+    if apart:
+        x, res = strided(x), res if res is None else strided(res, 8)
+    y, total = L.add_norm(x, res, w, pos=pos, eps=eps)
+    want = ref.add_norm(x, res, w, pos, eps)
+    if adds:
+        assert total.dtype is stream and same(total, want["total"])
+    else:
+        assert total is x
+    check(y, want["y"], "y")
+    back = ref.add_norm(None, None, w, pos, eps, dy, dt, total)
+    dx, dr, dw = L.add_norm_backward(dy, dt, total, w, pos=pos, eps=eps)
+    assert dx.dtype is dtype and dr.dtype is total.dtype
+    check(dx, back["dx"], "dx")
+    check(dr, back["d_residual"], "d_residual")
+    check(dw, back["dw"], "d_weight")
+    rows, total8 = L.add_norm_rows8(x, res, w, pos=pos, eps=eps)
+    assert same(total8, total)
+    ref.rows8(*want["y32"], rows.values, rows.scales, ref.live_rows(tokens, pos, "cuda"))
+
+
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("width", [1, 7, 8, 31, 32, 33, 100, 128, 129, 256, 257, 500, 512, 1000, 1024, 1025, 2048, 2049, 4096, 4100, 8192, 8193, 16384])
+def test_norm_of_every_width(width, dtype, stream):
+    for tokens in (1, 37):
+        run_norm(tokens, width, dtype, stream)
+    run_norm(70, width, dtype, stream, pos=slots(70, width), apart=True)
+
+
+@pytest.mark.parametrize("dtype,stream", TYPES)
+@pytest.mark.parametrize("tokens,width", [(5000, 256), (20_011, 40), (3001, 1024), (1500, 3000)])
+def test_norm_of_many_rows(tokens, width, dtype, stream):
+    run_norm(tokens, width, dtype, stream, pos=slots(tokens, 3))
+    run_norm(tokens, width, dtype, stream, later=False, eps=1e-3)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_norm_without_a_residual(dtype):
+    run_norm(300, 250, dtype, dtype, adds=False, pos=slots(300, 5))
+    run_norm(1, 4500, dtype, dtype, adds=False)
+
+
+def test_norm_of_nothing_and_of_zeros():
+    L = lgp()
+    w = torch.ones(40, device="cuda")
+    for n in (0, 1):
+        x = torch.zeros(n, 40, dtype=F16, device="cuda")
+        y, total = L.add_norm(x, x, w)
+        dx, dr, dw = L.add_norm_backward(x, x, total, w)
+        rows, _ = L.add_norm_rows8(x, x, w)
+        assert all(t.shape == (n, 40) and (t == 0).all() for t in (y, total, dx, dr)) and (dw == 0).all() and rows.shape == (n, 40) and (rows.values == 0).all()
+    pos = torch.full((9,), -1, dtype=torch.int32, device="cuda")          # no token at all, and an eps of zero
+    x = torch.full((9, 40), math.nan, device="cuda")
+    y, total = L.add_norm(x, x, w, pos=pos, eps=0.0)
+    dx, _, dw = L.add_norm_backward(x, x, total, w, pos=pos, eps=0.0)
+    assert (y == 0).all() and (total == 0).all() and (dx == 0).all() and (dw == 0).all()
+
+
+def test_norm_keeps_what_is_not_finite_in_its_row():
+    L = lgp()
+    x, res, w = draw((50, 130), BF16, 1), draw((50, 130), BF16, 2), 1 + draw((130,), F32, 3, 0.1)
+    clean, _ = L.add_norm(x, res, w)
+    clean8, _ = L.add_norm_rows8(x, res, w)
+    x[7, 3], x[9, 129], x[11, 0] = math.nan, math.inf, -math.inf
+    y, _ = L.add_norm(x, res, w)
+    rows, _ = L.add_norm_rows8(x, res, w)
+    odd = torch.zeros(50, dtype=torch.bool, device="cuda")
+    odd[[7, 9, 11]] = True
+    assert torch.equal(y[~odd], clean[~odd]) and torch.isnan(y[7]).all() and torch.isnan(y[9, 129]) and (y[9, :129] == 0).all()
+    assert torch.isnan(rows.scales[odd]).all() and (rows.values[odd] == 0).all()
+    assert torch.equal(rows.values[~odd], clean8.values[~odd]) and torch.equal(rows.scales[~odd], clean8.scales[~odd])
+
+
+def test_rows_of_broadcast_and_same_inputs():
+    """One row for all tokens, and the branch as its own residual."""
+    L = lgp()
+    one, res, w = draw((1, 96), F16, 1), draw((33, 96), F16, 2), 1 + draw((96,), F32, 3, 0.1)
+    x = one.expand(33, 96)
+    y, total = L.add_norm(x, res, w)
+    assert same(total, x.contiguous() + res)
+    check(y, ref.add_norm(x, res, w, None, 1e-6)["y"])
+    y, total = L.add_norm(res, res, w)
+    assert same(total, res + res)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("width", [1, 15, 16, 17, 100, 1000, 5000, 16384])
+def test_rows_in_8_bits(width, dtype):
+    L = lgp()
+    x = draw((50, width), dtype, width) * torch.exp2(torch.randint(-12, 8, (50, 1), generator=torch.Generator().manual_seed(1)).float()).cuda().to(dtype)
+    x[3] = 0
+    pos = slots(50, 2)
+    x[pos < 0] = math.nan
+    for t in (x, strided(x)):
+        rows = L.pack_rows(t, pos=pos)
+        ref.rows8(x.double(), torch.zeros_like(x, dtype=torch.float64), rows.values, rows.scales, pos >= 0)
+    assert L.pack_rows(x[:0]).shape == (0, width)
+
+
+def test_rows_in_8_bits_of_the_smallest_and_largest_numbers():
+    L = lgp()
+    x = torch.tensor([[1e-45, -1e-45, 0.0], [3e-38, 1e-38, -3e-38], [3e38, -3.4e38, 1.0], [math.inf, 1, 2], [1, math.nan, 2], [2e-36, -1e-36, 0]], device="cuda")
+    rows = L.pack_rows(x)
+    ref.rows8(x.double(), torch.zeros_like(x, dtype=torch.float64), rows.values, rows.scales, torch.ones(6, dtype=torch.bool, device="cuda"))
+    assert torch.isfinite(rows.scales[[0, 1, 2, 5]]).all()
+
+
+def test_norm_with_autograd():
+    L = lgp()
+    x, res, w = draw((60, 100), F32, 1).requires_grad_(), draw((60, 100), F32, 2).requires_grad_(), (1 + draw((100,), F32, 3, 0.2)).requires_grad_()
+    a, b = draw((60, 100), F32, 4), draw((60, 100), F32, 5)
+
+    def grads(f):
+        return torch.autograd.grad(f, (x, res, w))
+
+    y, total = L.add_norm(x, res, w)
+    got = grads((y * a).sum() + (total * b).sum())
+    t = (x + res).double()
+    n = t / torch.sqrt((t * t).mean(1, keepdim=True) + 1e-6)
+    want = torch.autograd.grad(((n * w) * a).sum() + (t * b).sum(), (x, res, w), retain_graph=True)
+    for g, v in zip(got, want):
+        assert torch.allclose(g, v, rtol=2e-5, atol=1e-5)
+    y, total = L.add_norm(x, res, w)                 # one of the results alone
+    want = grads(((n * w) * a).sum())
+    for g, v in zip(grads((y * a).sum()), want):
+        assert torch.allclose(g, v, rtol=2e-5, atol=1e-5)
+    y, total = L.add_norm(x, res, w)
+    g = torch.autograd.grad((total * b).sum(), (x, res, w), allow_unused=True)
+    assert torch.equal(g[0], b) and torch.equal(g[1], b) and (g[2] == 0).all()
+    y, total = L.add_norm(x, None, w)
+    assert total is x
+    gx, gw = torch.autograd.grad((y * a).sum() + (total * b).sum(), (x, w))
+    t = x.double()
+    wx, ww = torch.autograd.grad((t / torch.sqrt((t * t).mean(1, keepdim=True) + 1e-6) * w * a).sum() + (t * b).sum(), (x, w))
+    assert torch.allclose(gx, wx, rtol=2e-5, atol=1e-5) and torch.allclose(gw, ww, rtol=2e-5, atol=1e-5)
+    leaf, other = draw((4, 100), F32, 6).requires_grad_(), draw((4, 100), F32, 7).requires_grad_()
+    for _ in range(2):                                # the gradients of both are one tensor, and add up apart
+        L.add_norm(leaf, other, w)[1].sum().backward()
+    leaf.grad.mul_(5)
+    assert (other.grad == 2).all() and (leaf.grad == 10).all()
+
+
+def test_norm_beyond_32_bits():
+    """Elements whose place passes 2^31, and bytes 2^32."""
+    L = lgp()
+    tokens, width = 4_300_000, 512
+    x = torch.zeros(tokens, width, dtype=BF16, device="cuda")
+    w = torch.ones(width, device="cuda")
+    tail = draw((5, width), BF16, 1)
+    x[-5:] = tail
+    y, total = L.add_norm(x, x, w)
+    assert same(total[-5:], tail + tail)
+    check(y[-5:], ref.add_norm(tail, tail, w, None, 1e-6)["y"])
+    dx, _, dw = L.add_norm_backward(y, None, total, w)
+    check(dx[-5:], ref.add_norm(None, None, w, None, 1e-6, y[-5:], None, total[-5:])["dx"])
+    rows, _ = L.add_norm_rows8(x, x, w)
+    assert (rows.values[-5:].abs().amax(1) == 127).all() and (rows.values[-1000:-5] == 0).all()
+
+
+# ---- gradients' norm and clipping
+
+def gradients(shapes, seed=1, flat=False):
+    out = [draw(shape, dtype, seed + i, 10.0 ** -(i % 4)) for i, (shape, dtype) in enumerate(shapes)]
+    if flat:           # end to end in a bucket of each type
+        for dtype in (F32, F16, BF16):
+            of = [i for i, g in enumerate(out) if g.dtype is dtype]
+            bucket = torch.cat([torch.zeros(1, dtype=dtype, device="cuda"), *(out[i].flatten() for i in of)])
+            at = 1
+            for i in of:
+                n = out[i].numel()
+                out[i] = bucket[at:at + n].view(out[i].shape)
+                at += n
+    return out
+
+
+MANY = [((7,), F32), ((300, 70), BF16), ((0,), F16), ((1,), BF16), ((129, 129), F16), ((), F32), ((40_000,), BF16), ((16_384,), F32), ((16_385,), F16), ((5, 0), F32)]
+
+
+def check_clip(grads, most, stays):
+    L = lgp()
+    norm, want = ref.clip(grads, most)
+    given = [g.clone() for g in grads]
+    out = None if stays else [torch.full_like(g, 7.0) for g in grads]
+    got = L.clip_gradients(grads, most, out=out)
+    assert got.shape == () and got.dtype is F32 and abs(float(got) - norm) <= 2.0 ** -23 * norm
+    assert abs(float(L.gradient_norm(given)) - norm) <= 2.0 ** -23 * norm
+    for g, o, w in zip(given, grads if stays else out, want):
+        tiny = {F32: 2.0 ** -150, F16: 2.0 ** -25, BF16: 2.0 ** -134}[g.dtype]
+        check(o, (w, (UNIT[g.dtype] + 2.0 ** -23 * (g.dtype is not F32)) * w.abs() * (1 + 2.0 ** -20) + tiny))
+    if not stays:
+        assert all(torch.equal(a, b) for a, b in zip(grads, given))
+
+
+@pytest.mark.parametrize("flat", [False, True])
+@pytest.mark.parametrize("stays", [False, True])
+@pytest.mark.parametrize("most", [1e-3, 1.0, 1e9, math.inf, 0.0])
+def test_clipping(most, stays, flat):
+    check_clip(gradients(MANY, flat=flat), most, stays)
+    check_clip(gradients([((100, 100), F32)]), most, stays)
+
+
+def test_clipping_of_more_tensors_than_a_launch_takes():
+    for n in (119, 120, 121, 1000):
+        check_clip(gradients([((i % 7 * 40,), (F32, F16, BF16)[i % 3]) for i in range(n)]), 0.5, n % 2 == 0)
+    check_clip(gradients([((5_000_000,), BF16), ((3_000_001,), F32)] * 2), 0.5, True)
+
+
+def test_clipping_by_the_ends_of_the_numbers():
+    L = lgp()
+    check_clip([torch.full((1000,), 1e30, device="cuda"), torch.full((10,), -3e37, device="cuda")], 1.0, True)        # squares beyond fp32
+    check_clip([torch.full((1000,), 1e-38, device="cuda")], 1e-39, True)
+    check_clip([torch.full((10,), 60000.0, dtype=F16, device="cuda")], 60000.0, True)
+    check_clip([torch.zeros(70, device="cuda")], 1.0, True)
+    for bad in (math.inf, -math.inf, math.nan):
+        g = [draw((3000,), F32, 1), draw((500,), BF16, 2)]
+        g[1][77] = bad
+        kept = [t.clone() for t in g]
+        out = [torch.empty_like(t) for t in g]
+        for o in (None, out):
+            norm = L.clip_gradients(g, 0.1, out=o)
+            assert not math.isfinite(float(norm))
+            assert all(same(a, b) for a, b in zip(g, kept))
+        assert all(same(a, b) for a, b in zip(out, kept))
+    g = [torch.full((4,), 3e38, device="cuda")]                     # finite numbers whose norm is no float: left alone
+    assert float(L.clip_gradients(g, 1.0)) == math.inf and (g[0] == 3e38).all()
+
+
+def test_clipping_leaves_a_mark_for_autograd():
+    L = lgp()
+    w = torch.ones(5, device="cuda", requires_grad=True)
+    g = torch.full((5,), 3.0, device="cuda")
+    y = (w * g).sum()
+    L.clip_gradients([g], 1.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.backward()
+
+
+# ---- streams, graphs, repeated runs
+
+def pieces():
+    x, res, w = draw((700, 250), BF16, 1), draw((700, 250), F32, 2), 1 + draw((250,), F32, 3, 0.1)
+    pos = slots(700, 4)
+    grads = gradients(MANY)
+    out = [torch.empty_like(g) for g in grads]
+    L = lgp()
+
+    def run(stream=None):
+        y, total = L.add_norm(x, res, w, pos=pos, stream=stream)
+        back = L.add_norm_backward(y, total, total, w, pos=pos, stream=stream)
+        rows, _ = L.add_norm_rows8(x, res, w, pos=pos, stream=stream)
+        packed = L.pack_rows(x, pos=pos, stream=stream)
+        return [y, total, *back, rows.values, rows.scales, packed.values, packed.scales, L.clip_gradients(grads, 0.3, out=out, stream=stream),
+                *[o.clone() if stream is None else o for o in out]]
+    return run, (x, res, *grads)
+
+
+def test_runs_are_the_same_bit_by_bit():
+    run, _ = pieces()
+    first = run()
+    for _ in range(3):
+        assert all(torch.equal(a, b) for a, b in zip(run(), first))
+
+
+def test_another_stream():
+    run, _ = pieces()
+    first = run()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = run(side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+def test_captured_and_replayed():
+    run, inputs = pieces()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run()
+    for seed in range(4):
+        for t in inputs:
+            t.copy_(draw(t.shape, t.dtype, 100 + seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [h.clone() for h in held]
+        want = run()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), seed
+
+
+# ---- refusals
+
+def test_refusals():
+    L = lgp()
+    x, w = torch.zeros(4, 32, dtype=BF16, device="cuda"), torch.ones(32, device="cuda")
+    bad = [lambda: L.add_norm(x.cpu(), x, w), lambda: L.add_norm(x, x.half(), w), lambda: L.add_norm(x, x[:3], w), lambda: L.add_norm(x.float(), x, w),
+           lambda: L.add_norm(x, x, w[:31]), lambda: L.add_norm(x, x, w.half()), lambda: L.add_norm(x, x, w, pos=torch.zeros(3, dtype=torch.int32, device="cuda")),
+           lambda: L.add_norm(x, x, w, pos=torch.zeros(4, device="cuda")), lambda: L.add_norm(x.int(), None, w), lambda: L.add_norm(x[0], None, w),
+           lambda: L.add_norm(x.t(), None, w[:4]), lambda: L.add_norm(x, x, w, eps=-1.0), lambda: L.add_norm(x, x, w, eps=1e300), lambda: L.add_norm(x, x, w.cpu()),
+           lambda: L.add_norm(torch.zeros(1, 16385, device="cuda"), None, torch.ones(16385, device="cuda")),
+           lambda: L.add_norm_backward(x, None, x.half(), w), lambda: L.add_norm_backward(x, x.float(), x, w), lambda: L.add_norm_backward(x[:2], None, x, w),
+           lambda: L.add_norm_rows8(x, x.half(), w), lambda: L.pack_rows(x.int()), lambda: L.pack_rows(x.t()), lambda: L.pack_rows(torch.zeros(1, 16385, device="cuda")),
+           lambda: L.Rows8(x, w, 32), lambda: L.Rows8(torch.zeros(4, 32, dtype=torch.int8, device="cuda"), w, 32),
+           lambda: L.Rows8(torch.zeros(4, 20, dtype=torch.int8, device="cuda"), w[:4], 20),
+           lambda: L.clip_gradients([], 1.0), lambda: L.clip_gradients([x.t()], 1.0), lambda: L.clip_gradients([x.int()], 1.0), lambda: L.clip_gradients([x.cpu()], 1.0),
+           lambda: L.clip_gradients([x], -1.0), lambda: L.clip_gradients([x], math.nan), lambda: L.clip_gradients([x], "one"), lambda: L.clip_gradients([x, x], 1.0),
+           lambda: L.clip_gradients([x[:3], x[2:]], 1.0), lambda: L.clip_gradients([x[:2]], 1.0, out=[x[1:3]]), lambda: L.clip_gradients([x], 1.0, out=[x.half()]),
+           lambda: L.clip_gradients([x, w], 1.0, out=[x]), lambda: L.clip_gradients([x, x.clone()], 1.0, out=[w.new_zeros(4, 32, dtype=BF16)] * 2),
+           lambda: L.clip_gradients([x[:2], x[2:]], 1.0, out=[x[2:], x[:2]]), lambda: L.clip_gradients([x.cpu(), x], 1.0)]
+    for i, call in enumerate(bad):
+        with pytest.raises(L.LegionPrepError):
+            call()
+            pytest.fail(f"call {i} was taken")
+    assert float(L.gradient_norm([x, x])) == 0.0                # only read: may be the same
+    torch.cuda.synchronize()
