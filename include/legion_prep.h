@@ -543,6 +543,34 @@ int lgp_add_norm_backward(int device, const lgp_residual* in, const void* dy, co
 /* Rows of x (dtype, x_row elements from row to row, any alignment; up to 16384 wide) in 8 bits, by the same rule. */
 int lgp_pack_rows8(int device, const void* x, int64_t x_row, int32_t dtype, const lgp_rows8* out, void* stream);
 
+/* out [tokens, channels] = (sum over k of rows[t][k] weight[c][k]) * weight scale[c] * row scale[t] + bias[c] (float[channels] or NULL), rounded to dtype (LGP_F32, LGP_F16 or
+ * LGP_BF16), rows end to end.  weight is rows in 8 bits too, one for each channel.  Sums are exact; widths up to 2^17, tokens and channels up to 2^24. */
+int lgp_linear_rows8(int device, const lgp_rows8* rows, const lgp_rows8* weight, const float* bias, int32_t dtype, void* out, void* stream);
+
+/* The gated pair of projections of a feed-forward block.  x_row is in elements, a multiple of 8 below 2^22; pointers are aligned to 16 bytes. */
+#define LGP_SILU 0
+#define LGP_GELU 1                      /* of the error function */
+typedef struct {
+  const void* x;                        /* [tokens, width], x_row elements from row to row                   */
+  int64_t x_row, tokens;                /* tokens: up to 2^24                                                */
+  int32_t width;                        /* a multiple of 8, up to 65536                                      */
+  int32_t hidden;                       /* rows of each weight, up to 65536                                  */
+  int32_t dtype;                        /* LGP_F16 or LGP_BF16, of everything here                           */
+  int32_t act;                          /* LGP_SILU or LGP_GELU                                              */
+  const void *w_gate, *w_up;            /* [hidden, width] each, rows end to end                             */
+  const int32_t* pos;                   /* tokens entries, or NULL; a negative one: no token in this row     */
+} lgp_gated;
+
+/* h = act(x w_gate^T) * (x w_up^T), [tokens, hidden], rows end to end: one kernel, sums and activation in 32 bits, h rounded once. */
+int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* stream);
+
+/* Gradients of lgp_gated_linear by x (dx [tokens, width], zeros where no token is) and the weights (like them), from that of h (dh [tokens, hidden], rows end to
+ * end).  Both projections are computed again; the gradients of their results are rounded to the type of x for the products that follow, so in fp16 they have to be
+ * numbers that it holds. */
+int lgp_gated_linear_workspace(int device, const lgp_gated* in, size_t* bytes);
+int lgp_gated_linear_backward(int device, const lgp_gated* in, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
 /* A gradient: n consecutive elements, aligned to one.  out: where the scaled ones go; out = grad: they stay where they are. */
 typedef struct {
   const void* grad;

@@ -6,10 +6,11 @@ from .binding import (BlockBuffers, CachePlan, Context, LegionPrepError, PlanPoi
                       pinned_empty, worst_case_sizes)
 from .layer import (Documents, PackedActivations, attend, attend_backward, norm_rotate, norm_rotate_backward, pack_activations, packed_weight_grad,
                     rotation_table, unpack_activations)
-from .dense import Rows8, add_norm, add_norm_backward, add_norm_rows8, clip_gradients, gradient_norm, pack_rows
+from .dense import Rows8, add_norm, add_norm_backward, add_norm_rows8, clip_gradients, gated_linear, gated_linear_backward, gradient_norm, linear_rows8, pack_rows
 
 __all__ = ["BlockBuffers", "CachePlan", "Context", "LegionPrepError", "PlanPoint", "Profile", "SampleBuffers", "concurrent_streams", "cslp", "load_library", "shuffle_tablet", "pinned_copy",
            "pinned_empty", "worst_case_sizes",
            "Documents", "PackedActivations", "attend", "attend_backward", "norm_rotate", "norm_rotate_backward", "pack_activations", "packed_weight_grad",
            "rotation_table", "unpack_activations",
-           "Rows8", "add_norm", "add_norm_backward", "add_norm_rows8", "clip_gradients", "gradient_norm", "pack_rows"]
+           "Rows8", "add_norm", "add_norm_backward", "add_norm_rows8", "clip_gradients", "gated_linear", "gated_linear_backward", "gradient_norm",
+           "linear_rows8", "pack_rows"]

@@ -86,6 +86,11 @@ class _Rows8(C.Structure):
     _fields_ = [("tokens", C.c_int64), ("width", C.c_int32), ("values", C.c_void_p), ("scales", C.c_void_p), ("pos", C.c_void_p)]
 
 
+class _Gated(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("x_row", C.c_int64), ("tokens", C.c_int64), ("width", C.c_int32), ("hidden", C.c_int32), ("dtype", C.c_int32),
+                ("act", C.c_int32), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("pos", C.c_void_p)]
+
+
 class _Gradient(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int64)]
 
@@ -103,7 +108,7 @@ EXPORTS = ["lgp_host_alloc", "lgp_host_free", "lgp_shuffle_tablet", "lgp_create"
            "lgp_attend", "lgp_attend_workspace", "lgp_attend_backward", "lgp_norm_rotate", "lgp_norm_rotate_workspace", "lgp_norm_rotate_backward",
            "lgp_pack_activations", "lgp_unpack_activations", "lgp_packed_weight_grad_workspace", "lgp_packed_weight_grad",
            "lgp_add_norm", "lgp_add_norm_rows8", "lgp_add_norm_workspace", "lgp_add_norm_backward", "lgp_pack_rows8", "lgp_clip_gradients_workspace",
-           "lgp_clip_gradients",
+           "lgp_clip_gradients", "lgp_linear_rows8", "lgp_gated_linear", "lgp_gated_linear_workspace", "lgp_gated_linear_backward",
            "lgp_strerror", "lgp_last_error"]
 
 _lib = None
@@ -168,6 +173,10 @@ def load_library():
     L.lgp_add_norm_workspace.argtypes = [C.c_int, vp, vp]
     L.lgp_add_norm_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.lgp_pack_rows8.argtypes = [C.c_int, vp, i64, i32, vp, vp]
+    L.lgp_linear_rows8.argtypes = [C.c_int, vp, vp, vp, i32, vp, vp]
+    L.lgp_gated_linear.argtypes = [C.c_int, vp, vp, vp]
+    L.lgp_gated_linear_workspace.argtypes = [C.c_int, vp, vp]
+    L.lgp_gated_linear_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.lgp_clip_gradients_workspace.argtypes = [C.c_int, vp]
     L.lgp_clip_gradients.argtypes = [C.c_int, vp, i64, C.c_double, vp, vp, C.c_size_t, vp]
     L.lgp_strerror.argtypes = [C.c_int]

@@ -14,7 +14,7 @@ LIB = os.path.join(HERE, "liblegion_prep.so")
 STAMP = os.path.join(HERE, "liblegion_prep.srchash")   # hash of the sources the library was built from
 SOURCES = ["sampler.hip", "compact.hip", "bins.hip", "gather.hip", "extract.hip", "blocks.hip", "cache.hip", "api.hip",
            "attend_forward.hip", "attend_backward.hip", "attend_single.hip", "norm_rotate.hip", "pack.hip",
-           "add_norm.hip", "clip.hip"]
+           "add_norm.hip", "clip.hip", "gated.hip", "rows8.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-I" + INCLUDE, "-I" + CSRC]

@@ -1,0 +1,286 @@
+// Products of matrices by tiles: what the gated projections, their gradients and the products of rows in 8-bit integers share.
+#pragma once
+
+#include "rows_dev.hpp"
+
+namespace lgp {
+namespace layer {
+namespace {
+
+typedef int intx4 __attribute__((ext_vector_type(4)));
+typedef int intx16 __attribute__((ext_vector_type(16)));
+
+// D[32, 32] += A[32, K] B[K, 32] with K of two chunks of 16 bytes, of which lane l holds chunk l / 32 of A row l % 32 and of B column l % 32; D as in layer_dev.hpp.
+// few: D[16, 16] += A[16, K] B[K, 16] with K of four chunks, of which lane l holds chunk l / 16 of A row l % 16 and of B column l % 16; of D it holds column l % 16,
+// register r being row 4 (l / 16) + r.
+__device__ __forceinline__ floatx4 few_mfma(vec8<f16> a, vec8<f16> b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ floatx4 few_mfma(vec8<bf16> a, vec8<bf16> b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+template <typename T> struct Unit {
+  typedef vec8<T> chunk;
+  typedef floatx16 sums;
+  typedef float sum;
+  typedef floatx4 few_sums;
+  static constexpr int kSize = 2;
+  static __device__ __forceinline__ sums mfma(chunk a, chunk b, sums c) { return Elem<T>::mfma(a, b, c); }
+  static __device__ __forceinline__ few_sums few(chunk a, chunk b, few_sums c) { return few_mfma(a, b, c); }
+};
+template <> struct Unit<int8_t> {
+  typedef intx4 chunk;
+  typedef intx16 sums;
+  typedef int sum;
+  typedef intx4 few_sums;
+  static constexpr int kSize = 1;
+  static __device__ __forceinline__ few_sums few(chunk a, chunk b, few_sums c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ sums mfma(chunk a, chunk b, sums c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, b, c, 0, 0, 0); }
+};
+
+__device__ __align__(16) const uint32_t kNothing[4] = {};       // what is read where there is nothing to read
+
+// 16 bytes of each lane, from an address of its own; else as copy16.
+__device__ __forceinline__ void copy16_from(const void* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+template <int N> __device__ __forceinline__ void loads_left() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14); }      // all but the last N are done
+__device__ __forceinline__ void together() {       // everyone's reads of LDS are done, and so are the loads that each has waited for
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// One side of a product.  Along: a row of the tile is a row of memory, and the sum runs along it.  Across: the sum runs over rows of memory, whose columns
+// are the tile's rows.  `second` is the matrix of the other half: of the tile's rows (along, gated) or of the sum (across, from `half` on).
+struct Operand {
+  const char *first, *second;
+  int64_t row_bytes;
+  int32_t rows;                      // of memory, in each matrix; at least one
+  int32_t chunks;                    // of 16 bytes in a row; at least one
+  int32_t half;                      // across: where the second matrix begins in the sum (a multiple of a stage), or more than there is
+  const int32_t* pos;                // across: rows with a negative entry count as zeros; NULL: none
+};
+
+// BM x BN of a product by WM x WN waves, each 32 MI x 32 NJ of it.  A stage is CH chunks of the sum: while one is multiplied, STAGES - 1 are on their way to LDS, past the
+// registers.  Every copy is issued whatever there is to copy -- what lies beyond an end is another valid row whose results are not used, or zeros where it
+// is part of a sum -- so a wave knows how many of its loads are under way.
+//
+// The 32 rows of a block of A lie in LDS in an order (or are read in one) that leaves a lane 16 consecutive rows of D: register r of lane l is row 16 (l / 32) + r, so
+// results are written 32 bytes at a time.
+template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, bool GATED, bool A_ACROSS, bool B_ACROSS> struct Tiles {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, CH = CH_, STAGES = STAGES_;
+  static constexpr int kThreads = 64 * WM * WN, MI = BM / 32 / WM, NJ = BN / 32 / WN;
+  static constexpr int kStage = CH * 16 / Unit<T>::kSize;       // places of the sum
+  static constexpr int NA = BM * CH / kThreads, NB = BN * CH / kThreads;       // copies of a thread
+  static_assert(BM * CH % kThreads == 0 && BN * CH % kThreads == 0 && (!GATED || MI % 2 == 0), "whole copies");
+  typedef typename Unit<T>::chunk chunk;
+  typedef typename Unit<T>::sums sums;
+  struct Shared {
+    alignas(16) char a[STAGES][BM * CH * 16];
+    alignas(16) char b[STAGES][BN * CH * 16];
+  };
+
+  static __device__ __forceinline__ int turned(int row) { return int(__brev(uint32_t(row)) >> 28); }
+  static __device__ __forceinline__ int in_order(int m) { return (m & ~31) + 16 * (m >> 2 & 1) + 4 * (m >> 3 & 3) + (m & 3); }
+
+  // A thread's places in the tile of one side, and what it copies there.
+  template <int ROWS, int N, bool ACROSS, bool PAIR, bool ORDER> struct Side {
+    uint32_t offset[N];
+    static constexpr int kWide = ROWS / 8;           // across: chunks of a row in LDS
+
+    __device__ __forceinline__ Side(const Operand& o, int32_t row0, int tid) {       // along: o begins at the tile's first row
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int place = tid + j * kThreads;
+        if constexpr (ACROSS) {
+          const int r = place / kWide, c = row0 / 8 + ((place % kWide) ^ (turned(r) & (kWide - 1)));
+          offset[j] = uint32_t(r) * uint32_t(o.row_bytes) + (c < o.chunks ? c : 0) * 16;
+        } else {
+          const int r = place / CH, c = (place % CH) ^ (turned(r) & (CH - 1));
+          int at = PAIR ? r % (ROWS / 2) : r;
+          if (ORDER) at = in_order(at);
+          offset[j] = uint32_t(at < o.rows ? at : o.rows - 1) * uint32_t(o.row_bytes) + c * 16;
+        }
+      }
+    }
+    __device__ __forceinline__ void copy(const Operand& o, int32_t at, char* to, int tid) const {       // at: the stage's first place of the sum
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + (tid & ~63) * 16);
+      if constexpr (ACROSS) {
+        const bool later = at >= o.half;
+        const int32_t row = later ? at - o.half : at;
+        const char* from = (later ? o.second : o.first) + int64_t(row) * o.row_bytes;
+        if (row + kStage <= o.rows && !o.pos) {
+#pragma unroll
+          for (int j = 0; j < N; ++j) copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
+        } else {
+          // rows of a wave: the same in all its lanes but for the place in kEach
+          constexpr int kEach = 64 / kWide > 0 ? 64 / kWide : 1;
+          typedef const __attribute__((address_space(4))) int32_t* fixed;
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            const int r = (tid + j * kThreads) / kWide, r0 = __builtin_amdgcn_readfirstlane(r);
+            bool there = row + r < o.rows;
+            if (o.pos) {
+#pragma unroll
+              for (int e = 0; e < kEach; ++e) {
+                const int32_t t = row + r0 + e;
+                if (((fixed)(uintptr_t)o.pos)[t < o.rows ? t : o.rows - 1] < 0) there = there && r != r0 + e;
+              }
+            }
+            copy16_from(there ? static_cast<const void*>(from + offset[j]) : kNothing, lds + j * kThreads * 16);
+          }
+        }
+      } else {
+        const int32_t c0 = at / (16 / Unit<T>::kSize);
+        const bool whole = c0 + CH <= o.chunks;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const char* from = o.first;
+          if (PAIR && __builtin_amdgcn_readfirstlane((tid + j * kThreads) / CH) >= ROWS / 2) from = o.second;
+          from += int64_t(c0) * 16;
+          if (whole) {
+            copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
+          } else {
+            const int place = tid + j * kThreads, c = (place % CH) ^ (turned(place / CH) & (CH - 1));
+            copy16_from(c0 + c < o.chunks ? static_cast<const void*>(from + offset[j]) : kNothing, lds + j * kThreads * 16);
+          }
+        }
+        static_assert(!PAIR || (ROWS / 2) % (64 / CH) == 0, "a wave's rows are of one matrix");
+      }
+    }
+  };
+
+  // Where a lane finds the chunk of its row (along) or column (across) of a block of 32 in step kk of a stage.
+  template <int ROWS, bool ACROSS, bool ORDER> struct Place {
+    int at;
+    __device__ __forceinline__ explicit Place(int lane) {
+      if constexpr (ACROSS) {
+        // sixteen lanes read four rows of 16 columns, which the LDS hands out transposed: lanes of the upper half the later eight rows
+        const int i = lane & 15, r = 8 * (lane >> 5) + (i >> 2), p = 4 * (lane >> 4 & 1) + (i & 3), c = ORDER ? 16 * (p & 1) + 4 * (p >> 1) : 4 * p;
+        at = r * ROWS + (((c >> 3) ^ (turned(r) & (ROWS / 8 - 1))) << 3) + (c & 7);
+      } else {
+        const int r = lane & 31;
+        at = r * CH + ((lane >> 5) ^ (turned(r) & (CH - 1)));
+      }
+    }
+    __device__ __forceinline__ chunk read(const char* tile, int row0, int kk) const {
+      if constexpr (ACROSS) {
+        typedef __attribute__((address_space(3))) shortx4* place;
+        union { shortx4 s[2]; chunk v; } u;
+        const short* rows = reinterpret_cast<const short*>(tile) + kk * 16 * ROWS;
+        const int here = at ^ row0;
+        u.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(rows + here));
+        u.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(rows + 4 * ROWS + (here ^ 16)));       // the turn of a row four further on
+        return u.v;
+      } else {
+        return *reinterpret_cast<const chunk*>(tile + ((at ^ (2 * kk)) + row0 * CH) * 16);
+      }
+    }
+  };
+
+  // First row of a wave's block i of A, in the tile.
+  static __device__ __forceinline__ int block_of(int wm, int i) {
+    if constexpr (GATED) return (i < MI / 2 ? 0 : BM / 2) + (wm * (MI / 2) + i % (MI / 2)) * 32;
+    else return (wm * MI + i) * 32;
+  }
+
+  // acc += over places [begin, end) of the sum; begin is a multiple of a stage.
+  static __device__ __forceinline__ void run(Shared& s, Operand a, Operand b, int32_t a_row, int32_t b_row, int32_t begin, int32_t end,
+                                             sums (&acc)[MI][NJ]) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
+    if constexpr (!A_ACROSS) a.first += a_row * a.row_bytes, a.second += a_row * a.row_bytes, a.rows -= a_row;
+    if constexpr (!B_ACROSS) b.first += b_row * b.row_bytes, b.rows -= b_row;
+    const Side<BM, NA, A_ACROSS, GATED, true> from_a(a, a_row, tid);
+    const Side<BN, NB, B_ACROSS, false, false> from_b(b, b_row, tid);
+    const Place<BM, A_ACROSS, true> at_a(lane);
+    const Place<BN, B_ACROSS, false> at_b(lane);
+    const int32_t n = (end - begin + kStage - 1) / kStage;
+    auto fetch = [&](int32_t k) {
+      const int to = k % STAGES;
+      from_a.copy(a, begin + k * kStage, s.a[to], tid);
+      from_b.copy(b, begin + k * kStage, s.b[to], tid);
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+      if (k < n) fetch(k);
+    for (int32_t k = 0; k < n; ++k) {
+      if (n - k >= STAGES - 1) loads_left<(STAGES - 2) * (NA + NB)>();
+      else loads_done();
+      together();
+      if (k + STAGES - 1 < n) fetch(k + STAGES - 1);
+      const char *ta = s.a[k % STAGES], *tb = s.b[k % STAGES];
+#pragma unroll
+      for (int kk = 0; kk < CH / 2; ++kk) {
+        chunk x[MI], y[NJ];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) x[i] = at_a.read(ta, block_of(wm, i), kk);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) y[j] = at_b.read(tb, (wn * NJ + j) * 32, kk);
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NJ; ++j) acc[i][j] = Unit<T>::mfma(x[i], y[j], acc[i][j]);
+      }
+    }
+  }
+};
+
+// Few rows of B: a workgroup has 16 rows of A (of each of a pair), which it reads once, and 16 of B.  Its eight waves take every eighth four chunks of the sum, straight
+// to registers, many loads at a time, and are added in LDS in their order.  The result of A row r and B row c lies at sums[pair][c][r].
+constexpr int kFewWaves = 8, kFewTokens = 32;
+template <typename T, bool PAIR> struct Few {
+  typedef typename Unit<T>::chunk chunk;
+  typedef typename Unit<T>::sum sum;
+  static constexpr int kPair = PAIR ? 2 : 1;
+  struct Shared { sum sums[kFewWaves][kPair][16][17]; };
+  static __device__ __forceinline__ void run(Shared& s, const Operand& a, const Operand& b, int32_t a_row, int32_t b_row) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const char* pa = a.first + int64_t(min(a_row + (lane & 15), a.rows - 1)) * a.row_bytes;
+    const char* pa2 = PAIR ? a.second + int64_t(min(a_row + (lane & 15), a.rows - 1)) * a.row_bytes : nullptr;
+    const char* pb = b.first + int64_t(min(b_row + (lane & 15), b.rows - 1)) * b.row_bytes;
+    typename Unit<T>::few_sums acc[kPair] = {};
+    const chunk nothing = {};
+    constexpr int kAtOnce = PAIR ? 4 : 8;
+    for (int32_t c0 = 4 * wave; c0 < a.chunks; c0 += 4 * kFewWaves * kAtOnce) {
+      chunk x[kAtOnce], x2[kAtOnce], y[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        const int32_t c = c0 + 4 * kFewWaves * k + (lane >> 4);
+        const bool in = c < a.chunks;
+        x[k] = in ? *reinterpret_cast<const chunk*>(pa + 16 * int64_t(c)) : nothing;
+        if (PAIR) x2[k] = in ? *reinterpret_cast<const chunk*>(pa2 + 16 * int64_t(c)) : nothing;
+        y[k] = in ? *reinterpret_cast<const chunk*>(pb + 16 * int64_t(c)) : nothing;
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        acc[0] = Unit<T>::few(x[k], y[k], acc[0]);
+        if (PAIR) acc[kPair - 1] = Unit<T>::few(x2[k], y[k], acc[kPair - 1]);
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < kPair; ++q)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s.sums[wave][q][lane & 15][4 * (lane >> 4) + r] = acc[q][r];
+    __syncthreads();
+  }
+  static __device__ __forceinline__ sum of(const Shared& s, int q, int c, int r) {
+    sum x = s.sums[0][q][c][r];
+#pragma unroll
+    for (int w = 1; w < kFewWaves; ++w) x += s.sums[w][q][c][r];
+    return x;
+  }
+};
+
+// Which tile a workgroup has: consecutive ones, which go to one XCD, are those of eight tiles of B's rows with one of A's rows, then with the next.
+struct Tile { int32_t m, n, part; };
+__device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t blocks, int32_t tiles_m, int32_t tiles_n) {
+  const uint32_t piece = piece_of(block, blocks), all = uint32_t(tiles_m) * uint32_t(tiles_n);
+  Tile t;
+  t.part = int32_t(piece / all);
+  const uint32_t of = piece % all, group = of / (8 * uint32_t(tiles_m)), in = of % (8 * uint32_t(tiles_m));
+  const uint32_t left = uint32_t(tiles_n) - group * 8, wide = left < 8 ? left : 8;
+  t.m = int32_t(in / wide);
+  t.n = int32_t(group * 8 + in % wide);
+  return t;
+}
+
+}  // namespace
+}  // namespace layer
+}  // namespace lgp

@@ -1,0 +1,137 @@
+// Products of rows in 8-bit integers, with a scale for each row and each channel.
+#include "product_dev.hpp"
+
+#include <algorithm>
+
+namespace lgp {
+namespace layer {
+namespace {
+
+struct Product8Params {
+  Operand w, x;
+  const float *w_scales, *x_scales, *bias;
+  const int32_t* pos;
+  int32_t tokens, channels, chunks, tiles_m, tiles_n;
+  void* out;
+};
+
+// Sums are exact in 32-bit integers: 2^17 products of at most 127^2 are less than 2^31.  They are rounded to 32 bits, multiplied by the channel's scale and
+// then by the row's.
+template <typename T> __device__ __forceinline__ void write_channels(const Product8Params& p, int32_t token, bool live, float scale, int32_t c, const int* sums) {
+  const int32_t n = p.channels - c;
+  if (n <= 0) return;
+  float w[8], b[8], y[8];
+  read_row(p.w_scales + c, n, w);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) b[k] = 0.f;
+  if (p.bias) read_row(p.bias + c, n, b);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) y[k] = live ? float(sums[k]) * w[k] * scale + b[k] : 0.f;
+  write_row(static_cast<T*>(p.out) + int64_t(token) * p.channels + c, n, y);
+}
+
+template <typename T, class P>
+__global__ __launch_bounds__(P::kThreads, 2) void product8_kernel(const Product8Params p) {
+  __shared__ typename P::Shared lds;
+  const Tile t = tile_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
+  const int32_t c0 = t.m * P::BM, t0 = t.n * P::BN;
+  intx16 acc[P::MI][P::NJ] = {};
+  P::run(lds, p.w, p.x, c0, t0, 0, p.chunks * 16, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % P::WM, wn = wave / P::WM;
+#pragma unroll
+  for (int j = 0; j < P::NJ; ++j) {
+    const int32_t token = t0 + (wn * P::NJ + j) * 32 + (lane & 31);
+    if (token >= p.tokens) continue;
+    const bool live = !p.pos || p.pos[token] >= 0;
+    const float scale = p.x_scales[token];
+#pragma unroll
+    for (int i = 0; i < P::MI; ++i)
+#pragma unroll
+      for (int r0 = 0; r0 < 16; r0 += 8) {
+        int sums[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sums[k] = acc[i][j][r0 + k];
+        write_channels<T>(p, token, live, scale, c0 + (wm * P::MI + i) * 32 + 16 * (lane >> 5) + r0, sums);
+      }
+  }
+}
+
+// Few rows: a thread has one channel of one.
+template <typename T>
+__global__ __launch_bounds__(64 * kFewWaves) void product8_few_kernel(const Product8Params p) {
+  typedef Few<int8_t, false> F;
+  __shared__ F::Shared lds;
+  const int32_t c0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+  F::run(lds, p.w, p.x, c0, t0);
+  const int r = threadIdx.x & 15, c = threadIdx.x >> 4;
+  if (c >= 16 || t0 + c >= p.tokens || c0 + r >= p.channels) return;
+  const float y = float(F::of(lds, 0, c, r)) * p.w_scales[c0 + r] * p.x_scales[t0 + c] + (p.bias ? p.bias[c0 + r] : 0.f);
+  static_cast<T*>(p.out)[int64_t(t0 + c) * p.channels + c0 + r] = T(!p.pos || p.pos[t0 + c] >= 0 ? y : 0.f);
+}
+
+typedef Tiles<int8_t, 256, 256, 2, 4, 4, 4, false, false, false> Large8;
+typedef Tiles<int8_t, 128, 256, 2, 2, 4, 3, false, false, false> Middle8;
+typedef Tiles<int8_t, 64, 64, 2, 2, 8, 3, false, false, false> Small8;
+enum { kLarge = 0, kMiddle = 1, kSmall = 2 };       // forms of a tile
+
+template <typename T, class P> void launch8(Product8Params p, hipStream_t s) {
+  p.tiles_m = (p.channels + P::BM - 1) / P::BM;
+  p.tiles_n = (p.tokens + P::BN - 1) / P::BN;
+  product8_kernel<T, P><<<uint32_t(p.tiles_m) * uint32_t(p.tiles_n), P::kThreads, 0, s>>>(p);
+}
+template <typename T> void product8(const Product8Params& p, hipStream_t s) {
+  if (p.tokens <= kFewTokens) {
+    product8_few_kernel<T><<<dim3((p.channels + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
+    return;
+  }
+  const int f = p.tokens <= 1024 ? kSmall : kLarge;
+  if (f == kLarge) launch8<T, Large8>(p, s);
+  else if (f == kMiddle) launch8<T, Middle8>(p, s);
+  else launch8<T, Small8>(p, s);
+}
+
+int check_side(const lgp_rows8* r) {
+  if (!r || r->tokens < 0 || r->width < 1) return LGP_EINVAL;
+  if (r->width > (1 << 17) || r->tokens > (int64_t(1) << 24)) return LGP_EUNSUPPORTED;
+  if (r->tokens && (!r->values || !r->scales)) return LGP_EINVAL;
+  return aligned16(r->values) ? LGP_OK : LGP_EINVAL;
+}
+Operand side_of(const lgp_rows8* r) {
+  const int32_t chunks = (r->width + 15) / 16;
+  return Operand{reinterpret_cast<const char*>(r->values), nullptr, int64_t(chunks) * 16, int32_t(r->tokens), chunks, 1 << 30, nullptr};
+}
+
+}  // namespace
+}  // namespace layer
+}  // namespace lgp
+
+using namespace lgp::layer;
+
+extern "C" {
+
+int lgp_linear_rows8(int device, const lgp_rows8* rows, const lgp_rows8* weight, const float* bias, int32_t dtype, void* out, void* stream) {
+  if (int st = check_side(rows)) return st;
+  if (int st = check_side(weight)) return st;
+  if (rows->width != weight->width || weight->tokens < 1 || (rows->tokens && !out)) return LGP_EINVAL;
+  if (dtype != LGP_F32 && dtype != LGP_F16 && dtype != LGP_BF16) return LGP_EUNSUPPORTED;
+  if (int st = use_device(device)) return st;
+  if (rows->tokens == 0) return LGP_OK;
+  Product8Params p = {};
+  p.w = side_of(weight);
+  p.x = side_of(rows);
+  p.w_scales = weight->scales;
+  p.x_scales = rows->scales;
+  p.bias = bias;
+  p.pos = rows->pos;
+  p.tokens = int32_t(rows->tokens);
+  p.channels = int32_t(weight->tokens);
+  p.chunks = p.w.chunks;
+  p.out = out;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  if (dtype == LGP_F32) product8<float>(p, s);
+  else if (dtype == LGP_F16) product8<f16>(p, s);
+  else product8<bf16>(p, s);
+  return launched();
+}
+
+}  // extern "C"

@@ -1,9 +1,9 @@
 """What a layer over sampled neighbourhoods has around its attention: the residual's addition with the RMS norm, products in 8-bit integers for
-serving, and the clipping of gradients (argument checks and marshalling only; the kernels are the library's).
+serving, the gated pair of projections, and the clipping of gradients (argument checks and marshalling only; the kernels are the library's).
 
 As in layer.py: arguments that make no sense raise LegionPrepError before anything is launched, results and workspaces are allocated for the stream that the
-kernels run on, and a negative entry of pos (int32[tokens]) says that a row holds no token: it is not read, and its results are zeros.  add_norm is
-differentiable.  No gradient passes through rows in 8 bits.
+kernels run on, and a negative entry of pos (int32[tokens]) says that a row holds no token: it is not read, and its results are zeros.  add_norm and
+gated_linear are differentiable.  No gradient passes through rows in 8 bits.
 """
 from __future__ import annotations
 
@@ -13,10 +13,11 @@ import struct
 import torch
 from torch.autograd.function import once_differentiable
 
-from .binding import _Residual, _Rows8, load_library
+from .binding import _Gated, _Residual, _Rows8, load_library
 from .layer import _DTYPE, _bad, _ints, _like, _ok, _on, _packer, _ptr, _rows2, _workspace
 
-_residual, _rows8 = _packer(_Residual), _packer(_Rows8)
+_residual, _rows8, _gated = _packer(_Residual), _packer(_Rows8), _packer(_Gated)
+_ACT = {"silu": 0, "gelu": 1}
 
 
 def _plain(t, shape, name: str, dtype, index: int):
@@ -170,6 +171,85 @@ def add_norm_rows8(x, residual, weight, pos=None, eps: float = 1e-6, stream=None
         total = x if residual is None else torch.empty(x.shape, dtype=kind, device=x.device)
         _ok(L.lgp_add_norm_rows8(index, r, rows.c, total.data_ptr(), on))
     return rows, total
+
+
+def linear_rows8(rows: Rows8, weight: Rows8, bias=None, dtype=torch.bfloat16, stream=None):
+    """rows weight^T + bias, [tokens, channels] in `dtype` (float32, float16 or bfloat16): a product of 8-bit integers, exact up to its scales.  weight: a Rows8 of
+    [channels, width], as pack_rows gives it; bias: float32[channels].  No gradients pass."""
+    L = load_library()
+    index, channels = rows.index, weight.values.shape[0]
+    if weight.index != index or weight.width != rows.width or weight.pos is not None or not channels:
+        raise _bad(f"weight: rows of {rows.width} on cuda:{index}, one at least, all of them there")
+    if dtype not in _DTYPE:
+        raise _bad("dtype: float32, float16 or bfloat16")
+    at = 0 if bias is None else _vector(bias, channels, index, "bias")
+    with _on(index, stream) as on:
+        out = torch.empty((rows.values.shape[0], channels), dtype=dtype, device=rows.values.device)
+        _ok(L.lgp_linear_rows8(index, rows.c, weight.c, at, _DTYPE[dtype], out.data_ptr(), on))
+    return out
+
+
+def _pair(x, w_gate, w_up, act: str, pos):
+    """(device, arguments) of the gated pair."""
+    row, index, dtype, (tokens, width) = _rows2(x, "x"), x.get_device(), x.dtype, x.shape
+    if dtype is not torch.float16 and dtype is not torch.bfloat16:
+        raise _bad("x: float16 or bfloat16")
+    for w, name in ((w_gate, "w_gate"), (w_up, "w_up")):
+        if w.dtype is not dtype or w.get_device() != index or w.dim() != 2 or w.shape[1] != width or not w.is_contiguous() or w.data_ptr() % 16:
+            raise _bad(f"{name}: [hidden, {width}], {dtype}, on cuda:{index}, rows end to end, aligned to 16 bytes")
+    if w_gate.shape != w_up.shape:
+        raise _bad("w_up: like w_gate")
+    at = x.data_ptr()
+    if tokens < 2:
+        row = width
+    if width % 8 or ((row % 8 or at % 16 or row >= 1 << 22) and tokens):
+        raise _bad("x: a width and a stride between rows in multiples of 8, the stride below 2^22, aligned to 16 bytes")
+    if act not in _ACT:
+        raise _bad("act: silu or gelu")
+    return index, _gated(at, row, tokens, width, w_gate.shape[0], _DTYPE[dtype], _ACT[act], w_gate.data_ptr(), w_up.data_ptr(), _ints(pos, tokens, index, "pos"))
+
+
+class _GatedLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w_gate, w_up, act, pos):
+        ctx.save_for_backward(x, w_gate, w_up, pos)
+        ctx.act = act
+        return gated_linear(x, w_gate, w_up, act, pos)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh):
+        x, w_gate, w_up, pos = ctx.saved_tensors
+        return *gated_linear_backward(dh, x, w_gate, w_up, ctx.act, pos), None, None
+
+
+def gated_linear(x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
+    """act(x w_gate^T) * (x w_up^T), [tokens, hidden]: what stands before the last projection of a gated feed-forward block.
+
+    x [tokens, width] and the weights [hidden, width]: float16 or bfloat16, width a multiple of 8.  act: "silu" or "gelu" (of the error function).  For its
+    gradients nothing but x and the weights is kept."""
+    if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and torch.is_grad_enabled():
+        with _on(x.get_device(), stream):
+            return _GatedLinear.apply(x, w_gate, w_up, act, pos)
+    L = load_library()
+    index, g = _pair(x, w_gate, w_up, act, pos)
+    with _on(index, stream) as on:
+        h = torch.empty((x.shape[0], w_gate.shape[0]), dtype=x.dtype, device=x.device)
+        _ok(L.lgp_gated_linear(index, g, h.data_ptr(), on))
+    return h
+
+
+def gated_linear_backward(dh, x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
+    """Gradients (dx, dw_gate, dw_up) of gated_linear, in the type of x, from that of its result; the other arguments are what it was given."""
+    L = load_library()
+    index, g = _pair(x, w_gate, w_up, act, pos)
+    with _on(index, stream) as on:
+        dh = _plain(dh, (x.shape[0], w_gate.shape[0]), "dh", x.dtype, index)
+        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dg, du = torch.empty_like(w_gate), torch.empty_like(w_up)
+        w, size = _workspace(index, x.device, L.lgp_gated_linear_workspace, g)
+        _ok(L.lgp_gated_linear_backward(index, g, dh.data_ptr(), dx.data_ptr(), dg.data_ptr(), du.data_ptr(), _ptr(w), size, on))
+    return dx, dg, du
 
 
 def _clip(grads, most: float, out, stream):

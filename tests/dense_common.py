@@ -69,3 +69,40 @@ def clip(grads, most):
     norm = math.sqrt(math.fsum(float((g.double() ** 2).sum()) for g in grads))
     by = min(1.0, most / norm) if math.isfinite(norm) and norm > 0 else 1.0
     return norm, [g.double() * by for g in grads]
+
+
+def gated(x, w_gate, w_up, act, pos, dh=None):
+    """{name: (value, bound)}.  Sums in 32 bits of K products: K / 8 + 16 roundings of the sum of their sizes at most.  An activation has an error of its argument's
+    rounding (g^2 + |g| times E, relative) and a few of its own; its slope is below 1.13 and the slope's slope below 1."""
+    u, tiny = UNIT[x.dtype], TINY[x.dtype]
+    live = live_rows(x.shape[0], pos, x.device)[:, None]
+    X, G, U = torch.where(live, x.double(), 0.0), w_gate.double(), w_up.double()
+    g, v = X @ G.T, X @ U.T
+    e = E * (X.shape[1] / 8 + 16)
+    eg, ev = e * X.abs() @ G.abs().T, e * X.abs() @ U.abs().T
+    if act == "silu":
+        p = torch.sigmoid(g)
+        slope = p + g * p * (1 - p)
+    else:
+        p = 0.5 * torch.erfc(-g / math.sqrt(2))
+        slope = p + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    a = g * p
+    more = 2 * E * (g * g + g.abs() + 16)
+    ea, es = 1.13 * eg + more * a.abs(), eg + more * (p + (slope - p).abs())
+    h = a * v
+    ref = {"h": (h, u * h.abs() + 1.01 * (ea * v.abs() + a.abs() * ev) + 4 * E * h.abs() + tiny)}
+    if dh is None:
+        return ref
+    D = torch.where(live, dh.double(), 0.0)
+    dg, du = D * v * slope, D * a
+    e_dg = D.abs() * 1.01 * (ev * slope.abs() + v.abs() * es) + (u + 4 * E) * dg.abs() + tiny
+    e_du = D.abs() * ea + (u + 4 * E) * du.abs() + tiny
+    e_dg, e_du = torch.where(live, e_dg, 0.0), torch.where(live, e_du, 0.0)
+    dx = dg @ G + du @ U
+    e = E * (2 * G.shape[0] / 8 + 32)
+    ref["dx"] = (dx, u * dx.abs() + e_dg @ G.abs() + e_du @ U.abs() + e * 1.01 * (dg.abs() @ G.abs() + du.abs() @ U.abs()) + tiny)
+    e = E * (X.shape[0] / 8 + 32)
+    for name, d, ed in (("dw_gate", dg, e_dg), ("dw_up", du, e_du)):
+        w = d.T @ X
+        ref[name] = (w, u * w.abs() + ed.T @ X.abs() + e * 1.01 * d.abs().T @ X.abs() + tiny)
+    return ref

@@ -207,6 +207,166 @@ def test_norm_beyond_32_bits():
     assert (rows.values[-5:].abs().amax(1) == 127).all() and (rows.values[-1000:-5] == 0).all()
 
 
+# ---- products in 8 bits
+
+def rows_of(tokens, width, seed, pos=None):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.zeros(tokens, (width + 15) // 16 * 16, dtype=torch.int8, device="cuda")
+    v[:, :width] = torch.randint(-127, 128, (tokens, width), generator=g, device="cuda", dtype=torch.int8)
+    s = torch.rand(tokens, generator=g, device="cuda") * 0.1 + 0.001
+    if pos is not None:
+        s[pos < 0] = math.nan
+    return lgp().Rows8(v, s, width, pos=pos)
+
+
+def run_product(tokens, width, channels, dtype, bias=True, pos=None, seed=1):
+    rows, weight = rows_of(tokens, width, seed, pos), rows_of(channels, width, seed + 1)
+    b = draw((channels,), F32, seed + 2, 30.0) if bias else None
+    out = lgp().linear_rows8(rows, weight, bias=b, dtype=dtype)
+    assert out.dtype is dtype
+    v = (rows.values.double() @ weight.values.double().T) * weight.scales.double() * rows.scales.double()[:, None]
+    want = v + (b.double() if bias else 0.0)
+    tol = 4 * 2.0 ** -24 * (v.abs() + want.abs()) + UNIT[dtype] * want.abs() + ref.TINY[dtype]       # the sum's rounding, two products and the addition
+    if pos is not None:
+        want, tol = torch.where((pos < 0)[:, None], 0.0, want), torch.where((pos < 0)[:, None], 0.0, tol)
+    if dtype is F16:                                    # what is too large for the type
+        over = want.abs() >= 65520
+        want, tol = torch.where(over, torch.sign(want) * math.inf, want), torch.where(over, 0.0, tol)
+    check(out, (want, tol))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("tokens,width,channels", [(1, 1, 1), (1, 16, 16), (1, 1024, 1000), (2, 17, 33), (15, 100, 15), (16, 63, 64), (17, 64, 65), (32, 4097, 40), (33, 65, 31),
+                                                   (64, 128, 64), (65, 1000, 129), (276, 256, 768), (1000, 250, 300), (1024, 100, 47), (1025, 1008, 257), (3000, 40, 500),
+                                                   (40, 20_000, 40), (1100, 9000, 270)])
+def test_products_in_8_bits(tokens, width, channels, dtype):
+    run_product(tokens, width, channels, dtype)
+    run_product(tokens, width, channels, dtype, bias=False, pos=slots(tokens, 3), seed=7)
+
+
+def test_products_in_8_bits_of_the_largest_sums():
+    """Every product 127^2, as wide as rows may be: the sum is just below 2^31."""
+    L = lgp()
+    for tokens in (1, 40, 1030):
+        v = torch.full((tokens, 1 << 17), 127, dtype=torch.int8, device="cuda")
+        w = torch.full((40, 1 << 17), -127, dtype=torch.int8, device="cuda")
+        out = L.linear_rows8(L.Rows8(v, torch.ones(tokens, device="cuda"), 1 << 17), L.Rows8(w, torch.ones(40, device="cuda"), 1 << 17), dtype=F32)
+        assert (out == -float(127 * 127 << 17)).all()
+
+
+def test_products_in_8_bits_of_nothing_and_of_rows_that_are_not_finite():
+    L = lgp()
+    w = rows_of(50, 40, 1)
+    assert L.linear_rows8(rows_of(0, 40, 2), w).shape == (0, 50)
+    for tokens in (6, 60, 1100):
+        x = draw((tokens, 40), F32, 3)
+        clean = L.linear_rows8(L.pack_rows(x), w)
+        x[4, 7] = math.inf
+        out = L.linear_rows8(L.pack_rows(x), w)
+        odd = torch.arange(tokens, device="cuda") == 4
+        assert torch.isnan(out[4]).all() and torch.equal(out[~odd], clean[~odd])
+
+
+def test_from_the_residual_to_a_product():
+    """As a served layer goes: the residual's addition, the norm in 8 bits, the product with a packed weight; within what 8 bits lose."""
+    L = lgp()
+    x, res, w = draw((300, 250), BF16, 1), draw((300, 250), BF16, 2), 1 + draw((250,), F32, 3, 0.2)
+    weight, pos = draw((90, 250), F32, 4, 250 ** -0.5), slots(300, 5)
+    x[pos < 0] = math.nan
+    packed = L.pack_rows(weight)
+    rows, total = L.add_norm_rows8(x, res, w, pos=pos)
+    out = L.linear_rows8(rows, packed, dtype=F32)
+    y = ref.add_norm(x, res, w, pos, 1e-6)["y32"][0]
+    held = packed.values[:, :250].double() * packed.scales.double()[:, None]
+    want = y @ held.T
+    # half a step of each value, and what 32 bits add to it and to the product
+    tol = torch.nan_to_num(rows.scales.double())[:, None] * (0.5 + 2.0 ** -10) * held.abs().sum(1) + 2.0 ** -20 * y.abs() @ held.abs().T
+    check(out, (want, tol))
+    assert (out[pos < 0] == 0).all()
+
+
+# ---- the gated pair
+
+def run_gated(tokens, width, hidden, dtype, act, pos=None, seed=1, apart=0, train=True, size=1.0):
+    L = lgp()
+    x, dh = draw((tokens, width), dtype, seed, size), draw((tokens, hidden), dtype, seed + 1)
+    wg, wu = draw((hidden, width), dtype, seed + 2, width ** -0.5), draw((hidden, width), dtype, seed + 3, width ** -0.5)
+    if pos is not None:
+        x[pos < 0] = math.nan
+        dh[pos < 0] = math.nan
+    if apart:
+        wide = torch.full((tokens, width + apart), math.nan, dtype=dtype, device="cuda")
+        wide[:, 8:8 + width] = x
+        x = wide[:, 8:8 + width]
+    want = ref.gated(x, wg, wu, act, pos, dh if train else None)
+    check(L.gated_linear(x, wg, wu, act=act, pos=pos), want["h"], "h")
+    if train:
+        for got, name in zip(L.gated_linear_backward(dh, x, wg, wu, act=act, pos=pos), ("dx", "dw_gate", "dw_up")):
+            check(got, want[name], name)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
+                                                 (129, 136, 129), (276, 256, 352), (300, 520, 257), (1000, 96, 500), (1025, 256, 683), (1500, 72, 40), (2500, 264, 300)])
+def test_gated_of_every_size(tokens, width, hidden, dtype, act):
+    run_gated(tokens, width, hidden, dtype, act)
+    run_gated(tokens, width, hidden, dtype, act, pos=slots(tokens, 9), apart=24, seed=5)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_gated_of_many_tokens_and_of_wide_rows(dtype):
+    run_gated(20_001, 128, 200, dtype, "silu", pos=slots(20_001, 2))
+    run_gated(2100, 2048, 1100, dtype, "gelu")
+    run_gated(40, 4096, 2000, dtype, "silu")
+    run_gated(3, 24, 9000, dtype, "silu")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_gated_of_large_arguments(dtype, act):
+    """Gates from the far ends of the activation's range."""
+    run_gated(300, 64, 80, dtype, act, size=6.0, train=dtype is BF16)
+
+
+def test_gated_of_nothing():
+    L = lgp()
+    w = draw((40, 64), BF16, 1)
+    x = torch.empty((0, 64), dtype=BF16, device="cuda")
+    assert L.gated_linear(x, w, w).shape == (0, 40)
+    dx, dg, du = L.gated_linear_backward(torch.empty((0, 40), dtype=BF16, device="cuda"), x, w, w)
+    assert dx.shape == (0, 64) and (dg == 0).all() and (du == 0).all()
+    for tokens in (1, 50, 2000):                     # no token at all
+        x, pos = torch.full((tokens, 64), math.nan, dtype=BF16, device="cuda"), torch.full((tokens,), -1, dtype=torch.int32, device="cuda")
+        dh = torch.full((tokens, 40), math.nan, dtype=BF16, device="cuda")
+        assert (L.gated_linear(x, w, w, pos=pos) == 0).all()
+        assert all((t == 0).all() for t in L.gated_linear_backward(dh, x, w, w, pos=pos))
+
+
+def test_gated_keeps_what_is_not_finite_in_its_row():
+    L = lgp()
+    for tokens in (9, 700, 1500):
+        x, wg, wu, dh = draw((tokens, 72), BF16, 1), draw((90, 72), BF16, 2, 0.1), draw((90, 72), BF16, 3, 0.1), draw((tokens, 90), BF16, 4)
+        clean, back = L.gated_linear(x, wg, wu), L.gated_linear_backward(dh, x, wg, wu)
+        x[5, 3] = math.nan
+        h, (dx, _, _) = L.gated_linear(x, wg, wu), L.gated_linear_backward(dh, x, wg, wu)
+        odd = torch.arange(tokens, device="cuda") == 5
+        assert torch.isnan(h[5]).all() and torch.equal(h[~odd], clean[~odd]) and torch.isnan(dx[5]).all() and torch.equal(dx[~odd], back[0][~odd])
+
+
+def test_gated_with_autograd():
+    L = lgp()
+    x, wg, wu, dh = draw((70, 64), BF16, 1).requires_grad_(), draw((96, 64), BF16, 2, 0.1).requires_grad_(), draw((96, 64), BF16, 3, 0.1).requires_grad_(), draw((70, 96), BF16, 4)
+    got = torch.autograd.grad(L.gated_linear(x, wg, wu, act="gelu"), (x, wg, wu), dh)
+    want = ref.gated(x.detach(), wg.detach(), wu.detach(), "gelu", None, dh)
+    for g, name in zip(got, ("dx", "dw_gate", "dw_up")):
+        check(g, want[name], name)
+    one = draw((1, 64), BF16, 5).requires_grad_()      # a row for all tokens: its gradients add up
+    (g,) = torch.autograd.grad(L.gated_linear(one.expand(70, 64), wg.detach(), wu.detach()), one, dh)
+    val, tol = ref.gated(one.detach().expand(70, 64), wg.detach(), wu.detach(), "silu", None, dh)["dx"]
+    check(g, (val.sum(0, keepdim=True), tol.sum(0, keepdim=True) + 70 * UNIT[BF16] * val.abs().sum(0, keepdim=True)))
+
+
 # ---- gradients' norm and clipping
 
 def gradients(shapes, seed=1, flat=False):
@@ -288,7 +448,9 @@ def test_clipping_leaves_a_mark_for_autograd():
 # ---- streams, graphs, repeated runs
 
 def pieces():
-    x, res, w = draw((700, 250), BF16, 1), draw((700, 250), F32, 2), 1 + draw((250,), F32, 3, 0.1)
+    x, res, w = draw((700, 256), BF16, 1), draw((700, 256), F32, 2), 1 + draw((256,), F32, 3, 0.1)
+    wg, wu = draw((130, 248), BF16, 5, 0.06), draw((130, 248), BF16, 6, 0.06)
+    wide = draw((90, 256), BF16, 7)
     pos = slots(700, 4)
     grads = gradients(MANY)
     out = [torch.empty_like(g) for g in grads]
@@ -299,7 +461,9 @@ def pieces():
         back = L.add_norm_backward(y, total, total, w, pos=pos, stream=stream)
         rows, _ = L.add_norm_rows8(x, res, w, pos=pos, stream=stream)
         packed = L.pack_rows(x, pos=pos, stream=stream)
-        return [y, total, *back, rows.values, rows.scales, packed.values, packed.scales, L.clip_gradients(grads, 0.3, out=out, stream=stream),
+        h = L.gated_linear(y[:, :248], wg, wu, pos=pos, stream=stream)
+        more = L.gated_linear_backward(h, y[:, :248], wg, wu, pos=pos, stream=stream)
+        return [h, *more, y, total, *back, rows.values, rows.scales, packed.values, packed.scales, L.clip_gradients(grads, 0.3, out=out, stream=stream),
                 *[o.clone() if stream is None else o for o in out]]
     return run, (x, res, *grads)
 
@@ -346,6 +510,7 @@ def test_captured_and_replayed():
 def test_refusals():
     L = lgp()
     x, w = torch.zeros(4, 32, dtype=BF16, device="cuda"), torch.ones(32, device="cuda")
+    r8 = L.pack_rows(x)
     bad = [lambda: L.add_norm(x.cpu(), x, w), lambda: L.add_norm(x, x.half(), w), lambda: L.add_norm(x, x[:3], w), lambda: L.add_norm(x.float(), x, w),
            lambda: L.add_norm(x, x, w[:31]), lambda: L.add_norm(x, x, w.half()), lambda: L.add_norm(x, x, w, pos=torch.zeros(3, dtype=torch.int32, device="cuda")),
            lambda: L.add_norm(x, x, w, pos=torch.zeros(4, device="cuda")), lambda: L.add_norm(x.int(), None, w), lambda: L.add_norm(x[0], None, w),
@@ -355,6 +520,13 @@ def test_refusals():
            lambda: L.add_norm_rows8(x, x.half(), w), lambda: L.pack_rows(x.int()), lambda: L.pack_rows(x.t()), lambda: L.pack_rows(torch.zeros(1, 16385, device="cuda")),
            lambda: L.Rows8(x, w, 32), lambda: L.Rows8(torch.zeros(4, 32, dtype=torch.int8, device="cuda"), w, 32),
            lambda: L.Rows8(torch.zeros(4, 20, dtype=torch.int8, device="cuda"), w[:4], 20),
+           lambda: L.linear_rows8(r8, L.pack_rows(x[:, :24])), lambda: L.linear_rows8(r8, r8, bias=w[:3]), lambda: L.linear_rows8(r8, r8, bias=w[:4].half()),
+           lambda: L.linear_rows8(r8, r8, dtype=torch.int8), lambda: L.linear_rows8(r8, L.pack_rows(x[:0])),
+           lambda: L.linear_rows8(r8, L.pack_rows(x, pos=torch.zeros(4, dtype=torch.int32, device="cuda"))),
+           lambda: L.gated_linear(x, x, x[:3]), lambda: L.gated_linear(x, x.half(), x), lambda: L.gated_linear(x, x[:, :24], x[:, :24]), lambda: L.gated_linear(x.float(), x, x),
+           lambda: L.gated_linear(x, x, x, act="relu"), lambda: L.gated_linear(x[:, :20], x[:, :20].contiguous(), x[:, :20].contiguous()), lambda: L.gated_linear(x, x, x.cpu()),
+           lambda: L.gated_linear(x[:, 4:12], x[:, :8].contiguous(), x[:, :8].contiguous()), lambda: L.gated_linear(x.t(), x, x), lambda: L.gated_linear(x, x[:0], x[:0]),
+           lambda: L.gated_linear_backward(x, x[:2], x, x), lambda: L.gated_linear_backward(x[:, :2].float(), x, x[:2], x[:2]),
            lambda: L.clip_gradients([], 1.0), lambda: L.clip_gradients([x.t()], 1.0), lambda: L.clip_gradients([x.int()], 1.0), lambda: L.clip_gradients([x.cpu()], 1.0),
            lambda: L.clip_gradients([x], -1.0), lambda: L.clip_gradients([x], math.nan), lambda: L.clip_gradients([x], "one"), lambda: L.clip_gradients([x, x], 1.0),
            lambda: L.clip_gradients([x[:3], x[2:]], 1.0), lambda: L.clip_gradients([x[:2]], 1.0, out=[x[1:3]]), lambda: L.clip_gradients([x], 1.0, out=[x.half()]),
