@@ -561,13 +561,16 @@ typedef struct {
   const int32_t* pos;                   /* tokens entries, or NULL; a negative one: no token in this row     */
 } lgp_gated;
 
-/* h = act(x w_gate^T) * (x w_up^T), [tokens, hidden], rows end to end: one kernel, sums and activation in 32 bits, h rounded once. */
-int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* stream);
+/* h = act(x w_gate^T) * (x w_up^T), [tokens, hidden], rows end to end: one kernel, sums and activation in 32 bits, h rounded once.  Where many
+ * rows may have no token, those that have one are listed in `workspace` first (lgp_gated_linear_workspace). */
+int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that lgp_gated_linear (backward = 0) or lgp_gated_linear_backward (1) want for these arguments; may be 0. */
+int lgp_gated_linear_workspace(int device, const lgp_gated* in, int backward, size_t* bytes);
 
 /* Gradients of lgp_gated_linear by x (dx [tokens, width], zeros where no token is) and the weights (like them), from that of h (dh [tokens, hidden], rows end to
  * end).  Both projections are computed again; the gradients of their results are rounded to the type of x for the products that follow, so in fp16 they have to be
  * numbers that it holds. */
-int lgp_gated_linear_workspace(int device, const lgp_gated* in, size_t* bytes);
 int lgp_gated_linear_backward(int device, const lgp_gated* in, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
                               void* stream);
 

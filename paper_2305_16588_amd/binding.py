@@ -174,8 +174,8 @@ def load_library():
     L.lgp_add_norm_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.lgp_pack_rows8.argtypes = [C.c_int, vp, i64, i32, vp, vp]
     L.lgp_linear_rows8.argtypes = [C.c_int, vp, vp, vp, i32, vp, vp]
-    L.lgp_gated_linear.argtypes = [C.c_int, vp, vp, vp]
-    L.lgp_gated_linear_workspace.argtypes = [C.c_int, vp, vp]
+    L.lgp_gated_linear.argtypes = [C.c_int, vp, vp, vp, C.c_size_t, vp]
+    L.lgp_gated_linear_workspace.argtypes = [C.c_int, vp, C.c_int, vp]
     L.lgp_gated_linear_backward.argtypes = [C.c_int, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
     L.lgp_clip_gradients_workspace.argtypes = [C.c_int, vp]
     L.lgp_clip_gradients.argtypes = [C.c_int, vp, i64, C.c_double, vp, vp, C.c_size_t, vp]

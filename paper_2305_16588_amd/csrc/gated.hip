@@ -9,7 +9,7 @@ namespace {
 
 struct GatedParams {
   Operand w, x;                 // w: Wg and Wu
-  const int32_t* pos;
+  const int32_t *pos, *count;           // with x.order, count: how many tokens there are, and pos is NULL
   int32_t tokens, hidden, pitch;        // pitch: of half a row of `grads`
   int32_t width_chunks, tiles_m, tiles_n;
   void* h;
@@ -32,17 +32,21 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float 
 }
 
 template <typename T, int ACT, class P, bool BACK>
-__global__ __launch_bounds__(P::kThreads, P::kThreads == 512 ? 2 : 2) void gated_kernel(const GatedParams p) {
+__global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams p) {
   __shared__ typename P::Shared lds;
   const Tile t = tile_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
-  const int32_t f0 = t.m * (P::BM / 2), t0 = t.n * P::BN;
+  const int32_t f0 = t.m * (P::BM / 2), t0 = t.n * P::BN, tokens = p.count ? *fixed(p.count) : p.tokens;
+  if (t0 >= tokens) return;
   floatx16 acc[P::MI][P::NJ] = {};
-  P::run(lds, p.w, p.x, f0, t0, 0, p.width_chunks * 8, acc);
+  Operand x = p.x;
+  x.rows = tokens;
+  P::run(lds, p.w, x, f0, t0, 0, p.width_chunks * 8, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % P::WM, wn = wave / P::WM;
 #pragma unroll
   for (int j = 0; j < P::NJ; ++j) {
-    const int32_t token = t0 + (wn * P::NJ + j) * 32 + (lane & 31);
-    if (token >= p.tokens) continue;
+    const int32_t row = t0 + (wn * P::NJ + j) * 32 + (lane & 31);
+    if (row >= tokens) continue;
+    const int32_t token = x.order ? x.order[row] : row;
     const bool live = !p.pos || p.pos[token] >= 0;
 #pragma unroll
     for (int i = 0; i < P::MI / 2; ++i)
@@ -61,7 +65,7 @@ __global__ __launch_bounds__(P::kThreads, P::kThreads == 512 ? 2 : 2) void gated
             y[k] = live && k < n ? dh[k] * acc[i + P::MI / 2][j][r0 + k] * slope : 0.f;
             z[k] = live && k < n ? dh[k] * a : 0.f;
           }
-          T* out = static_cast<T*>(p.grads) + int64_t(token) * 2 * p.pitch + f;
+          T* out = static_cast<T*>(p.grads) + int64_t(row) * 2 * p.pitch + f;
           write_row(out, 8, y);
           write_row(out + p.pitch, 8, z);
         } else {
@@ -72,6 +76,122 @@ __global__ __launch_bounds__(P::kThreads, P::kThreads == 512 ? 2 : 2) void gated
           write_row(static_cast<T*>(p.h) + int64_t(token) * p.hidden + f, n, y);
         }
       }
+  }
+}
+
+// Narrow rows: what becomes of 32 tokens' results, lane l having token l % 32 and 16 consecutive hidden elements.
+template <typename T, int ACT, bool BACK> struct NarrowOut {
+  const GatedParams& p;
+  int32_t f, end, lane;              // the lane's first hidden element; the end of the workgroup's rows
+  int32_t row, token, next_row, next_token;        // of the list, and of memory; of the tokens worked on, and of those multiplied
+  int32_t ahead;                     // the token of memory after those
+  vec8<T> dh[2], next_dh[2];
+  float y[8], z[8];
+  __device__ __forceinline__ NarrowOut(const GatedParams& p, int32_t f, int32_t begin, int32_t end, int lane)
+      : p(p), f(f), end(end), lane(lane), row(-1), token(0), next_row(-1), next_token(0), ahead(listed(begin)) {
+    const vec8<T> nothing = {};
+    dh[0] = dh[1] = nothing;
+  }
+  __device__ __forceinline__ int32_t listed(int32_t first) const {
+    const int32_t at = first + (lane & 31);
+    return at >= end ? 0 : p.x.order ? p.x.order[at] : at;
+  }
+  __device__ __forceinline__ void start(int32_t first) {
+    next_row = first + (lane & 31);
+    const bool in = next_row < end;
+    if (!in) next_row = -1;
+    next_token = ahead;
+    ahead = listed(first + 32);
+    if constexpr (BACK) {
+      const vec8<T> nothing = {};
+      const T* from = static_cast<const T*>(p.dh) + int64_t(next_token) * p.hidden + f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int n = in ? p.hidden - f - 8 * i : 0;
+        next_dh[i] = nothing;
+        if (n >= 8) next_dh[i] = *reinterpret_cast<const typename AnyEight<T>::x8*>(from + 8 * i);
+        else
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < n) next_dh[i][e] = from[8 * i + e];
+      }
+    }
+  }
+  __device__ __forceinline__ void next() {
+    row = next_row;
+    token = next_token;
+    if constexpr (BACK) dh[0] = next_dh[0], dh[1] = next_dh[1];
+  }
+  template <int R, typename Sums> __device__ __forceinline__ void step(const Sums (&acc)[2]) {
+    constexpr int k = R % 8, i = R / 8;
+    const int n = p.hidden - f - 8 * i;
+    if constexpr (BACK) {
+      float slope;
+      const float a = activated<ACT, true>(acc[0][R], slope), d = float(dh[i][k]);
+      y[k] = k < n ? d * acc[1][R] * slope : 0.f;
+      z[k] = k < n ? d * a : 0.f;
+      if (k == 7 && row >= 0 && f + 8 * i < p.pitch) {
+        T* out = static_cast<T*>(p.grads) + int64_t(row) * 2 * p.pitch + f + 8 * i;
+        write_row(out, 8, y);
+        write_row(out + p.pitch, 8, z);
+      }
+    } else {
+      float none;
+      y[k] = activated<ACT, false>(acc[0][R], none) * acc[1][R];
+      if (k == 7 && row >= 0 && n > 0) write_row(static_cast<T*>(p.h) + int64_t(token) * p.hidden + f + 8 * i, n, y);
+    }
+  }
+};
+template <typename T, int ACT, class P, bool BACK>
+__global__ __launch_bounds__(P::kThreads, 2) void gated_narrow_kernel(const GatedParams p) {
+  __shared__ typename P::Shared lds;
+  // workgroups of one part of the tokens, which read the same rows, are on one XCD
+  const int32_t piece = int32_t(piece_of(blockIdx.x, gridDim.x)), part = piece / p.tiles_m, parts = int32_t(gridDim.x) / p.tiles_m;
+  const int32_t rows = p.count ? *fixed(p.count) : p.tokens, each = ((rows + parts - 1) / parts + 63) / 64 * 64;
+  const int32_t f0 = piece % p.tiles_m * 32 * P::WAVES, begin = part * each, end = min(begin + each, rows);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  NarrowOut<T, ACT, BACK> out(p, f0 + 32 * wave + 16 * (lane >> 5), begin, end, lane);
+  P::run(lds, p.w, p.x, f0, begin, end, out);
+}
+
+// Tokens that there are, in order: a workgroup has kListed of them.  First it counts them, then, knowing how many come before, it lists them and fills the rows of
+// `zeros` (cols wide) that have none.
+constexpr int32_t kListed = 1024;
+__global__ __launch_bounds__(256) void count_kernel(const int32_t* pos, int32_t tokens, int32_t* counts) {
+  int32_t n = 0;
+  for (int i = threadIdx.x; i < kListed; i += 256) {
+    const int32_t t = blockIdx.x * kListed + i;
+    n += __popcll(__ballot(t < tokens && pos[t < tokens ? t : 0] >= 0));
+  }
+  __shared__ int32_t lds[4];
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = n;
+  __syncthreads();
+  if (threadIdx.x == 0) counts[blockIdx.x] = lds[0] + lds[1] + lds[2] + lds[3];
+}
+template <typename T>
+__global__ __launch_bounds__(256) void list_kernel(const int32_t* pos, int32_t tokens, const int32_t* counts, int32_t* order, int32_t* count, T* zeros, int32_t cols) {
+  __shared__ int32_t lds[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int32_t before = 0;
+  for (uint32_t i = threadIdx.x; i < blockIdx.x; i += 256) before += counts[i];
+#pragma unroll
+  for (int i = 32; i; i >>= 1) before += __shfl_xor(before, i, 64);
+  if (lane == 0) lds[wave] = before;
+  __syncthreads();
+  before = lds[0] + lds[1] + lds[2] + lds[3];
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) *count = before + counts[blockIdx.x];
+  for (int i = 0; i < kListed; i += 64) {        // every wave looks at all of them, and each fills rows of its own
+    const int32_t t = blockIdx.x * kListed + i + lane;
+    const uint64_t there = __ballot(t < tokens && pos[t < tokens ? t : 0] >= 0), all = __ballot(t < tokens);
+    if (wave == 0 && (there >> lane & 1)) order[before + __popcll(there & ((uint64_t(1) << lane) - 1))] = t;
+    before += __popcll(there);
+    uint64_t gone = all & ~there & (uint64_t(0xffff) << (16 * wave));
+    while (gone) {
+      const int64_t row = int64_t(blockIdx.x) * kListed + i + __ffsll((unsigned long long)gone) - 1;
+      gone &= gone - 1;
+      const float nothing[8] = {};
+      for (int32_t c = 8 * lane; c < cols; c += 512) write_row(zeros + row * cols + c, cols - c, nothing);
+    }
   }
 }
 
@@ -91,14 +211,19 @@ __global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(const GatedPa
 
 struct GradParams {
   Operand a, b;
-  const int32_t* pos;           // of the rows of x's gradient
+  const int32_t *pos, *order, *count;        // of the rows of x's gradient; with a list, how many rows (x) or places of the sum (weights) there are
   int32_t rows, cols;           // of the result: tokens x width, or 2 x pitch rows of the weights' gradients x width
   int32_t hidden, pitch;        // weights: rows of each, and of each half of `rows`; x: hidden = 0
-  int32_t each, sum;            // places of the sum of a part, and all of them
+  int32_t sum;                  // places of the sum
   int32_t tiles_m, tiles_n, parts;
   void *out, *second;
   float* partial;               // [part][rows][cols], of rows that there are
 };
+
+__host__ __device__ __forceinline__ int32_t part_of_sum(int32_t sum, int32_t parts) {       // places of a part: whole stages
+  const int32_t each = ((sum + parts - 1) / parts + 63) / 64 * 64;
+  return each > 64 ? each : 64;
+}
 
 // dx = dg Wg + du Wu: A is the weights, across, B the gradients of the projections' results, along.  dWg = dg^T x and dWu = du^T x: A is x, across, and B those
 // gradients, across.
@@ -107,14 +232,23 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
   __shared__ typename P::Shared lds;
   const Tile t = tile_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
   const int32_t c0 = t.m * P::BM, row0 = t.n * P::BN;
+  Operand a = p.a, b = p.b;
+  int32_t rows = p.rows, sum = p.sum;
+  if (p.count) {
+    const int32_t n = *fixed(p.count);
+    b.rows = n;
+    if (p.hidden) sum = a.rows = n;
+    else rows = n;
+    if (row0 >= rows) return;
+  }
   floatx16 acc[P::MI][P::NJ] = {};
-  const int32_t begin = t.part * p.each, end = min(begin + p.each, p.sum);
-  P::run(lds, p.a, p.b, c0, row0, begin, end, acc);
+  const int32_t each = part_of_sum(sum, p.parts), begin = t.part * each, end = min(begin + each, sum);
+  P::run(lds, a, b, c0, row0, begin, end, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % P::WM, wn = wave / P::WM;
 #pragma unroll
   for (int j = 0; j < P::NJ; ++j) {
     int32_t row = row0 + (wn * P::NJ + j) * 32 + (lane & 31);
-    if (row >= p.rows) continue;
+    if (row >= rows) continue;
     T* out = static_cast<T*>(p.out);
     int64_t there = row;
     bool live = true;
@@ -126,6 +260,7 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
       }
       if (row >= p.hidden) continue;
     } else {
+      if (p.order) there = row = p.order[row];
       live = !p.pos || p.pos[row] >= 0;
     }
 #pragma unroll
@@ -144,10 +279,13 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
 }
 
 // Adds the parts of `n` elements each, eight a thread; those from `first` on go to `second`.
-template <typename T> __global__ __launch_bounds__(256) void join_kernel(const float* partial, int64_t n, int32_t parts, T* out, int64_t first, T* second) {
+// Rows (of `cols`) whose pos is negative become zeros.
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(const float* partial, int64_t n, int32_t parts, T* out, int64_t first, T* second, const int32_t* pos, int32_t cols) {
   const int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8;
   if (i >= n) return;
   float s[8] = {};
+  if (pos && pos[i / cols] < 0) parts = 0;
 #pragma unroll 4
   for (int32_t k = 0; k < parts; ++k) {
     float x[8];
@@ -159,39 +297,54 @@ template <typename T> __global__ __launch_bounds__(256) void join_kernel(const f
 }
 
 template <typename T> struct Forms {
-  typedef Tiles<T, 256, 256, 2, 4, 4, 4, true, false, false> LargePair;
+  typedef Narrow<T, 16, 8, true> Narrow256;
+  typedef Narrow<T, 8, 4, true> Narrow128;
+  typedef Narrow<T, 4, 4, true> Narrow64;
+  typedef Tiles<T, 256, 256, 2, 4, 8, 2, true, false, false> LargePair;
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, true, false, false> MiddlePair;
   typedef Tiles<T, 128, 64, 2, 2, 8, 3, true, false, false> SmallPair;
-  typedef Tiles<T, 256, 256, 2, 4, 4, 4, false, true, false> LargeX;
+  typedef Tiles<T, 256, 256, 2, 4, 8, 2, false, true, false> LargeX;
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, false, true, false> MiddleX;
   typedef Tiles<T, 64, 64, 2, 2, 8, 3, false, true, false> SmallX;
-  typedef Tiles<T, 256, 256, 2, 4, 4, 4, false, true, true> LargeW;
+  typedef Tiles<T, 256, 256, 2, 4, 8, 2, false, true, true> LargeW;
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, false, true, true> MiddleW;
   typedef Tiles<T, 64, 64, 2, 2, 8, 3, false, true, true> SmallW;
 };
 enum { kLarge = 0, kMiddle = 1, kSmall = 2 };       // forms of a tile
+constexpr int64_t kNarrowFrom = 1024, kListFrom = 4096;
 
 template <typename T, int ACT, class P, bool BACK> void launch_gated(GatedParams p, hipStream_t s) {
   p.tiles_m = ((BACK ? p.pitch : p.hidden) + P::BM / 2 - 1) / (P::BM / 2);
   p.tiles_n = (p.tokens + P::BN - 1) / P::BN;
   gated_kernel<T, ACT, P, BACK><<<uint32_t(p.tiles_m) * uint32_t(p.tiles_n), P::kThreads, 0, s>>>(p);
 }
-template <typename T, int ACT, bool BACK> void gated_by_size(const GatedParams& p, hipStream_t s) {
+template <typename T, int ACT, class P, bool BACK> void launch_narrow(GatedParams p, int cus, hipStream_t s) {
+  p.tiles_m = ((BACK ? p.pitch : p.hidden) + 32 * P::WAVES - 1) / (32 * P::WAVES);
+  const int32_t parts = std::max(1, std::min(cus * (8 / P::WAVES) / p.tiles_m, (p.tokens + 63) / 64));
+  gated_narrow_kernel<T, ACT, P, BACK><<<uint32_t(p.tiles_m) * uint32_t(parts), P::kThreads, 0, s>>>(p);
+}
+template <typename T, int ACT, bool BACK> void gated_by_size(const GatedParams& p, int cus, hipStream_t s) {
   typedef Forms<T> F;
   const int f = p.tokens <= 1024 ? kSmall : kLarge;
   if (!BACK && p.tokens <= kFewTokens) {
     gated_few_kernel<T, ACT><<<dim3((p.hidden + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
     return;
   }
+  if (p.width_chunks <= 32 && !p.pos && p.tokens > kNarrowFrom) {
+    if (p.width_chunks <= 8) launch_narrow<T, ACT, typename F::Narrow64, BACK>(p, cus, s);
+    else if (p.width_chunks <= 16) launch_narrow<T, ACT, typename F::Narrow128, BACK>(p, cus, s);
+    else launch_narrow<T, ACT, typename F::Narrow256, BACK>(p, cus, s);
+    return;
+  }
   if (f == kLarge) launch_gated<T, ACT, typename F::LargePair, BACK>(p, s);
   else if (f == kMiddle) launch_gated<T, ACT, typename F::MiddlePair, BACK>(p, s);
   else launch_gated<T, ACT, typename F::SmallPair, BACK>(p, s);
 }
-template <typename T, bool BACK> void gated_by_act(int32_t act, const GatedParams& p, hipStream_t s) {
-  if (act == LGP_SILU) gated_by_size<T, LGP_SILU, BACK>(p, s);
-  else gated_by_size<T, LGP_GELU, BACK>(p, s);
+template <typename T, bool BACK> void gated_by_act(int32_t act, const GatedParams& p, int cus, hipStream_t s) {
+  if (act == LGP_SILU) gated_by_size<T, LGP_SILU, BACK>(p, cus, s);
+  else gated_by_size<T, LGP_GELU, BACK>(p, cus, s);
 }
-struct GradShape { int32_t parts, each; int form; };
+struct GradShape { int32_t parts; int form; };
 // Parts of the sum: as many as make 512 workgroups, of at least 512 places each.
 GradShape grad_shape(int32_t rows, int32_t cols, int32_t sum, int f) {
   GradShape g;
@@ -199,22 +352,21 @@ GradShape grad_shape(int32_t rows, int32_t cols, int32_t sum, int f) {
   const int32_t bm = f == kLarge ? 256 : f == kMiddle ? 128 : 64, bn = f == kSmall ? 64 : 256;
   const int64_t tiles = std::max<int64_t>(1, int64_t((cols + bm - 1) / bm) * ((rows + bn - 1) / bn));
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, sum / 512));
-  g.each = std::max(64, int32_t(((sum + parts - 1) / parts + 63) / 64 * 64));
-  g.parts = std::max(1, (sum + g.each - 1) / g.each);
+  const int32_t each = part_of_sum(sum, int32_t(parts));
+  g.parts = std::max(1, (sum + each - 1) / each);
   return g;
 }
 GradShape shape_x(const lgp_gated* g, int32_t pitch) { return grad_shape(int32_t(g->tokens), g->width, 2 * pitch, g->tokens <= 1024 ? kSmall : kLarge); }
 GradShape shape_w(const lgp_gated* g, int32_t pitch) { return grad_shape(2 * pitch, g->width, int32_t(g->tokens), kLarge); }
 
-template <typename T, class P> void launch_grad(GradParams p, const GradShape& g, hipStream_t s) {
+template <typename T, class P> void launch_grad(GradParams p, const GradShape& g, const int32_t* pos, hipStream_t s) {
   p.tiles_m = (p.cols + P::BM - 1) / P::BM;
   p.tiles_n = (p.rows + P::BN - 1) / P::BN;
   p.parts = g.parts;
-  p.each = g.each;
   grad_kernel<T, P><<<uint32_t(p.tiles_m) * uint32_t(p.tiles_n) * uint32_t(g.parts), P::kThreads, 0, s>>>(p);
   if (g.parts > 1) {
     const int64_t first = p.hidden ? int64_t(p.hidden) * p.cols : int64_t(p.rows) * p.cols, n = p.hidden ? 2 * first : first;
-    join_kernel<T><<<uint32_t((n / 8 + 255) / 256), 256, 0, s>>>(p.partial, n, g.parts, static_cast<T*>(p.out), first, static_cast<T*>(p.second));
+    join_kernel<T><<<uint32_t((n / 8 + 255) / 256), 256, 0, s>>>(p.partial, n, g.parts, static_cast<T*>(p.out), first, static_cast<T*>(p.second), pos, p.cols);
   }
 }
 
@@ -230,8 +382,8 @@ int check_gated(const lgp_gated* g) {
 }
 GatedParams gated_params(const lgp_gated* g) {
   GatedParams p = {};
-  p.w = Operand{static_cast<const char*>(g->w_gate), static_cast<const char*>(g->w_up), int64_t(g->width) * 2, g->hidden, g->width / 8, 1 << 30, nullptr};
-  p.x = Operand{static_cast<const char*>(g->x), nullptr, g->x_row * 2, int32_t(g->tokens), g->width / 8, 1 << 30, nullptr};
+  p.w = Operand{static_cast<const char*>(g->w_gate), static_cast<const char*>(g->w_up), int64_t(g->width) * 2, g->hidden, g->width / 8, 1 << 30, nullptr, nullptr};
+  p.x = Operand{static_cast<const char*>(g->x), nullptr, g->x_row * 2, int32_t(g->tokens), g->width / 8, 1 << 30, nullptr, nullptr};
   p.pos = g->pos;
   p.tokens = int32_t(g->tokens);
   p.hidden = g->hidden;
@@ -239,40 +391,72 @@ GatedParams gated_params(const lgp_gated* g) {
   p.width_chunks = g->width / 8;
   return p;
 }
-struct Space { size_t grads, x, w; };          // bytes of the projections' gradients, and of the parts of x's and the weights', which are not there at once
-Space space_of(const lgp_gated* g) {
+// Where many rows may have no token, those that have one are listed, and the others cost nothing but their zeros.
+bool lists(const lgp_gated* g) { return g->pos && g->tokens > kListFrom && g->tokens * g->x_row < int64_t(1) << 35; }       // places of x are counted in 32 bits, by 16 bytes
+// Bytes of the list, of the projections' gradients, and of the parts of x's and the weights' gradients, which are not there at once.
+struct Space { size_t list, grads, parts; };
+Space space_of(const lgp_gated* g, bool backward) {
   const int32_t pitch = pitch_of(g->hidden);
+  Space s = {};
+  if (lists(g)) s.list = (size_t(g->tokens) + size_t(g->tokens + kListed - 1) / kListed + 1 + 63) / 64 * 64 * 4;
+  if (!backward) return s;
   const GradShape x = shape_x(g, pitch), w = shape_w(g, pitch);
-  return {size_t(g->tokens) * 2 * pitch * 2, x.parts > 1 ? size_t(x.parts) * g->tokens * g->width * 4 : 0, w.parts > 1 ? size_t(w.parts) * 2 * g->hidden * g->width * 4 : 0};
+  s.grads = size_t(g->tokens) * 2 * pitch * 2;
+  s.parts = std::max(x.parts > 1 ? size_t(x.parts) * g->tokens * g->width * 4 : 0, w.parts > 1 ? size_t(w.parts) * 2 * g->hidden * g->width * 4 : 0);
+  return s;
 }
+size_t bytes_of(const Space& s) { return s.list + s.grads + s.parts; }
 
-template <typename T> void backward(const lgp_gated* g, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, hipStream_t s) {
+// Lists tokens, for `p` too, and fills the other rows of `zeros`.
+template <typename T> void list_tokens(const lgp_gated* g, GatedParams& p, void* workspace, void* zeros, int32_t cols, hipStream_t s) {
+  int32_t *order = static_cast<int32_t*>(workspace), *counts = order + g->tokens;
+  const uint32_t groups = uint32_t((g->tokens + kListed - 1) / kListed);
+  count_kernel<<<groups, 256, 0, s>>>(g->pos, p.tokens, counts);
+  list_kernel<T><<<groups, 256, 0, s>>>(g->pos, p.tokens, counts, order, counts + groups, static_cast<T*>(zeros), cols);
+  p.x.order = order;
+  p.count = counts + groups;
+  p.pos = nullptr;
+}
+template <typename T> void forward(int device, const lgp_gated* g, void* h, void* workspace, hipStream_t s) {
+  GatedParams p = gated_params(g);
+  p.h = h;
+  if (lists(g)) list_tokens<T>(g, p, workspace, h, g->hidden, s);
+  gated_by_act<T, false>(g->act, p, compute_units(device), s);
+}
+template <typename T> void backward(int device, const lgp_gated* g, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, hipStream_t s) {
   typedef Forms<T> F;
   GatedParams p = gated_params(g);
+  const Space space = space_of(g, true);
+  char* grads = static_cast<char*>(workspace) + space.list;
+  float* partial = reinterpret_cast<float*>(grads + space.grads);
   p.dh = dh;
-  p.grads = workspace;
-  const Space space = space_of(g);
-  float* partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + space.grads);
-  if (p.tokens) gated_by_act<T, true>(g->act, p, s);
-  const char* grads = static_cast<const char*>(workspace);
+  p.grads = grads;
+  const Operand of_grads = {grads, nullptr, int64_t(p.pitch) * 4, p.tokens, p.pitch / 4, 1 << 30, nullptr, nullptr};
   if (p.tokens) {
+    if (lists(g)) list_tokens<T>(g, p, workspace, dx, g->width, s);
+    gated_by_act<T, true>(g->act, p, compute_units(device), s);
     GradParams d = {};
-    d.a = Operand{p.w.first, p.w.second, p.w.row_bytes, g->hidden, g->width / 8, p.pitch, nullptr};
-    d.b = Operand{grads, nullptr, int64_t(p.pitch) * 4, p.tokens, p.pitch / 4, 1 << 30, nullptr};
-    d.pos = g->pos;
+    d.a = p.w;
+    d.a.half = p.pitch;
+    d.b = of_grads;
+    d.pos = p.pos;
+    d.order = p.x.order;
+    d.count = p.count;
     d.rows = p.tokens;
     d.cols = g->width;
     d.sum = 2 * p.pitch;
     d.out = dx;
     d.partial = partial;
     const GradShape shape = shape_x(g, p.pitch);
-    if (shape.form == kLarge) launch_grad<T, typename F::LargeX>(d, shape, s);
-    else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleX>(d, shape, s);
-    else launch_grad<T, typename F::SmallX>(d, shape, s);
+    if (shape.form == kLarge) launch_grad<T, typename F::LargeX>(d, shape, g->pos, s);
+    else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleX>(d, shape, g->pos, s);
+    else launch_grad<T, typename F::SmallX>(d, shape, g->pos, s);
   }
   GradParams d = {};
-  d.a = Operand{p.x.first, nullptr, p.x.row_bytes, p.tokens, g->width / 8, 1 << 30, g->pos};
-  d.b = Operand{grads, nullptr, int64_t(p.pitch) * 4, p.tokens, p.pitch / 4, 1 << 30, nullptr};
+  d.a = p.x;
+  d.a.pos = p.pos;
+  d.b = of_grads;
+  d.count = p.count;
   d.rows = 2 * p.pitch;
   d.cols = g->width;
   d.hidden = g->hidden;
@@ -282,9 +466,9 @@ template <typename T> void backward(const lgp_gated* g, const void* dh, void* dx
   d.second = dw_up;
   d.partial = partial;
   const GradShape shape = shape_w(g, p.pitch);
-  if (shape.form == kLarge) launch_grad<T, typename F::LargeW>(d, shape, s);
-  else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleW>(d, shape, s);
-  else launch_grad<T, typename F::SmallW>(d, shape, s);
+  if (shape.form == kLarge) launch_grad<T, typename F::LargeW>(d, shape, nullptr, s);
+  else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleW>(d, shape, nullptr, s);
+  else launch_grad<T, typename F::SmallW>(d, shape, nullptr, s);
 }
 
 }  // namespace
@@ -295,25 +479,25 @@ using namespace lgp::layer;
 
 extern "C" {
 
-int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* stream) {
+int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* workspace, size_t workspace_bytes, void* stream) {
   if (int st = check_gated(in)) return st;
   if (in->tokens && !h) return LGP_EINVAL;
   if (int st = use_device(device)) return st;
   if (in->tokens == 0) return LGP_OK;
-  GatedParams p = gated_params(in);
-  p.h = h;
+  const size_t bytes = bytes_of(space_of(in, false));
+  if (workspace_bytes < bytes) return LGP_ECAPACITY;
+  if (bytes && (!workspace || !aligned16(workspace))) return LGP_EINVAL;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (in->dtype == LGP_F16) gated_by_act<f16, false>(in->act, p, s);
-  else gated_by_act<bf16, false>(in->act, p, s);
+  if (in->dtype == LGP_F16) forward<f16>(device, in, h, workspace, s);
+  else forward<bf16>(device, in, h, workspace, s);
   return launched();
 }
 
-int lgp_gated_linear_workspace(int device, const lgp_gated* in, size_t* bytes) {
+int lgp_gated_linear_workspace(int device, const lgp_gated* in, int backward, size_t* bytes) {
   if (!bytes) return LGP_EINVAL;
   *bytes = 0;
   if (int st = check_gated(in)) return st;
-  const Space s = space_of(in);
-  *bytes = std::max<size_t>(16, s.grads + std::max(s.x, s.w));
+  *bytes = bytes_of(space_of(in, backward != 0));
   return device < 0 ? LGP_EINVAL : LGP_OK;
 }
 
@@ -322,12 +506,12 @@ int lgp_gated_linear_backward(int device, const lgp_gated* in, const void* dh, v
   if ((in->tokens && (!dh || !dx)) || !dw_gate || !dw_up) return LGP_EINVAL;
   if (!aligned16(dx) || !aligned16(dw_gate) || !aligned16(dw_up)) return LGP_EINVAL;
   if (int st = use_device(device)) return st;
-  const Space space = space_of(in);
-  if (workspace_bytes < space.grads + std::max(space.x, space.w)) return LGP_ECAPACITY;
-  if (!workspace || !aligned16(workspace)) return LGP_EINVAL;
+  const size_t bytes = bytes_of(space_of(in, true));
+  if (workspace_bytes < bytes) return LGP_ECAPACITY;
+  if (bytes && (!workspace || !aligned16(workspace))) return LGP_EINVAL;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  if (in->dtype == LGP_F16) backward<f16>(in, dh, dx, dw_gate, dw_up, workspace, s);
-  else backward<bf16>(in, dh, dx, dw_gate, dw_up, workspace, s);
+  if (in->dtype == LGP_F16) backward<f16>(device, in, dh, dx, dw_gate, dw_up, workspace, s);
+  else backward<bf16>(device, in, dh, dx, dw_gate, dw_up, workspace, s);
   return launched();
 }
 

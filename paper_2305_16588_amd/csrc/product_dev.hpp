@@ -3,6 +3,8 @@
 
 #include "rows_dev.hpp"
 
+#include <type_traits>
+
 namespace lgp {
 namespace layer {
 namespace {
@@ -56,7 +58,13 @@ struct Operand {
   int32_t chunks;                    // of 16 bytes in a row; at least one
   int32_t half;                      // across: where the second matrix begins in the sum (a multiple of a stage), or more than there is
   const int32_t* pos;                // across: rows with a negative entry count as zeros; NULL: none
+  const int32_t* order;              // rows are order[0], order[1] ... of memory; NULL: 0, 1 ...
 };
+typedef const __attribute__((address_space(4))) int32_t* Fixed;        // read by the scalar unit: nothing writes it while the kernel runs
+__device__ __forceinline__ Fixed fixed(const int32_t* p) { return (Fixed)(uintptr_t)p; }
+__device__ __forceinline__ int turned(int row) { return int(__brev(uint32_t(row)) >> 28); }        // a row's low four bits in reverse
+// The order of 32 rows of A that leaves a lane 16 consecutive rows of D.
+__device__ __forceinline__ int in_order(int m) { return (m & ~31) + 16 * (m >> 2 & 1) + 4 * (m >> 3 & 3) + (m & 3); }
 
 // BM x BN of a product by WM x WN waves, each 32 MI x 32 NJ of it.  A stage is CH chunks of the sum: while one is multiplied, STAGES - 1 are on their way to LDS, past the
 // registers.  Every copy is issued whatever there is to copy -- what lies beyond an end is another valid row whose results are not used, or zeros where it
@@ -64,6 +72,14 @@ struct Operand {
 //
 // The 32 rows of a block of A lie in LDS in an order (or are read in one) that leaves a lane 16 consecutive rows of D: register r of lane l is row 16 (l / 32) + r, so
 // results are written 32 bytes at a time.
+template <int N> using Int = std::integral_constant<int, N>;
+template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F f) {       // f(0) ... f(N - 1), with constants
+  if constexpr (I < N) {
+    f(Int<I>());
+    each<N, I + 1>(f);
+  }
+}
+
 template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, bool GATED, bool A_ACROSS, bool B_ACROSS> struct Tiles {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, CH = CH_, STAGES = STAGES_;
   static constexpr int kThreads = 64 * WM * WN, MI = BM / 32 / WM, NJ = BN / 32 / WN;
@@ -76,9 +92,6 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
     alignas(16) char a[STAGES][BM * CH * 16];
     alignas(16) char b[STAGES][BN * CH * 16];
   };
-
-  static __device__ __forceinline__ int turned(int row) { return int(__brev(uint32_t(row)) >> 28); }
-  static __device__ __forceinline__ int in_order(int m) { return (m & ~31) + 16 * (m >> 2 & 1) + 4 * (m >> 3 & 3) + (m & 3); }
 
   // A thread's places in the tile of one side, and what it copies there.
   template <int ROWS, int N, bool ACROSS, bool PAIR, bool ORDER> struct Side {
@@ -96,7 +109,9 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
           const int r = place / CH, c = (place % CH) ^ (turned(r) & (CH - 1));
           int at = PAIR ? r % (ROWS / 2) : r;
           if (ORDER) at = in_order(at);
-          offset[j] = uint32_t(at < o.rows ? at : o.rows - 1) * uint32_t(o.row_bytes) + c * 16;
+          at = at < o.rows ? at : o.rows - 1;
+          if (!PAIR && o.order) offset[j] = uint32_t(o.order[at]) * uint32_t(o.row_bytes / 16) + c;       // in units of 16 bytes
+          else offset[j] = uint32_t(at) * uint32_t(o.row_bytes) + c * 16;
         }
       }
     }
@@ -105,26 +120,30 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
       if constexpr (ACROSS) {
         const bool later = at >= o.half;
         const int32_t row = later ? at - o.half : at;
-        const char* from = (later ? o.second : o.first) + int64_t(row) * o.row_bytes;
-        if (row + kStage <= o.rows && !o.pos) {
+        const char* from = (later ? o.second : o.first) + (o.order ? 0 : int64_t(row) * o.row_bytes);
+        if (row + kStage <= o.rows && !o.pos && !o.order) {
 #pragma unroll
           for (int j = 0; j < N; ++j) copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
         } else {
-          // rows of a wave: the same in all its lanes but for the place in kEach
-          constexpr int kEach = 64 / kWide > 0 ? 64 / kWide : 1;
-          typedef const __attribute__((address_space(4))) int32_t* fixed;
+          constexpr int kEach = 64 / kWide > 0 ? 64 / kWide : 1;       // rows of a wave
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             const int r = (tid + j * kThreads) / kWide, r0 = __builtin_amdgcn_readfirstlane(r);
+            const char* lane_from = from + offset[j];
             bool there = row + r < o.rows;
-            if (o.pos) {
+            if (o.pos || o.order) {
 #pragma unroll
               for (int e = 0; e < kEach; ++e) {
-                const int32_t t = row + r0 + e;
-                if (((fixed)(uintptr_t)o.pos)[t < o.rows ? t : o.rows - 1] < 0) there = there && r != r0 + e;
+                const int32_t t = row + r0 + e < o.rows ? row + r0 + e : o.rows - 1;
+                if (o.order) {
+                  const char* memory = from + int64_t(fixed(o.order)[t]) * o.row_bytes;
+                  lane_from = r == r0 + e ? memory + (offset[j] - uint32_t(r) * uint32_t(o.row_bytes)) : lane_from;
+                } else if (fixed(o.pos)[t] < 0) {
+                  there = there && r != r0 + e;
+                }
               }
             }
-            copy16_from(there ? static_cast<const void*>(from + offset[j]) : kNothing, lds + j * kThreads * 16);
+            copy16_from(there ? static_cast<const void*>(lane_from) : kNothing, lds + j * kThreads * 16);
           }
         }
       } else {
@@ -135,7 +154,10 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
           const char* from = o.first;
           if (PAIR && __builtin_amdgcn_readfirstlane((tid + j * kThreads) / CH) >= ROWS / 2) from = o.second;
           from += int64_t(c0) * 16;
-          if (whole) {
+          if (!PAIR && o.order) {
+            const int place = tid + j * kThreads, c = (place % CH) ^ (turned(place / CH) & (CH - 1));
+            copy16_from(c0 + c < o.chunks ? static_cast<const void*>(from + (uint64_t(offset[j]) << 4)) : kNothing, lds + j * kThreads * 16);
+          } else if (whole) {
             copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
           } else {
             const int place = tid + j * kThreads, c = (place % CH) ^ (turned(place / CH) & (CH - 1));
@@ -186,7 +208,11 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
                                              sums (&acc)[MI][NJ]) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave % WM, wn = wave / WM;
     if constexpr (!A_ACROSS) a.first += a_row * a.row_bytes, a.second += a_row * a.row_bytes, a.rows -= a_row;
-    if constexpr (!B_ACROSS) b.first += b_row * b.row_bytes, b.rows -= b_row;
+    if constexpr (!B_ACROSS) {
+      if (b.order) b.order += b_row;
+      else b.first += b_row * b.row_bytes;
+      b.rows -= b_row;
+    }
     const Side<BM, NA, A_ACROSS, GATED, true> from_a(a, a_row, tid);
     const Side<BN, NB, B_ACROSS, false, false> from_b(b, b_row, tid);
     const Place<BM, A_ACROSS, true> at_a(lane);
@@ -197,28 +223,142 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
       from_a.copy(a, begin + k * kStage, s.a[to], tid);
       from_b.copy(b, begin + k * kStage, s.b[to], tid);
     };
-#pragma unroll
-    for (int k = 0; k < STAGES - 1; ++k)
-      if (k < n) fetch(k);
-    for (int32_t k = 0; k < n; ++k) {
-      if (n - k >= STAGES - 1) loads_left<(STAGES - 2) * (NA + NB)>();
-      else loads_done();
-      together();
-      if (k + STAGES - 1 < n) fetch(k + STAGES - 1);
+    chunk x[2][MI], y[2][NJ];
+    auto read = [&](int32_t k, int kk) {
       const char *ta = s.a[k % STAGES], *tb = s.b[k % STAGES];
 #pragma unroll
-      for (int kk = 0; kk < CH / 2; ++kk) {
-        chunk x[MI], y[NJ];
+      for (int i = 0; i < MI; ++i) x[kk & 1][i] = at_a.read(ta, block_of(wm, i), kk);
 #pragma unroll
-        for (int i = 0; i < MI; ++i) x[i] = at_a.read(ta, block_of(wm, i), kk);
+      for (int j = 0; j < NJ; ++j) y[kk & 1][j] = at_b.read(tb, (wn * NJ + j) * 32, kk);
+    };
+    if (n <= 0) return;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) y[j] = at_b.read(tb, (wn * NJ + j) * 32, kk);
+    for (int k = 0; k < STAGES; ++k)
+      if (k < n) fetch(k);
+    if (n >= STAGES) loads_left<(STAGES - 1) * (NA + NB)>();
+    else loads_done();
+    together();
+    read(0, 0);
+    for (int32_t k = 0; k < n; ++k) {
+      each<CH / 2>([&](auto step) {
+        constexpr int kk = decltype(step)::value;
+        if (kk + 1 < CH / 2) {
+          read(k, kk + 1);
+        } else if (k + 1 < n) {        // all of this stage is in registers
+          if (n - k >= STAGES) loads_left<(STAGES - 2) * (NA + NB)>();
+          else loads_done();
+          together();
+          read(k + 1, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);       // the next operands are on their way before these are multiplied, not just before they are wanted
 #pragma unroll
         for (int i = 0; i < MI; ++i)
 #pragma unroll
-          for (int j = 0; j < NJ; ++j) acc[i][j] = Unit<T>::mfma(x[i], y[j], acc[i][j]);
+          for (int j = 0; j < NJ; ++j) acc[i][j] = Unit<T>::mfma(x[kk & 1][i], y[kk & 1][j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (kk + 1 == CH / 2 && k + STAGES < n) fetch(k + STAGES);
+      });
+    }
+  }
+};
+
+// Narrow rows: the weights stay in registers.  A sum of up to KS steps of two chunks leaves room for 64 rows of A in a wave (32 of each of a pair), which it loads once; the
+// rows of B pass by, 64 at a time, three times as many on their way to LDS, and every wave multiplies them with its own.  While 32 of them are multiplied, what came of
+// the 32 before is worked on and written (out.step), in the shadow of the matrix instructions.
+//
+// A wave waits for all but its last copies of two slots: what is newer than the copies of the slot that it wants are at least those of the next two, which are issued after
+// the slot's work, so the wait does not depend on how many results were written.
+template <typename T, int KS_, int WAVES_, bool PAIR> struct Narrow {
+  static constexpr int KS = KS_, WAVES = WAVES_, kThreads = 64 * WAVES, CH = 2 * KS, kRows = 64, SLOTS = 4, NC = kRows * CH / kThreads;
+  static constexpr int kSteps = 16 / KS;         // of the results' 16 registers, in each of the KS steps
+  static_assert(kRows * CH % kThreads == 0 && KS <= 16, "whole copies");
+  typedef typename Unit<T>::chunk chunk;
+  typedef typename Unit<T>::sums sums;
+  struct Shared { alignas(16) char rows[SLOTS][kRows * CH * 16]; };
+
+  // Rows [begin, end) of B (of its order) with rows a_row ... of A.  out.start(row) is told of the 32 rows that are multiplied next, and out.step<r>(acc) is given register r of
+  // those started before them; out.next() is called in between.
+  template <typename Out>
+  static __device__ __forceinline__ void run(Shared& s, const Operand& a, const Operand& b, int32_t a_row, int32_t begin, int32_t end, Out& out) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int kTurn = CH < 16 ? CH - 1 : 15;
+    chunk w[2][KS];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      int32_t row = a_row + (PAIR ? 32 * wave : 64 * wave + 32 * q) + in_order(lane & 31);
+      row = row < a.rows ? row : a.rows - 1;
+      const char* from = (PAIR && q ? a.second : a.first) + int64_t(row) * a.row_bytes;
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) {
+        const int c = 2 * kk + (lane >> 5);
+        const chunk nothing = {};
+        w[q][kk] = c < a.chunks ? *reinterpret_cast<const chunk*>(from + 16 * c) : nothing;
       }
     }
+    uint32_t offset[NC];
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      const int place = tid + j * kThreads, r = place / CH, c = (place % CH) ^ (turned(r) & kTurn);
+      offset[j] = uint32_t(r) * uint32_t(b.row_bytes) + 16 * c;
+    }
+    const int32_t n = (end - begin + kRows - 1) / kRows;
+    auto fetch = [&](int32_t k) {
+      const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s.rows[k % SLOTS]) + (tid & ~63) * 16);
+      const int32_t row0 = begin + k * kRows;
+      if (!b.order && row0 + kRows <= end && b.chunks >= CH) {
+        const char* from = b.first + int64_t(row0) * b.row_bytes;
+#pragma unroll
+        for (int j = 0; j < NC; ++j) copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
+        return;
+      }
+      constexpr int kEach = 64 / CH > 0 ? 64 / CH : 1;       // rows of a wave
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const int place = tid + j * kThreads, r = place / CH, c = (place % CH) ^ (turned(r) & kTurn), r0 = __builtin_amdgcn_readfirstlane(r);
+        const char* from = b.first;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          int32_t row = row0 + r0 + e;
+          row = row < end ? row : end - 1;
+          const char* memory = b.first + int64_t(b.order ? fixed(b.order)[row] : row) * b.row_bytes;
+          from = r == r0 + e ? memory + 16 * c : from;
+        }
+        copy16_from(c < b.chunks ? static_cast<const void*>(from) : kNothing, lds + j * kThreads * 16);
+      }
+    };
+    if (n <= 0) return;
+#pragma unroll
+    for (int k = 0; k < SLOTS - 1; ++k)
+      if (k < n) fetch(k);
+    const int at = (lane & 31) * CH + ((lane >> 5) ^ (turned(lane & 31) & kTurn));
+    sums acc[2][2] = {};
+    for (int32_t k = 0; k < n; ++k) {
+      if (n - k >= SLOTS - 1) loads_left<(SLOTS - 2) * NC>();
+      else loads_done();
+      together();
+      const char* tile = s.rows[k % SLOTS];
+      constexpr int kAhead = 3;
+      chunk y[kAhead + 1];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) y[i] = *reinterpret_cast<const chunk*>(tile + (at ^ (2 * i)) * 16);
+      each<2>([&](auto of_two) {
+        constexpr int half = decltype(of_two)::value;
+        out.start(begin + k * kRows + 32 * half);
+        each<KS>([&](auto step) {
+          constexpr int kk = decltype(step)::value, ahead = half * KS + kk + kAhead;
+          if constexpr (ahead < 2 * KS) y[ahead % (kAhead + 1)] = *reinterpret_cast<const chunk*>(tile + ((at ^ (2 * (ahead % KS))) + ahead / KS * 32 * CH) * 16);
+          constexpr int now = (half * KS + kk) % (kAhead + 1);
+          const sums nothing = {};
+          acc[half][0] = Unit<T>::mfma(w[0][kk], y[now], kk ? acc[half][0] : nothing);
+          each<kSteps>([&](auto r) { out.template step<kk * kSteps + decltype(r)::value>(acc[half ^ 1]); });
+          acc[half][1] = Unit<T>::mfma(w[1][kk], y[now], kk ? acc[half][1] : nothing);
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        out.next();
+      });
+      if (k + SLOTS - 1 < n) fetch(k + SLOTS - 1);
+    }
+    each<16>([&](auto r) { out.template step<decltype(r)::value>(acc[1]); });
   }
 };
 

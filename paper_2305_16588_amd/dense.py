@@ -14,7 +14,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from .binding import _Gated, _Residual, _Rows8, load_library
-from .layer import _DTYPE, _bad, _ints, _like, _ok, _on, _packer, _ptr, _rows2, _workspace
+from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _like, _ok, _on, _packer, _ptr, _rows2, _workspace
 
 _residual, _rows8, _gated = _packer(_Residual), _packer(_Rows8), _packer(_Gated)
 _ACT = {"silu": 0, "gelu": 1}
@@ -235,7 +235,11 @@ def gated_linear(x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
     index, g = _pair(x, w_gate, w_up, act, pos)
     with _on(index, stream) as on:
         h = torch.empty((x.shape[0], w_gate.shape[0]), dtype=x.dtype, device=x.device)
-        _ok(L.lgp_gated_linear(index, g, h.data_ptr(), on))
+        st = L.lgp_gated_linear(index, g, h.data_ptr(), 0, 0, on)
+        if st == _ECAPACITY:                    # nothing was launched: few calls want a workspace
+            w, size = _workspace(index, x.device, L.lgp_gated_linear_workspace, g, 0)
+            st = L.lgp_gated_linear(index, g, h.data_ptr(), _ptr(w), size, on)
+        _ok(st)
     return h
 
 
@@ -247,7 +251,7 @@ def gated_linear_backward(dh, x, w_gate, w_up, act: str = "silu", pos=None, stre
         dh = _plain(dh, (x.shape[0], w_gate.shape[0]), "dh", x.dtype, index)
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
         dg, du = torch.empty_like(w_gate), torch.empty_like(w_up)
-        w, size = _workspace(index, x.device, L.lgp_gated_linear_workspace, g)
+        w, size = _workspace(index, x.device, L.lgp_gated_linear_workspace, g, 1)
         _ok(L.lgp_gated_linear_backward(index, g, dh.data_ptr(), dx.data_ptr(), dg.data_ptr(), du.data_ptr(), _ptr(w), size, on))
     return dx, dg, du
 

@@ -238,7 +238,7 @@ def run_product(tokens, width, channels, dtype, bias=True, pos=None, seed=1):
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("tokens,width,channels", [(1, 1, 1), (1, 16, 16), (1, 1024, 1000), (2, 17, 33), (15, 100, 15), (16, 63, 64), (17, 64, 65), (32, 4097, 40), (33, 65, 31),
                                                    (64, 128, 64), (65, 1000, 129), (276, 256, 768), (1000, 250, 300), (1024, 100, 47), (1025, 1008, 257), (3000, 40, 500),
-                                                   (40, 20_000, 40), (1100, 9000, 270)])
+                                                   (40, 20_000, 40), (1100, 9000, 270), (5000, 256, 300), (2000, 500, 130), (1500, 128, 64), (9000, 33, 70)])
 def test_products_in_8_bits(tokens, width, channels, dtype):
     run_product(tokens, width, channels, dtype)
     run_product(tokens, width, channels, dtype, bias=False, pos=slots(tokens, 3), seed=7)
@@ -308,7 +308,8 @@ def run_gated(tokens, width, hidden, dtype, act, pos=None, seed=1, apart=0, trai
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [F16, BF16])
 @pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
-                                                 (129, 136, 129), (276, 256, 352), (300, 520, 257), (1000, 96, 500), (1025, 256, 683), (1500, 72, 40), (2500, 264, 300)])
+                                                 (129, 136, 129), (276, 256, 352), (300, 520, 257), (1000, 96, 500), (1025, 256, 683), (1500, 72, 40), (2500, 264, 300), (4097, 64, 96), (5000, 256, 130),
+                                                 (6000, 120, 683), (4500, 320, 90)])
 def test_gated_of_every_size(tokens, width, hidden, dtype, act):
     run_gated(tokens, width, hidden, dtype, act)
     run_gated(tokens, width, hidden, dtype, act, pos=slots(tokens, 9), apart=24, seed=5)
