@@ -22,7 +22,7 @@ struct GatedParams {
 template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float g, float& slope) {
   if constexpr (ACT == LGP_SILU) {
     const float s = rcp_fast(1.f + exp2_fast(-kLog2e * g)), a = g * s;
-    if (SLOPE) slope = s + a * (1.f - s);
+    if (SLOPE) slope = (s + a) - a * s;
     return a;
   } else {
     const float p = 0.5f * erfcf(-0.70710678118654752440f * g);
@@ -34,9 +34,10 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float 
 template <typename T, int ACT, class P, bool BACK>
 __global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams p) {
   __shared__ typename P::Shared lds;
-  const Tile t = tile_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
-  const int32_t f0 = t.m * (P::BM / 2), t0 = t.n * P::BN, tokens = p.count ? *fixed(p.count) : p.tokens;
-  if (t0 >= tokens) return;
+  const int32_t tokens = p.count ? *fixed(p.count) : p.tokens, tiles_n = (tokens + P::BN - 1) / P::BN;
+  if (int32_t(blockIdx.x) >= p.tiles_m * tiles_n) return;
+  const Tile t = tile_of(blockIdx.x, p.tiles_m * tiles_n, p.tiles_m, tiles_n);
+  const int32_t f0 = t.m * (P::BM / 2), t0 = t.n * P::BN;
   floatx16 acc[P::MI][P::NJ] = {};
   Operand x = p.x;
   x.rows = tokens;
@@ -79,79 +80,89 @@ __global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams
   }
 }
 
-// Narrow rows: what becomes of 32 tokens' results, lane l having token l % 32 and 16 consecutive hidden elements.
+// Narrow rows: what becomes of 32 tokens' results, lane l having token l % 32 and 16 consecutive hidden elements.  Loads and stores are made whatever there is to load and
+// store -- beyond the rows' end the last one's again -- but for what is behind hidden: the compiler counts those that are under way, and takes the fewest.
 template <typename T, int ACT, bool BACK> struct NarrowOut {
   const GatedParams& p;
   int32_t f, end, lane;              // the lane's first hidden element; the end of the workgroup's rows
-  int32_t row, token, next_row, next_token;        // of the list, and of memory; of the tokens worked on, and of those multiplied
-  int32_t ahead;                     // the token of memory after those
-  vec8<T> dh[2], next_dh[2];
-  float y[8], z[8];
-  __device__ __forceinline__ NarrowOut(const GatedParams& p, int32_t f, int32_t begin, int32_t end, int lane)
-      : p(p), f(f), end(end), lane(lane), row(-1), token(0), next_row(-1), next_token(0), ahead(listed(begin)) {
-    const vec8<T> nothing = {};
-    dh[0] = dh[1] = nothing;
+  bool whole;                        // in all lanes: 16 hidden elements are there
+  int32_t row[4], token[4];          // of the list, and of memory
+  vec8<T> dh[2], y, z;               // the gradients of h are on their way as soon as those before them are used
+  float held_y, held_z;
+  __device__ __forceinline__ int32_t clamped(int32_t first) const { return min(first + (lane & 31), end - 1); }
+  __device__ __forceinline__ int32_t token_of(int32_t first, const int32_t* listed) const {
+    return p.x.order ? listed[max(0, min(lane & 31, end - 1 - first))] : clamped(first);
   }
-  __device__ __forceinline__ int32_t listed(int32_t first) const {
-    const int32_t at = first + (lane & 31);
-    return at >= end ? 0 : p.x.order ? p.x.order[at] : at;
+  template <int Q> __device__ __forceinline__ void start(int32_t first, const int32_t* listed) {
+    row[Q] = clamped(first);
+    if constexpr (!BACK) token[Q] = token_of(first, listed);
   }
-  __device__ __forceinline__ void start(int32_t first) {
-    next_row = first + (lane & 31);
-    const bool in = next_row < end;
-    if (!in) next_row = -1;
-    next_token = ahead;
-    ahead = listed(first + 32);
+  __device__ __forceinline__ void next(int32_t first, const int32_t* listed) {
     if constexpr (BACK) {
-      const vec8<T> nothing = {};
-      const T* from = static_cast<const T*>(p.dh) + int64_t(next_token) * p.hidden + f;
+      if (first >= end) return;
+      const T* from = static_cast<const T*>(p.dh) + int64_t(token_of(first, listed)) * p.hidden;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int n = in ? p.hidden - f - 8 * i : 0;
-        next_dh[i] = nothing;
-        if (n >= 8) next_dh[i] = *reinterpret_cast<const typename AnyEight<T>::x8*>(from + 8 * i);
+      for (int i = 0; i < 2; ++i) dh[i] = *reinterpret_cast<const typename AnyEight<T>::x8*>(from + min(f + 8 * i, p.hidden - 8));
+    }
+  }
+  // Behind hidden the last eight of the row were read: those that are before these are shifted out.
+  __device__ __forceinline__ void shift() {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int by = 16 * min(8, f + 8 * i - min(f + 8 * i, p.hidden - 8));
+      union { vec8<T> v; uint64_t half[2]; } u;
+      u.v = dh[i];
+      if (by >= 64) u.half[0] = u.half[1], u.half[1] = 0;
+      if (by >= 128) u.half[0] = 0;
+      if (by & 63) u.half[0] = u.half[0] >> (by & 63) | u.half[1] << (64 - (by & 63)), u.half[1] >>= by & 63;
+      dh[i] = u.v;
+    }
+  }
+  template <int Q, int R, typename Sums> __device__ __forceinline__ void step(const Sums (&acc)[2]) {
+    constexpr int k = R % 8, i = R / 8;
+    float slope = 0.f;
+    const float a = activated<ACT, BACK>(acc[0][R], slope);
+    if constexpr (BACK) {
+      if (R == 0 && !whole) shift();
+      const float d = float(dh[i][k]);           // zero behind hidden, and so are the results
+      add<k>(y, held_y, d * acc[1][R] * slope);
+      add<k>(z, held_z, d * a);
+      if (k == 7) {
+        T* out = static_cast<T*>(p.grads) + int64_t(row[Q]) * 2 * p.pitch + f + 8 * i;
+        *reinterpret_cast<vec8<T>*>(out) = y;
+        *reinterpret_cast<vec8<T>*>(out + p.pitch) = z;
+      }
+    } else {
+      add<k>(y, held_y, a * acc[1][R]);
+      if (k == 7) {
+        T* out = static_cast<T*>(p.h) + int64_t(token[Q]) * p.hidden + f + 8 * i;
+        const int n = p.hidden - f - 8 * i;
+        if (whole || n >= 8) *reinterpret_cast<typename AnyEight<T>::x8*>(out) = y;
         else
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (e < n) next_dh[i][e] = from[8 * i + e];
+            if (e < n) out[e] = y[e];
       }
     }
   }
-  __device__ __forceinline__ void next() {
-    row = next_row;
-    token = next_token;
-    if constexpr (BACK) dh[0] = next_dh[0], dh[1] = next_dh[1];
-  }
-  template <int R, typename Sums> __device__ __forceinline__ void step(const Sums (&acc)[2]) {
-    constexpr int k = R % 8, i = R / 8;
-    const int n = p.hidden - f - 8 * i;
-    if constexpr (BACK) {
-      float slope;
-      const float a = activated<ACT, true>(acc[0][R], slope), d = float(dh[i][k]);
-      y[k] = k < n ? d * acc[1][R] * slope : 0.f;
-      z[k] = k < n ? d * a : 0.f;
-      if (k == 7 && row >= 0 && f + 8 * i < p.pitch) {
-        T* out = static_cast<T*>(p.grads) + int64_t(row) * 2 * p.pitch + f + 8 * i;
-        write_row(out, 8, y);
-        write_row(out + p.pitch, 8, z);
-      }
-    } else {
-      float none;
-      y[k] = activated<ACT, false>(acc[0][R], none) * acc[1][R];
-      if (k == 7 && row >= 0 && n > 0) write_row(static_cast<T*>(p.h) + int64_t(token) * p.hidden + f + 8 * i, n, y);
-    }
+  // Two at a time are rounded, so that they take one register.
+  template <int K> static __device__ __forceinline__ void add(vec8<T>& v, float& held, float x) {
+    if constexpr (K % 2 == 0) held = x;
+    else v[K - 1] = T(held), v[K] = T(x);
   }
 };
 template <typename T, int ACT, class P, bool BACK>
-__global__ __launch_bounds__(P::kThreads, 2) void gated_narrow_kernel(const GatedParams p) {
+__global__ __launch_bounds__(P::kThreads, P::kPerCu * P::WAVES / 4) void gated_narrow_kernel(const GatedParams p) {
   __shared__ typename P::Shared lds;
   // workgroups of one part of the tokens, which read the same rows, are on one XCD
   const int32_t piece = int32_t(piece_of(blockIdx.x, gridDim.x)), part = piece / p.tiles_m, parts = int32_t(gridDim.x) / p.tiles_m;
   const int32_t rows = p.count ? *fixed(p.count) : p.tokens, each = ((rows + parts - 1) / parts + 63) / 64 * 64;
   const int32_t f0 = piece % p.tiles_m * 32 * P::WAVES, begin = part * each, end = min(begin + each, rows);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  NarrowOut<T, ACT, BACK> out(p, f0 + 32 * wave + 16 * (lane >> 5), begin, end, lane);
-  P::run(lds, p.w, p.x, f0, begin, end, out);
+  // waves behind the last hidden element do what those before them do
+  const int32_t own = min(f0 + 32 * __builtin_amdgcn_readfirstlane(wave), ((BACK ? p.pitch : p.hidden) - 1) / 32 * 32);
+  NarrowOut<T, ACT, BACK> out = {p, own + 16 * (lane >> 5), end, lane, own + 32 <= p.hidden};
+  P::run(lds, p.w, p.x, own, begin, end, out);
 }
 
 // Tokens that there are, in order: a workgroup has kListed of them.  First it counts them, then, knowing how many come before, it lists them and fills the rows of
@@ -230,8 +241,6 @@ __host__ __device__ __forceinline__ int32_t part_of_sum(int32_t sum, int32_t par
 template <typename T, class P>
 __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p) {
   __shared__ typename P::Shared lds;
-  const Tile t = tile_of(blockIdx.x, gridDim.x, p.tiles_m, p.tiles_n);
-  const int32_t c0 = t.m * P::BM, row0 = t.n * P::BN;
   Operand a = p.a, b = p.b;
   int32_t rows = p.rows, sum = p.sum;
   if (p.count) {
@@ -239,8 +248,11 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
     b.rows = n;
     if (p.hidden) sum = a.rows = n;
     else rows = n;
-    if (row0 >= rows) return;
   }
+  const int32_t tiles_n = (rows + P::BN - 1) / P::BN;
+  if (int32_t(blockIdx.x) >= p.tiles_m * tiles_n * p.parts) return;
+  const Tile t = tile_of(blockIdx.x, p.tiles_m * tiles_n * p.parts, p.tiles_m, tiles_n);
+  const int32_t c0 = t.m * P::BM, row0 = t.n * P::BN;
   floatx16 acc[P::MI][P::NJ] = {};
   const int32_t each = part_of_sum(sum, p.parts), begin = t.part * each, end = min(begin + each, sum);
   P::run(lds, a, b, c0, row0, begin, end, acc);
@@ -297,9 +309,10 @@ __global__ __launch_bounds__(256) void join_kernel(const float* partial, int64_t
 }
 
 template <typename T> struct Forms {
+  typedef Narrow<T, 32, 4, true> Narrow512;
   typedef Narrow<T, 16, 8, true> Narrow256;
-  typedef Narrow<T, 8, 4, true> Narrow128;
-  typedef Narrow<T, 4, 4, true> Narrow64;
+  typedef Narrow<T, 8, 8, true> Narrow128;
+  typedef Narrow<T, 4, 8, true> Narrow64;
   typedef Tiles<T, 256, 256, 2, 4, 8, 2, true, false, false> LargePair;
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, true, false, false> MiddlePair;
   typedef Tiles<T, 128, 64, 2, 2, 8, 3, true, false, false> SmallPair;
@@ -320,7 +333,7 @@ template <typename T, int ACT, class P, bool BACK> void launch_gated(GatedParams
 }
 template <typename T, int ACT, class P, bool BACK> void launch_narrow(GatedParams p, int cus, hipStream_t s) {
   p.tiles_m = ((BACK ? p.pitch : p.hidden) + 32 * P::WAVES - 1) / (32 * P::WAVES);
-  const int32_t parts = std::max(1, std::min(cus * (8 / P::WAVES) / p.tiles_m, (p.tokens + 63) / 64));
+  const int32_t parts = std::max(1, std::min(cus * P::kPerCu / p.tiles_m, (p.tokens + 63) / 64));
   gated_narrow_kernel<T, ACT, P, BACK><<<uint32_t(p.tiles_m) * uint32_t(parts), P::kThreads, 0, s>>>(p);
 }
 template <typename T, int ACT, bool BACK> void gated_by_size(const GatedParams& p, int cus, hipStream_t s) {
@@ -330,10 +343,11 @@ template <typename T, int ACT, bool BACK> void gated_by_size(const GatedParams& 
     gated_few_kernel<T, ACT><<<dim3((p.hidden + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
     return;
   }
-  if (p.width_chunks <= 32 && !p.pos && p.tokens > kNarrowFrom) {
+  if (p.width_chunks <= 64 && !p.pos && p.tokens > kNarrowFrom && p.hidden >= 8) {
     if (p.width_chunks <= 8) launch_narrow<T, ACT, typename F::Narrow64, BACK>(p, cus, s);
     else if (p.width_chunks <= 16) launch_narrow<T, ACT, typename F::Narrow128, BACK>(p, cus, s);
-    else launch_narrow<T, ACT, typename F::Narrow256, BACK>(p, cus, s);
+    else if (p.width_chunks <= 32) launch_narrow<T, ACT, typename F::Narrow256, BACK>(p, cus, s);
+    else launch_narrow<T, ACT, typename F::Narrow512, BACK>(p, cus, s);
     return;
   }
   if (f == kLarge) launch_gated<T, ACT, typename F::LargePair, BACK>(p, s);

@@ -42,6 +42,10 @@ __device__ __align__(16) const uint32_t kNothing[4] = {};       // what is read 
 __device__ __forceinline__ void copy16_from(const void* from, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(from) : "memory");
 }
+// 4 bytes of each lane, as copy16.
+__device__ __forceinline__ void copy4(const void* from, uint32_t offset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(offset), "s"(from) : "memory");
+}
 template <int N> __device__ __forceinline__ void loads_left() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14); }      // all but the last N are done
 __device__ __forceinline__ void together() {       // everyone's reads of LDS are done, and so are the loads that each has waited for
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -126,10 +130,11 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
           for (int j = 0; j < N; ++j) copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
         } else {
           constexpr int kEach = 64 / kWide > 0 ? 64 / kWide : 1;       // rows of a wave
+          const void* lane_from[N];          // all places first: each is known when a list or the positions are read
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             const int r = (tid + j * kThreads) / kWide, r0 = __builtin_amdgcn_readfirstlane(r);
-            const char* lane_from = from + offset[j];
+            const char* place = from + offset[j];
             bool there = row + r < o.rows;
             if (o.pos || o.order) {
 #pragma unroll
@@ -137,14 +142,16 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
                 const int32_t t = row + r0 + e < o.rows ? row + r0 + e : o.rows - 1;
                 if (o.order) {
                   const char* memory = from + int64_t(fixed(o.order)[t]) * o.row_bytes;
-                  lane_from = r == r0 + e ? memory + (offset[j] - uint32_t(r) * uint32_t(o.row_bytes)) : lane_from;
+                  place = r == r0 + e ? memory + (offset[j] - uint32_t(r) * uint32_t(o.row_bytes)) : place;
                 } else if (fixed(o.pos)[t] < 0) {
                   there = there && r != r0 + e;
                 }
               }
             }
-            copy16_from(there ? static_cast<const void*>(lane_from) : kNothing, lds + j * kThreads * 16);
+            lane_from[j] = there ? static_cast<const void*>(place) : kNothing;
           }
+#pragma unroll
+          for (int j = 0; j < N; ++j) copy16_from(lane_from[j], lds + j * kThreads * 16);
         }
       } else {
         const int32_t c0 = at / (16 / Unit<T>::kSize);
@@ -262,30 +269,39 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
   }
 };
 
-// Narrow rows: the weights stay in registers.  A sum of up to KS steps of two chunks leaves room for 64 rows of A in a wave (32 of each of a pair), which it loads once; the
-// rows of B pass by, 64 at a time, three times as many on their way to LDS, and every wave multiplies them with its own.  While 32 of them are multiplied, what came of
-// the 32 before is worked on and written (out.step), in the shadow of the matrix instructions.
+// Narrow rows: the weights stay in registers.  With sums of up to KS steps of two chunks a wave has 64 rows of A (32 of each of a pair), which it loads once; the rows of B
+// pass by, 32 after 32, a few slots of them on their way to LDS, and each wave multiplies them with its own rows.  A SIMD has two waves: while one multiplies, the other
+// works on what came of its last 32 rows (out.step) -- the later four waves are half a turn behind.  With 32 steps there are registers for one wave, which does both in
+// turn.
 //
-// A wave waits for all but its last copies of two slots: what is newer than the copies of the slot that it wants are at least those of the next two, which are issued after
-// the slot's work, so the wait does not depend on how many results were written.
+// A wave waits for all but its last copies of SLOTS - 2 slots: what is newer than the copies of the slot that it wants are at least those of the next ones, which are issued
+// after a slot's work, so the wait does not depend on how many results were written.  Where there is a list, its part for a slot comes with the rows of
+// the slot that many before it.
 template <typename T, int KS_, int WAVES_, bool PAIR> struct Narrow {
-  static constexpr int KS = KS_, WAVES = WAVES_, kThreads = 64 * WAVES, CH = 2 * KS, kRows = 64, SLOTS = 4, NC = kRows * CH / kThreads;
-  static constexpr int kSteps = 16 / KS;         // of the results' 16 registers, in each of the KS steps
-  static_assert(kRows * CH % kThreads == 0 && KS <= 16, "whole copies");
+  static constexpr int KS = KS_, WAVES = WAVES_, kThreads = 64 * WAVES, kPerCu = KS < 16 && WAVES == 4 ? 2 : 1;       // workgroups
+  static constexpr int CH = 2 * KS, kRows = KS > 16 ? 32 : 64, SLOTS = 4, NC = kRows * CH / kThreads;
+  static constexpr int kRing = 4;                // blocks of 32 rows that the loop takes at once
+  static_assert(kRows * CH % kThreads == 0, "whole copies");
   typedef typename Unit<T>::chunk chunk;
   typedef typename Unit<T>::sums sums;
-  struct Shared { alignas(16) char rows[SLOTS][kRows * CH * 16]; };
+  struct Shared {
+    alignas(16) char rows[SLOTS][kRows * CH * 16];
+    int32_t listed[2 * SLOTS][64];               // of each slot
+  };
 
-  // Rows [begin, end) of B (of its order) with rows a_row ... of A.  out.start(row) is told of the 32 rows that are multiplied next, and out.step<r>(acc) is given register r of
-  // those started before them; out.next() is called in between.
+  // Rows [begin, end) of B (of its order) with rows a_row ... of A: a wave has 32 of each of a pair, or 64, from `own` on.  out.start<q>(row, listed) is told of the 32 rows that are
+  // multiplied next, q counting up to kRing, and where they are listed; out.step<q, r>(acc) is given register r of what came of them, as the q that they had; out.next(row, listed)
+  // is told afterwards which rows' results come next.  Rows from `end` on are the last row again, with the same results, but for 32 of
+  // them, which have none (with one wave on a SIMD, they too).
   template <typename Out>
-  static __device__ __forceinline__ void run(Shared& s, const Operand& a, const Operand& b, int32_t a_row, int32_t begin, int32_t end, Out& out) {
+  static __device__ __forceinline__ void run(Shared& s, const Operand& a, const Operand& b, int32_t own, int32_t begin, int32_t end, Out& out) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     constexpr int kTurn = CH < 16 ? CH - 1 : 15;
+    if (begin >= end) return;
     chunk w[2][KS];
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
-      int32_t row = a_row + (PAIR ? 32 * wave : 64 * wave + 32 * q) + in_order(lane & 31);
+      int32_t row = own + (PAIR ? 0 : 32 * q) + in_order(lane & 31);
       row = row < a.rows ? row : a.rows - 1;
       const char* from = (PAIR && q ? a.second : a.first) + int64_t(row) * a.row_bytes;
 #pragma unroll
@@ -295,70 +311,106 @@ template <typename T, int KS_, int WAVES_, bool PAIR> struct Narrow {
         w[q][kk] = c < a.chunks ? *reinterpret_cast<const chunk*>(from + 16 * c) : nothing;
       }
     }
-    uint32_t offset[NC];
-#pragma unroll
-    for (int j = 0; j < NC; ++j) {
-      const int place = tid + j * kThreads, r = place / CH, c = (place % CH) ^ (turned(r) & kTurn);
-      offset[j] = uint32_t(r) * uint32_t(b.row_bytes) + 16 * c;
-    }
     const int32_t n = (end - begin + kRows - 1) / kRows;
-    auto fetch = [&](int32_t k) {
+    // Copy j of a thread: row tid / CH + j * kThreads / CH of the slot.  Where a copy's rows are a multiple of 16, which the turn repeats after, all of them have the same chunk.
+    constexpr int kStep = kThreads / CH;
+    auto chunk_of = [&](int j) __attribute__((always_inline)) { return ((tid + j * kThreads) % CH) ^ (turned((tid + (kStep % 16 ? j * kThreads : 0)) / CH) & kTurn); };
+    auto list = [&](int32_t k) __attribute__((always_inline)) {
+      if (b.order && wave == 0 && k < n)
+        copy4(b.order + begin + k * kRows, lane * 4, __builtin_amdgcn_readfirstlane(lds_address(s.listed[k % (2 * SLOTS)])));
+    };
+    auto fetch = [&](int32_t k) __attribute__((always_inline)) {
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s.rows[k % SLOTS]) + (tid & ~63) * 16);
       const int32_t row0 = begin + k * kRows;
-      if (!b.order && row0 + kRows <= end && b.chunks >= CH) {
-        const char* from = b.first + int64_t(row0) * b.row_bytes;
+      if (b.order) {
+        list(k + SLOTS);
 #pragma unroll
-        for (int j = 0; j < NC; ++j) copy16(in_all_lanes(from), offset[j], lds + j * kThreads * 16);
-        return;
-      }
-      constexpr int kEach = 64 / CH > 0 ? 64 / CH : 1;       // rows of a wave
-#pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        const int place = tid + j * kThreads, r = place / CH, c = (place % CH) ^ (turned(r) & kTurn), r0 = __builtin_amdgcn_readfirstlane(r);
-        const char* from = b.first;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-          int32_t row = row0 + r0 + e;
-          row = row < end ? row : end - 1;
-          const char* memory = b.first + int64_t(b.order ? fixed(b.order)[row] : row) * b.row_bytes;
-          from = r == r0 + e ? memory + 16 * c : from;
+        for (int j = 0; j < NC; ++j) {
+          const int32_t row = s.listed[k % (2 * SLOTS)][min(tid / CH + j * kStep, end - 1 - row0)];
+          const int c = chunk_of(j);
+          copy16_from(c < b.chunks ? static_cast<const void*>(b.first + int64_t(row) * b.row_bytes + 16 * c) : kNothing, lds + j * kThreads * 16);
         }
-        copy16_from(c < b.chunks ? static_cast<const void*>(from) : kNothing, lds + j * kThreads * 16);
+      } else if (row0 + kRows <= end && b.chunks >= CH) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          const char* from = b.first + int64_t(row0 + j * kStep) * b.row_bytes;
+          copy16(in_all_lanes(from), uint32_t(tid / CH) * uint32_t(b.row_bytes) + 16 * chunk_of(j), lds + j * kThreads * 16);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          int32_t row = row0 + tid / CH + j * kStep;
+          row = row < end ? row : end - 1;
+          const int c = chunk_of(j);
+          copy16_from(c < b.chunks ? static_cast<const void*>(b.first + int64_t(row) * b.row_bytes + 16 * c) : kNothing, lds + j * kThreads * 16);
+        }
       }
     };
-    if (n <= 0) return;
+    if (b.order) {
+#pragma unroll
+      for (int k = 0; k < SLOTS; ++k) list(k);
+      loads_done();
+      together();
+    }
 #pragma unroll
     for (int k = 0; k < SLOTS - 1; ++k)
       if (k < n) fetch(k);
     const int at = (lane & 31) * CH + ((lane >> 5) ^ (turned(lane & 31) & kTurn));
-    sums acc[2][2] = {};
-    for (int32_t k = 0; k < n; ++k) {
+    constexpr int kAhead = WAVES == 8 ? 2 : 3, kBlocks = kRows / 32;        // loads of operands ahead of their use; blocks in a slot
+    const sums nothing = {};
+    auto slot_ready = [&](int32_t k) __attribute__((always_inline)) {
       if (n - k >= SLOTS - 1) loads_left<(SLOTS - 2) * NC>();
       else loads_done();
       together();
-      const char* tile = s.rows[k % SLOTS];
-      constexpr int kAhead = 3;
-      chunk y[kAhead + 1];
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) y[i] = *reinterpret_cast<const chunk*>(tile + (at ^ (2 * i)) * 16);
-      each<2>([&](auto of_two) {
-        constexpr int half = decltype(of_two)::value;
-        out.start(begin + k * kRows + 32 * half);
-        each<KS>([&](auto step) {
-          constexpr int kk = decltype(step)::value, ahead = half * KS + kk + kAhead;
-          if constexpr (ahead < 2 * KS) y[ahead % (kAhead + 1)] = *reinterpret_cast<const chunk*>(tile + ((at ^ (2 * (ahead % KS))) + ahead / KS * 32 * CH) * 16);
-          constexpr int now = (half * KS + kk) % (kAhead + 1);
-          const sums nothing = {};
-          acc[half][0] = Unit<T>::mfma(w[0][kk], y[now], kk ? acc[half][0] : nothing);
-          each<kSteps>([&](auto r) { out.template step<kk * kSteps + decltype(r)::value>(acc[half ^ 1]); });
-          acc[half][1] = Unit<T>::mfma(w[1][kk], y[now], kk ? acc[half][1] : nothing);
+    };
+    chunk y[kAhead + 1];
+    auto operand = [&](const char* tile, int i) __attribute__((always_inline)) { return *reinterpret_cast<const chunk*>(tile + ((at ^ (2 * (i % KS))) + i / KS * 32 * CH) * 16); };
+    auto start = [&](auto of_ring, int32_t k) __attribute__((always_inline)) {
+      constexpr int q = decltype(of_ring)::value, block = q % kBlocks;
+      out.template start<q>(begin + k * kRows + 32 * block, s.listed[k % (2 * SLOTS)] + 32 * block);
+    };
+    out.template start<kRing - 1>(begin, s.listed[0]);
+    out.next(begin, s.listed[0]);
+    constexpr bool kTwo = WAVES == 8;
+    const bool late = kTwo && wave >= WAVES / 2;
+    sums acc[kTwo ? 1 : 2][2] = {};
+    auto results = [&](auto of_ring, int32_t k) __attribute__((always_inline)) {       // of slot k
+      constexpr int q = decltype(of_ring)::value, after = (q + 1) % kBlocks;
+      if (begin + k * kRows + 32 * (q % kBlocks) >= end) return;
+      each<16>([&](auto r) __attribute__((always_inline)) { out.template step<q, decltype(r)::value>(acc[kTwo ? 0 : q & 1]); });
+      const int32_t then = after ? k : k + 1;
+      out.next(begin + then * kRows + 32 * after, s.listed[then % (2 * SLOTS)] + 32 * after);
+    };
+    for (int32_t k0 = 0; k0 < n; k0 += kRing / kBlocks) {
+      each<kRing>([&](auto of_ring) __attribute__((always_inline)) {
+        constexpr int q = decltype(of_ring)::value, block = q % kBlocks, before = (q + kRing - 1) % kRing;
+        const int32_t k = k0 + q / kBlocks;
+        const char* tile = s.rows[k % SLOTS];
+        if (block == 0) {
+          if (k < n) slot_ready(k);
+          if (kTwo ? late && k > 0 && k <= n : k == n) results(Int<before>(), k - 1);
+        }
+        if (k >= n) return;
+        if (block == 0) each<kAhead>([&](auto i) __attribute__((always_inline)) { y[decltype(i)::value] = operand(tile, decltype(i)::value); });
+        start(of_ring, k);
+        each<KS>([&](auto step) __attribute__((always_inline)) {
+          constexpr int kk = decltype(step)::value, here = block * KS + kk, ahead = here + kAhead, set = kTwo ? 0 : q & 1;
+          if constexpr (ahead < kBlocks * KS) y[ahead % (kAhead + 1)] = operand(tile, ahead);
+          acc[set][0] = Unit<T>::mfma(w[0][kk], y[here % (kAhead + 1)], kk ? acc[set][0] : nothing);
+          // one wave: registers kk * 16 / KS ... of the results before
+          if constexpr (!kTwo) each<(kk + 1) * 16 / KS - kk * 16 / KS>([&](auto r) __attribute__((always_inline)) {
+            out.template step<before, kk * 16 / KS + decltype(r)::value>(acc[set ^ 1]);
+          });
+          if (!kTwo && kk + 1 == KS) out.next(begin + k * kRows + 32 * block, s.listed[k % (2 * SLOTS)] + 32 * block);
+          acc[set][1] = Unit<T>::mfma(w[1][kk], y[here % (kAhead + 1)], kk ? acc[set][1] : nothing);
           __builtin_amdgcn_sched_barrier(0);
         });
-        out.next();
+        if (kTwo && (block + 1 < kBlocks || !late)) results(of_ring, k);
+        __builtin_amdgcn_sched_barrier(0);
+        if (block == kBlocks - 1 && k + SLOTS - 1 < n) fetch(k + SLOTS - 1);
       });
-      if (k + SLOTS - 1 < n) fetch(k + SLOTS - 1);
     }
-    each<16>([&](auto r) { out.template step<decltype(r)::value>(acc[1]); });
+    if ((!kTwo || late) && n % (kRing / kBlocks) == 0) results(Int<kRing - 1>(), n - 1);
   }
 };
 

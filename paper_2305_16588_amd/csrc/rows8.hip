@@ -56,40 +56,38 @@ __global__ __launch_bounds__(P::kThreads, 2) void product8_kernel(const Product8
   }
 }
 
-// Narrow rows: what becomes of 32 rows' results, lane l having row l % 32 and 16 consecutive channels in each of two blocks.
-template <typename T> struct NarrowOut8 {
+// Narrow rows: what becomes of 32 rows' results, lane l having row l % 32 and 16 consecutive channels in each of two blocks.  Beyond the rows' end it is the last one again.
+template <typename T, int CHANNELS> struct NarrowOut8 {
   const Product8Params& p;
   const float* lds;                  // the workgroup's scales and biases
   int32_t c, at, end, lane;          // the lane's first channel, and its place in the workgroup; the end of the workgroup's rows
-  int32_t token = -1, next_token = -1;
-  float scale = 0.f, next_scale = 0.f;
-  bool live = false, next_live = false;
+  bool whole;                        // in all lanes: all 16 channels of both blocks are there
+  int32_t token[4];
+  float scale[4];
+  bool live[4];
   float y[2][8];
-  __device__ __forceinline__ void start(int32_t first) {
-    next_token = first + (lane & 31);
-    if (next_token >= end) next_token = -1;
-    const int32_t t = next_token < 0 ? 0 : next_token;
-    next_scale = p.x_scales[t];
-    next_live = !p.pos || p.pos[t] >= 0;
+  __device__ __forceinline__ void next(int32_t, const int32_t*) {}
+  template <int Q> __device__ __forceinline__ void start(int32_t first, const int32_t*) {
+    token[Q] = min(first + (lane & 31), end - 1);
+    scale[Q] = p.x_scales[token[Q]];
+    live[Q] = !p.pos || p.pos[token[Q]] >= 0;
   }
-  __device__ __forceinline__ void next() { token = next_token, scale = next_scale, live = next_live; }
-  template <int R, int CHANNELS, typename Sums> __device__ __forceinline__ void step_of(const Sums (&acc)[2]) {
+  template <int Q, int R, typename Sums> __device__ __forceinline__ void step(const Sums (&acc)[2]) {
     constexpr int k = R % 8, i = R / 8;
-#pragma unroll
-    for (int q = 0; q < 2; ++q) {
+    each<2>([&](auto of_two) __attribute__((always_inline)) {
+      constexpr int q = decltype(of_two)::value;
       const int a = at + 32 * q + R;
-      const float v = float(acc[q][R]) * lds[a] * scale + lds[CHANNELS + a];
-      y[q][k] = live ? v : 0.f;
-      const int32_t to = c + 32 * q + 8 * i, n = p.channels - to;
-      if (k == 7 && token >= 0 && n > 0) write_row(static_cast<T*>(p.out) + int64_t(token) * p.channels + to, n, y[q]);
-    }
+      const float v = float(acc[q][R]) * lds[a] * scale[Q] + lds[CHANNELS + a];
+      y[q][k] = live[Q] ? v : 0.f;
+      if (k == 7) {
+        const int32_t to = c + 32 * q + 8 * i, n = p.channels - to;
+        if (whole || n > 0) write_row(static_cast<T*>(p.out) + int64_t(token[Q]) * p.channels + to, whole ? 8 : n, y[q]);
+      }
+    });
   }
-};
-template <typename T, class P> struct NarrowOf : NarrowOut8<T> {
-  template <int R, typename Sums> __device__ __forceinline__ void step(const Sums (&acc)[2]) { this->template step_of<R, 64 * P::WAVES>(acc); }
 };
 template <typename T, class P>
-__global__ __launch_bounds__(P::kThreads, 2) void product8_narrow_kernel(const Product8Params p) {
+__global__ __launch_bounds__(P::kThreads, P::kPerCu * P::WAVES / 4) void product8_narrow_kernel(const Product8Params p) {
   __shared__ typename P::Shared lds;
   __shared__ __align__(16) float more[2 * 64 * P::WAVES];
   const int32_t piece = int32_t(piece_of(blockIdx.x, gridDim.x)), part = piece / p.tiles_m, parts = int32_t(gridDim.x) / p.tiles_m;
@@ -99,9 +97,10 @@ __global__ __launch_bounds__(P::kThreads, 2) void product8_narrow_kernel(const P
     more[i] = in ? p.w_scales[c0 + i] : 0.f;
     more[64 * P::WAVES + i] = in && p.bias ? p.bias[c0 + i] : 0.f;
   }
-  const int lane = threadIdx.x & 63, at = (threadIdx.x >> 6) * 64 + 16 * (lane >> 5);
-  NarrowOf<T, P> out{{p, more, c0 + at, at, end, lane}};
-  P::run(lds, p.w, p.x, c0, begin, end, out);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int32_t own = c0 + 64 * wave;
+  NarrowOut8<T, 64 * P::WAVES> out = {p, more, own + 16 * (lane >> 5), 64 * wave + 16 * (lane >> 5), end, lane, own + 64 <= p.channels};
+  P::run(lds, p.w, p.x, own, begin, end, out);
 }
 
 // Few rows: a thread has one channel of one.
@@ -117,6 +116,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void product8_few_kernel(const Prod
   static_cast<T*>(p.out)[int64_t(t0 + c) * p.channels + c0 + r] = T(!p.pos || p.pos[t0 + c] >= 0 ? y : 0.f);
 }
 
+typedef Narrow<int8_t, 32, 4, false> Narrow1024;
 typedef Narrow<int8_t, 16, 8, false> Narrow512;
 typedef Narrow<int8_t, 8, 4, false> Narrow256;
 typedef Narrow<int8_t, 4, 4, false> Narrow128;
@@ -133,7 +133,7 @@ template <typename T, class P> void launch8(Product8Params p, hipStream_t s) {
 constexpr int64_t kNarrowFrom = 1024;
 template <typename T, class P> void narrow8(Product8Params p, int cus, hipStream_t s) {
   p.tiles_m = (p.channels + 64 * P::WAVES - 1) / (64 * P::WAVES);
-  const int32_t parts = std::max(1, std::min(cus * (8 / P::WAVES) / p.tiles_m, (p.tokens + 63) / 64));
+  const int32_t parts = std::max(1, std::min(cus * P::kPerCu / p.tiles_m, (p.tokens + 63) / 64));
   product8_narrow_kernel<T, P><<<uint32_t(p.tiles_m) * uint32_t(parts), P::kThreads, 0, s>>>(p);
 }
 template <typename T> void product8(const Product8Params& p, int cus, hipStream_t s) {
@@ -141,10 +141,11 @@ template <typename T> void product8(const Product8Params& p, int cus, hipStream_
     product8_few_kernel<T><<<dim3((p.channels + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
     return;
   }
-  if (p.chunks <= 32 && p.tokens > kNarrowFrom) {
+  if (p.chunks <= 64 && p.tokens > kNarrowFrom) {
     if (p.chunks <= 8) narrow8<T, Narrow128>(p, cus, s);
     else if (p.chunks <= 16) narrow8<T, Narrow256>(p, cus, s);
-    else narrow8<T, Narrow512>(p, cus, s);
+    else if (p.chunks <= 32) narrow8<T, Narrow512>(p, cus, s);
+    else narrow8<T, Narrow1024>(p, cus, s);
     return;
   }
   const int f = p.tokens <= 1024 ? kSmall : kLarge;

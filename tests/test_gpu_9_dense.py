@@ -238,7 +238,7 @@ def run_product(tokens, width, channels, dtype, bias=True, pos=None, seed=1):
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("tokens,width,channels", [(1, 1, 1), (1, 16, 16), (1, 1024, 1000), (2, 17, 33), (15, 100, 15), (16, 63, 64), (17, 64, 65), (32, 4097, 40), (33, 65, 31),
                                                    (64, 128, 64), (65, 1000, 129), (276, 256, 768), (1000, 250, 300), (1024, 100, 47), (1025, 1008, 257), (3000, 40, 500),
-                                                   (40, 20_000, 40), (1100, 9000, 270), (5000, 256, 300), (2000, 500, 130), (1500, 128, 64), (9000, 33, 70)])
+                                                   (40, 20_000, 40), (1100, 9000, 270), (5000, 256, 300), (2000, 500, 130), (1500, 128, 64), (9000, 33, 70), (2000, 1000, 130), (1100, 600, 70)])
 def test_products_in_8_bits(tokens, width, channels, dtype):
     run_product(tokens, width, channels, dtype)
     run_product(tokens, width, channels, dtype, bias=False, pos=slots(tokens, 3), seed=7)
