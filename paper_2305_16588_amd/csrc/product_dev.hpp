@@ -95,6 +95,7 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
   struct Shared {
     alignas(16) char a[STAGES][BM * CH * 16];
     alignas(16) char b[STAGES][BN * CH * 16];
+    int32_t listed[A_ACROSS ? 8 : 1][64];         // A's rows of a stage, where there is a list
   };
 
   // A thread's places in the tile of one side, and what it copies there.
@@ -119,7 +120,8 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
         }
       }
     }
-    __device__ __forceinline__ void copy(const Operand& o, int32_t at, char* to, int tid) const {       // at: the stage's first place of the sum
+    // at: the stage's first place of the sum; listed: its rows, where there is a list.
+    __device__ __forceinline__ void copy(const Operand& o, int32_t at, char* to, const int32_t* listed, int tid) const {
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(to) + (tid & ~63) * 16);
       if constexpr (ACROSS) {
         const bool later = at >= o.half;
@@ -136,16 +138,13 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
             const int r = (tid + j * kThreads) / kWide, r0 = __builtin_amdgcn_readfirstlane(r);
             const char* place = from + offset[j];
             bool there = row + r < o.rows;
-            if (o.pos || o.order) {
+            if (o.order) {
+              place = from + int64_t(listed[there ? r : 0]) * o.row_bytes + (offset[j] - uint32_t(r) * uint32_t(o.row_bytes));
+            } else if (o.pos) {
 #pragma unroll
               for (int e = 0; e < kEach; ++e) {
                 const int32_t t = row + r0 + e < o.rows ? row + r0 + e : o.rows - 1;
-                if (o.order) {
-                  const char* memory = from + int64_t(fixed(o.order)[t]) * o.row_bytes;
-                  place = r == r0 + e ? memory + (offset[j] - uint32_t(r) * uint32_t(o.row_bytes)) : place;
-                } else if (fixed(o.pos)[t] < 0) {
-                  there = there && r != r0 + e;
-                }
+                if (fixed(o.pos)[t] < 0) there = there && r != r0 + e;
               }
             }
             lane_from[j] = there ? static_cast<const void*>(place) : kNothing;
@@ -225,10 +224,16 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
     const Place<BM, A_ACROSS, true> at_a(lane);
     const Place<BN, B_ACROSS, false> at_b(lane);
     const int32_t n = (end - begin + kStage - 1) / kStage;
+    // A list's part for a stage comes with the stage two before it.
+    auto list = [&](int32_t k) {
+      if (wave == 0 && k < n)
+        copy4(a.order + begin + k * kStage, min(lane, end - 1 - begin - k * kStage) * 4, __builtin_amdgcn_readfirstlane(lds_address(s.listed[A_ACROSS ? k % 8 : 0])));
+    };
     auto fetch = [&](int32_t k) {
       const int to = k % STAGES;
-      from_a.copy(a, begin + k * kStage, s.a[to], tid);
-      from_b.copy(b, begin + k * kStage, s.b[to], tid);
+      if (A_ACROSS && a.order) list(k + 2);
+      from_a.copy(a, begin + k * kStage, s.a[to], s.listed[A_ACROSS ? k % 8 : 0], tid);
+      from_b.copy(b, begin + k * kStage, s.b[to], nullptr, tid);
     };
     chunk x[2][MI], y[2][NJ];
     auto read = [&](int32_t k, int kk) {
@@ -239,6 +244,12 @@ template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, 
       for (int j = 0; j < NJ; ++j) y[kk & 1][j] = at_b.read(tb, (wn * NJ + j) * 32, kk);
     };
     if (n <= 0) return;
+    if (A_ACROSS && a.order) {
+#pragma unroll
+      for (int k = 0; k < STAGES; ++k) list(k);
+      loads_done();
+      together();
+    }
 #pragma unroll
     for (int k = 0; k < STAGES; ++k)
       if (k < n) fetch(k);
