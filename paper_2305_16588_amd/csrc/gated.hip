@@ -314,7 +314,6 @@ template <typename T> struct Forms {
   typedef Narrow<T, 8, 8, true> Narrow128;
   typedef Narrow<T, 4, 8, true> Narrow64;
   typedef Tiles<T, 256, 256, 2, 4, 8, 2, true, false, false> LargePair;
-  typedef Tiles<T, 128, 256, 2, 2, 4, 3, true, false, false> MiddlePair;
   typedef Tiles<T, 128, 64, 2, 2, 8, 3, true, false, false> SmallPair;
   typedef Tiles<T, 256, 256, 2, 4, 8, 2, false, true, false> LargeX;
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, false, true, false> MiddleX;
@@ -323,8 +322,8 @@ template <typename T> struct Forms {
   typedef Tiles<T, 128, 256, 2, 2, 4, 3, false, true, true> MiddleW;
   typedef Tiles<T, 64, 64, 2, 2, 8, 3, false, true, true> SmallW;
 };
-enum { kLarge = 0, kMiddle = 1, kSmall = 2 };       // forms of a tile
-constexpr int64_t kNarrowFrom = 1024, kListFrom = 4096;
+enum { kLarge, kMiddle, kSmall };       // forms of a tile
+constexpr int64_t kListFrom = 4096;
 
 template <typename T, int ACT, class P, bool BACK> void launch_gated(GatedParams p, hipStream_t s) {
   p.tiles_m = ((BACK ? p.pitch : p.hidden) + P::BM / 2 - 1) / (P::BM / 2);
@@ -336,42 +335,48 @@ template <typename T, int ACT, class P, bool BACK> void launch_narrow(GatedParam
   const int32_t parts = std::max(1, std::min(cus * P::kPerCu / p.tiles_m, (p.tokens + 63) / 64));
   gated_narrow_kernel<T, ACT, P, BACK><<<uint32_t(p.tiles_m) * uint32_t(parts), P::kThreads, 0, s>>>(p);
 }
+// Up to 32 tokens by the kernel that reads the weights straight to registers (32 tokens, 1024 to 4096: 8.4 us, small tiles 12.0; 64 tokens: 13.1 and 12.0).  Then small tiles, up
+// to four for each CU (2048 tokens, 1024 to 2048, 1024 of them: 30.5 us, large ones 30.4; half as many tokens: 17.1 and 29.4; twice: 57 and 35).  Beyond that narrow rows,
+// where every workgroup has four slots of them at least (32768 tokens, 256 to 1024, eight slots: 40.7 us, large tiles 51.0; 8192, two slots: 18.9 and 15.6), and large tiles.
 template <typename T, int ACT, bool BACK> void gated_by_size(const GatedParams& p, int cus, hipStream_t s) {
   typedef Forms<T> F;
-  const int f = p.tokens <= 1024 ? kSmall : kLarge;
   if (!BACK && p.tokens <= kFewTokens) {
     gated_few_kernel<T, ACT><<<dim3((p.hidden + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
     return;
   }
-  if (p.width_chunks <= 64 && !p.pos && p.tokens > kNarrowFrom && p.hidden >= 8) {
-    if (p.width_chunks <= 8) launch_narrow<T, ACT, typename F::Narrow64, BACK>(p, cus, s);
-    else if (p.width_chunks <= 16) launch_narrow<T, ACT, typename F::Narrow128, BACK>(p, cus, s);
-    else if (p.width_chunks <= 32) launch_narrow<T, ACT, typename F::Narrow256, BACK>(p, cus, s);
-    else launch_narrow<T, ACT, typename F::Narrow512, BACK>(p, cus, s);
-    return;
-  }
-  if (f == kLarge) launch_gated<T, ACT, typename F::LargePair, BACK>(p, s);
-  else if (f == kMiddle) launch_gated<T, ACT, typename F::MiddlePair, BACK>(p, s);
-  else launch_gated<T, ACT, typename F::SmallPair, BACK>(p, s);
+  const int64_t small = int64_t((p.hidden + 63) / 64) * ((p.tokens + 63) / 64);
+  if (small <= 4 * cus) return launch_gated<T, ACT, typename F::SmallPair, BACK>(p, s);
+  if (p.width_chunks > 64 || p.pos || p.hidden < 8) return launch_gated<T, ACT, typename F::LargePair, BACK>(p, s);
+  const int64_t slots = int64_t(p.tokens + 63) / 64, groups = (p.hidden + (p.width_chunks <= 32 ? 255 : 127)) / (p.width_chunks <= 32 ? 256 : 128);
+  if (slots * groups < 4 * cus) return launch_gated<T, ACT, typename F::LargePair, BACK>(p, s);
+  if (p.width_chunks <= 8) launch_narrow<T, ACT, typename F::Narrow64, BACK>(p, cus, s);
+  else if (p.width_chunks <= 16) launch_narrow<T, ACT, typename F::Narrow128, BACK>(p, cus, s);
+  else if (p.width_chunks <= 32) launch_narrow<T, ACT, typename F::Narrow256, BACK>(p, cus, s);
+  else launch_narrow<T, ACT, typename F::Narrow512, BACK>(p, cus, s);
 }
 template <typename T, bool BACK> void gated_by_act(int32_t act, const GatedParams& p, int cus, hipStream_t s) {
   if (act == LGP_SILU) gated_by_size<T, LGP_SILU, BACK>(p, cus, s);
   else gated_by_size<T, LGP_GELU, BACK>(p, cus, s);
 }
+// Small tiles for products of few operations, which large ones would leave to few CUs, and those between for the next ones.  Measured, by tokens, width and hidden, for whole
+// backward passes: of x, 16384, 256, 704 (6e9 products): small 99 us, large 110; 4096, 1024, 2048 (2e10): 225, 250; 65536, 256, 704 (2e10): middle 279, small 307, large 332;
+// 65536, 512, 1024 (7e10): large 524, middle 542.  Of the weights, 16384, 256, 704: small 107, large 111; 65536, 256, 704: middle 307, large 329, small 351; 65536, 512, 1024:
+// middle 514, large 521; 65536, 1024, 2048 (3e11): large 1805, middle 1884.
 struct GradShape { int32_t parts; int form; };
-// Parts of the sum: as many as make 512 workgroups, of at least 512 places each.
-GradShape grad_shape(int32_t rows, int32_t cols, int32_t sum, int f) {
+GradShape grad_shape(int32_t rows, int32_t cols, int32_t sum, double most_small, double most_middle) {
   GradShape g;
-  g.form = f;
-  const int32_t bm = f == kLarge ? 256 : f == kMiddle ? 128 : 64, bn = f == kSmall ? 64 : 256;
+  const double products = double(rows) * cols * sum;
+  g.form = products <= most_small ? kSmall : products <= most_middle ? kMiddle : kLarge;
+  const int32_t bm = g.form == kLarge ? 256 : g.form == kMiddle ? 128 : 64, bn = g.form == kSmall ? 64 : 256;
+  // parts of the sum: as many as make 512 workgroups, of at least 512 places each
   const int64_t tiles = std::max<int64_t>(1, int64_t((cols + bm - 1) / bm) * ((rows + bn - 1) / bn));
   const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(512 / tiles, sum / 512));
   const int32_t each = part_of_sum(sum, int32_t(parts));
   g.parts = std::max(1, (sum + each - 1) / each);
   return g;
 }
-GradShape shape_x(const lgp_gated* g, int32_t pitch) { return grad_shape(int32_t(g->tokens), g->width, 2 * pitch, g->tokens <= 1024 ? kSmall : kLarge); }
-GradShape shape_w(const lgp_gated* g, int32_t pitch) { return grad_shape(2 * pitch, g->width, int32_t(g->tokens), kLarge); }
+GradShape shape_x(const lgp_gated* g, int32_t pitch) { return grad_shape(int32_t(g->tokens), g->width, 2 * pitch, 1.9e10, 5e10); }
+GradShape shape_w(const lgp_gated* g, int32_t pitch) { return grad_shape(2 * pitch, g->width, int32_t(g->tokens), 8e9, 5e10); }
 
 template <typename T, class P> void launch_grad(GradParams p, const GradShape& g, const int32_t* pos, hipStream_t s) {
   p.tiles_m = (p.cols + P::BM - 1) / P::BM;

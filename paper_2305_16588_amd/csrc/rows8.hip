@@ -56,16 +56,22 @@ __global__ __launch_bounds__(P::kThreads, 2) void product8_kernel(const Product8
   }
 }
 
+__device__ __forceinline__ void read8(const float* p, float* x) {
+  const floatx4 low = *reinterpret_cast<const floatx4*>(p), high = *reinterpret_cast<const floatx4*>(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = low[i], x[i + 4] = high[i];
+}
+
 // Narrow rows: what becomes of 32 rows' results, lane l having row l % 32 and 16 consecutive channels in each of two blocks.  Beyond the rows' end it is the last one again.
 template <typename T, int CHANNELS> struct NarrowOut8 {
   const Product8Params& p;
-  const float* lds;                  // the workgroup's scales and biases
+  const float* lds;                  // the workgroup's scales, and its biases CHANNELS further on
   int32_t c, at, end, lane;          // the lane's first channel, and its place in the workgroup; the end of the workgroup's rows
   bool whole;                        // in all lanes: all 16 channels of both blocks are there
   int32_t token[4];
   float scale[4];
   bool live[4];
-  float y[2][8];
+  float y[2][8], w[2][8], b[2][8];
   __device__ __forceinline__ void next(int32_t, const int32_t*) {}
   template <int Q> __device__ __forceinline__ void start(int32_t first, const int32_t*) {
     token[Q] = min(first + (lane & 31), end - 1);
@@ -76,8 +82,11 @@ template <typename T, int CHANNELS> struct NarrowOut8 {
     constexpr int k = R % 8, i = R / 8;
     each<2>([&](auto of_two) __attribute__((always_inline)) {
       constexpr int q = decltype(of_two)::value;
-      const int a = at + 32 * q + R;
-      const float v = float(acc[q][R]) * lds[a] * scale[Q] + lds[CHANNELS + a];
+      if (k == 0) {                  // of eight channels, two loads each
+        read8(lds + at + 32 * q + R, w[q]);
+        read8(lds + CHANNELS + at + 32 * q + R, b[q]);
+      }
+      const float v = float(acc[q][R]) * w[q][k] * scale[Q] + b[q][k];
       y[q][k] = live[Q] ? v : 0.f;
       if (k == 7) {
         const int32_t to = c + 32 * q + 8 * i, n = p.channels - to;
@@ -121,37 +130,32 @@ typedef Narrow<int8_t, 16, 8, false> Narrow512;
 typedef Narrow<int8_t, 8, 4, false> Narrow256;
 typedef Narrow<int8_t, 4, 4, false> Narrow128;
 typedef Tiles<int8_t, 256, 256, 2, 4, 8, 2, false, false, false> Large8;
-typedef Tiles<int8_t, 128, 256, 2, 2, 4, 3, false, false, false> Middle8;
 typedef Tiles<int8_t, 64, 64, 2, 2, 8, 3, false, false, false> Small8;
-enum { kLarge = 0, kMiddle = 1, kSmall = 2 };       // forms of a tile
 
 template <typename T, class P> void launch8(Product8Params p, hipStream_t s) {
   p.tiles_m = (p.channels + P::BM - 1) / P::BM;
   p.tiles_n = (p.tokens + P::BN - 1) / P::BN;
   product8_kernel<T, P><<<uint32_t(p.tiles_m) * uint32_t(p.tiles_n), P::kThreads, 0, s>>>(p);
 }
-constexpr int64_t kNarrowFrom = 1024;
 template <typename T, class P> void narrow8(Product8Params p, int cus, hipStream_t s) {
   p.tiles_m = (p.channels + 64 * P::WAVES - 1) / (64 * P::WAVES);
   const int32_t parts = std::max(1, std::min(cus * P::kPerCu / p.tiles_m, (p.tokens + 63) / 64));
   product8_narrow_kernel<T, P><<<uint32_t(p.tiles_m) * uint32_t(parts), P::kThreads, 0, s>>>(p);
 }
+// Up to 32 rows by the kernel that reads the weights straight to registers, then small tiles, up to eight for each CU (8192 rows of 2048, 1024 channels: 36 us, large ones 39;
+// 32768: 130 and 83), then narrow rows (32768 rows of 256, 1024 channels: 22.6 us, large tiles 34.7, small ones 41.2; of 1024: 49, 56, 77) and large tiles.
 template <typename T> void product8(const Product8Params& p, int cus, hipStream_t s) {
   if (p.tokens <= kFewTokens) {
     product8_few_kernel<T><<<dim3((p.channels + 15) / 16, (p.tokens + 15) / 16), 64 * kFewWaves, 0, s>>>(p);
     return;
   }
-  if (p.chunks <= 64 && p.tokens > kNarrowFrom) {
-    if (p.chunks <= 8) narrow8<T, Narrow128>(p, cus, s);
-    else if (p.chunks <= 16) narrow8<T, Narrow256>(p, cus, s);
-    else if (p.chunks <= 32) narrow8<T, Narrow512>(p, cus, s);
-    else narrow8<T, Narrow1024>(p, cus, s);
-    return;
-  }
-  const int f = p.tokens <= 1024 ? kSmall : kLarge;
-  if (f == kLarge) launch8<T, Large8>(p, s);
-  else if (f == kMiddle) launch8<T, Middle8>(p, s);
-  else launch8<T, Small8>(p, s);
+  const int64_t small = int64_t((p.channels + 63) / 64) * ((p.tokens + 63) / 64);
+  if (small <= 8 * cus) launch8<T, Small8>(p, s);
+  else if (p.chunks <= 8) narrow8<T, Narrow128>(p, cus, s);
+  else if (p.chunks <= 16) narrow8<T, Narrow256>(p, cus, s);
+  else if (p.chunks <= 32) narrow8<T, Narrow512>(p, cus, s);
+  else if (p.chunks <= 64) narrow8<T, Narrow1024>(p, cus, s);
+  else launch8<T, Large8>(p, s);
 }
 
 int check_side(const lgp_rows8* r) {

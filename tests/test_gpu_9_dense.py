@@ -244,6 +244,14 @@ def test_products_in_8_bits(tokens, width, channels, dtype):
     run_product(tokens, width, channels, dtype, bias=False, pos=slots(tokens, 3), seed=7)
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("tokens,width,channels", [(66_003, 100, 130), (66_003, 128, 200), (66_003, 250, 130), (40_000, 256, 260), (66_003, 500, 130), (66_003, 1000, 130), (66_003, 1040, 130),
+                                                   (33_001, 17, 300)])
+def test_products_in_8_bits_of_batches(tokens, width, channels, dtype):
+    run_product(tokens, width, channels, dtype)
+    run_product(tokens, width, channels, dtype, bias=False, pos=slots(tokens, 3), seed=7)
+
+
 def test_products_in_8_bits_of_the_largest_sums():
     """Every product 127^2, as wide as rows may be: the sum is just below 2^31."""
     L = lgp()
@@ -321,6 +329,29 @@ def test_gated_of_many_tokens_and_of_wide_rows(dtype):
     run_gated(2100, 2048, 1100, dtype, "gelu")
     run_gated(40, 4096, 2000, dtype, "silu")
     run_gated(3, 24, 9000, dtype, "silu")
+
+
+@pytest.mark.parametrize("dtype,act", [(F16, "gelu"), (BF16, "silu")])
+@pytest.mark.parametrize("tokens,width,hidden", [(66_003, 40, 100), (65_600, 64, 9), (66_003, 120, 64), (65_540, 128, 33), (66_003, 256, 100), (40_000, 200, 300), (66_003, 320, 70),
+                                                 (33_000, 512, 130), (66_003, 512, 352), (4000, 136, 1100), (40_010, 1024, 800)])
+def test_gated_of_batches(tokens, width, hidden, dtype, act):
+    """Rows that pass by the weights, and large tiles; rows without a token at the ends, in runs and among others."""
+    run_gated(tokens, width, hidden, dtype, act)
+    pos = slots(tokens, 3)
+    pos[:700] = -1
+    pos[tokens // 2:tokens // 2 + 3000] = -1
+    pos[-70:] = -1
+    run_gated(tokens, width, hidden, dtype, act, pos=pos, apart=8)
+
+
+def test_gated_of_batches_of_few_tokens():
+    """Many rows, of which hardly any have a token."""
+    L = lgp()
+    for width, hidden in ((256, 64), (1024, 1100)):
+        for n in (0, 1, 65):
+            pos = torch.full((70_000,), -1, dtype=torch.int32, device="cuda")
+            pos[torch.arange(n, device="cuda") * 1000 + 37] = 1
+            run_gated(70_000, width, hidden, BF16, "silu", pos=pos)
 
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
