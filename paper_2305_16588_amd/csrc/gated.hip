@@ -18,15 +18,28 @@ struct GatedParams {
 };
 
 // a = act(g) and, for the backward pass, its slope.  silu: g s with s = 1 / (1 + exp(-g)), slope s + a (1 - s).  gelu: g P with P = erfc(-g / sqrt(2)) / 2, slope
-// P + g exp(-g^2 / 2) / sqrt(2 pi).
+// P + g exp(-g^2 / 2) / sqrt(2 pi).  With x = |g| / sqrt(2) the smaller of P and 1 - P is exp(-x^2) t q(t), t = 1 / (1 + 0.36 x): a polynomial through t q(t) = exp(x^2) erfc(x) / 2 at
+// the ten Chebyshev nodes of (0, 1], which is off by at most 5e-8 of it, so that the tail keeps its digits (calling erfcf instead: 32768 rows of 2048 with 8192 hidden, fp16,
+// forward 2588 us).
 template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float g, float& slope) {
   if constexpr (ACT == LGP_SILU) {
     const float s = rcp_fast(1.f + exp2_fast(-kLog2e * g)), a = g * s;
     if (SLOPE) slope = (s + a) - a * s;
     return a;
   } else {
-    const float p = 0.5f * erfcf(-0.70710678118654752440f * g);
-    if (SLOPE) slope = p + g * (0.39894228040143267794f * exp2_fast(-0.5f * kLog2e * g * g));
+    const float t = rcp_fast(1.f + 2.545584413e-01f * fabsf(g)), e = exp2_fast(g * g * (-0.5f * kLog2e));
+    float q = 1.914578963e-02f;
+    q = q * t - 7.248302199e-02f;
+    q = q * t + 7.469616717e-02f;
+    q = q * t - 1.753483407e-02f;
+    q = q * t + 5.528966375e-02f;
+    q = q * t + 6.070376850e-02f;
+    q = q * t + 8.211907949e-02f;
+    q = q * t + 9.495467540e-02f;
+    q = q * t + 1.015546063e-01f;
+    q = q * t + 1.015541227e-01f;
+    const float tail = q * t * e, p = g < 0.f ? tail : 1.f - tail;
+    if (SLOPE) slope = p + g * (0.39894228040143267794f * e);
     return g * p;
   }
 }
