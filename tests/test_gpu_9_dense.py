@@ -315,7 +315,7 @@ def run_gated(tokens, width, hidden, dtype, act, pos=None, seed=1, apart=0, trai
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [F16, BF16])
-@pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
+@pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (5, 264, 300), (8, 1000, 130), (9, 264, 129), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
                                                  (129, 136, 129), (276, 256, 352), (300, 520, 257), (1000, 96, 500), (1025, 256, 683), (1500, 72, 40), (2500, 264, 300), (4097, 64, 96), (5000, 256, 130),
                                                  (6000, 120, 683), (4500, 320, 90)])
 def test_gated_of_every_size(tokens, width, hidden, dtype, act):
@@ -475,6 +475,48 @@ def test_clipping_leaves_a_mark_for_autograd():
     L.clip_gradients([g], 1.0)
     with pytest.raises(RuntimeError, match="modified by an inplace"):
         y.backward()
+
+
+# ---- together
+
+def test_a_training_step_of_the_second_half_of_a_layer():
+    """The residual's addition and norm, the gated pair, the last projection (torch's), the next addition and norm; all gradients, and their clipping.  Along the way from the inputs
+    to a gradient stand at most 14 roundings to fp16, each off by 2^-11 of what it rounds; the norms, the products and the activation's slope (1.13) hand an error on with no
+    more than its share of what they hand on, but for cancellation, for which a factor of 3 is allowed."""
+    L = lgp()
+    T, W, H = 3000, 128, 200
+    pos = slots(T, 1)
+    live = pos >= 0
+    leaf = dict(x=draw((T, W), F16, 2), res=draw((T, W), F32, 3, 2.0), n1=1 + draw((W,), F32, 4, 0.2), n2=1 + draw((W,), F32, 5, 0.2), wg=draw((H, W), F16, 6, W ** -0.5),
+                wu=draw((H, W), F16, 7, W ** -0.5), wd=draw((W, H), F16, 8, H ** -0.5))
+    leaf["x"][~live] = 0
+    a, b = draw((T, W), F16, 9), draw((T, W), F32, 10)
+
+    def step(v, norm, pair):
+        y, total = norm(v["x"], v["res"], v["n1"])
+        y, total = norm(pair(y, v["wg"], v["wu"]) @ v["wd"].t(), total, v["n2"])
+        return y, total
+
+    own = {n: t.clone().requires_grad_() for n, t in leaf.items()}
+    y, total = step(own, lambda x, r, w: L.add_norm(x, r, w, pos=pos), lambda y, g, u: L.gated_linear(y, g, u, pos=pos))
+    torch.autograd.backward([y, total], [a, b])
+
+    def norm64(x, r, w):
+        t = torch.where(live[:, None], x + r, 0.0)
+        return torch.where(live[:, None], t / torch.sqrt((t * t).mean(1, keepdim=True) + 1e-6) * w, 0.0), t
+
+    exact = {n: t.double().requires_grad_() for n, t in leaf.items()}
+    y64, total64 = step(exact, norm64, lambda y, g, u: torch.nn.functional.silu(y @ g.t()) * (y @ u.t()))
+    torch.autograd.backward([y64, total64], [a.double(), b.double()])
+    off = lambda g, w: float((g.detach().double() - w.detach()).norm() / w.detach().norm())  # noqa: E731
+    assert off(y, y64) <= 5 * 3 * 2.0 ** -11 and off(total, total64) <= 4 * 3 * 2.0 ** -11
+    for n in leaf:
+        assert off(own[n].grad, exact[n].grad) <= 14 * 3 * 2.0 ** -11, n
+    grads = [own[n].grad for n in leaf]
+    before = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    assert abs(float(L.clip_gradients(grads, before / 3)) - before) <= 1e-6 * before
+    after = math.sqrt(sum(float((g.double() ** 2).sum()) for g in grads))
+    assert abs(after - before / 3) <= 2.0 ** -11 * before / 3
 
 
 # ---- streams, graphs, repeated runs
