@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(const GatedPa
 }
 
 // Few tokens, backward: the projections' gradients are kept in 32 bits, since hardly any sum would average their rounding, and both products that follow are memory's work: each
-// weight is read, and each of its gradients written, once for eight tokens or all of them. 
+// weight is read, and each of its gradients written, once for eight tokens or all of them.
 struct FewParams {
   const char *w_gate, *w_up, *x;
   int64_t x_bytes;               // of a row
@@ -520,7 +520,9 @@ GatedParams gated_params(const lgp_gated* g) {
 }
 // Where many rows may have no token, those that have one are listed, and the others cost nothing but their zeros.
 bool lists(const lgp_gated* g) { return g->pos && g->tokens > kListFrom && g->tokens * g->x_row < int64_t(1) << 35; }       // places of x are counted in 32 bits, by 16 bytes
-bool few_tokens(const lgp_gated* g) { return g->tokens > 0 && g->tokens <= kFewBack; }
+bool few_tokens(const lgp_gated* g) {
+  return g->tokens > 0 && (g->tokens <= kFewBack || (g->tokens <= 64 && g->tokens * g->hidden <= 16384));
+}
 // Bytes of the list, of the projections' gradients, and of the parts of x's and the weights' gradients, which are not there at once.
 struct Space { size_t list, grads, parts; };
 Space space_of(const lgp_gated* g, bool backward) {
@@ -556,8 +558,9 @@ template <typename T> void forward(int device, const lgp_gated* g, void* h, void
   if (lists(g)) list_tokens<T>(g, p, workspace, h, g->hidden, s);
   gated_by_act<T, false>(g->act, p, compute_units(device), s);
 }
-// Up to eight tokens: the rounding of the projections' gradients to 16 bits would come out whole in the weights' gradients, which are sums over tokens (one token, bf16: 2.7e-3 of
-// dw_up off, where a result rounded once is 1.7e-3 off).  1024 to 4096, bf16: one token 32 us as with tiles, eight tokens 42, nine with tiles 35.
+// Up to eight tokens, and 64 with few hidden elements: the rounding of the projections' gradients to 16 bits would come out whole in the weights' gradients, which are sums over
+// tokens (one token, bf16: 2.7e-3 of dw_up off, where a result rounded once, as here, is 1.7e-3 off; from nine on 1.47 times that at most, in 20 draws).  1024 to 4096, bf16: one
+// token 32 us as with tiles, eight tokens 42, nine with tiles 35.
 template <typename T> void few_backward(const lgp_gated* g, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, hipStream_t s) {
   GatedParams p = gated_params(g);
   p.dh = dh;

@@ -315,7 +315,7 @@ def run_gated(tokens, width, hidden, dtype, act, pos=None, seed=1, apart=0, trai
 
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [F16, BF16])
-@pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (5, 264, 300), (8, 1000, 130), (9, 264, 129), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
+@pytest.mark.parametrize("tokens,width,hidden", [(1, 8, 1), (1, 64, 64), (2, 72, 65), (5, 264, 300), (8, 1000, 130), (9, 264, 129), (64, 72, 256), (64, 72, 257), (12, 256, 2000), (15, 256, 100), (16, 1000, 33), (17, 64, 130), (33, 40, 683), (64, 128, 128), (100, 8, 7),
                                                  (129, 136, 129), (276, 256, 352), (300, 520, 257), (1000, 96, 500), (1025, 256, 683), (1500, 72, 40), (2500, 264, 300), (4097, 64, 96), (5000, 256, 130),
                                                  (6000, 120, 683), (4500, 320, 90)])
 def test_gated_of_every_size(tokens, width, hidden, dtype, act):
