@@ -44,8 +44,8 @@ template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float 
   }
 }
 
-// A tile of both projections, and what becomes of them.  Measured: 32768 rows of 2048 with 8192 hidden, fp16, gelu: 2244 us, 0.98 PFLOP/s of products; with the projections' gradients
-// in place of h 2650 us.  Matrix instructions have half of the cycles; the activation is worked on after the products, and the next stage's rows arrive late (the same
+// A tile of both projections, and what becomes of them.  Measured: 32768 rows of 2048 with 8192 hidden, fp16, gelu: 2200 to 2300 us, 0.98 PFLOP/s of products; with the projections' gradients
+// in place of h 2570 to 2620 us.  Matrix instructions have half of the cycles; the activation is worked on after the products, and the next stage's rows arrive late (the same
 // with rows that are always cached: a tenth less; without any copies: a quarter).
 template <typename T, int ACT, class P, bool BACK>
 __global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams p) {
@@ -344,7 +344,7 @@ __host__ __device__ __forceinline__ int32_t part_of_sum(int32_t sum, int32_t par
 }
 
 // dx = dg Wg + du Wu: A is the weights, across, B the gradients of the projections' results, along.  dWg = dg^T x and dWu = du^T x: A is x, across, and B those
-// gradients, across.  Measured: 32768 rows of 2048 with 8192 hidden, fp16: 1990 to 2045 and 1950 us, 1.08 to 1.13 PFLOP/s; 282624 rows of 256, 30 % left out, 683 hidden, bf16: 222 and
+// gradients, across.  Measured: 32768 rows of 2048 with 8192 hidden, fp16: 1980 to 2040 and 1910 to 1980 us, 1.1 PFLOP/s; 282624 rows of 256, 30 % left out, 683 hidden, bf16: 222 and
 // 231 us, where bytes take 139 each.
 template <typename T, class P>
 __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p) {

@@ -70,12 +70,6 @@ __device__ __forceinline__ int turned(int row) { return int(__brev(uint32_t(row)
 // The order of 32 rows of A that leaves a lane 16 consecutive rows of D.
 __device__ __forceinline__ int in_order(int m) { return (m & ~31) + 16 * (m >> 2 & 1) + 4 * (m >> 3 & 3) + (m & 3); }
 
-// BM x BN of a product by WM x WN waves, each 32 MI x 32 NJ of it.  A stage is CH chunks of the sum: while one is multiplied, STAGES - 1 are on their way to LDS, past the
-// registers.  Every copy is issued whatever there is to copy -- what lies beyond an end is another valid row whose results are not used, or zeros where it
-// is part of a sum -- so a wave knows how many of its loads are under way.
-//
-// The 32 rows of a block of A lie in LDS in an order (or are read in one) that leaves a lane 16 consecutive rows of D: register r of lane l is row 16 (l / 32) + r, so
-// results are written 32 bytes at a time.
 template <int N> using Int = std::integral_constant<int, N>;
 template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F f) {       // f(0) ... f(N - 1), with constants
   if constexpr (I < N) {
@@ -84,6 +78,12 @@ template <int N, int I = 0, typename F> __device__ __forceinline__ void each(F f
   }
 }
 
+// BM x BN of a product by WM x WN waves, each 32 MI x 32 NJ of it.  A stage is CH chunks of the sum: while one is multiplied, STAGES - 1 are on their way to LDS, past the
+// registers.  Every copy is issued whatever there is to copy -- what lies beyond an end is another valid row whose results are not used, or zeros where it
+// is part of a sum -- so a wave knows how many of its loads are under way.
+//
+// The 32 rows of a block of A lie in LDS in an order (or are read in one) that leaves a lane 16 consecutive rows of D: register r of lane l is row 16 (l / 32) + r, so
+// results are written 32 bytes at a time.
 template <typename T, int BM_, int BN_, int WM_, int WN_, int CH_, int STAGES_, bool GATED, bool A_ACROSS, bool B_ACROSS> struct Tiles {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, CH = CH_, STAGES = STAGES_;
   static constexpr int kThreads = 64 * WM * WN, MI = BM / 32 / WM, NJ = BN / 32 / WN;
@@ -471,16 +471,19 @@ template <typename T, bool PAIR> struct Few {
   }
 };
 
-// Which tile a workgroup has: consecutive ones, which go to one XCD, are those of eight tiles of B's rows with one of A's rows, then with the next.
+// Which tile a workgroup has: consecutive ones, which go to one XCD, are those of four tiles of B's rows with one of A's rows, then with the next: the 32 CUs of an XCD work on four by
+// eight tiles at a time (65536 x 4096 with 4096 channels in 8 bits 1155 us; with two 1180, six 1160, eight by four 1222, sixteen 1300; 32768 rows of 2048 with 8192 hidden, a
+// whole step: 8.60, 8.61, 8.67, 8.79 and 9.15 ms).
+constexpr uint32_t kBeside = 4;
 struct Tile { int32_t m, n, part; };
 __device__ __forceinline__ Tile tile_of(uint32_t block, uint32_t blocks, int32_t tiles_m, int32_t tiles_n) {
   const uint32_t piece = piece_of(block, blocks), all = uint32_t(tiles_m) * uint32_t(tiles_n);
   Tile t;
   t.part = int32_t(piece / all);
-  const uint32_t of = piece % all, group = of / (8 * uint32_t(tiles_m)), in = of % (8 * uint32_t(tiles_m));
-  const uint32_t left = uint32_t(tiles_n) - group * 8, wide = left < 8 ? left : 8;
+  const uint32_t of = piece % all, group = of / (kBeside * uint32_t(tiles_m)), in = of % (kBeside * uint32_t(tiles_m));
+  const uint32_t left = uint32_t(tiles_n) - group * kBeside, wide = left < kBeside ? left : kBeside;
   t.m = int32_t(in / wide);
-  t.n = int32_t(group * 8 + in % wide);
+  t.n = int32_t(group * kBeside + in % wide);
   return t;
 }
 

@@ -7,14 +7,13 @@ gated_linear are differentiable.  No gradient passes through rows in 8 bits.
 """
 from __future__ import annotations
 
-import ctypes as C
 import struct
 
 import torch
 from torch.autograd.function import once_differentiable
 
 from .binding import _Gated, _Residual, _Rows8, load_library
-from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _like, _ok, _on, _packer, _ptr, _rows2, _workspace
+from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _ok, _on, _packer, _ptr, _rows2, _workspace
 
 _residual, _rows8, _gated = _packer(_Residual), _packer(_Rows8), _packer(_Gated)
 _ACT = {"silu": 0, "gelu": 1}
