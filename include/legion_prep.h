@@ -516,7 +516,7 @@ typedef struct {
   float eps;
 } lgp_residual;
 
-/* Rows in 8-bit integers: value = values * scales[row]. */
+/* Rows in 8-bit integers, -127 to 127: value = values * scales[row]. */
 typedef struct {
   int64_t tokens;
   int32_t width;

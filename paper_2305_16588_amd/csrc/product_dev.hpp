@@ -328,7 +328,7 @@ template <typename T, int KS_, int WAVES_, bool PAIR> struct Narrow {
     auto chunk_of = [&](int j) __attribute__((always_inline)) { return ((tid + j * kThreads) % CH) ^ (turned((tid + (kStep % 16 ? j * kThreads : 0)) / CH) & kTurn); };
     auto list = [&](int32_t k) __attribute__((always_inline)) {
       if (b.order && wave == 0 && k < n)
-        copy4(b.order + begin + k * kRows, lane * 4, __builtin_amdgcn_readfirstlane(lds_address(s.listed[k % (2 * SLOTS)])));
+        copy4(b.order + begin + k * kRows, min(lane, end - 1 - begin - k * kRows) * 4, __builtin_amdgcn_readfirstlane(lds_address(s.listed[k % (2 * SLOTS)])));
     };
     auto fetch = [&](int32_t k) __attribute__((always_inline)) {
       const uint32_t lds = __builtin_amdgcn_readfirstlane(lds_address(s.rows[k % SLOTS]) + (tid & ~63) * 16);

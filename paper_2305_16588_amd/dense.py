@@ -118,7 +118,7 @@ def add_norm_backward(dy, d_total, total, weight, pos=None, eps: float = 1e-6, s
 
 
 class Rows8:
-    """Rows in 8-bit integers: values (int8[tokens, width rounded up to 16], zeros behind width) times scales (float32[tokens]); of activations, or of the
+    """Rows in 8-bit integers, -127 to 127: values (int8[tokens, width rounded up to 16], zeros behind width) times scales (float32[tokens]); of activations, or of the
     channels of a weight [out, width]."""
 
     def __init__(self, values, scales, width: int, pos=None):

@@ -332,7 +332,7 @@ def test_gated_of_many_tokens_and_of_wide_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype,act", [(F16, "gelu"), (BF16, "silu")])
-@pytest.mark.parametrize("tokens,width,hidden", [(66_003, 40, 100), (65_600, 64, 9), (66_003, 120, 64), (65_540, 128, 33), (66_003, 256, 100), (40_000, 200, 300), (66_003, 320, 70),
+@pytest.mark.parametrize("tokens,width,hidden", [(66_003, 40, 100), (65_600, 64, 9), (66_003, 120, 64), (65_540, 128, 33), (66_003, 256, 100), (40_000, 200, 300), (66_003, 320, 70), (66_020, 264, 60),
                                                  (33_000, 512, 130), (66_003, 512, 352), (4000, 136, 1100), (40_010, 1024, 800)])
 def test_gated_of_batches(tokens, width, hidden, dtype, act):
     """Rows that pass by the weights, and large tiles; rows without a token at the ends, in runs and among others."""
