@@ -13,7 +13,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from .binding import _Gated, _Residual, _Rows8, load_library
-from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _ok, _on, _packer, _ptr, _rows2, _workspace
+from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _new, _ok, _on, _packer, _ptr, _rows2, _workspace
 
 _residual, _rows8, _gated = _packer(_Residual), _packer(_Rows8), _packer(_Gated)
 _ACT = {"silu": 0, "gelu": 1}
@@ -91,8 +91,7 @@ def add_norm(x, residual, weight, pos=None, eps: float = 1e-6, stream=None):
     index, at, kind, rest = _sum(x, residual, weight, pos, eps)
     r = _residual_of(at, x.dtype, kind, rest)
     with _on(index, stream) as on:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        total = x if residual is None else torch.empty(x.shape, dtype=kind, device=x.device)
+        y, total = _new(x), x if residual is None else _new(residual)
         _ok(L.lgp_add_norm(index, r, y.data_ptr(), total.data_ptr(), on))
     return y, total
 
@@ -109,7 +108,7 @@ def add_norm_backward(dy, d_total, total, weight, pos=None, eps: float = 1e-6, s
     with _on(index, stream) as on:
         dy = _plain(dy, total.shape, "dy", dtype, index)
         d_total = None if d_total is None else _plain(d_total, total.shape, "d_total", kind, index)
-        d = torch.empty(total.shape, dtype=kind, device=total.device)
+        d = _new(total)
         dx = d if kind is dtype else torch.empty(total.shape, dtype=dtype, device=total.device)
         dw = torch.empty_like(weight)
         w, size = _workspace(index, total.device, L.lgp_add_norm_workspace, r)
@@ -167,7 +166,7 @@ def add_norm_rows8(x, residual, weight, pos=None, eps: float = 1e-6, stream=None
     r = _residual_of(at, x.dtype, kind, rest)
     with _on(index, stream) as on:
         rows = _new_rows8(*x.shape, pos, index, x.device, rest[1])
-        total = x if residual is None else torch.empty(x.shape, dtype=kind, device=x.device)
+        total = x if residual is None else _new(residual)
         _ok(L.lgp_add_norm_rows8(index, r, rows.c, total.data_ptr(), on))
     return rows, total
 
@@ -248,7 +247,7 @@ def gated_linear_backward(dh, x, w_gate, w_up, act: str = "silu", pos=None, stre
     index, g = _pair(x, w_gate, w_up, act, pos)
     with _on(index, stream) as on:
         dh = _plain(dh, (x.shape[0], w_gate.shape[0]), "dh", x.dtype, index)
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        dx = _new(x)
         dg, du = torch.empty_like(w_gate), torch.empty_like(w_up)
         w, size = _workspace(index, x.device, L.lgp_gated_linear_workspace, g, 1)
         _ok(L.lgp_gated_linear_backward(index, g, dh.data_ptr(), dx.data_ptr(), dg.data_ptr(), du.data_ptr(), _ptr(w), size, on))
