@@ -17,14 +17,15 @@ struct GatedParams {
   void* grads;                  // [tokens][2][pitch]: the gradients of both projections' results, zeros behind hidden and where no token is
 };
 
-// a = act(g) and, for the backward pass, its slope.  silu: g s with s = 1 / (1 + exp(-g)), slope s + a (1 - s).  gelu: g P with P = erfc(-g / sqrt(2)) / 2, slope
+// a = act(g) and, for the backward pass, its slope.  silu: g s with s = 1 / (1 + exp(-g)), slope s + a (1 - s), where s is 1 from g of 17 on: a - a s in
+// place of a (1 - s) would lose it beside an a of 2^24 and more.  gelu: g P with P = erfc(-g / sqrt(2)) / 2, slope
 // P + g exp(-g^2 / 2) / sqrt(2 pi).  With x = |g| / sqrt(2) the smaller of P and 1 - P is exp(-x^2) t q(t), t = 1 / (1 + 0.36 x): a polynomial through t q(t) = exp(x^2) erfc(x) / 2 at
 // the ten Chebyshev nodes of (0, 1], which is off by at most 5e-8 of it, so that the tail keeps its digits (calling erfcf instead: 32768 rows of 2048 with 8192 hidden, fp16,
 // forward 2588 us).
 template <int ACT, bool SLOPE> __device__ __forceinline__ float activated(float g, float& slope) {
   if constexpr (ACT == LGP_SILU) {
     const float s = rcp_fast(1.f + exp2_fast(-kLog2e * g)), a = g * s;
-    if (SLOPE) slope = (s + a) - a * s;
+    if (SLOPE) slope = fmaf(a, 1.f - s, s);
     return a;
   } else {
     const float t = rcp_fast(1.f + 2.545584413e-01f * fabsf(g)), e = exp2_fast(g * g * (-0.5f * kLog2e));

@@ -1,0 +1,66 @@
+"""What a layer has around its attention at the ends of its range: numbers near the types' ends, sums that are known exactly, places beyond 32 bits, and every form of
+the products on streams, in captured graphs and repeated bit by bit."""
+import math
+
+import pytest
+import torch
+
+import dense_common as ref
+from test_gpu_9_dense import BF16, lgp, slots
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- the gated pair, where every number along the way is a power of two or a sum of few bits: results are known exactly, and one token in the wrong place shows
+
+# few tokens, small tiles, large tiles, rows that pass by the weights (all four lengths of the sum); gradients by tiles of every size, with parts of the sum
+FORMS = [(1, 8, 1), (8, 1000, 130), (40, 72, 300), (9, 264, 129), (300, 64, 80), (1025, 256, 683), (4097, 64, 96), (4000, 136, 1100), (66_003, 40, 100), (65_600, 64, 9), (66_003, 120, 64),
+         (66_003, 256, 100), (33_000, 512, 130), (40_010, 1024, 300), (40_010, 1024, 800)]
+
+
+def powers(shape, low, high, seed):
+    """+-2^low ... 2^high, drawn evenly."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    size = torch.randint(low, high + 1, shape, generator=g, device="cuda").double()
+    return torch.exp2(size) * (1 - 2 * torch.randint(0, 2, shape, generator=g, device="cuda").double())
+
+
+def one_hot(tokens, width, dtype, place, size):
+    x = torch.zeros(tokens, width, dtype=dtype, device="cuda")
+    x[torch.arange(tokens, device="cuda"), place] = size
+    return x
+
+
+def run_known(tokens, width, hidden, dtype, act, size, gate, up, grad, pos=None, share=1.0, seed=1):
+    """Token t is `size` at one place.  Gates are +-size 2^gate, at which an activation is its argument or zero and its slope 1 or 0; the other
+    projection's results are +-size 2^up and gradients of h +-2^grad, of `share` of the tokens.  Every product and every sum of them is exact in 32 bits."""
+    L = lgp()
+    place = torch.arange(tokens, device="cuda") * 7 % width
+    x, dh = one_hot(tokens, width, dtype, place, size), powers((tokens, hidden), *grad, seed).to(dtype)
+    if share < 1:
+        dh[torch.rand(tokens, generator=torch.Generator(device="cuda").manual_seed(seed + 3), device="cuda") >= share] = 0
+    wg, wu = powers((hidden, width), *gate, seed + 1).to(dtype), powers((hidden, width), *up, seed + 2).to(dtype)
+    live = ref.live_rows(tokens, pos, "cuda")[:, None]
+    g, u = size * wg.double().t()[place], size * wu.double().t()[place]
+    on, d = (g > 0) & live, torch.where(live, dh.double(), 0.0)
+    a = torch.where(on, g, 0.0)
+    dg, du = torch.where(on, d * u, 0.0), d * a
+    X = torch.where(live, x.double(), 0.0)
+    want = dict(h=a * u, dx=dg @ wg.double() + du @ wu.double(), dw_gate=dg.t() @ X, dw_up=du.t() @ X)
+    if pos is not None:
+        x[pos < 0], dh[pos < 0] = math.nan, math.nan
+    got = dict(h=L.gated_linear(x, wg, wu, act=act, pos=pos))
+    got.update(zip(("dx", "dw_gate", "dw_up"), L.gated_linear_backward(dh, x, wg, wu, act=act, pos=pos)))
+    for name, w in want.items():
+        # all of them have less than 24 bits: fp32 holds them, and they are rounded once from there
+        assert torch.equal(w.float().double(), w), name
+        assert torch.isfinite(w.to(dtype)).all(), name
+        assert torch.equal(got[name], w.float().to(dtype)), (name, int((got[name] != w.float().to(dtype)).sum()))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("tokens,width,hidden", FORMS)
+def test_gated_of_gates_beyond_24_bits(tokens, width, hidden, act):
+    """From 2^24 on 1 + g is g or its neighbour, but the activation's slope is 1."""
+    run_known(tokens, width, hidden, BF16, act, 2.0 ** 13, gate=(11, 13), up=(-13, -12), grad=(0, 1))
+    run_known(tokens, width, hidden, BF16, act, 2.0 ** 13, gate=(11, 13), up=(-13, -12), grad=(0, 1), pos=slots(tokens, 3), seed=7)
