@@ -2,6 +2,8 @@
 #include "product_dev.hpp"
 
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 namespace lgp {
 namespace layer {
@@ -15,7 +17,9 @@ struct GatedParams {
   void* h;
   const void* dh;
   void* grads;                  // [tokens][2][pitch]: the gradients of both projections' results, zeros behind hidden and where no token is
+  const float* lift;            // fp16: what those are multiplied by, and its reciprocal; see lift_kernel
 };
+template <typename T> constexpr bool kLifted = std::is_same_v<T, f16>;
 
 // a = act(g) and, for the backward pass, its slope.  silu: g s with s = 1 / (1 + exp(-g)), slope s + a (1 - s), where s is 1 from g of 17 on: a - a s in
 // place of a (1 - s) would lose it beside an a of 2^24 and more.  gelu: g P with P = erfc(-g / sqrt(2)) / 2, slope
@@ -59,6 +63,8 @@ __global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams
   Operand x = p.x;
   x.rows = tokens;
   P::run(lds, p.w, x, f0, t0, 0, p.width_chunks * 8, acc);
+  float lift = 1.f;
+  if constexpr (BACK && kLifted<T>) lift = p.lift[0];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % P::WM, wn = wave / P::WM;
 #pragma unroll
   for (int j = 0; j < P::NJ; ++j) {
@@ -80,6 +86,7 @@ __global__ __launch_bounds__(P::kThreads, 2) void gated_kernel(const GatedParams
           for (int k = 0; k < 8; ++k) {
             float slope;
             const float a = activated<ACT, true>(acc[i][j][r0 + k], slope);
+            if (kLifted<T>) dh[k] *= lift;
             y[k] = live && k < n ? dh[k] * acc[i + P::MI / 2][j][r0 + k] * slope : 0.f;
             z[k] = live && k < n ? dh[k] * a : 0.f;
           }
@@ -103,6 +110,7 @@ template <typename T, int ACT, bool BACK> struct NarrowOut {
   const GatedParams& p;
   int32_t f, end, lane;              // the lane's first hidden element; the end of the workgroup's rows
   bool whole;                        // in all lanes: 16 hidden elements are there
+  float lift;
   int32_t row[4], token[4];          // of the list, and of memory
   vec8<T> dh[2], y, z;               // the gradients of h are on their way as soon as those before them are used
   float held_y, held_z;
@@ -141,7 +149,7 @@ template <typename T, int ACT, bool BACK> struct NarrowOut {
     const float a = activated<ACT, BACK>(acc[0][R], slope);
     if constexpr (BACK) {
       if (R == 0 && !whole) shift();
-      const float d = float(dh[i][k]);           // zero behind hidden, and so are the results
+      const float d = kLifted<T> ? float(dh[i][k]) * lift : float(dh[i][k]);           // zero behind hidden, and so are the results
       add<k>(y, held_y, d * acc[1][R] * slope);
       add<k>(z, held_z, d * a);
       if (k == 7) {
@@ -179,7 +187,7 @@ __global__ __launch_bounds__(P::kThreads, P::kPerCu * P::WAVES / 4) void gated_n
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // waves behind the last hidden element do what those before them do
   const int32_t own = min(f0 + 32 * __builtin_amdgcn_readfirstlane(wave), ((BACK ? p.pitch : p.hidden) - 1) / 32 * 32);
-  NarrowOut<T, ACT, BACK> out = {p, own + 16 * (lane >> 5), end, lane, own + 32 <= p.hidden};
+  NarrowOut<T, ACT, BACK> out = {p, own + 16 * (lane >> 5), end, lane, own + 32 <= p.hidden, BACK && kLifted<T> ? p.lift[0] : 1.f};
   P::run(lds, p.w, p.x, own, begin, end, out);
 }
 
@@ -223,6 +231,85 @@ __global__ __launch_bounds__(256) void list_kernel(const int32_t* pos, int32_t t
       for (int32_t c = 8 * lane; c < cols; c += 512) write_row(zeros + row * cols + c, cols - c, nothing);
     }
   }
+}
+
+// fp16, backward.  The gradients of the projections' results are kept in 16 bits between the products, whose range is that of their inputs and results but not theirs: dh u
+// act'(g) may pass 65504 or vanish below 2^-25 where dx and dW do neither.  All of them are lifted by one power of two, which both products take back from their sums:
+// |dg| <= 1.13 |dh| |x| |w_up| and |du| <= |dh| |x| |w_gate| (|x|, |w|: norms of rows), so with B the largest |dh| |x| of a token times the largest |w| they end below
+// 2^15, whatever they are.  The bound is some 2^3 beyond the largest, of 2^30 that fp16 has; what is below B 2^-29 is off by up to B 2^-39.  bf16 has the range.  Numbers that are not finite
+// spoil their own rows and are left out.  Sixteen lanes read a row; bound by bytes.  Measured: 32768 rows of 2048 with 8192 hidden
+// 160 us, 4.6 TB/s; 282624 of 256 with 683 hidden, 30 % left out, 137 us, 2.7 TB/s (odd rows); 300 rows 4.7, and 1.6 to 4.8 us for the power of two.
+constexpr uint32_t kBoundGroups = 2048;
+struct BoundParams {
+  const char *x, *w_gate, *w_up;
+  int64_t x_bytes;               // of a row
+  const f16* dh;
+  const int32_t* pos;
+  int32_t tokens, width, hidden;
+  float* partial;                // [2][workgroup]: of tokens, and of the weights' squares
+};
+__device__ __forceinline__ void finite8(const f16* p, int n, float* x) {
+  read_row(p, n, x);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.f;
+}
+__device__ __forceinline__ float group_max(float x, float* lds) {        // over 16 lanes each of the workgroup's sixteen groups, in all threads; no number is negative
+  if ((threadIdx.x & 15) == 0) lds[threadIdx.x >> 4] = x;
+  __syncthreads();
+  x = lds[0];
+#pragma unroll
+  for (int i = 1; i < 16; ++i) x = fmaxf(x, lds[i]);
+  return x;
+}
+__global__ __launch_bounds__(256) void bound_kernel(const BoundParams p) {
+  __shared__ float lds[2][16];
+  const int lane = threadIdx.x & 15;
+  float of_tokens = 0.f, of_weights = 0.f;
+  for (int32_t r = int32_t(blockIdx.x) * 16 + (threadIdx.x >> 4); r < p.tokens + 2 * p.hidden; r += int32_t(gridDim.x) * 16) {
+    const bool token = r < p.tokens;
+    if (token && p.pos && p.pos[r] < 0) continue;
+    const int32_t f = r - p.tokens;
+    const char* row = token ? p.x + r * p.x_bytes : f < p.hidden ? p.w_gate + int64_t(f) * p.width * 2 : p.w_up + int64_t(f - p.hidden) * p.width * 2;
+    float squares = 0.f, most = 0.f;
+#pragma unroll 4
+    for (int32_t c = 8 * lane; c < p.width; c += 128) {
+      float x[8];
+      finite8(reinterpret_cast<const f16*>(row) + c, 8, x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) squares += x[i] * x[i];
+    }
+    squares = lanes_sum<16>(squares);
+    if (token) {
+#pragma unroll 4
+      for (int32_t c = 8 * lane; c < p.hidden; c += 128) {
+        float x[8];
+        finite8(p.dh + int64_t(r) * p.hidden + c, p.hidden - c, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = fmaxf(most, x[i]);
+      }
+      most = __builtin_bit_cast(float, lanes_max<16>(__builtin_bit_cast(uint32_t, most)));
+      of_tokens = fmaxf(of_tokens, most * sqrtf(squares));
+    } else {
+      of_weights = fmaxf(of_weights, squares);
+    }
+  }
+  of_tokens = group_max(of_tokens, lds[0]);
+  of_weights = group_max(of_weights, lds[1]);
+  if (threadIdx.x == 0) p.partial[blockIdx.x] = of_tokens, p.partial[gridDim.x + blockIdx.x] = of_weights;
+}
+// lift[0]: the power of two, lift[1]: its reciprocal.
+__global__ __launch_bounds__(256) void lift_kernel(const float* partial, int32_t groups, float* lift) {
+  __shared__ float lds[2][16];
+  float x[2] = {};
+#pragma unroll 8
+  for (int32_t i = threadIdx.x; i < groups; i += 256)
+#pragma unroll
+    for (int q = 0; q < 2; ++q) x[q] = fmaxf(x[q], partial[q * groups + i]);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) x[q] = group_max(__builtin_bit_cast(float, lanes_max<16>(__builtin_bit_cast(uint32_t, x[q]))), lds[q]);
+  const float bound = 1.2f * x[0] * sqrtf(x[1]);               // 1.13, and the rounding of the sums
+  const int up = bound > 0.f ? 14 - (int(__builtin_bit_cast(uint32_t, bound) >> 23) - 127) : 0;
+  if (threadIdx.x == 0) lift[0] = ldexpf(1.f, up), lift[1] = ldexpf(1.f, -up);
 }
 
 // Few tokens: a thread has one element of h.  Measured: one token, 1024 to 4096, bf16: 4.8 us on the device, 3.5 TB/s of weights.
@@ -337,6 +424,7 @@ struct GradParams {
   int32_t tiles_m, tiles_n, parts;
   void *out, *second;
   float* partial;               // [part][rows][cols], of rows that there are
+  const float* lift;            // as in GatedParams; NULL: nothing was multiplied
 };
 
 __host__ __device__ __forceinline__ int32_t part_of_sum(int32_t sum, int32_t parts) {       // places of a part: whole stages
@@ -365,6 +453,8 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
   floatx16 acc[P::MI][P::NJ] = {};
   const int32_t each = part_of_sum(sum, p.parts), begin = t.part * each, end = min(begin + each, sum);
   P::run(lds, a, b, c0, row0, begin, end, acc);
+  float drop = 1.f;
+  if (kLifted<T> && p.lift) drop = p.lift[1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave % P::WM, wn = wave / P::WM;
 #pragma unroll
   for (int j = 0; j < P::NJ; ++j) {
@@ -392,7 +482,7 @@ __global__ __launch_bounds__(P::kThreads, 2) void grad_kernel(const GradParams p
         if (c >= p.cols) continue;
         float y[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) y[k] = live ? acc[i][j][r0 + k] : 0.f;
+        for (int k = 0; k < 8; ++k) y[k] = live ? (kLifted<T> ? acc[i][j][r0 + k] * drop : acc[i][j][r0 + k]) : 0.f;
         if (p.parts > 1) write_row(p.partial + (int64_t(t.part) * (p.hidden ? 2 * int64_t(p.hidden) : p.rows) + there) * p.cols + c, 8, y);
         else write_row(out + int64_t(row) * p.cols + c, 8, y);
       }
@@ -524,8 +614,8 @@ bool lists(const lgp_gated* g) { return g->pos && g->tokens > kListFrom && g->to
 bool few_tokens(const lgp_gated* g) {
   return g->tokens > 0 && (g->tokens <= kFewBack || (g->tokens <= 64 && g->tokens * g->hidden <= 16384));
 }
-// Bytes of the list, of the projections' gradients, and of the parts of x's and the weights' gradients, which are not there at once.
-struct Space { size_t list, grads, parts; };
+// Bytes of the list, of the lift, of the projections' gradients, and of the parts of x's and the weights' gradients, which are not there at once.
+struct Space { size_t list, lift, grads, parts; };
 Space space_of(const lgp_gated* g, bool backward) {
   const int32_t pitch = pitch_of(g->hidden);
   Space s = {};
@@ -537,11 +627,12 @@ Space space_of(const lgp_gated* g, bool backward) {
     return s;
   }
   const GradShape x = shape_x(g, pitch), w = shape_w(g, pitch);
+  if (g->dtype == LGP_F16 && g->tokens) s.lift = (64 + 2 * kBoundGroups) * sizeof(float);
   s.grads = size_t(g->tokens) * 2 * pitch * 2;
   s.parts = std::max(x.parts > 1 ? size_t(x.parts) * g->tokens * g->width * 4 : 0, w.parts > 1 ? size_t(w.parts) * 2 * g->hidden * g->width * 4 : 0);
   return s;
 }
-size_t bytes_of(const Space& s) { return s.list + s.grads + s.parts; }
+size_t bytes_of(const Space& s) { return s.list + s.lift + s.grads + s.parts; }
 
 // Lists tokens, for `p` too, and fills the other rows of `zeros`.
 template <typename T> void list_tokens(const lgp_gated* g, GatedParams& p, void* workspace, void* zeros, int32_t cols, hipStream_t s) {
@@ -553,13 +644,20 @@ template <typename T> void list_tokens(const lgp_gated* g, GatedParams& p, void*
   p.count = counts + groups;
   p.pos = nullptr;
 }
+// Finds the lift of the projections' gradients.
+const float* lift_of(const lgp_gated* g, const GatedParams& p, const void* dh, float* space, hipStream_t s) {
+  const uint32_t groups = uint32_t(std::min<int64_t>((g->tokens + 2 * g->hidden + 15) / 16, kBoundGroups));
+  bound_kernel<<<groups, 256, 0, s>>>(BoundParams{p.x.first, p.w.first, p.w.second, p.x.row_bytes, static_cast<const f16*>(dh), g->pos, p.tokens, g->width, g->hidden, space + 64});
+  lift_kernel<<<1, 256, 0, s>>>(space + 64, int32_t(groups), space);
+  return space;
+}
 template <typename T> void forward(int device, const lgp_gated* g, void* h, void* workspace, hipStream_t s) {
   GatedParams p = gated_params(g);
   p.h = h;
   if (lists(g)) list_tokens<T>(g, p, workspace, h, g->hidden, s);
   gated_by_act<T, false>(g->act, p, compute_units(device), s);
 }
-// Up to eight tokens, and 64 with few hidden elements: the rounding of the projections' gradients to 16 bits would come out whole in the weights' gradients, which are sums over
+// Up to eight tokens, and 64 with few hidden elements, want no lift either: the rounding of the projections' gradients to 16 bits would come out whole in the weights' gradients, which are sums over
 // tokens (one token, bf16: 2.7e-3 of dw_up off, where a result rounded once, as here, is 1.7e-3 off; from nine on 1.47 times that at most, in 20 draws).  1024 to 4096, bf16: one
 // token 32 us as with tiles, eight tokens 42, nine with tiles 35.
 template <typename T> void few_backward(const lgp_gated* g, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, hipStream_t s) {
@@ -582,12 +680,13 @@ template <typename T> void backward(int device, const lgp_gated* g, const void* 
   if (few_tokens(g)) return few_backward<T>(g, dh, dx, dw_gate, dw_up, workspace, s);
   GatedParams p = gated_params(g);
   const Space space = space_of(g, true);
-  char* grads = static_cast<char*>(workspace) + space.list;
+  char* grads = static_cast<char*>(workspace) + space.list + space.lift;
   float* partial = reinterpret_cast<float*>(grads + space.grads);
   p.dh = dh;
   p.grads = grads;
   const Operand of_grads = {grads, nullptr, int64_t(p.pitch) * 4, p.tokens, p.pitch / 4, 1 << 30, nullptr, nullptr};
   if (p.tokens) {
+    if (kLifted<T>) p.lift = lift_of(g, p, dh, reinterpret_cast<float*>(static_cast<char*>(workspace) + space.list), s);
     if (lists(g)) list_tokens<T>(g, p, workspace, dx, g->width, s);
     gated_by_act<T, true>(g->act, p, compute_units(device), s);
     GradParams d = {};
@@ -602,6 +701,7 @@ template <typename T> void backward(int device, const lgp_gated* g, const void* 
     d.sum = 2 * p.pitch;
     d.out = dx;
     d.partial = partial;
+    d.lift = p.lift;
     const GradShape shape = shape_x(g, p.pitch);
     if (shape.form == kLarge) launch_grad<T, typename F::LargeX>(d, shape, g->pos, s);
     else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleX>(d, shape, g->pos, s);
@@ -620,6 +720,7 @@ template <typename T> void backward(int device, const lgp_gated* g, const void* 
   d.out = dw_gate;
   d.second = dw_up;
   d.partial = partial;
+  d.lift = p.lift;
   const GradShape shape = shape_w(g, p.pitch);
   if (shape.form == kLarge) launch_grad<T, typename F::LargeW>(d, shape, nullptr, s);
   else if (shape.form == kMiddle) launch_grad<T, typename F::MiddleW>(d, shape, nullptr, s);

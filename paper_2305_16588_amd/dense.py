@@ -242,7 +242,10 @@ def gated_linear(x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
 
 
 def gated_linear_backward(dh, x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
-    """Gradients (dx, dw_gate, dw_up) of gated_linear, in the type of x, from that of its result; the other arguments are what it was given."""
+    """Gradients (dx, dw_gate, dw_up) of gated_linear, in the type of x, from that of its result; the other arguments are what it was given.
+
+    Sums are in 32 bits.  The gradients of both projections' results are rounded to the type of x between the products (not for up to 8 tokens, or 64 with few hidden
+    elements); float16's are lifted by a power of two for that, so that they may be beyond its range."""
     L = load_library()
     index, g = _pair(x, w_gate, w_up, act, pos)
     with _on(index, stream) as on:

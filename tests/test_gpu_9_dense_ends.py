@@ -6,7 +6,8 @@ import pytest
 import torch
 
 import dense_common as ref
-from test_gpu_9_dense import BF16, lgp, slots
+from layer_common import check
+from test_gpu_9_dense import BF16, F16, draw, lgp, slots
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +65,59 @@ def test_gated_of_gates_beyond_24_bits(tokens, width, hidden, act):
     """From 2^24 on 1 + g is g or its neighbour, but the activation's slope is 1."""
     run_known(tokens, width, hidden, BF16, act, 2.0 ** 13, gate=(11, 13), up=(-13, -12), grad=(0, 1))
     run_known(tokens, width, hidden, BF16, act, 2.0 ** 13, gate=(11, 13), up=(-13, -12), grad=(0, 1), pos=slots(tokens, 3), seed=7)
+
+
+@pytest.mark.parametrize("tokens,width,hidden", FORMS)
+def test_gated_of_fp16_gradients_far_below_its_smallest(tokens, width, hidden):
+    """The gradients of a gate are 2^-26 and 2^-25, neither of which fp16 holds; those of x and the weights it does."""
+    for pos in (None, slots(tokens, 3)):
+        run_known(tokens, width, hidden, F16, "silu", 8.0, gate=(4, 5), up=(-16, -16), grad=(-13, -12), pos=pos)
+
+
+@pytest.mark.parametrize("tokens,width,hidden", FORMS)
+def test_gated_of_fp16_gradients_beyond_its_largest(tokens, width, hidden):
+    """The gradient of a gate is 2^19 half of the time, beyond fp16; those of x and the weights are not.  Gates are zero, where silu's slope is 1/2."""
+    L = lgp()
+    half = width // 2
+    for pos in (None, slots(tokens, 3)):
+        live = ref.live_rows(tokens, pos, "cuda")[:, None]
+        place = torch.arange(tokens, device="cuda") * 7 % half
+        x, dh = one_hot(tokens, width, F16, place, 2.0 ** -9), powers((tokens, hidden), 13, 14, 1).to(F16)
+        dh[torch.rand(dh.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda") > 1 / 16] = 0
+        wg, wu = powers((hidden, width), -10, -9, 3).to(F16), powers((hidden, width), 14, 15, 4).to(F16)
+        wg[:, :half] = 0
+        dg = torch.where(live, dh.double(), 0.0) * 2.0 ** -9 * wu.double().t()[place] / 2
+        want = dict(dx=dg @ wg.double(), dw_gate=dg.t() @ torch.where(live, x.double(), 0.0), dw_up=torch.zeros(hidden, width, dtype=torch.float64, device="cuda"))
+        if pos is not None:
+            x[pos < 0], dh[pos < 0] = math.nan, math.nan
+        for (name, w), got in zip(want.items(), L.gated_linear_backward(dh, x, wg, wu, pos=pos)):
+            assert torch.equal(w.float().double(), w) and torch.isfinite(w.half()).all(), name
+            assert torch.equal(got, w.half()), name
+
+
+@pytest.mark.parametrize("tokens", [8, 9, 64, 65, 300, 4097])
+def test_gated_of_fp16_keeps_its_error_at_every_size_of_gradients(monkeypatch, tokens):
+    """Gradients of h from 2^-20 to 2^12 and a row of zeros: but for results below fp16's smallest, errors are those of roundings by 2^-11.  The gradients of the projections'
+    results are lifted by a power of two, and what is 2^-29 of the largest that they might be, |dh| |x| |w|, is off by 2^-39 of it."""
+    L = lgp()
+    x, wg, wu = draw((tokens, 96), F16, 1, 0.1), draw((200, 96), F16, 2, 0.1), draw((200, 96), F16, 3, 0.1)
+    dh = draw((tokens, 200), F16, 4, 0.25)
+    dh[3] = 0
+    monkeypatch.setitem(ref.TINY, F16, 0.0)
+    norm = max(float(w.double().norm(dim=1).max()) for w in (wg, wu))
+    for power in (-18, -10, 0, 8):
+        d = (dh.double() * 2.0 ** power).half()
+        want = ref.gated(x, wg, wu, "silu", None, d)
+        low = 2.0 ** -39 * 1.2 * float((d.abs().amax(1).double() * x.double().norm(dim=1)).max()) * norm
+        more = dict(dx=low * (wg.double().abs() + wu.double().abs()).sum(0), dw_gate=low * x.double().abs().sum(0), dw_up=low * x.double().abs().sum(0))
+        for name, got in zip(("dx", "dw_gate", "dw_up"), L.gated_linear_backward(d, x, wg, wu)):
+            val, tol = want[name]
+            check(got, (val, tol + more[name] + 2.0 ** -25), (name, power))
+    clean = L.gated_linear_backward(dh, x, wg, wu)[0]
+    for bad in (math.inf, math.nan):
+        d = dh.clone()
+        d[5, 7] = bad
+        dx, dg, _ = L.gated_linear_backward(d, x, wg, wu)
+        odd = torch.arange(tokens, device="cuda") == 5
+        assert torch.equal(dx[~odd], clean[~odd]) and not torch.isfinite(dx[5]).any() and not torch.isfinite(dg[7]).any()
+        assert torch.isfinite(dg[torch.arange(200, device="cuda") != 7]).all()
