@@ -3,7 +3,7 @@ serving, the gated pair of projections, and the clipping of gradients (argument 
 
 As in layer.py: arguments that make no sense raise LegionPrepError before anything is launched, results and workspaces are allocated for the stream that the
 kernels run on, and a negative entry of pos (int32[tokens]) says that a row holds no token: whatever it holds, its results are zeros, and it counts for nothing.  add_norm and
-gated_linear are differentiable.  No gradient passes through rows in 8 bits.
+gated_linear are differentiable, but for forward-mode derivatives, which are refused.  No derivative passes through rows in 8 bits, a norm of gradients or clipping.
 """
 from __future__ import annotations
 
@@ -13,7 +13,7 @@ import torch
 from torch.autograd.function import once_differentiable
 
 from .binding import _Gated, _Residual, _Rows8, load_library
-from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _new, _ok, _on, _packer, _ptr, _rows2, _workspace
+from .layer import _DTYPE, _ECAPACITY, _bad, _ints, _new, _no_tangents, _ok, _on, _packer, _ptr, _rows2, _workspace
 
 _residual, _rows8, _gated = _packer(_Residual), _packer(_Rows8), _packer(_Gated)
 _ACT = {"silu": 0, "gelu": 1}
@@ -83,6 +83,7 @@ def add_norm(x, residual, weight, pos=None, eps: float = 1e-6, stream=None):
     x [tokens, width] (float32, float16 or bfloat16, width up to 16384, values of a row side by side), residual like x, in the type of x or in float32, weight
     float32[width].  total has the type of the residual and y that of x; y is the norm of the total as it is rounded.  Without a residual (None) total is x
     itself."""
+    _no_tangents(x, residual, weight)
     if (x.requires_grad or weight.requires_grad or (residual is not None and residual.requires_grad)) and torch.is_grad_enabled():
         with _on(x.get_device(), stream):
             y, total = _AddNorm.apply(x, residual, weight, pos, eps)
@@ -226,6 +227,7 @@ def gated_linear(x, w_gate, w_up, act: str = "silu", pos=None, stream=None):
 
     x [tokens, width] and the weights [hidden, width]: float16 or bfloat16, width a multiple of 8.  act: "silu" or "gelu" (of the error function).  For its
     gradients nothing but x and the weights is kept."""
+    _no_tangents(x, w_gate, w_up)
     if (x.requires_grad or w_gate.requires_grad or w_up.requires_grad) and torch.is_grad_enabled():
         with _on(x.get_device(), stream):
             return _GatedLinear.apply(x, w_gate, w_up, act, pos)

@@ -2,8 +2,8 @@
 held in 8 bits (argument checks and marshalling only; the kernels are the library's).
 
 Arguments that make no sense raise LegionPrepError before anything is launched.  Results and workspaces are allocated for the stream
-that the kernels run on.  attend and norm_rotate are differentiable: where a gradient is wanted of an input, their results carry it.  Packed
-activations are what a backward pass keeps, and no gradient passes through them.
+that the kernels run on.  attend and norm_rotate are differentiable: where a gradient is wanted of an input, their results carry it; forward-mode
+derivatives are refused.  Packed activations are what a backward pass keeps, and no gradient passes through them.
 """
 from __future__ import annotations
 
@@ -11,6 +11,7 @@ import ctypes as C
 import struct
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from .binding import LegionPrepError, _Attention, _Documents, _Heads, _Packed, _raw_stream, load_library
@@ -38,6 +39,12 @@ def _bad(text: str) -> LegionPrepError:
 def _ok(st: int):
     if st != 0:
         raise LegionPrepError(st, load_library().lgp_strerror(st).decode())
+
+
+def _no_tangents(*tensors):
+    """Forward-mode derivatives need no requires_grad and would be lost without a word."""
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise _bad("forward-mode derivatives are not computed")
 
 
 class _Here:
@@ -190,6 +197,7 @@ def attend(q, k, v, docs: Documents, slopes=None, cap: float = 0.0, scale: float
     given.  out is like q, end to end; lse (float32[q_rows, heads]) is the logarithm of the sum of exp(score).  Queries without keys and rows
     without tokens get zeros and -inf.  rest: also return what the rounding of out took off, for attend_backward.  Gradients pass through out, not
     through lse or rest."""
+    _no_tangents(q, k, v, slopes)
     if (q.requires_grad or k.requires_grad or v.requires_grad or (slopes is not None and slopes.requires_grad)) and torch.is_grad_enabled():
         with _on(docs.index, stream):
             out, lse, left = _Attend.apply(q, k, v, slopes, docs, cap, scale)
@@ -280,6 +288,7 @@ def norm_rotate(q, k, q_weight, k_weight, pos=None, table=None, eps: float = 1e-
     """RMS norm of every head of q [tokens, heads, dim] and k [tokens, kv_heads, dim] with weights (float32[dim]), and the rotation of its first
     table.shape[1] elements by the token's position (rotation_table); new tensors (q, k), rows end to end.  dim: a multiple of 8 up to 256.
     Rows of a negative pos have no token and become zeros; those of a position beyond the table become NaN."""
+    _no_tangents(q, k, q_weight, k_weight)
     if (q.requires_grad or k.requires_grad or q_weight.requires_grad or k_weight.requires_grad) and torch.is_grad_enabled():
         with _on(q.get_device(), stream):
             return _NormRotate.apply(q, k, q_weight, k_weight, pos, table, eps)
