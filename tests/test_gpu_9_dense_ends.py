@@ -7,7 +7,7 @@ import torch
 
 import dense_common as ref
 from layer_common import check
-from test_gpu_9_dense import BF16, F16, draw, lgp, slots
+from test_gpu_9_dense import BF16, F16, F32, draw, lgp, slots
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,33 @@ def test_gated_of_fp16_keeps_its_error_at_every_size_of_gradients(monkeypatch, t
         odd = torch.arange(tokens, device="cuda") == 5
         assert torch.equal(dx[~odd], clean[~odd]) and not torch.isfinite(dx[5]).any() and not torch.isfinite(dg[7]).any()
         assert torch.isfinite(dg[torch.arange(200, device="cuda") != 7]).all()
+
+
+# ---- gradients' clipping
+
+def rounded_once(x, dtype):
+    """Numbers of 64 bits as the nearest of `dtype`, ties to even, in whole numbers of its last places."""
+    bits, low = {F16: (11, -24), BF16: (8, -133), F32: (24, -149)}[dtype]
+    step = torch.exp2((torch.frexp(x.abs())[1] - bits).clamp(min=low).double())
+    return torch.round(x / step) * step
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16, F32])
+def test_clipped_gradients_are_rounded_once(dtype):
+    """Every positive number of the type below 2^14 (fp32: many), by factors that are known exactly: the norm is a power of two, which one gradient has almost alone."""
+    L = lgp()
+    if dtype is F32:
+        g = torch.rand(200_000, generator=torch.Generator().manual_seed(1)).cuda()
+    else:
+        g = torch.arange(1, 1 << 15).to(torch.int16).view(dtype)
+        g = g[torch.isfinite(g) & (g < 2.0 ** 14)].cuda()
+    whole = 2.0 ** 60                            # beside it all other squares, below 2^28 each and 2^43 together, are less than half of a place of 2^120
+    first = torch.full((1,), whole, device="cuda")
+    off = 0
+    for i in range(40):
+        most = whole * (1 - math.ldexp(1 + 977 * i, -17))          # the factor has 17 bits, so products with numbers of 24 are exact in 64
+        out = [torch.empty_like(first), torch.empty_like(g)]
+        assert float(L.clip_gradients([first, g], most, out=out)) == whole and float(out[0]) == most
+        want = rounded_once(g.double() * (most / whole), dtype)
+        off += int((out[1].double() != want).sum())
+    assert off == 0
