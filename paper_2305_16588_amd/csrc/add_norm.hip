@@ -42,6 +42,11 @@ template <int L, int N> __device__ __forceinline__ void row_sums(float* x, float
   }
 }
 
+// Squares pass the range of 32 bits from 2^64 on and lose digits below 2^-63, where the norm does neither: a row whose mean square (with eps) says so is multiplied by a power of two
+// in the registers, and its sums are taken again.  Infinities and NaN come here too, and stay.
+__device__ __forceinline__ bool out_of_range(float mean) { return !(mean <= 3.402823466e+38f) || mean < 0x1p-100f; }
+__device__ __forceinline__ float into_range(float mean) { return mean < 1.f ? 0x1p+100f : 0x1p-80f; }
+
 // L lanes have a row, each of them every L-th eight elements, C of them: a row is read once and stays in registers, and a wave's loads are whole
 // lines.  The sum of squares, the root and the products are in 32 bits; the total is rounded first, so that the backward pass, which reads it, has the
 // gradients of what was computed.  Bound by bytes.  Measured: 400000 rows of 1024, fp16 with a residual in fp32: 855 us, 5.7 TB/s; 282624 rows of
@@ -87,7 +92,19 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void add_norm_kernel(const AddPa
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[0] += t[c][i] * t[c][i];
     row_sums<L, 1>(sum, lds, 0);
-    const float r = live ? 1.f / sqrtf(sum[0] / float(p.width) + p.eps) : 0.f;
+    float mean = sum[0] / float(p.width) + p.eps;
+    if (live && out_of_range(mean)) {          // in all lanes of a row
+      const float by = into_range(mean);
+      sum[0] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[c][i] *= by, sum[0] += t[c][i] * t[c][i];
+      if constexpr (L > 64) __syncthreads();
+      row_sums<L, 1>(sum, lds, 0);
+      mean = sum[0] / float(p.width) + p.eps * by * by;
+    }
+    const float r = live ? 1.f / sqrtf(mean) : 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = 8 * (c * L + c0), n = in ? p.width - at : 0;
@@ -95,7 +112,7 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void add_norm_kernel(const AddPa
       float w[8];
       read_row(p.weight + at, n, w);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t[c][i] *= r * w[i];
+      for (int i = 0; i < 8; ++i) t[c][i] = t[c][i] * r * w[i];
       if (MODE == kNorm) write_row(static_cast<T*>(p.y) + row * p.width + at, n, t[c]);
     }
   }
@@ -170,8 +187,24 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void add_norm_backward_kernel(co
         sum[1] += g[c][i] * w[c][i] * t[c][i];
       }
     row_sums<L, 2>(sum, lds, turn);
-    const float r = live ? 1.f / sqrtf(sum[0] / float(p.width) + p.eps) : 0.f;        // 0: with an eps of zero it would be infinite
-    const float dot = sum[1] * r / float(p.width);
+    float mean = sum[0] / float(p.width) + p.eps, by = 1.f;
+    if (live && out_of_range(mean)) {
+      by = into_range(mean);
+      sum[0] = sum[1] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float v = t[c][i] * by;
+          sum[0] += v * v;
+          sum[1] += g[c][i] * w[c][i] * v;
+        }
+      if constexpr (L > 64) __syncthreads();
+      row_sums<L, 2>(sum, lds, turn);
+      mean = sum[0] / float(p.width) + p.eps * by * by;
+    }
+    const float r0 = live ? 1.f / sqrtf(mean) : 0.f;       // 0: with an eps of zero it would be infinite
+    const float dot = sum[1] * r0 / float(p.width), r = fminf(r0 * by, 3.402823466e+38f);       // beyond that only in rows without any normal number
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = 8 * (c * L + c0), n = in ? p.width - at : 0;

@@ -151,3 +151,38 @@ def test_clipped_gradients_are_rounded_once(dtype):
         want = rounded_once(g.double() * (most / whole), dtype)
         off += int((out[1].double() != want).sum())
     assert off == 0
+
+
+# ---- the norm
+
+def run_far(tokens, width, dtype, stream, size, eps, pos=None, g_size=1.0, seed=1, back=True):
+    """Rows of numbers around `size`, their norm and gradients, within the bounds of other rows."""
+    L = lgp()
+    res = (draw((tokens, width), F32, seed).double() * size).to(stream)
+    x, w = torch.zeros(tokens, width, dtype=dtype, device="cuda"), 1 + draw((width,), F32, seed + 1, 0.3)
+    dy = (draw((tokens, width), F32, seed + 2).double() * g_size).to(dtype)
+    if pos is not None:
+        res[pos < 0] = math.nan
+    assert torch.isfinite(res[ref.live_rows(tokens, pos, "cuda")]).all()
+    y, total = L.add_norm(x, res, w, pos=pos, eps=eps)
+    want = ref.add_norm(x, res, w, pos, eps)
+    check(y, want["y"], "y")
+    if back:
+        exact = ref.add_norm(None, None, w, pos, eps, dy, None, total)
+        for got, name in zip(L.add_norm_backward(dy, None, total, w, pos=pos, eps=eps), ("dx", "d_residual", "dw")):
+            val, tol = exact[name]
+            check(got, (val, tol + 2.0 ** -134), name)          # the smallest numbers lose digits
+    rows, _ = L.add_norm_rows8(x, res, w, pos=pos, eps=eps)
+    ref.rows8(*want["y32"], rows.values, rows.scales, ref.live_rows(tokens, pos, "cuda"))
+
+
+@pytest.mark.parametrize("width", [3, 33, 256, 1000, 2500, 9000])
+@pytest.mark.parametrize("dtype,stream", [(F32, F32), (BF16, BF16), (BF16, F32), (F16, F32)])
+def test_norm_of_rows_whose_squares_32_bits_do_not_hold(width, dtype, stream):
+    """Sums of squares beyond 2^128 or below 2^-126; with an eps that matters beside them and without."""
+    for size in (2.0 ** 63, 2.0 ** 80, 2.0 ** 118):
+        for eps in (1e-6, 0.0):
+            run_far(21, width, dtype, stream, size, eps, g_size=1.0 if dtype is F16 else 2.0 ** 20, pos=slots(21, width))
+    for size in (2.0 ** -50, 2.0 ** -64, 2.0 ** -80, 2.0 ** -110):
+        for eps in (1e-6, size * size if size > 2.0 ** -63 else 0.0, 0.0):
+            run_far(21, width, dtype, stream, size, eps, g_size=2.0 ** -30, pos=slots(21, width), back=dtype is not F16)       # fp16 does not hold such gradients
