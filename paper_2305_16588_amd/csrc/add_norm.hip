@@ -204,7 +204,8 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void add_norm_backward_kernel(co
       mean = sum[0] / float(p.width) + p.eps * by * by;
     }
     const float r0 = live ? 1.f / sqrtf(mean) : 0.f;       // 0: with an eps of zero it would be infinite
-    const float dot = sum[1] * r0 / float(p.width), r = fminf(r0 * by, 3.402823466e+38f);       // beyond that only in rows without any normal number
+    const float dot = sum[1] * r0 / float(p.width);
+    const float r = r0 <= 3.402823466e+38f && r0 * by > 3.402823466e+38f ? 3.402823466e+38f : r0 * by;       // of rows without any normal number; NaN stays
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int at = 8 * (c * L + c0), n = in ? p.width - at : 0;

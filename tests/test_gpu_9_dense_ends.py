@@ -186,3 +186,23 @@ def test_norm_of_rows_whose_squares_32_bits_do_not_hold(width, dtype, stream):
     for size in (2.0 ** -50, 2.0 ** -64, 2.0 ** -80, 2.0 ** -110):
         for eps in (1e-6, size * size if size > 2.0 ** -63 else 0.0, 0.0):
             run_far(21, width, dtype, stream, size, eps, g_size=2.0 ** -30, pos=slots(21, width), back=dtype is not F16)       # fp16 does not hold such gradients
+
+
+def test_gradients_of_a_norm_that_is_not_finite_are_not():
+    """A NaN spoils its row's gradients and all of the weight's, an infinity its own element's; zeros with an eps of zero have no norm."""
+    L = lgp()
+    for width in (40, 300, 3000):
+        total, dy, w = draw((50, width), F32, 1), draw((50, width), F32, 2), 1 + draw((width,), F32, 3, 0.1)
+        clean, _, _ = L.add_norm_backward(dy, None, total, w)
+        odd, place = torch.arange(50, device="cuda") == 7, torch.arange(width, device="cuda") == 3
+        total[7, 3] = math.nan
+        dx, _, dw = L.add_norm_backward(dy, None, total, w)
+        assert torch.isnan(dx[7]).all() and torch.isnan(dw).all() and torch.equal(dx[~odd], clean[~odd])
+        total[7, 3] = math.inf
+        dx, _, dw = L.add_norm_backward(dy, None, total, w)
+        assert torch.isnan(dw[3]) and torch.isfinite(dw[~place]).all() and torch.equal(dx[~odd], clean[~odd])
+        total[7] = 0
+        dx, _, dw = L.add_norm_backward(dy, None, total, w, eps=0.0)
+        assert torch.isnan(dx[7]).all() and torch.isnan(dw).all()
+        y, _ = L.add_norm(total, None, w, eps=0.0)
+        assert torch.isnan(y[7]).all() and torch.isfinite(y[~odd]).all()
