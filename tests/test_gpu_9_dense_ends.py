@@ -7,7 +7,7 @@ import torch
 
 import dense_common as ref
 from layer_common import check
-from test_gpu_9_dense import BF16, F16, F32, draw, lgp, slots
+from test_gpu_9_dense import BF16, F16, F32, draw, lgp, rows_of, slots
 
 pytestmark = pytest.mark.gpu
 
@@ -206,3 +206,151 @@ def test_gradients_of_a_norm_that_is_not_finite_are_not():
         assert torch.isnan(dx[7]).all() and torch.isnan(dw).all()
         y, _ = L.add_norm(total, None, w, eps=0.0)
         assert torch.isnan(y[7]).all() and torch.isfinite(y[~odd]).all()
+
+
+# ---- every form on streams, in captured graphs and repeated bit by bit
+
+def all_forms():
+    """(calls, inputs): the gated pair and its gradients with lists and without, by rows that pass and by tiles of every size, and the products in 8 bits by every form."""
+    L = lgp()
+    calls, inputs = [], []
+    for tokens, width, hidden, dtype, listed in ((30, 64, 48, BF16, False), (700, 256, 130, F16, True), (5000, 128, 96, F16, True), (4500, 256, 683, BF16, True), (66_003, 64, 40, F16, False),
+                                                 (70_001, 128, 40, BF16, True), (66_003, 250 // 8 * 8, 100, F16, True), (33_000, 512, 130, BF16, True), (4000, 136, 1100, F16, False),
+                                                 (9000, 520, 700, BF16, True)):
+        x, dh = draw((tokens, width), dtype, tokens), draw((tokens, hidden), dtype, tokens + 1, 0.1)
+        wg, wu = draw((hidden, width), dtype, tokens + 2, width ** -0.5), draw((hidden, width), dtype, tokens + 3, width ** -0.5)
+        pos = slots(tokens, tokens) if listed else None
+        calls.append(lambda stream=None, a=(x, wg, wu), p=pos: [L.gated_linear(*a, pos=p, stream=stream)])
+        calls.append(lambda stream=None, d=dh, a=(x, wg, wu), p=pos: list(L.gated_linear_backward(d, *a, pos=p, stream=stream)))
+        inputs += [x, dh]
+    for tokens, width, channels in ((20, 1000, 300), (276, 256, 768), (70_001, 100, 130), (70_001, 256, 130), (70_001, 500, 130), (70_001, 1000, 130), (33_001, 1040, 300)):
+        x, weight, bias = draw((tokens, width), F16, tokens + width), rows_of(channels, width, tokens + 1), draw((channels,), F32, tokens + 2)
+        pos = slots(tokens, width)
+        calls.append(lambda stream=None, x=x, w=weight, b=bias, p=pos: [L.linear_rows8(L.pack_rows(x, pos=p, stream=stream), w, bias=b, dtype=F32, stream=stream)])
+        inputs.append(x)
+    return calls, inputs
+
+
+def run_all(calls, stream=None):
+    return [t for call in calls for t in call(stream)]
+
+
+def alike(got, want):
+    assert len(got) == len(want)
+    for i, (a, b) in enumerate(zip(got, want)):
+        assert torch.equal(a, b), i
+
+
+def test_all_forms_are_the_same_bit_by_bit_and_on_another_stream():
+    calls, _ = all_forms()
+    first = run_all(calls)
+    assert all(torch.isfinite(t).all() for t in first)
+    alike(run_all(calls), first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = run_all(calls, side)
+    torch.cuda.current_stream().wait_stream(side)
+    alike(got, first)
+
+
+def test_all_forms_captured_and_replayed():
+    calls, inputs = all_forms()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run_all(calls)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = run_all(calls)
+    for seed in range(3):
+        for t in inputs:
+            t.copy_(draw(t.shape, t.dtype, 100 + seed, 0.5 ** seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        alike(got, run_all(calls))
+
+
+# ---- places beyond 32 bits
+
+def few_rows(tokens):
+    return torch.tensor([0, 1, 255, tokens // 2 + 3, tokens - 300, tokens - 1], device="cuda")
+
+
+def check_far(tokens, width, hidden, dtype, pos=None, x=None):
+    """All rows are zeros but for a few, whose results stand where they belong; all others are zeros."""
+    L = lgp()
+    at = few_rows(tokens)
+    if x is None:
+        x = torch.zeros(tokens, width, dtype=dtype, device="cuda")
+    dh = torch.zeros(tokens, hidden, dtype=dtype, device="cuda")
+    x[at], dh[at] = draw((len(at), width), dtype, 1), draw((len(at), hidden), dtype, 2)
+    wg, wu = draw((hidden, width), dtype, 3, width ** -0.5), draw((hidden, width), dtype, 4, width ** -0.5)
+    if pos is not None:
+        pos[at] = 1
+    want = ref.gated(x[at], wg, wu, "silu", None, dh[at])
+    h = L.gated_linear(x, wg, wu, pos=pos)
+    check(h[at], want["h"], "h")
+    h[at] = 0
+    assert not h.any()
+    del h
+    dx, dg, du = L.gated_linear_backward(dh, x, wg, wu, pos=pos)
+    check(dx[at], want["dx"], "dx")
+    dx[at] = 0
+    assert not dx.any()
+    check(dg, want["dw_gate"], "dw_gate")
+    check(du, want["dw_up"], "dw_up")
+
+
+def test_gated_beyond_32_bits():
+    """Elements of h, of its gradient and of x whose places pass 2^31, bytes beyond 2^32; the projections' gradients, two for each element of h, pass 2^32."""
+    check_far(300_000, 520, 7400, BF16)               # large tiles
+    check_far((1 << 24) - 5, 136, 40, F16)            # rows of x
+    check_far((1 << 24) - 5, 64, 136, BF16)           # rows that pass by the weights
+
+
+def test_gated_with_lists_beyond_32_bits():
+    pos = torch.full(((1 << 24) - 5,), -1, dtype=torch.int32, device="cuda")
+    pos[::3] = 0
+    check_far((1 << 24) - 5, 64, 136, F16, pos=pos)
+    # rows of x so far apart that units of 16 bytes come near 2^32, and further, where there is no list
+    for tokens, listed in ((8190, 1), (8300, 0)):
+        row = (1 << 22) - 8
+        assert (tokens * row < 1 << 35) == listed
+        x = torch.empty(tokens * row, dtype=BF16, device="cuda").as_strided((tokens, 64), (row, 1))
+        x.zero_()
+        pos = torch.zeros(tokens, dtype=torch.int32, device="cuda")
+        pos[1::2] = -1
+        for hidden in (96, 600, 2100):
+            check_far(tokens, 64, hidden, BF16, pos=pos, x=x)
+        del x
+
+
+@pytest.mark.parametrize("tokens,width,channels", [((1 << 24) - 5, 64, 136), ((1 << 24) - 5, 1040, 136), (600_000, 300, 4000), (200, 40, (1 << 24) - 5)])
+def test_products_in_8_bits_beyond_32_bits(tokens, width, channels):
+    """Results whose places pass 2^31 (and bytes of rows 2^32)."""
+    L = lgp()
+    weight, rows = rows_of(channels, width, 1), rows_of(tokens, width, 2)
+    out = L.linear_rows8(rows, weight, dtype=BF16)
+    for at in (slice(0, 300), slice(tokens // 2, tokens // 2 + 100), slice(tokens - 300, None)):
+        v, s = rows.values[at].float(), rows.scales[at].double()
+        for c in (slice(0, 200), slice(max(0, channels - 200), None)):
+            want = (v @ weight.values[c].float().t()).double() * weight.scales[c].double() * s[:, None]        # sums of 1040 products below 2^14: exact in fp32
+            check(out[at, c], (want, 2.0 ** -22 * want.abs() + 2.0 ** -8 * want.abs()))
+
+
+# ---- weights' gradients of large batches
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("tokens,width,hidden", FORMS)
+def test_gated_of_sums_that_are_exact(tokens, width, hidden, act, dtype):
+    """A token that is left out, read twice or put elsewhere changes a whole number."""
+    for pos in (None, slots(tokens, 3)):
+        run_known(tokens, width, hidden, dtype, act, 8.0, gate=(4, 5), up=(-3, -2), grad=(-6, -5), pos=pos)
+    run_known(tokens, width, hidden, dtype, act, 8.0, gate=(4, 5), up=(-3, -2), grad=(-6, -5), share=min(1.0, 300 / tokens))
+    pos = slots(tokens, 3)
+    pos[:tokens // 3] = -1
+    pos[-tokens // 5:] = -1
+    run_known(tokens, width, hidden, dtype, act, 8.0, gate=(4, 5), up=(-3, -2), grad=(-6, -5), pos=pos)
