@@ -529,7 +529,8 @@ typedef struct {
  * width], rows end to end.  Without a residual, total is x itself and not written (it may be NULL), and the types have to be the same. */
 int lgp_add_norm(int device, const lgp_residual* in, void* y, void* total, void* stream);
 
-/* The same with y in 8 bits, from its 32-bit value: scale = max |y| / 127, at least 2^-126, and values = y / scale, rounded to even.  A row with an infinity or a
+/* The same with y in 8 bits, from its 32-bit value: scale = max |y| / 127, at least 2^-126, and values = y / scale (y times
+ * the reciprocal of scale, in 32 bits), rounded to even.  A row with an infinity or a
  * NaN has a scale of NaN.  out->pos is not read: in->pos says where tokens are. */
 int lgp_add_norm_rows8(int device, const lgp_residual* in, const lgp_rows8* out, void* total, void* stream);
 
@@ -571,8 +572,8 @@ int lgp_gated_linear_workspace(int device, const lgp_gated* in, int backward, si
 
 /* Gradients of lgp_gated_linear by x (dx [tokens, width], zeros where no token is) and the weights (like them), from that of h (dh [tokens, hidden], rows end to
  * end).  Both projections are computed again; but in the smallest calls (8 tokens, or 64 with few hidden elements) the gradients of their results are rounded to the type of x for the products that follow, which
- * makes a gradient's error 1.4 times that of rounding it once.  In fp16 they are lifted by one power of two for a call, so that none passes its range: what is below 2^-29 of
- * the largest |dh| |x| of a token times the largest |w| of a row is off by up to 2^-39 of that. */
+ * makes a gradient's error 1.4 times that of rounding it once.  In fp16 they are lifted by one power of two for a call, so that none passes its range: what is below 2^-27 of
+ * the largest |dh| |x| of a token times the largest |w| of a row is off by up to 2^-38 of that. */
 int lgp_gated_linear_backward(int device, const lgp_gated* in, const void* dh, void* dx, void* dw_gate, void* dw_up, void* workspace, size_t workspace_bytes,
                               void* stream);
 

@@ -50,7 +50,8 @@ __device__ __forceinline__ float into_range(float mean) { return mean < 1.f ? 0x
 // L lanes have a row, each of them every L-th eight elements, C of them: a row is read once and stays in registers, and a wave's loads are whole
 // lines.  The sum of squares, the root and the products are in 32 bits; the total is rounded first, so that the backward pass, which reads it, has the
 // gradients of what was computed.  Bound by bytes.  Measured: 400000 rows of 1024, fp16 with a residual in fp32: 855 us, 5.7 TB/s; 282624 rows of
-// 256, bf16, 30 % without a token: 88 us, 5.6 TB/s, and 97 to 104 with the result in 8 bits (4.2 TB/s).
+// 256, bf16, 30 % without a token: 88 us, 5.6 TB/s, and 97 to 104 with the result in 8 bits (4.2 TB/s); rows packed alone: 282624 of 256, bf16, 38 us, 5.7 TB/s,
+// 65536 of 4096 153 us, 5.3 TB/s.
 enum { kNorm = 0, kNorm8 = 1, kPack8 = 2 };
 template <typename T, typename S, int MODE, int L, int C>
 __global__ __launch_bounds__(L > 256 ? L : 256) void add_norm_kernel(const AddParams p) {

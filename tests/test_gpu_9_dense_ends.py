@@ -98,7 +98,7 @@ def test_gated_of_fp16_gradients_beyond_its_largest(tokens, width, hidden):
 @pytest.mark.parametrize("tokens", [8, 9, 64, 65, 300, 4097])
 def test_gated_of_fp16_keeps_its_error_at_every_size_of_gradients(monkeypatch, tokens):
     """Gradients of h from 2^-20 to 2^12 and a row of zeros: but for results below fp16's smallest, errors are those of roundings by 2^-11.  The gradients of the projections'
-    results are lifted by a power of two, and what is 2^-29 of the largest that they might be, |dh| |x| |w|, is off by 2^-39 of it."""
+    results are lifted by a power of two, B 1.2 to 2^14 or more where B is the largest |dh| |x| of a token times the largest |w|, and fp16 keeps 2^-25: 1.2 2^-39 of B."""
     L = lgp()
     x, wg, wu = draw((tokens, 96), F16, 1, 0.1), draw((200, 96), F16, 2, 0.1), draw((200, 96), F16, 3, 0.1)
     dh = draw((tokens, 200), F16, 4, 0.25)
